@@ -531,6 +531,141 @@ aal_status_t aal_vp_grad(const void* z_draft, const void* z_target, aal_dtype_t 
                          float temp_draft, float temp_target, const aal_vp_row_t* row,
                          void* grad_draft, aal_dtype_t grad_dtype, hipStream_t stream);
 
+/* Longest list of a row's top logits. */
+#define AAL_TOPK_MAX 512
+
+/* Workspace bytes of aal_topk_logits (0 for invalid arguments). */
+size_t aal_topk_workspace_bytes(int64_t rows, int32_t V, int32_t k);
+
+/*
+ * A row's k largest logits, their ids, and the log-sum-exp of all others: what
+ * a data set keeps of a target's logits, and what aal_topk_loss_fwd_bwd reads.
+ *
+ *   order  : v before w iff z_v > z_w, or z_v = z_w and v < w (-0 equals +0)
+ *   rest_r = ln sum_{v not among the k} exp(z_v / temperature), -inf where no
+ *            finite logit remains
+ *
+ * z : [rows, V] of in_dtype, finite or -inf; a row may have fewer than k finite
+ *     logits, or none: its list then ends in -inf entries, lowest ids first.
+ * 1 <= rows < 2^31, 1 <= V <= 2^30, 1 <= k <= min(V, AAL_TOPK_MAX); temperature
+ * finite and > 0 (it bears on rest alone).
+ * top_logits : [rows, k] of in_dtype, the logits themselves, in order.  top_ids : [rows, k].
+ * rest : [rows] float, or NULL.
+ * workspace : at least aal_topk_workspace_bytes(rows, V, k) bytes, 256-byte aligned.
+ */
+aal_status_t aal_topk_logits(const void* z, aal_dtype_t in_dtype, int64_t rows, int32_t V, int32_t k,
+                             float temperature, void* top_logits, int32_t* top_ids, float* rest,
+                             void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of aal_topk_loss_fwd_bwd for the given layout and sizes (0
+ * for invalid arguments). */
+size_t aal_topk_loss_workspace_bytes(aal_layout_t layout, int64_t B, int32_t S, int32_t K);
+
+/*
+ * The objectives of aal_loss_fwd_bwd with the target known by its top logits
+ * alone (Section "Settings": the target's logits are precomputed), forward and
+ * backward.
+ *
+ *   p_i  = exp(t_i / temp_target) / Z for the entries i of the row's list,
+ *   p_r  = exp(rest_r) / Z, Z = sum_i exp(t_i / temp_target) + exp(rest_r): the
+ *          remainder counts as one more entry.  Without `rest` p_r = 0: the
+ *          list is renormalised.
+ *   q    = softmax(z_draft / temp_draft), q_i = q(id_i), q_r = sum of q outside
+ *          the list
+ *   a_tv = sum_i min(p_i, q_i) + min(p_r, q_r)
+ *   KL_r = sum_i p_i (ln p_i - ln q_i) + p_r (ln p_r - ln q_r)
+ *   a_eal = q(x*), x* the list's largest logit (lowest id on ties)
+ *   terms, loss, windows and layouts as for aal_loss_fwd_bwd
+ *   grad_draft = scale * dloss/dz_draft, with m = 1[q < p] per entry and m_r =
+ *          1[q_r < p_r], Q = sum_i m_i q_i + m_r q_r:
+ *     d a_tv/dz_v  = q(v) (m(v) - Q) / temp_draft, m(v) = m_r outside the list,
+ *     d a_eal/dz_v = a_eal (1[v = x*] - q(v)) / temp_draft,
+ *     d KL/dz_v    = (q(v) - p(v)) / temp_draft in the list, q(v) (1 - p_r / q_r) / temp_draft outside.
+ *
+ * With a list of all V entries this is aal_loss_fwd_bwd.
+ * z_draft : [R, V] of in_dtype.  top_logits : [R, k] of top_dtype and top_ids [R, k]: the lists, in any
+ *     order, ids distinct.  An entry whose id is outside [0, V) or whose logit is -inf is no part
+ *     of its list, so lists of different lengths are padded with either.
+ * rest : [R] float, as from aal_topk_logits at temp_target, or NULL.
+ * A row with an empty list and no (or a -inf) remainder has no target: its
+ *     acceptances and KL are 0, x* is -1, its gradient is 0.  It still counts
+ *     in the means over positions and windows.
+ * B >= 1, 1 <= K <= 64, fewer than 2^31 rows, 1 <= V <= 2^19, 1 <= k <= min(V, AAL_TOPK_MAX).
+ * loss [1] is required; terms, e_tv, e_eal, accept_tv, accept_eal, xstar: as there, or NULL, and
+ *     evaluated whatever the weights (a term whose weight is 0 reads 0).
+ * grad_draft, grad_dtype, grad_scale, flags : as there.  AAL_FLAG_STREAMING forces the
+ *     multi-kernel schedule.
+ * workspace : at least aal_topk_loss_workspace_bytes(layout, B, S, K) bytes, 256-byte aligned.
+ */
+aal_status_t aal_topk_loss_fwd_bwd(const void* z_draft, aal_dtype_t in_dtype, const void* top_logits,
+                                   aal_dtype_t top_dtype, const int32_t* top_ids, const float* rest,
+                                   aal_layout_t layout, int64_t B, int32_t S, int32_t K, int32_t V,
+                                   int32_t k, float temp_draft, float temp_target,
+                                   aal_loss_weights_t weights, float* loss, float* terms, float* e_tv,
+                                   float* e_eal, float* accept_tv, float* accept_eal, int32_t* xstar,
+                                   void* grad_draft, aal_dtype_t grad_dtype, const float* grad_scale,
+                                   uint32_t flags, void* workspace, size_t workspace_bytes,
+                                   hipStream_t stream);
+
+/* What a row's logits go through before they are sampled from or compared.
+ * All arrays are device memory; a part that is not wanted is NULL.
+ *   tokens [n_tokens]    the histories: row r's is tokens[hist_start[r]] on, hist_len[r] long
+ *                        (cut to the array), its first prompt_len[r] tokens the prompt and the
+ *                        others generated (prompt_len NULL: all of them).  Rows may
+ *                        share or overlap; a token outside [0, V) counts nowhere.
+ *   repetition, frequency, presence [rows]   (NULL: 1, 0, 0); repetition finite and > 0.
+ *   bias_offsets [rows + 1], bias_ids, bias_values [n_bias]   row r's are entries
+ *                        bias_offsets[r] to bias_offsets[r + 1]; of equal ids the last one counts.
+ *   mask [n_masks, ceil(V / 32)]   bit v % 32 of word v / 32 set: entry v is allowed.
+ *   mask_row [rows]      the mask of each row, none where it is outside [0, n_masks).  NULL: the
+ *                        only mask, or mask r for row r. */
+typedef struct {
+  const int32_t* tokens;
+  int64_t n_tokens;
+  const int64_t* hist_start;
+  const int32_t* hist_len;
+  const int32_t* prompt_len;
+  const float* repetition;
+  const float* frequency;
+  const float* presence;
+  const int64_t* bias_offsets;
+  const int32_t* bias_ids;
+  const float* bias_values;
+  int64_t n_bias;
+  const uint32_t* mask;
+  int64_t n_masks;
+  const int32_t* mask_row;
+} aal_logits_rules_t;
+
+/*
+ * Biases, penalties for repeated tokens and grammar masks, in this order:
+ *
+ *   x  = z + bias
+ *   x  = x > 0 ? x / repetition : x * repetition      for every token of the history
+ *   x -= frequency * c + presence * 1[c > 0]          c: its number among the generated tokens
+ *   out = x where the row's mask allows the entry, else -inf
+ *
+ * in fp32, rounded once to dtype; an entry that nothing bears on keeps its bits, and a
+ * blocked one is -inf whatever it held (NaN too).  A mask that allows nothing leaves a row of -inf.
+ * z, out : [rows, V] of dtype, 16-byte aligned; out may be z itself (no other overlap).
+ * rules  : host memory, read before the call returns.  1 <= rows < 2^31, 1 <= V <= 2^24.
+ */
+aal_status_t aal_logits_process(const void* z, aal_dtype_t dtype, int64_t rows, int32_t V,
+                                const aal_logits_rules_t* rules, void* out, hipStream_t stream);
+
+/*
+ * The gradient through aal_logits_process with respect to z:
+ *
+ *   grad_z = 0 where the mask blocks the entry, else grad_out, at a token of the history
+ *            grad_out / repetition where z + bias > 0 and grad_out * repetition elsewhere
+ *
+ * z : [rows, V] of in_dtype, the logits that went in.  grad_out, grad_z : [rows, V] of grad_dtype,
+ *     16-byte aligned; grad_z may be grad_out itself.  The rest as for aal_logits_process.
+ */
+aal_status_t aal_logits_process_bwd(const void* grad_out, aal_dtype_t grad_dtype, const void* z,
+                                    aal_dtype_t in_dtype, int64_t rows, int32_t V,
+                                    const aal_logits_rules_t* rules, void* grad_z, hipStream_t stream);
+
 /*
  * Measurement aid, not part of the method: streams 1 to 3 device buffers of
  * `bytes` bytes each (src0, then src1 and src2 when non-NULL) with 16-byte

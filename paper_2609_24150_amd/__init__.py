@@ -11,15 +11,22 @@ from .api import (  # noqa: F401
     AAL_FLAG_STREAMING,
     AAL_LAYOUT_SEQUENCES,
     AAL_LAYOUT_WINDOWS,
+    AAL_TOPK_MAX,
     AAL_VP_EAL,
     AAL_VP_WTV,
     aal_eal_fwd_bwd,
     aal_grpo_fwd_bwd,
     aal_grpo_workspace_bytes,
+    aal_logits_process,
+    aal_logits_process_bwd,
     aal_loss_fwd_bwd,
     aal_loss_workspace_bytes,
     aal_sim_accept_grpo,
     aal_stream_probe,
+    aal_topk_logits,
+    aal_topk_loss_fwd_bwd,
+    aal_topk_loss_workspace_bytes,
+    aal_topk_workspace_bytes,
     aal_vp_accept_partials,
     aal_vp_grad,
     aal_vp_merge_rows,

@@ -29,11 +29,21 @@ AAL_VP_WTV = 1
 VP_PART_BYTES = 32
 VP_ACC_BYTES = 8
 VP_ROW_BYTES = 32
+AAL_TOPK_MAX = 512
 
 
 class LossWeights(C.Structure):
     """aal_loss_weights_t (passed by value)."""
     _fields_ = [("wtv", C.c_float), ("eal", C.c_float), ("kl", C.c_float), ("tv", C.c_float)]
+
+
+class LogitsRules(C.Structure):
+    """aal_logits_rules_t (passed by address)."""
+    _fields_ = [("tokens", C.c_void_p), ("n_tokens", C.c_int64), ("hist_start", C.c_void_p),
+                ("hist_len", C.c_void_p), ("prompt_len", C.c_void_p), ("repetition", C.c_void_p),
+                ("frequency", C.c_void_p), ("presence", C.c_void_p), ("bias_offsets", C.c_void_p),
+                ("bias_ids", C.c_void_p), ("bias_values", C.c_void_p), ("n_bias", C.c_int64),
+                ("mask", C.c_void_p), ("n_masks", C.c_int64), ("mask_row", C.c_void_p)]
 
 
 class GrpoParams(C.Structure):
@@ -103,6 +113,18 @@ _SIGNATURES = {
         _vp, _vp, C.c_int32, C.c_int64, C.c_int32, C.c_int, C.c_float, _vp, _vp, _vp, _vp, _vp, _vp]),
     "aal_vp_sequence_scan": (C.c_int, [
         _vp, _vp, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int, C.c_float, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "aal_topk_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int32, C.c_int32]),
+    "aal_topk_logits": (C.c_int, [
+        _vp, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_float, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
+    "aal_topk_loss_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int64, C.c_int32, C.c_int32]),
+    "aal_topk_loss_fwd_bwd": (C.c_int, [
+        _vp, C.c_int, _vp, C.c_int, _vp, _vp, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+        C.c_float, C.c_float, LossWeights, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_int, _vp, C.c_uint32,
+        _vp, C.c_size_t, _vp]),
+    "aal_logits_process": (C.c_int, [
+        _vp, C.c_int, C.c_int64, C.c_int32, C.POINTER(LogitsRules), _vp, _vp]),
+    "aal_logits_process_bwd": (C.c_int, [
+        _vp, C.c_int, _vp, C.c_int, C.c_int64, C.c_int32, C.POINTER(LogitsRules), _vp, _vp]),
     "aal_stream_probe": (C.c_int, [_vp, _vp, _vp, _vp, C.c_size_t, _vp, _vp]),
     "aal_vp_grad": (C.c_int, [
         _vp, _vp, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_int, C.c_float, C.c_float, _vp, _vp, C.c_int,

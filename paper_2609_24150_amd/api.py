@@ -5,12 +5,15 @@ and returns.  It computes nothing itself.
 """
 from __future__ import annotations
 
+import contextlib
+import ctypes as C
+
 import torch
 
 from . import _lib
 from ._lib import (  # noqa: F401
     AAL_BF16, AAL_F32, AAL_FLAG_COOPERATIVE, AAL_FLAG_STREAMING, AAL_LAYOUT_SEQUENCES, AAL_LAYOUT_WINDOWS,
-    AAL_VP_EAL, AAL_VP_WTV,
+    AAL_TOPK_MAX, AAL_VP_EAL, AAL_VP_WTV,
 )
 
 _DT = {torch.bfloat16: AAL_BF16, torch.float32: AAL_F32}
@@ -427,6 +430,249 @@ def aal_vp_grad(z_draft: torch.Tensor, z_target: torch.Tensor | None, row: torch
                                 _dtype_code(g.dtype), _stream(dev, stream))
     _lib.check(st, "aal_vp_grad")
     return g
+
+
+# ----------------------------------------------------------------------------
+# Training against a target's top logits, and the processing of logits.
+
+def _guard(device, stream):
+    """Allocations and launches of a call: on the device of its tensors and in the stream's own pool."""
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    if device.index != torch.cuda.current_device():
+        return torch.cuda.device(device)
+    return contextlib.nullcontext()
+
+
+def _device_array(t, name: str, dtype, numel: int | None, device):
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or (numel is not None and t.numel() != numel):
+        size = "" if numel is None else f" of {numel} entries"
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor{size} on {device}")
+
+
+def _check_rows(z: torch.Tensor, name: str):
+    if z.dim() < 1 or z.numel() == 0:
+        raise ValueError(f"{name} must be [..., V] with at least one row")
+    if not z.is_cuda or not z.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous device tensor")
+    V = z.shape[-1]
+    return z.numel() // V, V
+
+
+def aal_topk_workspace_bytes(rows: int, V: int, k: int) -> int:
+    return int(_lib.lib().aal_topk_workspace_bytes(int(rows), int(V), int(k)))
+
+
+def aal_topk_logits(z: torch.Tensor, k: int, temperature: float = 1.0, *, rest: bool = True,
+                    ws: torch.Tensor | None = None, stream=None) -> dict:
+    """The k largest logits of each row of z [..., V] (larger first, the lower
+    id first among equal ones) and the log-sum-exp of all others at
+    `temperature`: what a data set keeps of a target's logits.
+
+    Returns a dict: logits [..., k] of z's dtype, ids [..., k] int32 and rest
+    [...] float32 (None with rest=False)."""
+    rows, V = _check_rows(z, "z")
+    code, dev, lead = _dtype_code(z.dtype), z.device, z.shape[:-1]
+    if not 1 <= k <= min(V, AAL_TOPK_MAX):
+        raise ValueError(f"k must be in [1, min(V, {AAL_TOPK_MAX})]; got {k}")
+    with _guard(dev, stream):
+        out = {
+            "logits": torch.empty(*lead, k, dtype=z.dtype, device=dev),
+            "ids": torch.empty(*lead, k, dtype=torch.int32, device=dev),
+            "rest": torch.empty(lead, dtype=torch.float32, device=dev) if rest else None,
+        }
+        if ws is None:
+            ws = torch.empty(aal_topk_workspace_bytes(rows, V, k), dtype=torch.uint8, device=dev)
+        st = _lib.lib().aal_topk_logits(_ptr(z), code, rows, V, int(k), float(temperature), _ptr(out["logits"]),
+                                        _ptr(out["ids"]), _ptr(out["rest"]), _ptr(ws), ws.numel(),
+                                        _stream(dev, stream))
+    _lib.check(st, "aal_topk_logits")
+    return out
+
+
+def aal_topk_loss_workspace_bytes(layout: int, B: int, S: int, K: int) -> int:
+    return int(_lib.lib().aal_topk_loss_workspace_bytes(int(layout), int(B), int(S), int(K)))
+
+
+def aal_topk_loss_fwd_bwd(z_draft: torch.Tensor, top_logits: torch.Tensor, top_ids: torch.Tensor, K: int, *,
+                          rest: torch.Tensor | None = None, weights=(0.0, 0.0, 0.0, 0.0), temp_draft: float = 1.0,
+                          temp_target: float = 1.0, layout: int = AAL_LAYOUT_WINDOWS, grad: bool = True,
+                          grad_dtype: torch.dtype | None = None, grad_scale: torch.Tensor | None = None,
+                          flags: int = 0, outputs: bool = True, ws: torch.Tensor | None = None, stream=None) -> dict:
+    """The objectives of aal_loss_fwd_bwd (weights = (wtv, eal, kl, tv)) with
+    the target known by its top logits, forward + backward.
+
+    z_draft: [N, K, V] (windows layout) or [B, S, V] (sequences).  top_logits
+    [N or B, K or S, k] and int32 top_ids of that shape: each row's list, as
+    from aal_topk_logits; an entry with an id outside [0, V) or a logit of
+    -inf is no part of it.  rest: [N or B, K or S] float32, the log-sum-exp of
+    the target's other logits at temp_target, counted as one more entry; None:
+    the list is renormalised.  A row without any target gets no gradient.
+
+    Returns the dict of aal_loss_fwd_bwd: loss [1], terms [4], E_tv [W],
+    E_eal [W], accept_tv [R], accept_eal [R], xstar [R] int32, grad."""
+    if z_draft.dim() != 3:
+        raise ValueError("z_draft must be a contiguous [B, S or K, V] device tensor")
+    R, V = _check_rows(z_draft, "z_draft")
+    B, S = z_draft.shape[:2]
+    dev = z_draft.device
+    if layout == AAL_LAYOUT_WINDOWS and S != K:
+        raise ValueError("windows layout needs logits of shape [N, K, V]")
+    if top_logits.dim() != 3 or top_logits.shape[:2] != z_draft.shape[:2]:
+        raise ValueError("top_logits must be [B, S or K, k]")
+    k = top_logits.shape[-1]
+    if not 1 <= k <= min(V, AAL_TOPK_MAX):
+        raise ValueError(f"lists must have 1 to min(V, {AAL_TOPK_MAX}) entries; got {k}")
+    _device_array(top_logits, "top_logits", top_logits.dtype, R * k, dev)
+    if top_ids.shape != top_logits.shape:
+        raise ValueError("top_ids must have the shape of top_logits")
+    _device_array(top_ids, "top_ids", torch.int32, R * k, dev)
+    if rest is not None:
+        _device_array(rest, "rest", torch.float32, R, dev)
+    if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.device != dev):
+        raise TypeError("grad_scale must be a float32 device tensor")
+    code, top_code = _dtype_code(z_draft.dtype), _dtype_code(top_logits.dtype)
+    gcode = _dtype_code(grad_dtype or z_draft.dtype) if grad else AAL_F32
+    W = B if layout == AAL_LAYOUT_WINDOWS else B * max(0, S - K + 1)
+    with _guard(dev, stream):
+        new = lambda n, dtype=torch.float32: torch.empty(n, dtype=dtype, device=dev)  # noqa: E731
+        out = {
+            "loss": new(1), "terms": new(4),
+            "E_tv": new(W) if outputs else None, "E_eal": new(W) if outputs else None,
+            "accept_tv": new(R) if outputs else None, "accept_eal": new(R) if outputs else None,
+            "xstar": new(R, torch.int32) if outputs else None,
+            "grad": new((B, S, V), grad_dtype or z_draft.dtype) if grad else None,
+        }
+        if ws is None:
+            ws = new(aal_topk_loss_workspace_bytes(layout, B, S, K), torch.uint8)
+        st = _lib.lib().aal_topk_loss_fwd_bwd(
+            _ptr(z_draft), code, _ptr(top_logits), top_code, _ptr(top_ids), _ptr(rest), int(layout), B, S, int(K), V, k,
+            float(temp_draft), float(temp_target), _lib.LossWeights(*(float(x) for x in weights)), _ptr(out["loss"]),
+            _ptr(out["terms"]), _ptr(out["E_tv"]) if W and outputs else None,
+            _ptr(out["E_eal"]) if W and outputs else None, _ptr(out["accept_tv"]), _ptr(out["accept_eal"]),
+            _ptr(out["xstar"]), _ptr(out["grad"]), gcode, _ptr(grad_scale), int(flags), _ptr(ws), ws.numel(),
+            _stream(dev, stream))
+    _lib.check(st, "aal_topk_loss_fwd_bwd")
+    return out
+
+
+def _logits_rules(rows, V, dev, tokens, hist_start, hist_len, prompt_len, repetition, frequency, presence,
+                  bias_offsets, bias_ids, bias_values, mask, mask_row) -> _lib.LogitsRules:
+    r = _lib.LogitsRules()
+    history = (hist_start, hist_len, prompt_len, repetition, frequency, presence)
+    if tokens is None:
+        if any(t is not None for t in history):
+            raise ValueError("penalties need tokens")
+    else:
+        if hist_start is None or hist_len is None:
+            raise ValueError("tokens need hist_start and hist_len")
+        _device_array(tokens, "tokens", torch.int32, None, dev)
+        for t, name, dtype in zip(history, ("hist_start", "hist_len", "prompt_len", "repetition", "frequency",
+                                            "presence"),
+                                  (torch.int64, torch.int32, torch.int32) + (torch.float32,) * 3):
+            if t is not None:
+                _device_array(t, name, dtype, rows, dev)
+        if tokens.numel():  # without a token every history is empty
+            r.tokens, r.n_tokens, r.hist_start, r.hist_len = _ptr(tokens), tokens.numel(), _ptr(hist_start), _ptr(hist_len)
+            r.prompt_len, r.repetition = _ptr(prompt_len), _ptr(repetition)
+            r.frequency, r.presence = _ptr(frequency), _ptr(presence)
+    if bias_offsets is None:
+        if bias_ids is not None or bias_values is not None:
+            raise ValueError("biases need bias_offsets")
+    else:
+        if bias_ids is None or bias_values is None:
+            raise ValueError("bias_offsets need bias_ids and bias_values")
+        _device_array(bias_offsets, "bias_offsets", torch.int64, rows + 1, dev)
+        _device_array(bias_ids, "bias_ids", torch.int32, None, dev)
+        _device_array(bias_values, "bias_values", torch.float32, bias_ids.numel(), dev)
+        if bias_ids.numel():
+            r.bias_offsets, r.bias_ids = _ptr(bias_offsets), _ptr(bias_ids)
+            r.bias_values, r.n_bias = _ptr(bias_values), bias_ids.numel()
+    if mask is None:
+        if mask_row is not None:
+            raise ValueError("mask_row needs mask")
+    else:
+        words = (V + 31) // 32
+        if mask.dim() < 1 or mask.shape[-1] != words or mask.numel() == 0:
+            raise ValueError(f"mask must be [..., {words}]: a bit for each entry of the vocabulary")
+        _device_array(mask, "mask", torch.int32, None, dev)
+        r.mask, r.n_masks = _ptr(mask), mask.numel() // words
+        if mask_row is not None:
+            _device_array(mask_row, "mask_row", torch.int32, rows, dev)
+            r.mask_row = _ptr(mask_row)
+        elif r.n_masks not in (1, rows):
+            raise ValueError("without mask_row there must be one mask, or one for each row")
+    return r
+
+
+def aal_logits_process(z: torch.Tensor, *, tokens: torch.Tensor | None = None, hist_start: torch.Tensor | None = None,
+                       hist_len: torch.Tensor | None = None, prompt_len: torch.Tensor | None = None,
+                       repetition: torch.Tensor | None = None, frequency: torch.Tensor | None = None,
+                       presence: torch.Tensor | None = None, bias_offsets: torch.Tensor | None = None,
+                       bias_ids: torch.Tensor | None = None, bias_values: torch.Tensor | None = None,
+                       mask: torch.Tensor | None = None, mask_row: torch.Tensor | None = None,
+                       out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Biases, penalties for repeated tokens and grammar masks on the rows of
+    z [..., V], in that order; blocked entries become -inf.
+
+    tokens: int32, the histories of all rows; row r's is the hist_len[r]
+    (int32) tokens from hist_start[r] (int64) on, the first prompt_len[r]
+    (int32; None: none) of them the prompt.  repetition, frequency, presence:
+    float32 per row, or None (1, 0, 0).  bias_offsets int64 [rows + 1],
+    bias_ids int32, bias_values float32: the rows' biases one after the other.
+    mask: int32 [..., ceil(V / 32)], bit v % 32 of word v / 32 allows entry v;
+    mask_row: int32 per row, -1 for none (None: the one mask, or one per row).
+    out: where the result goes (z itself for in place), or None.
+
+    Returns out, [..., V] of z's dtype."""
+    rows, V = _check_rows(z, "z")
+    code, dev = _dtype_code(z.dtype), z.device
+    rules = _logits_rules(rows, V, dev, tokens, hist_start, hist_len, prompt_len, repetition, frequency, presence,
+                          bias_offsets, bias_ids, bias_values, mask, mask_row)
+    if out is not None:
+        if out.shape != z.shape:
+            raise ValueError("out must have the shape of z")
+        _device_array(out, "out", z.dtype, z.numel(), dev)
+    with _guard(dev, stream):
+        if out is None:
+            out = torch.empty_like(z)
+        st = _lib.lib().aal_logits_process(_ptr(z), code, rows, V, C.byref(rules), _ptr(out), _stream(dev, stream))
+    _lib.check(st, "aal_logits_process")
+    return out
+
+
+def aal_logits_process_bwd(grad_out: torch.Tensor, z: torch.Tensor, *, tokens: torch.Tensor | None = None,
+                           hist_start: torch.Tensor | None = None, hist_len: torch.Tensor | None = None,
+                           prompt_len: torch.Tensor | None = None, repetition: torch.Tensor | None = None,
+                           frequency: torch.Tensor | None = None, presence: torch.Tensor | None = None,
+                           bias_offsets: torch.Tensor | None = None, bias_ids: torch.Tensor | None = None,
+                           bias_values: torch.Tensor | None = None, mask: torch.Tensor | None = None,
+                           mask_row: torch.Tensor | None = None, grad_z: torch.Tensor | None = None,
+                           stream=None) -> torch.Tensor:
+    """The gradient through aal_logits_process: from grad_out (with respect to
+    its result) to the gradient with respect to z, the logits that went in.
+    The rules are those of that call.  grad_z: where the gradient goes
+    (grad_out itself for in place), or None.
+
+    Returns grad_z, of grad_out's shape and dtype."""
+    rows, V = _check_rows(z, "z")
+    code, gcode, dev = _dtype_code(z.dtype), _dtype_code(grad_out.dtype), z.device
+    if grad_out.shape != z.shape:
+        raise ValueError("grad_out must have the shape of z")
+    _device_array(grad_out, "grad_out", grad_out.dtype, z.numel(), dev)
+    rules = _logits_rules(rows, V, dev, tokens, hist_start, hist_len, prompt_len, repetition, frequency, presence,
+                          bias_offsets, bias_ids, bias_values, mask, mask_row)
+    if grad_z is not None:
+        if grad_z.shape != z.shape:
+            raise ValueError("grad_z must have the shape of z")
+        _device_array(grad_z, "grad_z", grad_out.dtype, z.numel(), dev)
+    with _guard(dev, stream):
+        if grad_z is None:
+            grad_z = torch.empty_like(grad_out)
+        st = _lib.lib().aal_logits_process_bwd(_ptr(grad_out), gcode, _ptr(z), code, rows, V, C.byref(rules),
+                                               _ptr(grad_z), _stream(dev, stream))
+    _lib.check(st, "aal_logits_process_bwd")
+    return grad_z
 
 
 def aal_stream_probe(srcs, dst: torch.Tensor | None = None, flag: torch.Tensor | None = None, stream=None):

@@ -1,12 +1,7 @@
 // C ABI of libaal: argument validation, workspace carve-up and dispatch.
 // Declarations and the contract of every entry point are in include/aal.h.
-#include "aal.h"
-#include "aal_internal.h"
+#include "aal_api_common.h"
 #include "aal_vp.h"
-
-#include <stdarg.h>
-#include <stdio.h>
-#include <string.h>
 
 #include <atomic>
 
@@ -22,54 +17,7 @@ constexpr uint32_t kKnownFlags = AAL_FLAG_STREAMING | AAL_FLAG_COOPERATIVE;
 
 // A plain per-thread buffer: nothing to construct or destroy at thread or
 // process exit.
-thread_local char g_last_error[512];
-
-void clear_error() { g_last_error[0] = '\0'; }
-
-aal_status_t fail(aal_status_t s, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
-  va_end(ap);
-  return s;
-}
-
-// Finite and > 0, checked on the bit pattern so that no floating-point
-// compilation mode can fold the test away.
-bool positive_finite(float x) {
-  uint32_t u;
-  memcpy(&u, &x, sizeof u);
-  const bool sign = (u >> 31) != 0;
-  const uint32_t expo = (u >> 23) & 0xffu;
-  return !sign && expo != 0xffu && (u & 0x7fffffffu) != 0;
-}
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-// The integer held by an enum argument, read without loading it as the enum
-// type: a C caller may pass any int, and values outside the enumerators are
-// validated here rather than assumed away.
-template <class E>
-int raw(const E& e) {
-  static_assert(sizeof(E) == sizeof(int), "enum arguments are int-sized");
-  int v;
-  memcpy(&v, &e, sizeof v);
-  return v;
-}
-
-bool valid_dtype(int d) { return d == AAL_BF16 || d == AAL_F32; }
-
-aal::DType to_dtype(int d) { return d == AAL_BF16 ? aal::DType::kBf16 : aal::DType::kF32; }
-
-constexpr double kLog2e = 1.4426950408889634073599246810019;
-
-// log2(e)/T as a finite positive float, or 0 if it is not representable.
-float scale_for(float T) {
-  const double s = kLog2e / double(T);
-  if (!(s < 3.0e38)) return 0.f;
-  const float f = float(s);
-  return positive_finite(f) ? f : 0.f;
-}
+thread_local char g_last_error[aal::kErrorTextBytes];
 
 struct CommonIn {
   const void* zd;
@@ -172,6 +120,8 @@ aal_status_t scratch_for_current_device(void** out) {
 }
 
 }  // namespace
+
+char* aal::error_text() { return g_last_error; }
 
 extern "C" {
 

@@ -1,0 +1,118 @@
+// Host-side interfaces of the operators on a target's top logits: extraction
+// of a row's largest logits, the training objectives against such lists, and
+// the processing of logits (biases, penalties, grammar masks).
+#pragma once
+
+#include "aal_internal.h"
+
+namespace aal {
+
+// ------------------------------------------------------------ extraction
+struct TopkArgs {
+  DType in;
+  const void* z;
+  int64_t rows;
+  int V, k;
+  float sc;        // log2(e)/T
+  void* top;       // [rows, k] of the logits' type
+  int32_t* ids;    // [rows, k]
+  float* rest;     // [rows], may be null
+  uint8_t* ws;
+  hipStream_t stream;
+};
+
+size_t topk_workspace_bytes(int64_t rows, int V, int k);
+hipError_t launch_topk(const TopkArgs& a);
+
+// ------------------------------------------- objectives against top lists
+// Per-row results of the row pass and coefficients of the gradient.  64 bytes.
+struct TopRow {
+  float msc, inv_s;   // draft: fl(max * sc), 1 / sum of 2^(z*sc - msc)
+  float mt, inv_zt;   // target: largest t*sct of the list and the remainder, 1 / sum
+  float a_tv, a_eal;  // acceptances
+  float qlt;          // sum of q over the entries (the remainder among them) with q < p
+  float kl;           // KL(p || q) in nats
+  float share;        // p_rest / q_rest, 0 where q_rest = 0
+  int32_t xstar;      // greedy token of the list, -1 for an empty one
+  int32_t flags;      // kTopHas: the list holds any mass; kTopRestBelow: q_rest < p_rest
+  float cR;           // unlisted entries: g = cR 2^(z*sc - msc)
+  float cA, cB;       // listed entries: g = q (q < p ? cA : cB) - cP p + cX [v = x*]
+  float cP, cX;
+};
+static_assert(sizeof(TopRow) == 64, "TopRow layout");
+constexpr int kTopHas = 1, kTopRestBelow = 2;
+
+struct TopLossArgs {
+  DType in, td, gd;        // draft logits, listed logits, gradient
+  const void* zd;
+  const void* top;
+  const int32_t* ids;
+  const float* rest;       // may be null
+  int layout;              // 0 windows, 1 sequences
+  int64_t B;
+  int S, K, V, k;
+  int64_t R, W;            // rows, windows
+  float sc_d, sc_t, inv_t_d;
+  float w_wtv, w_eal, w_kl, w_tv;
+  float* loss;
+  float* terms;            // the rest may be null
+  float* e_tv;
+  float* e_eal;
+  float* accept_tv;
+  float* accept_eal;
+  int32_t* xstar;
+  void* grad;
+  const float* grad_scale;
+  TopRow* stats;           // workspace [R]
+  float2* win;             // workspace [W]: E_tv, E_eal
+  float2* row_loss;        // workspace [R]: KL, windows that contain the row * (1 - a_tv)
+  double* loss_parts;      // workspace [kTopLossParts][4]
+  uint64_t* slots;         // workspace [R][2]: tagged acceptances of the resident schedule
+  unsigned* err;           // workspace: poll time-out flag of the resident schedule
+  bool streaming, coop;
+  hipStream_t stream;
+};
+constexpr int kTopLossParts = 64;
+
+inline size_t top_loss_workspace_bytes(int64_t rows, int64_t windows) {
+  return align256(size_t(rows) * sizeof(TopRow)) + align256(size_t(windows) * sizeof(float2)) +
+         align256(size_t(rows) * sizeof(float2)) + align256(size_t(kTopLossParts) * 4 * sizeof(double)) +
+         align256(size_t(rows) * 2 * sizeof(uint64_t)) + 256;
+}
+
+hipError_t launch_top_loss(const TopLossArgs& a);
+
+// ------------------------------------------------------ logits processing
+struct LogitsRules {
+  const int32_t* tokens;
+  int64_t n_tokens;
+  const int64_t* hist_start;
+  const int32_t* hist_len;
+  const int32_t* prompt_len;   // may be null: nothing but generated tokens
+  const float* repetition;     // may be null: 1
+  const float* frequency;      // may be null: 0
+  const float* presence;       // may be null: 0
+  const int64_t* bias_offsets;
+  const int32_t* bias_ids;
+  const float* bias_values;
+  int64_t n_bias;
+  const uint32_t* mask;
+  int64_t n_masks;
+  const int32_t* mask_row;     // may be null: row r takes mask r (or the only one)
+};
+
+struct LogitsArgs {
+  DType in;                // logits
+  DType gd;                // backward: gradients
+  const void* z;
+  const void* grad_out;    // null: forward
+  void* out;               // processed logits, or the gradient w.r.t. z
+  int64_t rows;
+  int V;
+  LogitsRules rules;
+  hipStream_t stream;
+};
+
+hipError_t launch_logits(const LogitsArgs& a);
+
+}  // namespace aal

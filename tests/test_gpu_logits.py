@@ -1,0 +1,280 @@
+"""aal_logits_process and aal_logits_process_bwd against the fp64 oracle.
+
+Tolerances: the value of an entry takes at most five fp32 roundings (bias,
+division or product, frequency times count, the sum of the two penalties, the
+difference), each half an ulp of a magnitude of at most M = |z| + |bias| (times
+repetition) + frequency c + presence, then one rounding to the result's type:
+3e-7 M, and 2^-8 of the result for bf16.  The gradient has one rounding and
+that of the type.  Entries that nothing bears on are equal bit for bit."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import toplist_oracle as T
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def A():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_24150_amd as lib
+    return lib
+
+
+def make_rules(rows, V, seed, hist=50, bias=3, masks=3, prompt=True):
+    g = torch.Generator().manual_seed(seed)
+    rnd = lambda *s: torch.rand(*s, generator=g)  # noqa: E731
+    r = {}
+    if hist:
+        n = 3 * hist + 5
+        words = torch.randint(0, max(1, V // 7), (n,), generator=g) * 7 % V
+        words[rnd(n) < 0.1] = V - 1
+        words[rnd(n) < 0.05] = V + 3
+        words[rnd(n) < 0.05] = -1
+        r["tokens"] = words.int()
+        r["hist_start"] = torch.randint(0, n, (rows,), generator=g)
+        r["hist_len"] = torch.randint(0, hist + 1, (rows,), generator=g).int()
+        if prompt:
+            r["prompt_len"] = (r["hist_len"] * rnd(rows)).int()
+        r["repetition"] = 0.7 + rnd(rows)
+        r["frequency"] = rnd(rows) - 0.3
+        r["presence"] = rnd(rows)
+    if bias:
+        n = torch.randint(0, bias + 1, (rows,), generator=g)
+        r["bias_offsets"] = torch.cat([n.new_zeros(1), n.cumsum(0)])
+        r["bias_ids"] = torch.randint(-1, V + 1, (int(n.sum()),), generator=g).int()
+        r["bias_values"] = torch.randn(int(n.sum()), generator=g) * 5
+    if masks:
+        r["mask"] = torch.randint(-2 ** 31, 2 ** 31, (masks, (V + 31) // 32), generator=g).int()
+        r["mask"][0] = 0  # a mask that allows nothing
+        r["mask_row"] = torch.randint(-1, masks + 1, (rows,), generator=g).int()
+    return r
+
+
+def dev(rules):
+    return {k: v.cuda() for k, v in rules.items()}
+
+
+def check(A, z, rules, inplace=False, g_dtype=None):
+    """Both directions; z on the host."""
+    rows, V = z.shape
+    host = {k: v.numpy() for k, v in rules.items()}
+    finite = torch.where(torch.isnan(z.float()), 0.0, z.float()).double().numpy()
+    ref = T.process_logits(finite, host)
+    zc = z.cuda()
+    out = A.aal_logits_process(zc.clone() if inplace else zc, **dev(rules), **(dict(out=None)))
+    if inplace:
+        buf = zc.clone()
+        assert A.aal_logits_process(buf, **dev(rules), out=buf) is buf
+        assert torch.equal(buf, out)
+    got = out.cpu()
+    # what bears on an entry, and how large its parts are
+    mags = np.abs(np.where(np.isfinite(finite), finite, 0.0))
+    touched = np.zeros((rows, V), bool)
+    for r in range(rows):
+        seen, times, bias, allowed, rep, freq, pres = T._row_rules(host, r, V)
+        mags[r] = (mags[r] + np.abs(bias)) * max(rep, 1 / rep, 1) + np.abs(freq) * times + abs(pres)
+        touched[r] = seen | (bias != 0) | ~allowed
+    same = torch.from_numpy(~touched)
+    bits = torch.int16 if z.dtype == BF16 else torch.int32
+    assert torch.equal(got.view(bits)[same], z.view(bits)[same])
+    gv = got.double().numpy()
+    ok = np.isfinite(ref)
+    assert np.array_equal(gv[~ok & touched], ref[~ok & touched])
+    tol = 3e-7 * mags + (2.0 ** -8 * np.abs(ref) if z.dtype == BF16 else 0.0)
+    with np.errstate(invalid="ignore"):
+        bad = touched & ok & (np.abs(gv - ref) > tol)
+    assert not bad.any(), (np.argwhere(bad)[:4], gv[bad][:4], ref[bad][:4])
+    # backwards
+    g = torch.randn(rows, V, generator=torch.Generator().manual_seed(1)).to(g_dtype or z.dtype)
+    gin = A.aal_logits_process_bwd(g.cuda(), zc, **dev(rules)).cpu()
+    gref = T.process_logits_bwd(g.double().numpy(), finite, host)
+    err = np.abs(gin.double().numpy() - gref)
+    assert (err <= (2.0 ** -8 if g.dtype == BF16 else 2e-7) * np.abs(gref)).all()
+    buf = g.cuda()
+    A.aal_logits_process_bwd(buf, zc, **dev(rules), grad_z=buf)
+    assert torch.equal(buf.cpu(), gin)
+
+
+def logits(rows, V, dtype, seed=0):
+    z = torch.randn(rows, V, generator=torch.Generator().manual_seed(seed)) * 4
+    z[torch.rand(rows, V, generator=torch.Generator().manual_seed(seed + 1)) < 0.02] = -math.inf
+    z[:, :: 11] = 0.0
+    return z.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("rows,V", [(1, 1), (3, 5), (4, 31), (5, 33), (7, 1000), (6, 1027), (3, 8192), (3, 16387),
+                                    (2, 32768), (2, 50001), (2, 128256), (400, 65)])
+def test_shapes(A, rows, V, dtype):
+    check(A, logits(rows, V, dtype, V), make_rules(rows, V, V + 1), inplace=True)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("parts", ["none", "history", "bias", "mask", "history+mask", "bias+mask", "no prompt"])
+def test_parts(A, parts, dtype):
+    rules = make_rules(6, 20003, 2, hist=300 if "history" in parts or parts == "no prompt" else 0,
+                       bias=40 if "bias" in parts else 0, masks=3 if "mask" in parts else 0, prompt=parts != "no prompt")
+    check(A, logits(6, 20003, dtype), rules, inplace=True)
+    for left_out in ("repetition", "frequency", "presence"):
+        if left_out in rules:
+            check(A, logits(6, 20003, dtype), {k: v for k, v in rules.items() if k != left_out})
+
+
+@pytest.mark.parametrize("z_dtype,g_dtype", [(BF16, F32), (F32, BF16)])
+def test_gradient_types(A, z_dtype, g_dtype):
+    check(A, logits(5, 3001, z_dtype), make_rules(5, 3001, 3, hist=200, bias=20), g_dtype=g_dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("bias", [0, 5])
+def test_long_histories_of_few_words(A, dtype, bias):
+    # counts around what 15 bits hold, of one token and of neighbours
+    V = 40000
+    for n in (32766, 32767, 32768, 70001):
+        rules = make_rules(3, V, 4, hist=0, bias=bias, masks=0)
+        words = torch.full((n + 10,), 17)
+        words[n // 2:] = 16
+        words[-10:] = V - 1
+        rules.update(tokens=words.int(), hist_start=torch.tensor([0, 10, 0]),
+                     hist_len=torch.tensor([n, n, n + 10]).int(), prompt_len=torch.tensor([0, 0, 10]).int(),
+                     repetition=torch.tensor([1.0, 1.1, 1.2]), frequency=torch.tensor([1e-4, 0.0, 2e-4]),
+                     presence=torch.tensor([0.0, 0.5, 0.25]))
+        check(A, logits(3, V, dtype), rules)
+        rules["hist_start"] = torch.zeros(3, dtype=torch.int64)
+        rules["tokens"] = torch.full((n + 10,), 17).int()
+        check(A, logits(3, V, dtype), rules)
+
+
+def test_ranges_outside_the_arrays_are_cut(A):
+    V = 500
+    rules = make_rules(4, V, 5, hist=20, bias=4, masks=2)
+    n = len(rules["tokens"])
+    rules["hist_start"] = torch.tensor([-5, n - 3, n + 10, 0])
+    rules["hist_len"] = torch.tensor([10, 50, 3, -2]).int()
+    rules["prompt_len"] = torch.tensor([99, -1, 0, 2]).int()
+    rules["mask_row"] = torch.tensor([7, -9, 1, 0]).int()
+    check(A, logits(4, V, F32), rules)
+    off = dev(rules)
+    off["bias_offsets"] = torch.tensor([-4, 1 << 40, 0, 3, 1], device="cuda")  # reads stay inside; the result is any
+    A.aal_logits_process(logits(4, V, F32).cuda(), **off)
+    torch.cuda.synchronize()
+
+
+def test_blocked_entries_may_hold_anything(A):
+    V = 2003
+    rules = make_rules(2, V, 6, hist=40, bias=0, masks=1)
+    rules["mask"] = torch.full((1, (V + 31) // 32), 0x55555555).int()
+    rules["mask_row"] = torch.zeros(2, dtype=torch.int32)
+    for dtype in (BF16, F32):
+        z = logits(2, V, dtype)
+        z[:, 1::4], z[:, 3::4] = math.nan, math.inf
+        out = A.aal_logits_process(z.cuda(), **dev(rules)).cpu()
+        assert (out[:, 1::2] == -math.inf).all() and not torch.isnan(out).any()
+        g = torch.full((2, V), math.nan, dtype=dtype)
+        g[:, ::2] = 1.0
+        gin = A.aal_logits_process_bwd(g.cuda(), z.cuda(), **dev(rules)).cpu()
+        assert (gin[:, 1::2] == 0).all() and not torch.isnan(gin).any()
+
+
+def test_masks_without_rows(A):
+    V = 777
+    z = logits(3, V, F32)
+    m = torch.randint(-2 ** 31, 2 ** 31, (3, 25), generator=torch.Generator().manual_seed(3)).int()
+    check(A, z, {"mask": m})
+    check(A, z, {"mask": m[:1].contiguous()})
+    with pytest.raises(ValueError):
+        A.aal_logits_process(z.cuda(), mask=m[:2].contiguous().cuda())
+
+
+def test_empty_histories_and_biases(A):
+    z = logits(3, 100, F32).cuda()
+    out = A.aal_logits_process(z, tokens=torch.zeros(0, dtype=torch.int32, device="cuda"),
+                               hist_start=torch.zeros(3, dtype=torch.int64, device="cuda"),
+                               hist_len=torch.zeros(3, dtype=torch.int32, device="cuda"),
+                               presence=torch.ones(3, device="cuda"),
+                               bias_offsets=torch.zeros(4, dtype=torch.int64, device="cuda"),
+                               bias_ids=torch.zeros(0, dtype=torch.int32, device="cuda"),
+                               bias_values=torch.zeros(0, device="cuda"))
+    assert torch.equal(out, z)
+
+
+def test_writes_nothing_outside(A):
+    for dtype in (BF16, F32):
+        for V in (1001, 16387, 4096):
+            rules = dev(make_rules(3, V, 8, hist=60))
+            pad = 64
+            buf = torch.full((2 * pad + 3 * V,), 7.0, dtype=dtype, device="cuda")
+            out = buf[pad:pad + 3 * V].view(3, V)
+            A.aal_logits_process(logits(3, V, dtype).cuda(), **rules, out=out)
+            assert (buf[:pad] == 7).all() and (buf[pad + 3 * V:] == 7).all()
+
+
+def test_offsets_past_32_bits(A):
+    rows, V = 16800, 128256
+    z = torch.empty(rows, V, dtype=BF16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))
+    rules = dev(make_rules(rows, V, 9, hist=64, bias=0, masks=3))
+    out = A.aal_logits_process(z, **rules)
+    n = 8
+    tail = {k: v[-n:].contiguous() if v.shape[0] == rows else v for k, v in rules.items()}
+    assert torch.equal(out[-n:], A.aal_logits_process(z[-n:].contiguous(), **tail))
+    check(A, z[-2:].cpu(), {k: (v[-2:].contiguous() if v.shape[0] == rows else v).cpu() for k, v in rules.items()})
+    gin = A.aal_logits_process_bwd(out, z, **rules)
+    assert torch.equal(gin[-n:], A.aal_logits_process_bwd(out[-n:].contiguous(), z[-n:].contiguous(), **tail))
+
+
+def test_on_another_stream_and_in_a_graph(A):
+    z = logits(5, 50001, BF16).cuda()
+    rules = dev(make_rules(5, 50001, 10, hist=500))
+    want = A.aal_logits_process(z, **rules)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = A.aal_logits_process(z, **rules, stream=s)
+    s.synchronize()
+    assert torch.equal(want, got)
+    buf = z.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cap = A.aal_logits_process(buf, **rules)
+        cap2 = A.aal_logits_process_bwd(cap, buf, **rules)
+    for i in range(3):
+        buf.copy_(torch.roll(z, i, 1))
+        graph.replay()
+        torch.cuda.synchronize()
+        ref = A.aal_logits_process(buf, **rules)
+        assert torch.equal(cap, ref)
+        assert torch.equal(cap2.nan_to_num(), A.aal_logits_process_bwd(ref, buf, **rules).nan_to_num())
+
+
+def test_refusals(A):
+    z = logits(3, 100, F32).cuda()
+    rules = dev(make_rules(3, 100, 1))
+    without = lambda *names: {k: v for k, v in rules.items() if k not in names}  # noqa: E731
+    for bad in (without("tokens"), without("hist_len"), without("hist_start"), without("bias_ids"),
+                without("bias_offsets"), without("mask"), dict(rules, tokens=rules["tokens"].long()),
+                dict(rules, hist_start=rules["hist_start"].int()), dict(rules, hist_len=rules["hist_len"][:2]),
+                dict(rules, repetition=rules["repetition"].double()), dict(rules, mask=rules["mask"][:, :3]),
+                dict(rules, mask_row=rules["mask_row"].cpu()), dict(rules, bias_offsets=rules["bias_offsets"][:3]),
+                dict(rules, bias_values=torch.zeros(rules["bias_ids"].numel() + 1, device="cuda")), dict(rules, out=torch.empty(3, 99, device="cuda")),
+                dict(rules, out=torch.empty(3, 100, dtype=BF16, device="cuda"))):
+        with pytest.raises(ValueError):
+            A.aal_logits_process(z, **bad)
+    with pytest.raises(ValueError):
+        A.aal_logits_process(z.t(), **rules)
+    with pytest.raises(ValueError):
+        A.aal_logits_process(z[:0], **rules)
+    with pytest.raises(TypeError):
+        A.aal_logits_process(z.half(), **rules)
+    with pytest.raises(ValueError):
+        A.aal_logits_process_bwd(z[:2], z, **rules)
+    with pytest.raises(TypeError):
+        A.aal_logits_process_bwd(z.half(), z, **rules)
+    with pytest.raises(A.AalError):
+        A.aal_logits_process(torch.zeros(301, device="cuda")[1:].view(3, 100), **rules)
