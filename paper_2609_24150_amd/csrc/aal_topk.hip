@@ -4,19 +4,23 @@
 //   order: v before w iff z_v > z_w, or z_v = z_w and v < w
 //   rest  = ln sum_{v not among the k} exp(z_v / T)
 //
-// One workgroup per row.  k_topk_rows reads the row once: a thread cuts its
-// vectors into eight groups and keeps of each the largest logit and the sum
-// of 2^(z sc - that) in registers.  k groups hold a logit at least as large as
-// the k-th largest of the groups' maxima, so a threshold t that k to 1.25 k + 16
-// maxima reach (found by bisection over whole numbers that order as logits,
-// one ballot count per group and step) is passed by all of the k largest and
-// by few others; the groups that reach t, a few hundred vectors, are read
-// again, their entries from t on are ranked by counting.  The remainder is the sum of
-// the groups below t and of the entries not taken: never a difference of sums.
+// One workgroup per row, which reads it once.  k_topk_rows cuts the row into lines of up
+// to four vectors and keeps of each the largest logit and the sum of 2^(z sc - that) in
+// a register of a thread.  k lines hold a logit at least as large as the k-th
+// largest of the lines' maxima, so a threshold t that k maxima reach is passed
+// by all of the k largest and by few others; it is found by bisection over whole
+// numbers that order as logits, one ballot count per line and step, in every
+// wave for its share of k.  The lines that reach t are read again (k = 64 of
+// 128,256: 2% of the row), their entries from t on sorted.  The remainder is
+// the sum of the lines below t and of the entries not taken: never a
+// difference of sums, so it keeps its digits where the list has nearly all mass.
 // k_topk_short, for rows of up to 16 logits per thread, bisects over the logits.
-// Where ties put more entries at t than the candidates' list holds (rows of
-// few distinct values), the workgroup takes select_slowly, a radix select
-// over the row that is right for everything.
+// Where ties or clusters put more entries at t than the candidates' list holds
+// (rows of few distinct values, rows with fewer than k finite ones), the
+// workgroup takes select_slowly, a radix select over the row that is right for everything.
+//
+// Bound by memory where rows are long: 14,336 rows of 128,256 bf16, k = 64: 578
+// us, 6.4 TB/s, 91% of what a lone read of them takes (k = 8 95%, k = 256 75%: sorting).
 #include "aal_device.h"
 #include "aal_rowops.h"
 #include "aal_toplist.h"
@@ -25,8 +29,6 @@ namespace aal {
 namespace {
 
 constexpr int kTopkMax = 512;
-constexpr int kCap = 1024;     // candidates, and groups read again
-constexpr int kGroups = 8;     // groups of a thread
 constexpr float kLn2 = 0.693147180559945309417f;
 
 // A whole number that orders as the logits do, -0 as +0: 16 bits for bf16
@@ -43,13 +45,26 @@ __device__ __forceinline__ float key_logit(uint32_t key) {
   return __builtin_bit_cast(float, key ^ ((key >> 31) ? 0x80000000u : key_bits<TI>() == 16 ? 0xffff0000u : 0xffffffffu));
 }
 
+// A candidate as one whole number of 63 bits: larger for a larger logit, then
+// for a lower index; the lowest bit tells -0, which has the key of +0.  Read as a
+// double it is positive, finite and normal (for every logit that is no NaN), so that it
+// compares at the rate of doubles, four times that of 64-bit whole numbers.
+__device__ __forceinline__ uint64_t entry_of(uint32_t key, int v, bool neg_zero) {
+  return (uint64_t(key) << 31) | ((0x3fffffffu - uint32_t(v)) << 1) | (neg_zero ? 1u : 0u);
+}
+__device__ __forceinline__ uint32_t entry_key(uint64_t e) { return uint32_t(e >> 31); }
+__device__ __forceinline__ int entry_index(uint64_t e) { return int(0x3fffffffu - (uint32_t(e) << 1 >> 2)); }
+
+// CAP: the most candidates, and groups read again, that fit.
+template <int CAP_>
 struct TopkShared {
-  alignas(16) uint64_t cand[kCap];    // (key, ~index) of the candidates
-  alignas(16) uint64_t sorted[kCap];  // the same by rank
-  uint16_t queue[kCap];               // groups read again
-  uint32_t hist[256];
+  static constexpr int CAP = CAP_;
+  alignas(16) uint64_t cand[CAP];    // entry_of() of the candidates
+  alignas(16) uint64_t sorted[CAP];  // the same by rank
+  uint16_t queue[CAP];               // groups read again
+  alignas(16) uint32_t hist[256];
   float f[16];
-  int i[2][16];
+  int i[1][16];
   uint32_t n, digit, need;
 };
 
@@ -57,7 +72,7 @@ struct TopkParams {
   const void* z;
   int64_t rows;
   int V, k;
-  float sc;
+  float sc, inv_t;
   void* top;
   int32_t* ids;
   float* rest;
@@ -76,36 +91,25 @@ __device__ __forceinline__ float block_max(float v, float* sh) {
   return m;
 }
 
-// The number of the block's keys (N per thread) that reach t, to every thread.
-// `turn` alternates between calls.
-template <int WAVES, int N>
-__device__ __forceinline__ int count_from(const uint32_t (&key)[N], uint32_t t, int (*sh)[16], int turn) {
-  int c = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) c += __popcll(__builtin_amdgcn_ballot_w64(key[i] >= t));
-  if constexpr (WAVES == 1) return c;
-  if ((threadIdx.x & (kWave - 1)) == 0) sh[turn][threadIdx.x / kWave] = c;
-  __syncthreads();
-  c = 0;
-#pragma unroll
-  for (int i = 0; i < WAVES; ++i) c += sh[turn][i];
-  return c;
-}
-
-// A threshold that at least `k` of the block's keys reach, and at most k + k/4
-// + 16 unless ties forbid it; `top` is the largest key.  Keys of 0 are none.
+// A threshold that at least k of the block's values (N per thread) reach, and
+// few more: every wave bisects for one that its share of k reaches, without a
+// barrier, and the lowest of them serves for all.  -inf where some wave has
+// fewer finite values than its share.
 template <class TI, int WAVES, int N>
-__device__ __forceinline__ uint32_t threshold(const uint32_t (&key)[N], int k, uint32_t top, int (*sh)[16]) {
+__device__ __forceinline__ float threshold(const float (&x)[N], int k, float top, float* sh) {
   constexpr int kShift = 32 - key_bits<TI>();
-  uint32_t lo = 0, hi = (top >> kShift) + 1u;  // lo is reached by k keys or all, hi by none (1 past the top)
-  const int most = k + k / 4 + 16;
-  int turn = 0;
-  // the first probe two octaves below the top, where k keys mostly are above: less to bisect
-  uint32_t probe = hi > (2u << (23 - kShift)) ? hi - (2u << (23 - kShift)) : hi / 2;
-  while (hi - lo > 1u) {
-    const int c = count_from<WAVES>(key, probe << kShift, sh, turn);
-    turn ^= 1;
-    if (c >= k) {
+  const uint32_t least = order_key<TI>(kNegInf) >> kShift;
+  uint32_t lo = least, hi = (order_key<TI>(top) >> kShift) + 1u;  // lo is reached by the share or all, hi by none
+  const int share = (k + WAVES - 1) / WAVES, most = share + share / 8 + 1;
+  // the first probe two octaves below the top, where the share mostly is above: less to bisect
+  const uint32_t octaves = 2u << (23 - kShift);
+  uint32_t probe = hi > least + octaves ? hi - octaves : lo + (hi - lo) / 2;
+  while (hi > lo + 1u) {
+    const float t = key_logit<TI>(probe << kShift);
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) c += __popcll(__builtin_amdgcn_ballot_w64(x[i] >= t));
+    if (c >= share) {
       lo = probe;
       if (c <= most) break;
     } else {
@@ -113,52 +117,119 @@ __device__ __forceinline__ uint32_t threshold(const uint32_t (&key)[N], int k, u
     }
     probe = lo + (hi - lo) / 2;
   }
-  __syncthreads();
-  return lo << kShift;
+  float t = key_logit<TI>(lo << kShift);
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & (kWave - 1)) == 0) sh[threadIdx.x / kWave] = t;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) t = fminf(t, sh[i]);
+    __syncthreads();
+  }
+  return t;
 }
 
-// Ranks the n >= k candidates, writes the first k and returns the sum of 2^(z sc - msc) over
-// the others (this thread's share).
-template <class TI, int BLK>
-__device__ __forceinline__ float write_ranked(const TopkParams& p, int64_t row, int n, float msc, TopkShared& sh) {
-  const int even = (n + 1) & ~1;
-  if (threadIdx.x == 0 && even != n) sh.cand[n] = 0;  // below every candidate
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += BLK) {
-    const uint64_t mine = sh.cand[i];
-    int rank = 0;
-    for (int j = 0; j < even; j += 2) {
-      const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(&sh.cand[j]);
-      rank += (two.x > mine) + (two.y > mine);
+// The bucket of a candidate among 256 over [t, m], larger logits first: monotone in the logit.
+template <class TI>
+__device__ __forceinline__ int bucket_of(uint64_t e, float t, float scale) {
+  return 255 - min(255, int((key_logit<TI>(entry_key(e)) - t) * scale));
+}
+
+// Sorts the n candidates, all in [t, m], writes the first k and returns the sum of
+// 2^(z sc - msc) over the others (this thread's share).  Up to 64 are ranked by
+// counting; more go through 256 buckets and are ranked in theirs (lists of
+// 256 of 14,336 rows of 4,000: 207 us with counting alone).
+template <class TI, int BLK, class Sh>
+__device__ __forceinline__ float write_ranked(const TopkParams& p, int64_t row, int n, float t, float m, float sc,
+                                              float msc, Sh& sh) {
+  const uint64_t* sorted = sh.sorted;
+  if (n <= kWave) {
+    if (int(threadIdx.x) < (n & 1)) sh.cand[n] = 0;  // below every candidate
+    __syncthreads();
+    if (int(threadIdx.x) < n) {
+      const uint64_t mine = sh.cand[threadIdx.x];
+      const double at = __builtin_bit_cast(double, mine);
+      int rank = 0;
+#pragma unroll 4
+      for (int j = 0; j < n; j += 2) {
+        const double2 two = *reinterpret_cast<const double2*>(&sh.cand[j]);
+        rank += (two.x > at) + (two.y > at);
+      }
+      sh.sorted[rank] = mine;
     }
-    sh.sorted[rank] = mine;
+  } else {
+    const float range = m - t;
+    const float scale = range > 0.f && range < 1e38f ? 255.f / range : 0.f;  // 0: one bucket
+    const float from = scale > 0.f ? t : 0.f;
+    for (int i = threadIdx.x; i < 256; i += BLK) sh.hist[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += BLK)
+      atomicAdd(&sh.hist[scale > 0.f ? bucket_of<TI>(sh.cand[i], from, scale) : 0], 1u);
+    __syncthreads();
+    if (threadIdx.x < kWave) {  // where each bucket starts
+      uint4& mine = reinterpret_cast<uint4*>(sh.hist)[threadIdx.x];
+      const uint4 c = mine;
+      int end = int(c.x + c.y + c.z + c.w);
+      const int own = end;
+      for (int off = 1; off < kWave; off <<= 1) {
+        const int o = __shfl_up(end, off, kWave);
+        if (int(threadIdx.x) >= off) end += o;
+      }
+      const uint32_t s0 = uint32_t(end - own);
+      mine = make_uint4(s0, s0 + c.x, s0 + c.x + c.y, s0 + c.x + c.y + c.z);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += BLK) {
+      const uint64_t e = sh.cand[i];
+      sh.sorted[atomicAdd(&sh.hist[scale > 0.f ? bucket_of<TI>(e, from, scale) : 0], 1u)] = e;
+    }
+    __syncthreads();
+    // a bucket's entries now end where the next one's start
+    for (int i = threadIdx.x; i < n; i += BLK) {
+      const uint64_t e = sh.sorted[i];
+      const int b = scale > 0.f ? bucket_of<TI>(e, from, scale) : 0;
+      const int first = b > 0 ? int(sh.hist[b - 1]) : 0, end = int(sh.hist[b]);
+      int rank = first;
+      for (int j = first; j < end; ++j) rank += sh.sorted[j] > e;
+      sh.cand[rank] = e;
+    }
+    sorted = sh.cand;
   }
   __syncthreads();
-  const int64_t e0 = row * int64_t(p.V), o0 = row * int64_t(p.k);
+  const int64_t o0 = row * int64_t(p.k);
   float s = 0.f;
   for (int j = threadIdx.x; j < n; j += BLK) {
-    const uint64_t key = sh.sorted[j];
+    const uint64_t key = sorted[j];
     if (j < p.k) {
-      const int v = int(0xffffffffu - uint32_t(key));
-      p.ids[o0 + j] = v;
-      static_cast<typename TI::storage*>(p.top)[o0 + j] = static_cast<const typename TI::storage*>(p.z)[e0 + v];
+      p.ids[o0 + j] = entry_index(key);
+      const uint32_t b = key & 1u ? 0x80000000u : __builtin_bit_cast(uint32_t, key_logit<TI>(entry_key(key)));
+      static_cast<typename TI::bits*>(p.top)[o0 + j] = typename TI::bits(key_bits<TI>() == 16 ? b >> 16 : b);
     } else {
-      s += ex2(__builtin_fmaf(key_logit<TI>(uint32_t(key >> 32)), p.sc, -msc));
+      s += ex2(__builtin_fmaf(key_logit<TI>(entry_key(key)), sc, -msc));
     }
   }
   return s;
 }
 
-__device__ __forceinline__ void add_candidate(TopkShared& sh, uint32_t key, int v) {
-  const uint32_t slot = atomicAdd(&sh.n, 1u);
-  if (slot < uint32_t(kCap)) sh.cand[slot] = (uint64_t(key) << 32) | (0xffffffffu - uint32_t(v));
+// Adds the entries of x (indices v0 on) that `take` has a bit for.
+template <class TI, class Sh, int E>
+__device__ __forceinline__ void add_candidates(Sh& sh, const float (&x)[E], int v0, uint32_t take) {
+  if (take == 0u) return;
+  uint32_t slot = atomicAdd(&sh.n, uint32_t(__popc(take)));
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (take >> e & 1u) {
+      if (slot < uint32_t(Sh::CAP))
+        sh.cand[slot] = entry_of(order_key<TI>(x[e]), v0 + e, __builtin_bit_cast(uint32_t, x[e]) == 0x80000000u);
+      ++slot;
+    }
 }
 
 // Any row: the k-th largest key digit by digit, then a pass in index order that
 // collects the larger entries and the first of its ties.  Returns this thread's share of the
 // others' sum of 2^(z sc - msc).
-template <class TI, bool VEC, int BLK>
-__device__ __attribute__((noinline)) float select_slowly(const TopkParams& p, int64_t row, float msc, TopkShared& sh) {
+template <class TI, bool VEC, int BLK, class Sh>
+__device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row, float sc, float msc, Sh& sh,
+                                               float& t) {
   using Rv = RowVecs<TI, VEC>;
   constexpr int E = Rv::E;
   constexpr int WV = BLK / kWave;
@@ -193,6 +264,7 @@ __device__ __attribute__((noinline)) float select_slowly(const TopkParams& p, in
     prefix |= sh.digit << shift;
     need = sh.need;  // of the entries whose key starts with `prefix`
   }
+  t = key_logit<TI>(prefix);
   if (tid == 0) sh.n = 0;
   uint32_t ties = 0;  // before this round
   float s = 0.f;
@@ -225,196 +297,267 @@ __device__ __attribute__((noinline)) float select_slowly(const TopkParams& p, in
       ties += uint32_t(sh.i[0][i]);
     }
     if (gi >= rv.ng) continue;
+    uint32_t take = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int v = rv.index(gi, e);
       if (v < 0 || v >= p.V) continue;
       const bool tie = key[e] == prefix;
       if (key[e] > prefix || (tie && at < need))
-        add_candidate(sh, key[e], v);
+        take |= 1u << e;
       else
-        s += ex2(__builtin_fmaf(x[e], p.sc, -msc));
+        s += ex2(__builtin_fmaf(x[e], sc, -msc));
       at += tie;
     }
+    add_candidates<TI>(sh, x, rv.index(gi, 0), take);
   }
   __syncthreads();
   return s;
 }
 
-template <int WAVES>
-__device__ __forceinline__ void write_rest(const TopkParams& p, int64_t row, float s, float msc, TopkShared& sh) {
+// The reference of a row's sums.  All entries of a row whose largest is below
+// -1e30 / sc differ by more than any exponential holds or not at all: any power of two that
+// keeps the products finite takes the place of sc there.
+struct RowScale {
+  float sc, msc;
+};
+__device__ __forceinline__ RowScale row_scale(float m, float sc) {
+  const float s = m * sc < -1e30f ? 0x1p-64f : sc;
+  return {s, m == kNegInf ? 0.f : m * s};
+}
+
+template <int WAVES, class Sh>
+__device__ __forceinline__ void write_rest(const TopkParams& p, int64_t row, float s, float m, RowScale rs,
+                                           Sh& sh) {
   if (p.rest == nullptr) return;
   s = block_sum<WAVES>(s, sh.f);
-  if (threadIdx.x == 0) p.rest[row] = s > 0.f ? (msc + __log2f(s)) * kLn2 : kNegInf;
+  if (threadIdx.x != 0) return;
+  const float at = rs.sc == p.sc ? rs.msc * kLn2 : m * p.inv_t;
+  p.rest[row] = s > 0.f ? __builtin_fmaf(__log2f(s), kLn2, at) : kNegInf;
 }
 
 // Rows of up to 16 BLK logits: all of them in registers.
-template <class TI, bool VEC, int BLK>
+template <class TI, bool VEC, int BLK, int CAP>
 __global__ __launch_bounds__(BLK) void k_topk_short(TopkParams p) {
   using Rv = RowVecs<TI, VEC>;
   constexpr int E = Rv::E;
   constexpr int WV = BLK / kWave;
   constexpr int U = 16 / E + (VEC ? 0 : 1);  // a row may start and end inside a vector
-  __shared__ TopkShared sh;
+  __shared__ TopkShared<CAP> sh;
   const int64_t row = blockIdx.x;
   const Rv rv(row, p.rows, p.V);
   u32x4 w[1][U];
   rv.load({p.z}, int(threadIdx.x), BLK, w);
-  uint32_t key[U * E];
+  float x[U][E], y[U * E];
+  rv.unpack(w[0], x);
   float m = kNegInf;
   if (threadIdx.x == 0) sh.n = 0;
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int gi = int(threadIdx.x) + u * BLK;
-    float x[E];
-    TI::unpack(to_uint4(w[0][u]), x);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int v = rv.index(gi, e);
-      m = fmaxf(m, x[e]);
-      key[u * E + e] = gi < rv.ng && (VEC || (v >= 0 && v < p.V)) ? order_key<TI>(x[e]) : 0u;
-    }
-  }
-  m = block_max<WV>(m, sh.f);
-  const float msc = m == kNegInf ? 0.f : m * p.sc;
-  const uint32_t t = threshold<TI, WV>(key, p.k, order_key<TI>(m), sh.i);
-  float s = 0.f;
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const uint32_t c = key[u * E + e];
-      if (c == 0u) continue;
-      if (c >= t)
-        add_candidate(sh, c, rv.index(int(threadIdx.x) + u * BLK, e));
-      else
-        s += ex2(__builtin_fmaf(key_logit<TI>(c), p.sc, -msc));
+      y[u * E + e] = x[u][e];
+      m = fmaxf(m, x[u][e]);
     }
+  m = block_max<WV>(m, sh.f);
+  const RowScale rs = row_scale(m, p.sc);
+  float t = threshold<TI, WV>(y, p.k, m, sh.f);
+  float s = 0.f;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int gi = int(threadIdx.x) + u * BLK;
+    uint32_t take = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int v = rv.index(gi, e);
+      if (x[u][e] >= t)
+        take |= gi < rv.ng && v >= 0 && v < p.V ? 1u << e : 0u;
+      else
+        s += ex2(__builtin_fmaf(x[u][e], rs.sc, -rs.msc));
+    }
+    add_candidates<TI>(sh, x[u], rv.index(gi, 0), take);
+  }
   __syncthreads();
   int n = int(sh.n);
-  if (n > kCap) {
-    s = select_slowly<TI, VEC, BLK>(p, row, msc, sh);
+  if (n > CAP) {
+    s = select_slowly<TI, VEC, BLK>(p, row, rs.sc, rs.msc, sh, t);
     n = p.k;
   }
-  s += write_ranked<TI, BLK>(p, row, n, msc, sh);
-  write_rest<WV>(p, row, s, msc, sh);
+  s += write_ranked<TI, BLK>(p, row, n, t, m, rs.sc, rs.msc, sh);
+  write_rest<WV>(p, row, s, m, rs, sh);
 }
 
-// Longer rows: a group of a thread is `rounds` rounds of U vectors.
-template <class TI, bool VEC, int U, int BLK>
-__global__ __launch_bounds__(BLK) void k_topk_rows(TopkParams p, int rounds) {
+// The largest, or the sum, over the L lanes that share a line (L = 1, 2, 4).
+template <int L>
+__device__ __forceinline__ float line_max(float v) {
+  if constexpr (L >= 2) v = fmaxf(v, dppm<0xB1>(v));
+  if constexpr (L >= 4) v = fmaxf(v, dppm<0x4E>(v));
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float line_sum(float v) {
+  if constexpr (L >= 2) v += dppm<0xB1>(v);
+  if constexpr (L >= 4) v += dppm<0x4E>(v);
+  return v;
+}
+// Longer rows.  In every round a thread loads U vectors, each U adjacent lanes
+// a line of U adjacent vectors at every step, and the lane takes the line of
+// the step that it is in the U lanes.  A group of a thread is its lines of `rounds` rounds.
+template <class TI, bool VEC, int U, int BLK, int NG, int CAP, bool ONE>
+__global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_) {
   using Rv = RowVecs<TI, VEC>;
   constexpr int E = Rv::E;
   constexpr int WV = BLK / kWave;
-  __shared__ TopkShared sh;
+  __shared__ TopkShared<CAP> sh;
   const int64_t row = blockIdx.x;
   const Rv rv(row, p.rows, p.V);
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
-  float gm[kGroups], gs[kGroups];
-  uint32_t key[kGroups];
+  const int rounds = ONE ? 1 : rounds_;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave, mu = tid & (U - 1);
+  float gm[NG], gs[NG];  // of each group: the largest, the sum of 2^(z sc - max(largest sc, -1e30))
   float m = kNegInf;
   if (tid == 0) sh.n = 0;
 #pragma unroll
-  for (int g = 0; g < kGroups; ++g) {
-    LseState st = lse_init();
+  for (int g = 0; g < NG; ++g) {
+    gm[g] = kNegInf;
+    gs[g] = 0.f;
     for (int r = 0; r < rounds; ++r) {
-      const int base = (g * rounds + r) * U * BLK + tid;
+      const int base = (g * rounds + r) * U * BLK;
       if (base >= rv.ng) break;
       u32x4 w[1][U];
-      float x[U][E];
-      rv.load({p.z}, base, BLK, w);
+      float x[U][E], lm = kNegInf, ls = 0.f;
+      rv.load({p.z}, base + tid, BLK, w);
       rv.unpack(w[0], x);
-      lse_fold(st, x, p.sc);
-    }
-    gm[g] = st.m;
-    gs[g] = st.s;
-    key[g] = g * rounds * U * BLK + tid < rv.ng ? order_key<TI>(st.m) : 0u;
-    m = fmaxf(m, st.m);
-  }
-  m = block_max<WV>(m, sh.f);
-  const float msc = m == kNegInf ? 0.f : m * p.sc;
-  const uint32_t t = threshold<TI, WV>(key, p.k, order_key<TI>(m), sh.i);
-  // the groups that reach t, in an order that does not depend on timing; the sums of the others
-  float s = 0.f;
-  int mine = 0;
 #pragma unroll
-  for (int g = 0; g < kGroups; ++g) {
-    if (key[g] == 0u) continue;
-    if (key[g] >= t)
-      ++mine;
-    else if (gm[g] != kNegInf)
-      s += gs[g] * ex2(gm[g] * p.sc - msc);
-  }
-  int before = mine;
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int o = __shfl_up(before, off, kWave);
-    if (lane >= off) before += o;
-  }
-  if (lane == kWave - 1) sh.i[0][wv] = before;
-  __syncthreads();
-  int at = before - mine, nq = 0;
+      for (int u = 0; u < U; ++u) {
+        float um = x[u][0];
 #pragma unroll
-  for (int i = 0; i < WV; ++i) {
-    if (i < wv) at += sh.i[0][i];
-    nq += sh.i[0][i];
-  }
-  int n = kCap + 1;
-  if (nq <= kCap) {
+        for (int e = 1; e < E; ++e) um = fmaxf(um, x[u][e]);
+        um = line_max<U>(um);
+        const float at = fmaxf(um * p.sc, -1e30f);
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g)
-      if (key[g] != 0u && key[g] >= t) sh.queue[at++] = uint16_t(g * BLK + tid);
-    __syncthreads();
-    const int per = rounds * U;  // vectors of a group
-    for (int j = tid; j < nq * per; j += BLK) {
-      const int q = sh.queue[j / per], sub = j % per;
-      const int gi = ((q / BLK) * per + sub) * BLK + q % BLK;
-      if (gi >= rv.ng) continue;
-      float x[E];
-      TI::unpack(to_uint4(rv.load(p.z, gi)), x);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int v = rv.index(gi, e);
-        if (!VEC && (v < 0 || v >= p.V)) continue;
-        const uint32_t c = order_key<TI>(x[e]);
-        if (c >= t)
-          add_candidate(sh, c, v);
-        else
-          s += ex2(__builtin_fmaf(x[e], p.sc, -msc));
+        for (int e = 0; e < E; ++e) x[u][e] = ex2(__builtin_fmaf(x[u][e], p.sc, -at));
+        const float us = line_sum<U>(tree_sum(x[u]));
+        lm = mu == u ? um : lm;
+        ls = mu == u ? us : ls;
+      }
+      if (r == 0) {
+        gm[g] = lm;
+        gs[g] = ls;
+      } else {
+        const float nm = fmaxf(gm[g], lm), at = fmaxf(nm * p.sc, -1e30f);
+        gs[g] = gs[g] * ex2(fmaxf(gm[g] * p.sc, -1e30f) - at) + ls * ex2(fmaxf(lm * p.sc, -1e30f) - at);
+        gm[g] = nm;
       }
     }
-    __syncthreads();
-    n = int(sh.n);
+    m = fmaxf(m, gm[g]);
   }
-  if (n > kCap) {
-    s = select_slowly<TI, VEC, BLK>(p, row, msc, sh);
+  m = block_max<WV>(m, sh.f);
+  const RowScale rs = row_scale(m, p.sc);
+  int n = CAP + 1;
+  float s = 0.f, t = kNegInf;
+  if (rs.sc == p.sc) {
+    t = threshold<TI, WV>(gm, p.k, m, sh.f);
+    // the groups that reach t, in an order that does not depend on timing; the sums of the others
+    int mine = 0;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      if (g * rounds * U * BLK + mu * BLK + tid - mu >= rv.ng) continue;
+      if (gm[g] >= t)
+        ++mine;
+      else
+        s += gs[g] * ex2(fmaxf(gm[g] * p.sc, -1e30f) - rs.msc);
+    }
+    int before = mine;
+    for (int off = 1; off < kWave; off <<= 1) {
+      const int o = __shfl_up(before, off, kWave);
+      if (lane >= off) before += o;
+    }
+    if (lane == kWave - 1) sh.i[0][wv] = before;
+    __syncthreads();
+    int at = before - mine, nq = 0;
+#pragma unroll
+    for (int i = 0; i < WV; ++i) {
+      if (i < wv) at += sh.i[0][i];
+      nq += sh.i[0][i];
+    }
+    if (nq <= CAP) {
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+        if (g * rounds * U * BLK + mu * BLK + tid - mu < rv.ng && gm[g] >= t) sh.queue[at++] = uint16_t(g * BLK + tid);
+      __syncthreads();
+      const int per = rounds * U;  // vectors of a group
+      for (int j = tid; j < nq * per; j += BLK) {
+        const int q = sh.queue[j / per], sub = j % per, qt = q % BLK, qu = qt % U;
+        const int gi = (((q / BLK) * rounds + sub / U) * U + qu) * BLK + qt - qu + sub % U;
+        if (gi >= rv.ng) continue;
+        float x[E];
+        TI::unpack(to_uint4(rv.load(p.z, gi)), x);
+        uint32_t take = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int v = rv.index(gi, e);
+          if (x[e] >= t)
+            take |= VEC || (v >= 0 && v < p.V) ? 1u << e : 0u;
+          else
+            s += ex2(__builtin_fmaf(x[e], rs.sc, -rs.msc));
+        }
+        add_candidates<TI>(sh, x, rv.index(gi, 0), take);
+      }
+      __syncthreads();
+      n = int(sh.n);
+    }
+  }
+  if (n > CAP) {
+    s = select_slowly<TI, VEC, BLK>(p, row, rs.sc, rs.msc, sh, t);
     n = p.k;
   }
-  s += write_ranked<TI, BLK>(p, row, n, msc, sh);
-  write_rest<WV>(p, row, s, msc, sh);
+  s += write_ranked<TI, BLK>(p, row, n, t, m, rs.sc, rs.msc, sh);
+  write_rest<WV>(p, row, s, m, rs, sh);
 }
 
+template <class TI, bool VEC, int U, int BLK, int NG, int CAP>
+void rows_launch(const TopkArgs& a, const TopkParams& p, int ng) {
+  const int64_t round = int64_t(NG) * U * BLK;
+  const dim3 grid{unsigned(a.rows)};
+  if (ng <= round)
+    k_topk_rows<TI, VEC, U, BLK, NG, CAP, true><<<grid, BLK, 0, a.stream>>>(p, 1);
+  else if constexpr (U * BLK == 2048)
+    k_topk_rows<TI, VEC, U, BLK, NG, CAP, false><<<grid, BLK, 0, a.stream>>>(p, int((ng + round - 1) / round));
+}
+
+// Short lists of short rows take one wavefront a row, without barriers and
+// with room for 320 candidates, so that 27 rows fit a CU; the others as many
+// threads as the row fills with eight groups of four vectors.  us per call, against 512
+// threads for every row: 14,336 rows of 8,000 bf16, k = 20, 139 -> 53; 4,096 of
+// 16,032, k = 50, 54 -> 36; 4,096 of 32,000, k = 64, 68 -> 57 (128 threads: 59); 14,336 of
+// 1,000, k = 8, 23 with all logits in registers.  256 threads of 16 groups and 1,024
+// of 4 are slower at 14,336 rows of 128,256 (k = 64: 588 and 640 against 578).
 template <class TI, bool VEC>
 hipError_t launch_vec(const TopkArgs& a) {
-  const TopkParams p{a.z, a.rows, a.V, a.k, a.sc, a.top, a.ids, a.rest};
+  const TopkParams p{a.z, a.rows, a.V, a.k, a.sc, a.inv_t, a.top, a.ids, a.rest};
   const dim3 grid{unsigned(a.rows)};
-  constexpr int kBlk = 512;
-  // vectors that cover a row, at most
-  const int ng = a.V / TI::kVec + (VEC ? 0 : 2);
-  if (a.V <= 16 * 64)
-    k_topk_short<TI, VEC, 64><<<grid, 64, 0, a.stream>>>(p);
+  const int ng = a.V / TI::kVec + (VEC ? 0 : 2);  // vectors that cover a row, at most
+  // lines of U vectors have to be several times k for few of them to reach the threshold
+  auto lines = [&](int U) { return ng / U >= 3 * a.k; };
+  const bool few = a.k <= 128;
+  if (few && a.V <= 16 * 64)
+    k_topk_short<TI, VEC, 64, 320><<<grid, 64, 0, a.stream>>>(p);
+  else if (few && ng <= 1024 && lines(2))
+    rows_launch<TI, VEC, 2, 64, 8, 320>(a, p, ng);
+  else if (few && ng <= 2048 && lines(4))
+    rows_launch<TI, VEC, 4, 64, 8, 320>(a, p, ng);
   else if (a.V <= 16 * 128)
-    k_topk_short<TI, VEC, 128><<<grid, 128, 0, a.stream>>>(p);
+    k_topk_short<TI, VEC, 128, 1024><<<grid, 128, 0, a.stream>>>(p);
   else if (a.V <= 16 * 256)
-    k_topk_short<TI, VEC, 256><<<grid, 256, 0, a.stream>>>(p);
-  else if (a.V <= 16 * kBlk)
-    k_topk_short<TI, VEC, kBlk><<<grid, kBlk, 0, a.stream>>>(p);
-  else if (ng <= kGroups * kBlk)
-    k_topk_rows<TI, VEC, 1, kBlk><<<grid, kBlk, 0, a.stream>>>(p, 1);
-  else if (ng <= kGroups * kBlk * 2)
-    k_topk_rows<TI, VEC, 2, kBlk><<<grid, kBlk, 0, a.stream>>>(p, 1);
+    k_topk_short<TI, VEC, 256, 1024><<<grid, 256, 0, a.stream>>>(p);
+  else if (a.V <= 16 * 512)
+    k_topk_short<TI, VEC, 512, 1024><<<grid, 512, 0, a.stream>>>(p);
+  else if (ng <= 4096 && !lines(4))
+    rows_launch<TI, VEC, 1, 512, 8, 1024>(a, p, ng);
+  else if (ng <= 8192)
+    rows_launch<TI, VEC, 4, 256, 8, 1024>(a, p, ng);
   else
-    k_topk_rows<TI, VEC, 4, kBlk><<<grid, kBlk, 0, a.stream>>>(
-        p, int((int64_t(ng) + kGroups * kBlk * 4 - 1) / (kGroups * kBlk * 4)));
+    rows_launch<TI, VEC, 4, 512, 8, 1024>(a, p, ng);
   return hipGetLastError();
 }
 

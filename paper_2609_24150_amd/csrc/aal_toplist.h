@@ -13,7 +13,7 @@ struct TopkArgs {
   const void* z;
   int64_t rows;
   int V, k;
-  float sc;        // log2(e)/T
+  float sc, inv_t; // log2(e)/T, 1/T
   void* top;       // [rows, k] of the logits' type
   int32_t* ids;    // [rows, k]
   float* rest;     // [rows], may be null

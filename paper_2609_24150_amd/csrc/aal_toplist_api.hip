@@ -105,6 +105,7 @@ aal_status_t aal_topk_logits(const void* z, aal_dtype_t in_dtype, int64_t rows, 
   a.V = V;
   a.k = k;
   a.sc = sc;
+  a.inv_t = 1.0f / temperature;
   a.top = top_logits;
   a.ids = top_ids;
   a.rest = rest;
