@@ -11,16 +11,29 @@
 //   dloss/dz_i = q_i (c_tv (m_i - Q) - c_eal + c_kl) - c_kl p_i + c_eal [i = x*]   listed
 // with Q = sum of q over the entries with q < p (the remainder among them).
 //
-// Multi-kernel schedule, every shape:
+// Resident schedule (k_top_fused): a workgroup keeps a row in registers from
+// its one read to the one write of its gradient, and takes row after row, loading the
+// next one's vectors as it stores this one's.  Where a coefficient depends on the row's
+// windows (WTV or EAL terms), it publishes the row's acceptances and waits for
+// those of the at most K - 1 rows on either side: all workgroups of the grid
+// run at once and take rows in order, and publishing waits for nothing, so the waits
+// end; they are bounded all the same.
+// Multi-kernel schedule, every shape (rows too long for a workgroup's registers):
 //   k_top_rows  one workgroup per row: the draft's max / sum-exp over the
-//               unlisted entries (a bitmap of the list in LDS keeps the listed
-//               ones out, so that q_r is a sum and not a difference), then the
-//               first wave does the list.
+//               unlisted entries, then the first wave does the list.
 //   k_top_scan  one thread per row: dE/da over the windows that contain it and
-//               the row's coefficients; the row that starts a window writes its E.
-//   k_top_loss  the four terms and the weighted loss, fixed summation order.
+//               the row's coefficients.
 //   k_top_grad  one constant times 2^x for every entry, then the listed ones.
+// Both end with k_top_loss: every window's E, the four terms and the weighted
+// loss, in a fixed order of summation.
+//
+// The listed entries are kept out of the unlisted sum by a bitmap of the
+// vocabulary in LDS, so that q_r is a sum and not a difference.  A row whose largest logit
+// is below -1e30 / sc ("deep": filled with the type's lowest value) has entries that are
+// equal or further apart than any exponential holds: 2^-64 takes the place of sc
+// there, so that the products stay finite.
 #include "aal_device.h"
+#include "aal_resident_common.h"
 #include "aal_rowops.h"
 #include "aal_toplist.h"
 
@@ -32,6 +45,7 @@ namespace {
 constexpr int kTopMax = 512;
 constexpr float kLn2 = 0.693147180559945309417f;
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kDeepScale = 0x1p-64f;
 
 struct TopLossParams {
   const void* zd;
@@ -42,178 +56,162 @@ struct TopLossParams {
   int V, k;
   float scd, sct;
   int top_bf16;
-  TopRow* stats;
+  TopRow* stats;       // multi-kernel schedule
+  uint64_t* slots;     // [R][2]: the rows' acceptances, tagged
+  float2* row_loss;    // [R]: KL, windows that contain the row * (1 - a_tv)
+  unsigned* err;       // poll time-out
+  unsigned* counter;   // of k_top_loss's workgroups: zeroed by the first kernel
+  float* accept_tv;    // may be null
+  float* accept_eal;
+  int32_t* xstar;
+  // windows and weights
+  int layout;
+  int S, K;
+  int64_t W;
+  float w_wtv, w_eal, w_kl, w_tv;
+  float inv_t_d;
+  const float* grad_scale;
 };
 
 __device__ __forceinline__ float load_top(const TopLossParams& p, int64_t i) {
   return p.top_bf16 ? Bf16::load1(p.top, i) : F32::load1(p.top, i);
 }
 
+// The reference of a draft row's sums: 2^(z sc - msc).
+struct RowRef {
+  float m, sc, msc;
+  bool deep;
+};
+__device__ __forceinline__ RowRef row_ref(float m, float sc) {
+  const bool deep = m * sc < -1e30f && m != kNegInf;
+  const float s = deep ? kDeepScale : sc;
+  return {m, s, m == kNegInf ? 0.f : m * s, deep};
+}
+// log2 of q's numerator at a listed entry (exact where a deep row's is huge)
+__device__ __forceinline__ float listed_log2(const RowRef& r, float z, float sc) {
+  return r.deep ? (z - r.m) * sc : __builtin_fmaf(z, r.sc, -r.msc);
+}
+
 // The bitmap of a row's listed ids, one bit per element counted from the row's
 // first vector on, so that a vector's bits lie in one byte (or half a byte).
-__device__ __forceinline__ int bitmap_words(int V) { return (V + 7) / 32 + 1; }
+__host__ __device__ constexpr int bitmap_words(int V) { return (V + 7) / 32 + 1; }
 template <int E>
 __device__ __forceinline__ uint32_t listed_bits(const uint32_t* map, int gi) {
   if constexpr (E == 8) return reinterpret_cast<const uint8_t*>(map)[gi];
   return (reinterpret_cast<const uint8_t*>(map)[gi >> 1] >> (4 * (gi & 1))) & 15u;
 }
 
-// What the first wave makes of a row's list: t and z of its entries in LDS
-// (t = -inf marks one that is no part of the list), the draft's state over
-// the unlisted entries in `un`.
-__device__ TopRow list_row(const TopLossParams& p, int64_t row, const float* sh_t, const float* sh_z, LseState un) {
+// What one wave makes of a row's list, its entries' t and z in LDS (t = -inf marks
+// one that is no part of it), in three steps: the target alone, the listed draft
+// logits against the row's reference, and the sums with the draft's unlisted mass.
+struct ListTarget {
+  float tmax, D, inv_zt, lzt, pr;  // p_i = inv_zt 2^((t - tmax) sct); lzt = log2 of that sum's inverse
+  int star;
+  bool has;
+};
+__device__ ListTarget list_target(const TopLossParams& p, int64_t row, const float* sh_t, const int* sh_id) {
   const int lane = threadIdx.x & (kWave - 1);
-  const bool has_rest = p.rest != nullptr;
-  float tmax = kNegInf, zmax = kNegInf, best = kNegInf;
+  float best = kNegInf;
   int star = INT_MAX;
   for (int i = lane; i < p.k; i += kWave) {
     const float t = sh_t[i];
     if (t == kNegInf) continue;
-    tmax = fmaxf(tmax, t);
-    zmax = fmaxf(zmax, sh_z[i]);
-    const int id = p.ids[row * p.k + i];
+    const int id = sh_id[i];
     if (t > best || (t == best && id < star)) {
       best = t;
       star = id;
     }
   }
-  tmax = wave_max(tmax);
-  zmax = wave_max(zmax);
-  star = wave_min_i(best == tmax ? star : INT_MAX);
-  const float rest2 = has_rest ? p.rest[row] * kLog2e : kNegInf;
-  const float tm = tmax == kNegInf ? kNegInf : tmax * p.sct;
-  float mt = fmaxf(tm, rest2);
-  const bool has = mt != kNegInf;
-  if (!has) mt = 0.f;
-  float zm = fmaxf(zmax, un.m);
-  const float msc = zm == kNegInf ? 0.f : zm * p.scd;
-  float st = 0.f, sz = 0.f;
-  for (int i = lane; i < p.k; i += kWave) {
-    const float t = sh_t[i];
-    if (t == kNegInf) continue;
-    st += ex2(__builtin_fmaf(t, p.sct, -mt));
-    sz += ex2(__builtin_fmaf(sh_z[i], p.scd, -msc));
-  }
+  ListTarget o;
+  o.tmax = wave_max(best);
+  o.star = wave_min_i(best == o.tmax ? star : INT_MAX);
+  const bool any = o.tmax != kNegInf;
+  const float rest = p.rest != nullptr ? p.rest[row] : kNegInf;
+  o.has = any || rest != kNegInf;
+  float st = 0.f;
+  for (int i = lane; i < p.k; i += kWave)
+    if (sh_t[i] != kNegInf) st += ex2((sh_t[i] - o.tmax) * p.sct);
   st = wave_sum(st);
-  sz = wave_sum(sz);
-  const float er = ex2(rest2 - mt);
-  const float su = un.m == kNegInf ? 0.f : un.s * ex2(un.msc - msc);
-  const float zt = st + er, zd = sz + su;
-  const float inv_zt = has ? 1.f / zt : 0.f, inv_s = zd > 0.f ? 1.f / zd : 0.f;
-  // log2 of the sums' ratio (a draft row without a finite entry has q = 0 everywhere)
-  const float dl = (zd > 0.f ? __log2f(zd) : 0.f) - (has ? __log2f(zt) : 0.f);
-  const float pr = er * inv_zt, qr = has_rest ? su * inv_s : 0.f;
-  float a = 0.f, q_lt = 0.f, kl = 0.f, ae = 0.f;
-  for (int i = lane; i < p.k; i += kWave) {
-    const float t = sh_t[i];
-    if (t == kNegInf) continue;
-    const float lt = __builtin_fmaf(t, p.sct, -mt), lz = __builtin_fmaf(sh_z[i], p.scd, -msc);
-    const float pv = ex2(lt) * inv_zt, qv = ex2(lz) * inv_s;
-    a += fminf(pv, qv);
-    q_lt += qv < pv ? qv : 0.f;
-    kl += pv > 0.f ? pv * ((lt - lz) + dl) : 0.f;
-    ae += p.ids[row * p.k + i] == star ? qv : 0.f;
+  // the remainder against the list's largest, in log2: the larger of the two is the reference
+  float D = 0.f, f = 1.f, g = 0.f;  // list terms times f, the remainder's g
+  if (!any) {
+    f = 0.f;
+    g = rest != kNegInf ? 1.f : 0.f;
+  } else if (rest != kNegInf) {
+    D = float(double(rest) * 1.4426950408889634 - double(o.tmax) * double(p.sct));
+    f = ex2(-fmaxf(D, 0.f));
+    g = ex2(fminf(D, 0.f));
   }
-  a = wave_sum(a);
-  q_lt = wave_sum(q_lt);
-  kl = wave_sum(kl);
-  ae = wave_sum(ae);
-  TopRow o{};
-  o.msc = msc;
-  o.inv_s = inv_s;
-  o.mt = mt;
-  o.inv_zt = inv_zt;
-  o.a_tv = a + fminf(pr, qr);
-  o.a_eal = ae;
-  const bool below = qr < pr;
-  o.qlt = q_lt + (below ? qr : 0.f);
-  if (pr > 0.f) kl += pr * (__log2f(pr) - __log2f(qr));
-  o.kl = kl * kLn2;
-  o.share = qr > 0.f ? pr / qr : 0.f;
-  o.xstar = star == INT_MAX ? -1 : star;
-  o.flags = (has ? kTopHas : 0) | (below ? kTopRestBelow : 0);
+  const float zt = __builtin_fmaf(st, f, g);
+  o.inv_zt = o.has ? f / zt : 0.f;
+  o.lzt = o.has ? -__log2f(zt) - fmaxf(D, 0.f) : 0.f;
+  o.pr = o.has ? g / zt : 0.f;
   return o;
 }
-
-template <class TI, bool VEC, int U, int BLK>
-__global__ __launch_bounds__(BLK) void k_top_rows(TopLossParams p) {
-  using Rv = RowVecs<TI, VEC>;
-  constexpr int E = Rv::E;
-  extern __shared__ uint32_t sh_map[];
-  __shared__ float sh_t[kTopMax], sh_z[kTopMax];
-  __shared__ LseState sh_lse[BLK / kWave];
-
-  const int64_t row = blockIdx.x;
-  const Rv rv(row, p.R, p.V);
-  const int64_t e0 = row * int64_t(p.V), l0 = row * p.k;
-  const int words = bitmap_words(p.V);
-  for (int i = threadIdx.x; i < words; i += BLK) sh_map[i] = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < p.k; i += BLK) {
-    const int id = p.ids[l0 + i];
-    const float t = load_top(p, l0 + i);
-    const bool in = id >= 0 && id < p.V && t != kNegInf;
-    sh_t[i] = in ? t : kNegInf;
-    sh_z[i] = in ? TI::load1(p.zd, e0 + id) : kNegInf;
-    if (in) atomicOr(&sh_map[(id + rv.head) >> 5], 1u << ((id + rv.head) & 31));
+__device__ __forceinline__ float list_draft(const TopLossParams& p, const float* sh_t, const float* sh_z, RowRef ref) {
+  float sz = 0.f;
+  for (int i = threadIdx.x & (kWave - 1); i < p.k; i += kWave)
+    if (sh_t[i] != kNegInf) sz += ex2(listed_log2(ref, sh_z[i], p.scd));
+  return wave_sum(sz);
+}
+__device__ TopRow list_row(const TopLossParams& p, const ListTarget& o, const float* sh_t, const float* sh_z,
+                           const int* sh_id, RowRef ref, float sz, float su) {
+  const float zd = sz + su, inv_s = zd > 0.f ? 1.f / zd : 0.f;
+  // log2 of the sums' ratio (a draft row without a finite entry has q = 0 everywhere)
+  const float dl = (zd > 0.f ? __log2f(zd) : 0.f) + o.lzt;
+  const float qr = p.rest != nullptr ? su * inv_s : 0.f;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};  // sums of min(p, q), q where q < p, p log2(p / q), q at x*
+  for (int i = threadIdx.x & (kWave - 1); i < p.k; i += kWave) {
+    const float t = sh_t[i];
+    if (t == kNegInf) continue;
+    const float lt = (t - o.tmax) * p.sct, lz = listed_log2(ref, sh_z[i], p.scd);
+    const float pv = ex2(lt) * o.inv_zt, qv = ex2(lz) * inv_s;
+    v[0] += fminf(pv, qv);
+    v[1] += qv < pv ? qv : 0.f;
+    v[2] += pv > 0.f ? pv * ((lt - lz) + dl) : 0.f;
+    v[3] += sh_id[i] == o.star ? qv : 0.f;
   }
-  __syncthreads();
-  LseState un = lse_init();
-  for (int base = threadIdx.x; base < rv.ng; base += BLK * U) {
-    u32x4 w[1][U];
-    float x[U][E];
-    rv.load({p.zd}, base, BLK, w);
-    rv.unpack(w[0], x);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int gi = base + u * BLK;
-      const uint32_t bits = gi < rv.ng ? listed_bits<E>(sh_map, gi) : 0u;
-      if (bits)
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (bits >> e & 1u) x[u][e] = kNegInf;
-    }
-    lse_fold(un, x, p.scd);
-  }
-  un = block_lse<BLK / kWave>(un, p.scd, sh_lse);
-  if (threadIdx.x < kWave) {
-    const TopRow o = list_row(p, row, sh_t, sh_z, un);
-    if (threadIdx.x == 0) p.stats[row] = o;
-  }
+  wave_sum_n(v);
+  TopRow r{};
+  r.msc = ref.msc;
+  r.inv_s = inv_s;
+  r.tmax = o.tmax;
+  r.inv_zt = o.inv_zt;
+  r.a_tv = v[0] + fminf(o.pr, qr);
+  r.a_eal = v[3];
+  const bool below = qr < o.pr;
+  r.qlt = v[1] + (below ? qr : 0.f);
+  r.kl = (v[2] + (o.pr > 0.f ? o.pr * (__log2f(o.pr) - __log2f(qr)) : 0.f)) * kLn2;
+  r.share = qr > 0.f ? o.pr / qr : 0.f;
+  r.xstar = o.star == INT_MAX ? -1 : o.star;
+  r.flags = (o.has ? kTopHas : 0) | (below ? kTopRestBelow : 0) | (ref.deep ? kTopDeep : 0);
+  return r;
 }
 
-struct TopScanParams {
-  TopRow* stats;
-  int layout;
-  int64_t B;
-  int S, K;
-  int64_t R, W;
-  float w_wtv, w_eal, w_kl, w_tv;
-  float inv_t_d;
-  const float* grad_scale;
-  float2* win;
-  float2* row_loss;
-  float* e_tv;
-  float* e_eal;
-  float* accept_tv;
-  float* accept_eal;
-  int32_t* xstar;
-};
+// p and the gradient at a listed entry.
+__device__ __forceinline__ float listed_p(const TopRow& s, float t, float sct) {
+  return ex2((t - s.tmax) * sct) * s.inv_zt;
+}
+__device__ __forceinline__ float listed_grad(const TopRow& s, float q, float pv, int id) {
+  float g = q * (q < pv ? s.cA : s.cB) - s.cP * pv;
+  if (id == s.xstar) g += s.cX;
+  return g;
+}
 
 // The windows that contain row r: starts t0..t1 (none if t1 < t0), the first
-// row of its sequence, its place s there, and the index of its own window.
+// row of its sequence, and its place s there.
 struct RowWindows {
-  int64_t base, own;
+  int64_t base, own;  // own: the window that starts at r, where `starts`
   int s, t0, t1;
   bool starts;
 };
 __device__ __forceinline__ RowWindows row_windows(int64_t r, int layout, int S, int K) {
   RowWindows w;
   if (layout == 0) {
-    w.base = (r / K) * K;
+    w.own = r / K;
+    w.base = w.own * K;
     w.s = int(r - w.base);
     w.t0 = w.t1 = 0;
-    w.own = r / K;
     w.starts = w.s == 0;
   } else {
     const int64_t b = r / S;
@@ -226,9 +224,19 @@ __device__ __forceinline__ RowWindows row_windows(int64_t r, int layout, int S, 
   }
   return w;
 }
+__device__ __forceinline__ double windows_of(const RowWindows& w) { return w.t1 >= w.t0 ? double(w.t1 - w.t0 + 1) : 0.0; }
+
+// dE/da at place j of a window whose rows' acceptances are a[0..K-1].
+template <class F>
+__device__ __forceinline__ double window_d(F a, int K, int j) {
+  double P = 1.0, S = 1.0;
+  for (int i = 0; i < j; ++i) P *= double(a(i));
+  for (int i = K - 1; i > j; --i) S = 1.0 + double(a(i)) * S;
+  return P * S;
+}
 
 // The coefficients of a row from dE/da summed over its windows.
-__device__ void row_coefs(TopRow& o, const TopScanParams& p, double d_tv, double d_eal, double count) {
+__device__ void row_coefs(TopRow& o, const TopLossParams& p, double d_tv, double d_eal, double count) {
   const double f = (p.grad_scale ? double(*p.grad_scale) : 1.0) * double(p.inv_t_d);
   const double W = double(p.W);
   const double c_tv = p.W > 0 ? f * (-double(p.w_wtv) * d_tv - double(p.w_tv) * count / p.K) / W : 0.0;
@@ -243,143 +251,389 @@ __device__ void row_coefs(TopRow& o, const TopScanParams& p, double d_tv, double
   o.cX = float(c_eal);
 }
 
-__global__ __launch_bounds__(kRowBlock) void k_top_scan(TopScanParams p) {
+// What a row leaves for the caller and for the sums of the loss.
+__device__ __forceinline__ void write_row(const TopLossParams& p, int64_t r, const TopRow& o, double count) {
+  p.row_loss[r] = make_float2(o.kl, float(count * (1.0 - double(o.a_tv))));
+  if (p.accept_tv) p.accept_tv[r] = o.a_tv;
+  if (p.accept_eal) p.accept_eal[r] = o.a_eal;
+  if (p.xstar) p.xstar[r] = o.xstar;
+}
+
+// ------------------------------------------------------- resident schedule
+// The bitmap reaches to the end of the last vectors that a workgroup holds.
+inline size_t fused_lds_bytes(int held, int k) { return size_t(bitmap_words(held) + 4 * k) * 4; }
+
+// WK waves hold the row, NV vectors a thread; the last wave does the list, the
+// windows and the coefficients beside their passes, so that neither's registers add to the other's.
+// Three barriers a row:
+//   holders: the row arrives; its largest logit  |1| sum over the unlisted entries |2|   |3| gradient, next row's loads
+//   list:    the list arrives; bitmap; target    |1| listed entries of the row     |2| row, windows |3| listed gradient, next list
+// The listed entries' gradient is stored after the next first barrier, when
+// every holder has waited for its stores of the row.
+template <class TI, class TG, bool VEC, int WK, int NV, bool COUPLED>
+__global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p, int grid, void* __restrict__ grad) {
+  using Rv = RowVecs<TI, VEC>;
+  constexpr int E = Rv::E;
+  constexpr int BLK = WK * kWave;  // threads that hold the row
+  constexpr int kWords = bitmap_words(NV * BLK * E);
+  constexpr int GS = sizeof(typename TG::storage);
+  extern __shared__ uint32_t sh_dyn[];
+  __shared__ float sh_m[WK], sh_s[WK], sh_cR;
+  __shared__ float sh_a[2][128];  // acceptances of the row's neighbours (COUPLED)
+  uint32_t* const map = sh_dyn;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  const int wv = __builtin_amdgcn_readfirstlane(tid / kWave);
+
+  if (wv == WK) {
+    // ------------------------------------------------------- the list
+    float* const lt = reinterpret_cast<float*>(map + kWords);  // target logits
+    float* const lz = lt + p.k;                                // the draft's
+    int* const li = reinterpret_cast<int*>(lz + p.k);          // ids
+    float* const lg = reinterpret_cast<float*>(li + p.k);      // gradient
+    if (blockIdx.x == 0 && lane == 0) *p.counter = 0u;
+    for (int i = lane; i < kWords; i += kWave) map[i] = 0;
+    int64_t before = -1;
+    auto finish = [&] {
+      if (before < 0 || grad == nullptr) return;
+      const int64_t e0 = before * int64_t(p.V);
+      for (int i = lane; i < p.k; i += kWave)
+        if (lt[i] != kNegInf) TG::store1(grad, e0 + li[i], lg[i]);
+    };
+    for (int64_t row = blockIdx.x; row < p.R; row += grid) {
+      const int head = Rv(row, p.R, p.V).head;
+      const int64_t l0 = row * p.k, e0 = row * int64_t(p.V);
+      // this list's entries wait in registers while the row before is finished
+      constexpr int kKeep = kTopMax / kWave;
+      int id[kKeep];
+      float t[kKeep], z[kKeep];
+#pragma unroll
+      for (int n = 0; n < kKeep; ++n) {
+        const int i = lane + n * kWave;
+        id[n] = -1;
+        if (n * kWave < p.k && i < p.k) {
+          id[n] = p.ids[l0 + i];
+          t[n] = load_top(p, l0 + i);
+          if (id[n] >= p.V || t[n] == kNegInf) id[n] = -1;
+          if (id[n] >= 0) {
+            z[n] = TI::load1(p.zd, e0 + id[n]);
+            atomicOr(&map[(id[n] + head) >> 5], 1u << ((id[n] + head) & 31));
+          }
+        }
+      }
+      lds_barrier();  // 1
+      finish();
+#pragma unroll
+      for (int n = 0; n < kKeep; ++n) {
+        const int i = lane + n * kWave;
+        if (n * kWave < p.k && i < p.k) {
+          li[i] = id[n];
+          lt[i] = id[n] >= 0 ? t[n] : kNegInf;
+          lz[i] = id[n] >= 0 ? z[n] : kNegInf;
+        }
+      }
+      wait_lds_all();
+      const RowRef ref = row_ref(wave_max(lane < WK ? sh_m[lane] : kNegInf), p.scd);
+      const ListTarget lt_row = list_target(p, row, lt, li);
+      const float sz = list_draft(p, lt, lz, ref);
+      const RowWindows rw = row_windows(row, p.layout, p.S, p.K);
+      lds_barrier();  // 2
+      const float su = wave_sum(lane < WK ? sh_s[lane] : 0.f);
+      TopRow o = list_row(p, lt_row, lt, lz, li, ref, sz, su);
+      if (lane == 0) {
+        publish(p.slots + 2 * row, o.a_tv, 1u);
+        publish(p.slots + 2 * row + 1, o.a_eal, 1u);
+      }
+      double d_tv = 0.0, d_eal = 0.0;
+      if constexpr (COUPLED) {
+        // the rows that share a window with this one: places lo..hi of its sequence
+        const int lo = p.layout == 0 ? 0 : max(0, rw.s - p.K + 1);
+        const int hi = p.layout == 0 ? p.K - 1 : min(p.S - 1, rw.s + p.K - 1);
+        for (int i = lo + lane; i <= hi; i += kWave) {
+          float a[2] = {o.a_tv, o.a_eal};
+          if (i != rw.s && rw.t1 >= rw.t0) collect<2>(p.slots + 2 * (rw.base + i), 1u, p.err, a);
+          sh_a[0][i - lo] = a[0];
+          sh_a[1][i - lo] = a[1];
+        }
+        wait_lds_all();
+        // one window a lane
+        if (rw.t0 + lane <= rw.t1) {
+          const int w0 = rw.t0 + lane - lo, j = rw.s - (rw.t0 + lane);
+          if (p.w_wtv != 0.f) d_tv = window_d([&](int i) { return sh_a[0][w0 + i]; }, p.K, j);
+          if (p.w_eal != 0.f) d_eal = window_d([&](int i) { return sh_a[1][w0 + i]; }, p.K, j);
+        }
+        if (p.w_wtv != 0.f) d_tv = wave_sum_d(d_tv);
+        if (p.w_eal != 0.f) d_eal = wave_sum_d(d_eal);
+      }
+      const double count = windows_of(rw);
+      row_coefs(o, p, d_tv, d_eal, count);
+      if (lane == 0) sh_cR = o.cR;
+      lds_barrier();  // 3
+      if (lane == 0) write_row(p, row, o, count);
+      // the list's gradient, stored once the row's other entries are; the bitmap is emptied
+      for (int i = lane; i < p.k; i += kWave) {
+        if (lt[i] == kNegInf) continue;
+        const float q = ex2(listed_log2(ref, lz[i], p.scd)) * o.inv_s;
+        lg[i] = listed_grad(o, q, listed_p(o, lt[i], p.sct), li[i]);
+        map[(li[i] + head) >> 5] = 0;
+      }
+      wait_lds_all();
+      before = row;
+    }
+    lds_barrier();  // the holders' last stores
+    finish();
+    return;
+  }
+
+  // -------------------------------------------------------- the row
+  // rows of whole vectors go through buffer resources, which read zeros and store
+  // nothing past the row
+  const uint32_t row_bytes = uint32_t(p.V) * sizeof(typename TI::storage), grow_bytes = uint32_t(p.V) * GS;
+  u32x4 w[NV];
+  auto row_rsrc = [&](int64_t r) { return make_rsrc(static_cast<const uint8_t*>(p.zd) + r * int64_t(row_bytes), row_bytes); };
+  auto load_vec = [&](const rsrc_t& rs, const Rv& rv, int v) {
+    if constexpr (VEC) {
+      w[v] = bld16(rs, uint32_t(tid) * 16u, uint32_t(v) * (BLK * 16u));
+    } else {
+      const int gi = v * BLK + tid;
+      w[v] = Rv::none();
+      if (gi < rv.nload) w[v] = rv.raw(p.zd, gi);
+    }
+  };
+  // a wave-uniform number that the compiler takes as new, so that it makes the
+  // conditions that follow from it where they are used, not once for every vector
+  auto fresh = [](int x) {
+    asm volatile("" : "+s"(x));
+    return x;
+  };
+  // keeps the packed vectors, not unpacked copies of them, between two passes
+  auto pin_all = [&] {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) pin(w[v]);
+  };
+  {
+    const Rv rv(int64_t(blockIdx.x), p.R, p.V);
+    const rsrc_t rs = row_rsrc(blockIdx.x);
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+      if (v * BLK < rv.ng) load_vec(rs, rv, v);
+  }
+  for (int64_t row = blockIdx.x; row < p.R; row += grid) {
+    const Rv rv(row, p.R, p.V);
+    wait_vmem_all();  // the row is here, and the stores of the row before are done
+    // -inf outside the row: in its edge vectors and in those past its last one
+    const int last_v = fresh((rv.ng - 1) / BLK), last_t = fresh((rv.ng - 1) % BLK);
+    if constexpr (!VEC)
+      if (tid == 0 && !rv.whole(0)) w[0] = rv.edge(p.zd, 0, w[0]);
+    {
+      u32x4 x = Rv::none();
+      if (tid <= last_t) {
+        x = w[0];
+#pragma unroll
+        for (int v = 1; v < NV; ++v)
+          if (v == last_v) x = w[v];
+        if constexpr (!VEC)
+          if (tid == last_t && rv.ng > 1 && !rv.whole(rv.ng - 1)) x = rv.edge(p.zd, rv.ng - 1, x);
+      }
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        if (v == last_v) w[v] = x;
+    }
+    float m = kNegInf;
+    pin_all();
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if (v <= last_v) {
+        float x[E];
+        unpackv<TI>(w[v], x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) m = fmaxf(m, x[e]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    m = wave_max(m);
+    if (lane == 0) sh_m[wv] = m;
+    lds_barrier();  // 1
+    const RowRef ref = row_ref(wave_max(lane < WK ? sh_m[lane] : kNegInf), p.scd);
+    float s = 0.f;
+    pin_all();
+    const int last_v2 = fresh(last_v);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if (v <= last_v2) {
+        float x[E];
+        unpackv<TI>(w[v], x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
+        const uint32_t bits = listed_bits<E>(map, v * BLK + tid);
+        if (bits)
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (bits >> e & 1u) x[e] = 0.f;
+        s += tree_sum(x);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    s = wave_sum(s);
+    if (lane == 0) sh_s[wv] = s;
+    lds_barrier();  // 2
+    lds_barrier();  // 3
+    const int64_t next = row + grid;
+    const bool more = next < p.R;
+    const Rv rn(more ? next : row, p.R, p.V);
+    const rsrc_t rsn = row_rsrc(more ? next : row);
+    const float cR = sh_cR;
+    pin_all();
+    const int last_v3 = fresh(last_v), last_n = fresh(more ? (rn.ng - 1) / BLK : -1);
+    if (grad != nullptr) {
+      const rsrc_t gr = make_rsrc(static_cast<uint8_t*>(grad) + row * int64_t(grow_bytes), grow_bytes);
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        if (v <= last_v3) {
+          const int gi = v * BLK + tid;
+          float x[E];
+          unpackv<TI>(w[v], x);
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[e] = cR * ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
+          if constexpr (VEC) {
+            store_g<TG, E>(gr, uint32_t(gi) * (E * GS), x);  // dropped past the row
+          } else if (rv.whole(gi)) {
+            store_vec<TG, E>(grad, (rv.g0 + gi) * E, x);
+          } else if (gi < rv.ng) {
+#pragma unroll 1
+            for (int e = 0; e < E; ++e) {
+              const int i = rv.index(gi, e);
+              float ge = x[0];
+#pragma unroll
+              for (int q = 1; q < E; ++q) ge = e == q ? x[q] : ge;
+              if (i >= 0 && i < p.V) TG::store1(grad, (rv.g0 + gi) * E + e, ge);
+            }
+          }
+        }
+        if (v <= last_n) load_vec(rsn, rn, v);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        if (v <= last_n) load_vec(rsn, rn, v);
+    }
+  }
+  wait_vmem_all();
+  lds_barrier();  // the last stores
+}
+
+// -------------------------------------------------- multi-kernel schedule
+template <class TI, bool VEC, int U, int BLK>
+__global__ __launch_bounds__(BLK) void k_top_rows(TopLossParams p) {
+  using Rv = RowVecs<TI, VEC>;
+  constexpr int E = Rv::E;
+  extern __shared__ uint32_t sh_map[];
+  __shared__ float sh_t[kTopMax], sh_z[kTopMax];
+  __shared__ int sh_id[kTopMax];
+  __shared__ float sh_m[BLK / kWave], sh_s[BLK / kWave];
+
+  const int64_t row = blockIdx.x;
+  const Rv rv(row, p.R, p.V);
+  const int64_t e0 = row * int64_t(p.V), l0 = row * p.k;
+  const int words = bitmap_words(p.V);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.counter = 0u;
+  for (int i = threadIdx.x; i < words; i += BLK) sh_map[i] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.k; i += BLK) {
+    const int id = p.ids[l0 + i];
+    const float t = load_top(p, l0 + i);
+    const bool in = id >= 0 && id < p.V && t != kNegInf;
+    sh_id[i] = id;
+    sh_t[i] = in ? t : kNegInf;
+    sh_z[i] = in ? TI::load1(p.zd, e0 + id) : kNegInf;
+    if (in) atomicOr(&sh_map[(id + rv.head) >> 5], 1u << ((id + rv.head) & 31));
+  }
+  __syncthreads();
+  // the largest logit of all entries, the sum over the unlisted ones against
+  // max(largest sc, -1e30) so far
+  float m = kNegInf, s = 0.f;
+  for (int base = threadIdx.x; base < rv.ng; base += BLK * U) {
+    u32x4 w[1][U];
+    float x[U][E];
+    rv.load({p.zd}, base, BLK, w);
+    rv.unpack(w[0], x);
+    float cm = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < E; ++e) cm = fmaxf(cm, x[u][e]);
+    const float at = fmaxf(cm * p.scd, -1e30f);
+    s *= ex2(fmaxf(m * p.scd, -1e30f) - at);
+    m = cm;
+    float c[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int gi = base + u * BLK;
+      const uint32_t bits = gi < rv.ng ? listed_bits<E>(sh_map, gi) : 0u;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[u][e] = ex2(__builtin_fmaf(x[u][e], p.scd, -at));
+      if (bits)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (bits >> e & 1u) x[u][e] = 0.f;
+      c[u] = tree_sum(x[u]);
+    }
+    s += tree_sum(c);
+  }
+  const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
+  const float wm = wave_max(m);
+  if (lane == 0) sh_m[wv] = wm;
+  __syncthreads();
+  float bm = sh_m[0];
+  for (int i = 1; i < BLK / kWave; ++i) bm = fmaxf(bm, sh_m[i]);
+  const RowRef ref = row_ref(bm, p.scd);
+  if (ref.deep) {
+    s = 0.f;
+    for (int gi = threadIdx.x; gi < rv.ng; gi += BLK) {
+      float x[E];
+      TI::unpack(to_uint4(rv.load(p.zd, gi)), x);
+      const uint32_t bits = listed_bits<E>(sh_map, gi);
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (!(bits >> e & 1u)) s += ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
+    }
+  } else {
+    s *= ex2(fmaxf(m * p.scd, -1e30f) - ref.msc);
+  }
+  s = wave_sum(s);
+  if (lane == 0) sh_s[wv] = s;
+  __syncthreads();
+  if (threadIdx.x < kWave) {
+    s = wave_sum(lane < BLK / kWave ? sh_s[lane] : 0.f);
+    const TopRow o = list_row(p, list_target(p, row, sh_t, sh_id), sh_t, sh_z, sh_id, ref,
+                              list_draft(p, sh_t, sh_z, ref), s);
+    if (lane == 0) {
+      p.stats[row] = o;
+      publish(p.slots + 2 * row, o.a_tv, 1u);
+      publish(p.slots + 2 * row + 1, o.a_eal, 1u);
+    }
+  }
+}
+
+__global__ __launch_bounds__(kRowBlock) void k_top_scan(TopLossParams p) {
   const int64_t r = int64_t(blockIdx.x) * kRowBlock + threadIdx.x;
   if (r >= p.R) return;
-  const int K = p.K;
-  const RowWindows rw = row_windows(r, p.layout, p.S, K);
+  const RowWindows rw = row_windows(r, p.layout, p.S, p.K);
   const TopRow* st = p.stats + rw.base;
   double d_tv = 0.0, d_eal = 0.0;
   for (int t = rw.t0; t <= rw.t1; ++t) {
-    const int j = rw.s - t;
-    double Pt = 1.0, Pe = 1.0, St = 1.0, Se = 1.0;
-    for (int i = 0; i < j; ++i) {
-      Pt *= double(st[t + i].a_tv);
-      Pe *= double(st[t + i].a_eal);
-    }
-    for (int i = K - 1; i > j; --i) {
-      St = 1.0 + double(st[t + i].a_tv) * St;
-      Se = 1.0 + double(st[t + i].a_eal) * Se;
-    }
-    d_tv += Pt * St;
-    d_eal += Pe * Se;
+    if (p.w_wtv != 0.f) d_tv += window_d([&](int i) { return st[t + i].a_tv; }, p.K, rw.s - t);
+    if (p.w_eal != 0.f) d_eal += window_d([&](int i) { return st[t + i].a_eal; }, p.K, rw.s - t);
   }
-  const double count = double(rw.t1 - rw.t0 + 1 > 0 ? rw.t1 - rw.t0 + 1 : 0);
   TopRow o = p.stats[r];
-  row_coefs(o, p, d_tv, d_eal, count);
+  row_coefs(o, p, d_tv, d_eal, windows_of(rw));
   TopRow& out = p.stats[r];
   out.cR = o.cR;
   out.cA = o.cA;
   out.cB = o.cB;
   out.cP = o.cP;
   out.cX = o.cX;
-  p.row_loss[r] = make_float2(o.kl, float(count * (1.0 - double(o.a_tv))));
-  if (p.accept_tv) p.accept_tv[r] = o.a_tv;
-  if (p.accept_eal) p.accept_eal[r] = o.a_eal;
-  if (p.xstar) p.xstar[r] = o.xstar;
-  if (rw.starts) {
-    double Pt = 1.0, Pe = 1.0, Et = 0.0, Ee = 0.0;
-    for (int i = 0; i < K; ++i) {
-      Pt *= double(st[rw.s + i].a_tv);
-      Pe *= double(st[rw.s + i].a_eal);
-      Et += Pt;
-      Ee += Pe;
-    }
-    p.win[rw.own] = make_float2(float(Et), float(Ee));
-    if (p.e_tv) p.e_tv[rw.own] = float(Et);
-    if (p.e_eal) p.e_eal[rw.own] = float(Ee);
-  }
-}
-
-constexpr int kLossBlock = 1024;
-
-__device__ double block_sum_d(double v, double* sh) {
-  v = wave_sum_d(v);
-  if ((threadIdx.x & (kWave - 1)) == 0) sh[threadIdx.x / kWave] = v;
-  __syncthreads();
-  double t = 0.0;
-  for (int i = 0; i < kLossBlock / kWave; ++i) t += sh[i];
-  __syncthreads();
-  return t;
-}
-
-struct TopLossSum {
-  const float2* win;
-  const float2* row_loss;
-  int64_t R, W;
-  int K;
-  float w_wtv, w_eal, w_kl, w_tv;
-  double* parts;
-  float* loss;
-  float* terms;
-  const unsigned* err;  // the resident schedule's error word, or null
-};
-
-__device__ void write_loss(const TopLossSum& p, double etv, double eeal, double kl, double tvs) {
-  // a term whose weight is 0 reads 0
-  const double t0 = p.W > 0 && p.w_wtv != 0.f ? -etv / double(p.W) : 0.0;
-  const double t1 = p.W > 0 && p.w_eal != 0.f ? -eeal / double(p.W) : 0.0;
-  const double t2 = p.w_kl != 0.f ? kl / double(p.R) : 0.0;
-  const double t3 = p.W > 0 && p.w_tv != 0.f ? tvs / (double(p.W) * p.K) : 0.0;
-  p.loss[0] = (p.err != nullptr && *p.err != 0u) ? __builtin_nanf("")
-                                                 : float(double(p.w_wtv) * t0 + double(p.w_eal) * t1 +
-                                                         double(p.w_kl) * t2 + double(p.w_tv) * t3);
-  if (p.terms) {
-    p.terms[0] = float(t0);
-    p.terms[1] = float(t1);
-    p.terms[2] = float(t2);
-    p.terms[3] = float(t3);
-  }
-}
-
-// Block b of n sums the windows and rows of its contiguous slice; a lone block
-// writes the loss itself.
-__global__ __launch_bounds__(kLossBlock) void k_top_loss_parts(TopLossSum p, int n) {
-  __shared__ double sh[kLossBlock / kWave];
-  const int64_t b = blockIdx.x;
-  const int64_t w0 = p.W * b / n, w1 = p.W * (b + 1) / n, r0 = p.R * b / n, r1 = p.R * (b + 1) / n;
-  double etv = 0.0, eeal = 0.0, kl = 0.0, tvs = 0.0;
-  for (int64_t i = w0 + threadIdx.x; i < w1; i += kLossBlock) {
-    const float2 e = p.win[i];
-    etv += double(e.x);
-    eeal += double(e.y);
-  }
-  for (int64_t i = r0 + threadIdx.x; i < r1; i += kLossBlock) {
-    const float2 e = p.row_loss[i];
-    kl += double(e.x);
-    tvs += double(e.y);
-  }
-  etv = block_sum_d(etv, sh);
-  eeal = block_sum_d(eeal, sh);
-  kl = block_sum_d(kl, sh);
-  tvs = block_sum_d(tvs, sh);
-  if (threadIdx.x != 0) return;
-  if (n == 1) {
-    write_loss(p, etv, eeal, kl, tvs);
-  } else {
-    double* o = p.parts + b * 4;
-    o[0] = etv;
-    o[1] = eeal;
-    o[2] = kl;
-    o[3] = tvs;
-  }
-}
-__global__ void k_top_loss(TopLossSum p, int n) {
-  if (threadIdx.x != 0) return;
-  double s[4] = {0.0, 0.0, 0.0, 0.0};
-  for (int b = 0; b < n; ++b)
-    for (int i = 0; i < 4; ++i) s[i] += p.parts[b * 4 + i];
-  write_loss(p, s[0], s[1], s[2], s[3]);
-}
-
-// The gradient at list entry i of a row: q_i and p_i again from the logits.
-template <class TI>
-__device__ __forceinline__ float listed_grad(const TopRow& s, float t, float z, int id, float scd, float sct) {
-  const float q = ex2(__builtin_fmaf(z, scd, -s.msc)) * s.inv_s;
-  const float pv = ex2(__builtin_fmaf(t, sct, -s.mt)) * s.inv_zt;
-  float g = q * (q < pv ? s.cA : s.cB) - s.cP * pv;
-  if (id == s.xstar) g += s.cX;
-  return g;
+  write_row(p, r, o, windows_of(rw));
 }
 
 template <class TI, class TG, bool VEC, int U>
@@ -389,6 +643,7 @@ __global__ __launch_bounds__(kRowBlock) void k_top_grad(TopLossParams p, int spl
   const int64_t row = blockIdx.x;
   const Rv rv(row, p.R, p.V);
   const TopRow s = p.stats[row];
+  const float sc = s.flags & kTopDeep ? kDeepScale : p.scd;
   const int64_t e0 = row * int64_t(p.V), l0 = row * p.k;
   for (int base = blockIdx.y * kRowBlock * U + threadIdx.x; base < rv.ng; base += splits * kRowBlock * U) {
     u32x4 w[1][U];
@@ -400,7 +655,7 @@ __global__ __launch_bounds__(kRowBlock) void k_top_grad(TopLossParams p, int spl
       float x[E], g[E];
       TI::unpack(to_uint4(w[0][u]), x);
 #pragma unroll
-      for (int e = 0; e < E; ++e) g[e] = s.cR * ex2(__builtin_fmaf(x[e], p.scd, -s.msc));
+      for (int e = 0; e < E; ++e) g[e] = s.cR * ex2(__builtin_fmaf(x[e], sc, -s.msc));
       rv.template store<TG>(grad, gi, g);
     }
   }
@@ -412,8 +667,94 @@ __global__ __launch_bounds__(kRowBlock) void k_top_grad(TopLossParams p, int spl
     if (((id + rv.head) / E / (kRowBlock * U)) % splits != int(blockIdx.y)) continue;
     const float t = load_top(p, l0 + i);
     if (t == kNegInf) continue;
-    TG::store1(grad, e0 + id, listed_grad<TI>(s, t, TI::load1(p.zd, e0 + id), id, p.scd, p.sct));
+    const float q = ex2(__builtin_fmaf(TI::load1(p.zd, e0 + id), sc, -s.msc)) * s.inv_s;
+    TG::store1(grad, e0 + id, listed_grad(s, q, listed_p(s, t, p.sct), id));
   }
+}
+
+// ------------------------------------------------------------------- loss
+constexpr int kLossBlock = 256;
+
+__device__ double block_sum_d(double v, double* sh) {
+  v = wave_sum_d(v);
+  if ((threadIdx.x & (kWave - 1)) == 0) sh[threadIdx.x / kWave] = v;
+  __syncthreads();
+  double t = 0.0;
+  for (int i = 0; i < kLossBlock / kWave; ++i) t += sh[i];
+  __syncthreads();
+  return t;
+}
+
+// Every window's E and the loss: workgroup b sums the rows of its slice (a window
+// counts where it starts); the last one to end adds the slices' sums in order.
+__global__ __launch_bounds__(kLossBlock) void k_top_loss(TopLossParams p, int n, double* parts, float* loss,
+                                                         float* terms, float* e_tv, float* e_eal,
+                                                         const unsigned* err) {
+  __shared__ double sh[kLossBlock / kWave];
+  __shared__ int sh_last;
+  const int64_t r0 = p.R * blockIdx.x / n, r1 = p.R * (int64_t(blockIdx.x) + 1) / n;
+  double v[4] = {0.0, 0.0, 0.0, 0.0};  // sums of E_tv, E_eal, KL, TV
+  const bool tv = p.w_wtv != 0.f || e_tv != nullptr, eal = p.w_eal != 0.f || e_eal != nullptr;
+  for (int64_t r = r0 + threadIdx.x; r < r1; r += kLossBlock) {
+    const RowWindows rw = row_windows(r, p.layout, p.S, p.K);
+    if (rw.starts && (tv || eal)) {
+      double Pt = 1.0, Pe = 1.0, Et = 0.0, Ee = 0.0;
+      for (int i = 0; i < p.K; ++i) {
+        Pt *= double(value_of(p.slots[2 * (r + i)]));
+        Pe *= double(value_of(p.slots[2 * (r + i) + 1]));
+        Et += Pt;
+        Ee += Pe;
+      }
+      // the sums are of the E that the caller gets
+      if (e_tv) e_tv[rw.own] = float(Et);
+      if (e_eal) e_eal[rw.own] = float(Ee);
+      v[0] += double(float(Et));
+      v[1] += double(float(Ee));
+    }
+    const float2 l = p.row_loss[r];
+    v[2] += double(l.x);
+    v[3] += double(l.y);
+  }
+  for (int i = 0; i < 4; ++i) v[i] = block_sum_d(v[i], sh);
+  if (n > 1) {
+    if (threadIdx.x == 0) {
+      for (int i = 0; i < 4; ++i)
+        __hip_atomic_store(parts + 4 * blockIdx.x + i, v[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      sh_last = __hip_atomic_fetch_add(p.counter, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == unsigned(n - 1);
+    }
+    __syncthreads();
+    if (!sh_last) return;
+    for (int i = 0; i < 4; ++i) {
+      double s = 0.0;
+      for (int b = threadIdx.x; b < n; b += kLossBlock)
+        s += __hip_atomic_load(parts + 4 * b + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      v[i] = block_sum_d(s, sh);
+    }
+  }
+  if (threadIdx.x != 0) return;
+  // a term whose weight is 0 reads 0
+  const double t0 = p.W > 0 && p.w_wtv != 0.f ? -v[0] / double(p.W) : 0.0;
+  const double t1 = p.W > 0 && p.w_eal != 0.f ? -v[1] / double(p.W) : 0.0;
+  const double t2 = p.w_kl != 0.f ? v[2] / double(p.R) : 0.0;
+  const double t3 = p.W > 0 && p.w_tv != 0.f ? v[3] / (double(p.W) * p.K) : 0.0;
+  // a set error word (a poll of the resident schedule timed out): NaN
+  loss[0] = (err != nullptr && *err != 0u) ? __builtin_nanf("")
+                                           : float(double(p.w_wtv) * t0 + double(p.w_eal) * t1 +
+                                                   double(p.w_kl) * t2 + double(p.w_tv) * t3);
+  if (terms) {
+    terms[0] = float(t0);
+    terms[1] = float(t1);
+    terms[2] = float(t2);
+    terms[3] = float(t3);
+  }
+}
+
+// Empties the acceptances' words and sets the error word.
+__global__ void k_top_clear(uint64_t* p, int64_t n, unsigned* err, unsigned value) {
+  const int64_t stride = int64_t(gridDim.x) * blockDim.x;
+  const int64_t t = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
+  for (int64_t i = t; i < n; i += stride) p[i] = 0;
+  if (t == 0) *err = value;
 }
 
 TopLossParams params_of(const TopLossArgs& a) {
@@ -429,17 +770,16 @@ TopLossParams params_of(const TopLossArgs& a) {
   p.sct = a.sc_t;
   p.top_bf16 = a.td == DType::kBf16;
   p.stats = a.stats;
-  return p;
-}
-
-TopScanParams scan_of(const TopLossArgs& a) {
-  TopScanParams p{};
-  p.stats = a.stats;
+  p.slots = a.slots;
+  p.row_loss = a.row_loss;
+  p.err = a.err;
+  p.counter = a.err + 1;
+  p.accept_tv = a.accept_tv;
+  p.accept_eal = a.accept_eal;
+  p.xstar = a.xstar;
   p.layout = a.layout;
-  p.B = a.B;
   p.S = a.S;
   p.K = a.K;
-  p.R = a.R;
   p.W = a.W;
   p.w_wtv = a.w_wtv;
   p.w_eal = a.w_eal;
@@ -447,35 +787,63 @@ TopScanParams scan_of(const TopLossArgs& a) {
   p.w_tv = a.w_tv;
   p.inv_t_d = a.inv_t_d;
   p.grad_scale = a.grad_scale;
-  p.win = a.win;
-  p.row_loss = a.row_loss;
-  p.e_tv = a.e_tv;
-  p.e_eal = a.e_eal;
-  p.accept_tv = a.accept_tv;
-  p.accept_eal = a.accept_eal;
-  p.xstar = a.xstar;
   return p;
 }
 
-hipError_t loss_launch(const TopLossArgs& a, const unsigned* err) {
-  TopLossSum p{};
-  p.win = a.win;
-  p.row_loss = a.row_loss;
-  p.R = a.R;
-  p.W = a.W;
-  p.K = a.K;
-  p.w_wtv = a.w_wtv;
-  p.w_eal = a.w_eal;
-  p.w_kl = a.w_kl;
-  p.w_tv = a.w_tv;
-  p.parts = a.loss_parts;
-  p.loss = a.loss;
-  p.terms = a.terms;
-  p.err = err;
-  const int n = a.R <= 32 * kLossBlock ? 1 : kTopLossParts;
-  k_top_loss_parts<<<dim3(unsigned(n)), kLossBlock, 0, a.stream>>>(p, n);
-  if (n > 1) k_top_loss<<<1, kWave, 0, a.stream>>>(p, n);
+hipError_t loss_launch(const TopLossArgs& a, bool waited) {
+  const int64_t want = (a.R + kLossBlock - 1) / kLossBlock;
+  const int n = int(want < kTopLossParts ? want : kTopLossParts);
+  k_top_loss<<<dim3(unsigned(n)), kLossBlock, 0, a.stream>>>(params_of(a), n, a.loss_parts, a.loss, a.terms, a.e_tv,
+                                                            a.e_eal, waited ? a.err : nullptr);
   return hipGetLastError();
+}
+
+template <class TI, class TG, bool VEC, int WK, int NV, bool COUPLED>
+hipError_t fused_launch(const TopLossArgs& a, bool* used) {
+  constexpr int BLK = (WK + 1) * kWave;
+  auto kern = k_top_fused<TI, TG, VEC, WK, NV, COUPLED>;
+  const DevInfo di = device_info();
+  if (di.cus == 0 || (COUPLED && a.coop && !di.coop)) return hipSuccess;
+  const size_t lds = fused_lds_bytes(NV * WK * kWave * TI::kVec, a.k);
+  int per_cu = 0;
+  hipError_t e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kern, BLK, lds);
+  if (e != hipSuccess) return e;
+  int64_t grid = int64_t(per_cu) * di.cus;
+  if (grid > a.R) grid = a.R;
+  // a row's neighbours have to be in other workgroups' hands at the same time
+  if (grid < 1 || (COUPLED && grid < a.R && grid < a.K)) return hipSuccess;
+  TopLossParams p = params_of(a);
+  int g = int(grid);
+  void* grad = a.grad;
+  if constexpr (COUPLED) {
+    const int64_t words = 2 * a.R;
+    k_top_clear<<<dim3(unsigned(words < 256 * 256 ? (words + 255) / 256 : 256)), 256, 0, a.stream>>>(
+        a.slots, words, a.err, unsigned(initial_error_word()));
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (a.coop) {
+      void* args[] = {&p, &g, &grad};
+      e = hipLaunchCooperativeKernel(reinterpret_cast<const void*>(kern), dim3(unsigned(g)), dim3(BLK), args,
+                                     unsigned(lds), a.stream);
+      *used = e == hipSuccess;
+      return e;
+    }
+  }
+  // the grid fits the device at once (see the occupancy bound above)
+  kern<<<dim3(unsigned(g)), BLK, lds, a.stream>>>(p, g, grad);
+  e = hipGetLastError();
+  *used = e == hipSuccess;
+  return e;
+}
+
+template <class TI, class TG, bool VEC, bool COUPLED>
+hipError_t fused_size(const TopLossArgs& a, bool* used) {
+  const int ng = a.V / TI::kVec + (VEC ? 0 : 2);  // vectors that cover a row, at most
+  if (ng <= 1 * 64 * 18) return fused_launch<TI, TG, VEC, 1, 18, COUPLED>(a, used);
+  if (ng <= 3 * 64 * 18) return fused_launch<TI, TG, VEC, 3, 18, COUPLED>(a, used);
+  if (ng <= 7 * 64 * 18) return fused_launch<TI, TG, VEC, 7, 18, COUPLED>(a, used);
+  if (ng <= 15 * 64 * 18) return fused_launch<TI, TG, VEC, 15, 18, COUPLED>(a, used);
+  if (ng <= 15 * 64 * 20) return fused_launch<TI, TG, VEC, 15, 20, COUPLED>(a, used);
+  return hipSuccess;
 }
 
 template <class TI, class TG, bool VEC>
@@ -490,16 +858,26 @@ void grad_launch(const TopLossArgs& a) {
 
 template <class TI, bool VEC>
 hipError_t launch_vec(const TopLossArgs& a) {
-  const size_t map = size_t((a.V + 7) / 32 + 1) * 4;
+  const bool coupled = a.w_wtv != 0.f || a.w_eal != 0.f;
+  bool used = false;
   hipError_t e = hipSuccess;
+  if (!a.streaming) {
+    if (a.gd == DType::kBf16)
+      e = coupled ? fused_size<TI, GBf16, VEC, true>(a, &used) : fused_size<TI, GBf16, VEC, false>(a, &used);
+    else
+      e = coupled ? fused_size<TI, GF32, VEC, true>(a, &used) : fused_size<TI, GF32, VEC, false>(a, &used);
+    if (e != hipSuccess) return e;
+    if (used) return loss_launch(a, coupled);
+  }
   with_row_shape<4>(a.R, a.V, TI::kVec, [&](auto sh) {
     using Sh = decltype(sh);
-    k_top_rows<TI, VEC, Sh::kU, Sh::kBlock><<<dim3(unsigned(a.R)), Sh::kBlock, map, a.stream>>>(params_of(a));
+    k_top_rows<TI, VEC, Sh::kU, Sh::kBlock>
+        <<<dim3(unsigned(a.R)), Sh::kBlock, size_t(bitmap_words(a.V)) * 4, a.stream>>>(params_of(a));
     e = hipGetLastError();
   });
   if (e != hipSuccess) return e;
-  k_top_scan<<<dim3(unsigned((a.R + kRowBlock - 1) / kRowBlock)), kRowBlock, 0, a.stream>>>(scan_of(a));
-  if ((e = loss_launch(a, nullptr)) != hipSuccess) return e;
+  k_top_scan<<<dim3(unsigned((a.R + kRowBlock - 1) / kRowBlock)), kRowBlock, 0, a.stream>>>(params_of(a));
+  if ((e = loss_launch(a, false)) != hipSuccess) return e;
   if (a.grad) a.gd == DType::kBf16 ? grad_launch<TI, GBf16, VEC>(a) : grad_launch<TI, GF32, VEC>(a);
   return hipGetLastError();
 }

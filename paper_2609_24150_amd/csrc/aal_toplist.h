@@ -28,19 +28,19 @@ hipError_t launch_topk(const TopkArgs& a);
 // Per-row results of the row pass and coefficients of the gradient.  64 bytes.
 struct TopRow {
   float msc, inv_s;   // draft: fl(max * sc), 1 / sum of 2^(z*sc - msc)
-  float mt, inv_zt;   // target: largest t*sct of the list and the remainder, 1 / sum
+  float tmax, inv_zt; // target: largest logit of the list, p_i = inv_zt 2^((t - tmax)*sct)
   float a_tv, a_eal;  // acceptances
   float qlt;          // sum of q over the entries (the remainder among them) with q < p
   float kl;           // KL(p || q) in nats
   float share;        // p_rest / q_rest, 0 where q_rest = 0
   int32_t xstar;      // greedy token of the list, -1 for an empty one
-  int32_t flags;      // kTopHas: the list holds any mass; kTopRestBelow: q_rest < p_rest
+  int32_t flags;      // kTopHas: the row has a target; kTopRestBelow: q_rest < p_rest; kTopDeep: see aal_topk_loss.hip
   float cR;           // unlisted entries: g = cR 2^(z*sc - msc)
   float cA, cB;       // listed entries: g = q (q < p ? cA : cB) - cP p + cX [v = x*]
   float cP, cX;
 };
 static_assert(sizeof(TopRow) == 64, "TopRow layout");
-constexpr int kTopHas = 1, kTopRestBelow = 2;
+constexpr int kTopHas = 1, kTopRestBelow = 2, kTopDeep = 4;
 
 struct TopLossArgs {
   DType in, td, gd;        // draft logits, listed logits, gradient
@@ -64,18 +64,17 @@ struct TopLossArgs {
   void* grad;
   const float* grad_scale;
   TopRow* stats;           // workspace [R]
-  float2* win;             // workspace [W]: E_tv, E_eal
   float2* row_loss;        // workspace [R]: KL, windows that contain the row * (1 - a_tv)
   double* loss_parts;      // workspace [kTopLossParts][4]
   uint64_t* slots;         // workspace [R][2]: tagged acceptances of the resident schedule
-  unsigned* err;           // workspace: poll time-out flag of the resident schedule
+  unsigned* err;           // workspace [2]: poll time-out flag of the resident schedule, a counter
   bool streaming, coop;
   hipStream_t stream;
 };
 constexpr int kTopLossParts = 64;
 
-inline size_t top_loss_workspace_bytes(int64_t rows, int64_t windows) {
-  return align256(size_t(rows) * sizeof(TopRow)) + align256(size_t(windows) * sizeof(float2)) +
+inline size_t top_loss_workspace_bytes(int64_t rows) {
+  return align256(size_t(rows) * sizeof(TopRow)) +
          align256(size_t(rows) * sizeof(float2)) + align256(size_t(kTopLossParts) * 4 * sizeof(double)) +
          align256(size_t(rows) * 2 * sizeof(uint64_t)) + 256;
 }

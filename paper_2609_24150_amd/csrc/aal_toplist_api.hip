@@ -116,7 +116,7 @@ aal_status_t aal_topk_logits(const void* z, aal_dtype_t in_dtype, int64_t rows, 
 
 size_t aal_topk_loss_workspace_bytes(aal_layout_t layout, int64_t B, int32_t S, int32_t K) {
   int64_t rows = 0, windows = 0;
-  return layout_sizes(raw(layout), B, S, K, &rows, &windows) ? aal::top_loss_workspace_bytes(rows, windows) : 0;
+  return layout_sizes(raw(layout), B, S, K, &rows, &windows) ? aal::top_loss_workspace_bytes(rows) : 0;
 }
 
 aal_status_t aal_topk_loss_fwd_bwd(const void* z_draft, aal_dtype_t in_dtype, const void* top_logits,
@@ -148,7 +148,7 @@ aal_status_t aal_topk_loss_fwd_bwd(const void* z_draft, aal_dtype_t in_dtype, co
   if (flags & ~(AAL_FLAG_STREAMING | AAL_FLAG_COOPERATIVE)) return fail(AAL_ERR_ARG, "unknown flags 0x%x", flags);
   if (!aligned(z_draft, 16)) return fail(AAL_ERR_ALIGN, "logit pointers must be 16-byte aligned");
   if (grad_draft && !aligned(grad_draft, 16)) return fail(AAL_ERR_ALIGN, "grad_draft must be 16-byte aligned");
-  if (aal_status_t s = check_workspace(workspace, workspace_bytes, aal::top_loss_workspace_bytes(rows, windows));
+  if (aal_status_t s = check_workspace(workspace, workspace_bytes, aal::top_loss_workspace_bytes(rows));
       s != AAL_OK)
     return s;
   aal::TopLossArgs a{};
@@ -190,7 +190,6 @@ aal_status_t aal_topk_loss_fwd_bwd(const void* z_draft, aal_dtype_t in_dtype, co
     return at;
   };
   a.stats = reinterpret_cast<aal::TopRow*>(carve(size_t(rows) * sizeof(aal::TopRow)));
-  a.win = reinterpret_cast<float2*>(carve(size_t(windows) * sizeof(float2)));
   a.row_loss = reinterpret_cast<float2*>(carve(size_t(rows) * sizeof(float2)));
   a.loss_parts = reinterpret_cast<double*>(carve(size_t(aal::kTopLossParts) * 4 * sizeof(double)));
   a.slots = reinterpret_cast<uint64_t*>(carve(size_t(rows) * 2 * sizeof(uint64_t)));
