@@ -261,15 +261,22 @@ __device__ __forceinline__ void write_row(const TopLossParams& p, int64_t r, con
 
 // ------------------------------------------------------- resident schedule
 // The bitmap reaches to the end of the last vectors that a workgroup holds.
-inline size_t fused_lds_bytes(int held, int k) { return size_t(bitmap_words(held) + 4 * k) * 4; }
+inline size_t fused_lds_bytes(int held, int k) { return size_t(bitmap_words(held) + 5 * k) * 4; }
 
 // WK waves hold the row, NV vectors a thread; the last wave does the list, the
-// windows and the coefficients beside their passes, so that neither's registers add to the other's.
-// Three barriers a row:
-//   holders: the row arrives; its largest logit  |1| sum over the unlisted entries |2|   |3| gradient, next row's loads
-//   list:    the list arrives; bitmap; target    |1| listed entries of the row     |2| row, windows |3| listed gradient, next list
-// The listed entries' gradient is stored after the next first barrier, when
-// every holder has waited for its stores of the row.
+// windows and the coefficients beside their passes, so that neither's registers
+// add to the other's.  Three barriers a row:
+//   holders                                                list
+//   gradient of the row before, this row's loads           finishes the row before last; this list, bitmap, p
+//   1
+//   each vector as it arrives: largest, sum of the unlisted
+//   2
+//                                                          q, acceptances, neighbours, coefficients
+//   3
+// So the loads of a row run under the gradient pass of the one before and under
+// its own sums, and only the step between 2 and 3 (about 3 us) has none.
+// The listed entries' gradient is stored over the others' after the next row's barrier 2,
+// when every holder has waited for its stores.
 template <class TI, class TG, bool VEC, int WK, int NV, bool COUPLED>
 __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p, int grid, void* __restrict__ grad) {
   using Rv = RowVecs<TI, VEC>;
@@ -289,7 +296,8 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
     float* const lt = reinterpret_cast<float*>(map + kWords);  // target logits
     float* const lz = lt + p.k;                                // the draft's
     int* const li = reinterpret_cast<int*>(lz + p.k);          // ids
-    float* const lg = reinterpret_cast<float*>(li + p.k);      // gradient
+    int* const done_id = li + p.k;                             // of the row before: ids
+    float* const done_g = reinterpret_cast<float*>(done_id + p.k);  // and gradient
     if (blockIdx.x == 0 && lane == 0) *p.counter = 0u;
     for (int i = lane; i < kWords; i += kWave) map[i] = 0;
     int64_t before = -1;
@@ -297,48 +305,34 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
       if (before < 0 || grad == nullptr) return;
       const int64_t e0 = before * int64_t(p.V);
       for (int i = lane; i < p.k; i += kWave)
-        if (lt[i] != kNegInf) TG::store1(grad, e0 + li[i], lg[i]);
+        if (done_id[i] >= 0) TG::store1(grad, e0 + done_id[i], done_g[i]);
     };
     for (int64_t row = blockIdx.x; row < p.R; row += grid) {
       const int head = Rv(row, p.R, p.V).head;
       const int64_t l0 = row * p.k, e0 = row * int64_t(p.V);
-      // this list's entries wait in registers while the row before is finished
-      constexpr int kKeep = kTopMax / kWave;
-      int id[kKeep];
-      float t[kKeep], z[kKeep];
-#pragma unroll
-      for (int n = 0; n < kKeep; ++n) {
-        const int i = lane + n * kWave;
-        id[n] = -1;
-        if (n * kWave < p.k && i < p.k) {
-          id[n] = p.ids[l0 + i];
-          t[n] = load_top(p, l0 + i);
-          if (id[n] >= p.V || t[n] == kNegInf) id[n] = -1;
-          if (id[n] >= 0) {
-            z[n] = TI::load1(p.zd, e0 + id[n]);
-            atomicOr(&map[(id[n] + head) >> 5], 1u << ((id[n] + head) & 31));
-          }
+      for (int i = lane; i < p.k; i += kWave) {
+        int id = p.ids[l0 + i];
+        const float t = load_top(p, l0 + i);
+        if (id >= p.V || t == kNegInf) id = -1;
+        float z = kNegInf;
+        if (id >= 0) {
+          z = TI::load1(p.zd, e0 + id);
+          atomicOr(&map[(id + head) >> 5], 1u << ((id + head) & 31));
         }
-      }
-      lds_barrier();  // 1
-      finish();
-#pragma unroll
-      for (int n = 0; n < kKeep; ++n) {
-        const int i = lane + n * kWave;
-        if (n * kWave < p.k && i < p.k) {
-          li[i] = id[n];
-          lt[i] = id[n] >= 0 ? t[n] : kNegInf;
-          lz[i] = id[n] >= 0 ? z[n] : kNegInf;
-        }
+        li[i] = id;
+        lt[i] = id >= 0 ? t : kNegInf;
+        lz[i] = z;
       }
       wait_lds_all();
-      const RowRef ref = row_ref(wave_max(lane < WK ? sh_m[lane] : kNegInf), p.scd);
+      lds_barrier();  // 1
       const ListTarget lt_row = list_target(p, row, lt, li);
-      const float sz = list_draft(p, lt, lz, ref);
       const RowWindows rw = row_windows(row, p.layout, p.S, p.K);
       lds_barrier();  // 2
-      const float su = wave_sum(lane < WK ? sh_s[lane] : 0.f);
-      TopRow o = list_row(p, lt_row, lt, lz, li, ref, sz, su);
+      const float wm = lane < WK ? sh_m[lane] : kNegInf;
+      const RowRef ref = row_ref(wave_max(wm), p.scd);
+      if (ref.deep) lds_barrier();
+      const float su = wave_sum(lane < WK ? sh_s[lane] * (ref.deep ? 1.f : ex2(fmaxf(wm * p.scd, -1e30f) - ref.msc)) : 0.f);
+      TopRow o = list_row(p, lt_row, lt, lz, li, ref, list_draft(p, lt, lz, ref), su);
       if (lane == 0) {
         publish(p.slots + 2 * row, o.a_tv, 1u);
         publish(p.slots + 2 * row + 1, o.a_eal, 1u);
@@ -368,13 +362,16 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
       row_coefs(o, p, d_tv, d_eal, count);
       if (lane == 0) sh_cR = o.cR;
       lds_barrier();  // 3
+      finish();
       if (lane == 0) write_row(p, row, o, count);
-      // the list's gradient, stored once the row's other entries are; the bitmap is emptied
+      // the list's gradient; the bitmap is emptied
       for (int i = lane; i < p.k; i += kWave) {
-        if (lt[i] == kNegInf) continue;
+        const int id = li[i];
+        done_id[i] = id;
+        if (id < 0) continue;
         const float q = ex2(listed_log2(ref, lz[i], p.scd)) * o.inv_s;
-        lg[i] = listed_grad(o, q, listed_p(o, lt[i], p.sct), li[i]);
-        map[(li[i] + head) >> 5] = 0;
+        done_g[i] = listed_grad(o, q, listed_p(o, lt[i], p.sct), id);
+        map[(id + head) >> 5] = 0;
       }
       wait_lds_all();
       before = row;
@@ -385,19 +382,21 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
   }
 
   // -------------------------------------------------------- the row
-  // rows of whole vectors go through buffer resources, which read zeros and store
-  // nothing past the row
+  // Every load is issued unconditionally, so that a vector's registers have one
+  // definition a row (with conditions the compiler kept old and new vectors side by side
+  // and spilled 63 registers).  Rows of whole vectors go through buffer resources, which
+  // read zeros and store nothing past their end (0 bytes where there is no next
+  // row); lanes past a ragged row's last vector read that one.
   const uint32_t row_bytes = uint32_t(p.V) * sizeof(typename TI::storage), grow_bytes = uint32_t(p.V) * GS;
   u32x4 w[NV];
-  auto row_rsrc = [&](int64_t r) { return make_rsrc(static_cast<const uint8_t*>(p.zd) + r * int64_t(row_bytes), row_bytes); };
-  auto load_vec = [&](const rsrc_t& rs, const Rv& rv, int v) {
-    if constexpr (VEC) {
+  auto load_row_vec = [&](const rsrc_t& rs, const Rv& rv, int last, int v) {
+    if constexpr (VEC)
       w[v] = bld16(rs, uint32_t(tid) * 16u, uint32_t(v) * (BLK * 16u));
-    } else {
-      const int gi = v * BLK + tid;
-      w[v] = Rv::none();
-      if (gi < rv.nload) w[v] = rv.raw(p.zd, gi);
-    }
+    else
+      w[v] = rv.raw(p.zd, min(v * BLK + tid, last));
+  };
+  auto row_rsrc = [&](int64_t r, bool there) {
+    return make_rsrc(static_cast<const uint8_t*>(p.zd) + r * int64_t(row_bytes), there ? row_bytes : 0u);
   };
   // a wave-uniform number that the compiler takes as new, so that it makes the
   // conditions that follow from it where they are used, not once for every vector
@@ -405,117 +404,124 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
     asm volatile("" : "+s"(x));
     return x;
   };
-  // keeps the packed vectors, not unpacked copies of them, between two passes
-  auto pin_all = [&] {
-#pragma unroll
-    for (int v = 0; v < NV; ++v) pin(w[v]);
-  };
   {
     const Rv rv(int64_t(blockIdx.x), p.R, p.V);
-    const rsrc_t rs = row_rsrc(blockIdx.x);
+    const rsrc_t rs = row_rsrc(blockIdx.x, true);
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-      if (v * BLK < rv.ng) load_vec(rs, rv, v);
+    for (int v = 0; v < NV; ++v) load_row_vec(rs, rv, rv.ng - 1, v);
   }
   for (int64_t row = blockIdx.x; row < p.R; row += grid) {
     const Rv rv(row, p.R, p.V);
-    wait_vmem_all();  // the row is here, and the stores of the row before are done
-    // -inf outside the row: in its edge vectors and in those past its last one
     const int last_v = fresh((rv.ng - 1) / BLK), last_t = fresh((rv.ng - 1) % BLK);
+    lds_barrier();  // 1
+    float m = kNegInf, s = 0.f;  // s against max(m sc, -1e30)
+    auto fold = [&](const u32x4& wx, int v) {
+      float x[E];
+      unpackv<TI>(wx, x);
+      float cm = m;
+#pragma unroll
+      for (int e = 0; e < E; ++e) cm = fmaxf(cm, x[e]);
+      const float at = fmaxf(cm * p.scd, -1e30f);
+      const float keep = ex2(fmaxf(m * p.scd, -1e30f) - at);
+      m = cm;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = ex2(__builtin_fmaf(x[e], p.scd, -at));
+      const uint32_t bits = listed_bits<E>(map, v * BLK + tid);
+      if (bits)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (bits >> e & 1u) x[e] = 0.f;
+      s = __builtin_fmaf(s, keep, tree_sum(x));
+    };
     if constexpr (!VEC)
       if (tid == 0 && !rv.whole(0)) w[0] = rv.edge(p.zd, 0, w[0]);
-    {
-      u32x4 x = Rv::none();
-      if (tid <= last_t) {
-        x = w[0];
 #pragma unroll
-        for (int v = 1; v < NV; ++v)
-          if (v == last_v) x = w[v];
-        if constexpr (!VEC)
-          if (tid == last_t && rv.ng > 1 && !rv.whole(rv.ng - 1)) x = rv.edge(p.zd, rv.ng - 1, x);
+    for (int v = 0; v < NV; ++v) {
+      if (v < last_v) {
+        pin(w[v]);
+        fold(w[v], v);
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the row's last vectors, on their own: -inf past its end
+    u32x4 wl = w[0];
+#pragma unroll
+    for (int v = 1; v < NV; ++v)
+      if (v == last_v) wl = w[v];
+    if (tid > last_t) wl = Rv::none();
+    if constexpr (!VEC)
+      if (tid == last_t && rv.ng > 1 && !rv.whole(rv.ng - 1)) wl = rv.edge(p.zd, rv.ng - 1, wl);
+    pin(wl);
+    fold(wl, last_v);
+    wait_vmem_all();  // the stores of the row before are done
+    {
+      const float M = wave_max(m);
+      s = wave_sum(s * ex2(fmaxf(m * p.scd, -1e30f) - fmaxf(M * p.scd, -1e30f)));
+      if (lane == 0) {
+        sh_m[wv] = M;
+        sh_s[wv] = s;
+      }
+      m = M;
+    }
+    lds_barrier();  // 2
+    m = wave_max(lane < WK ? sh_m[lane] : kNegInf);
+    const RowRef ref = row_ref(m, p.scd);
+    if (ref.deep) {  // nothing was above -1e30: the sum again, at its scale
+      s = 0.f;
+      auto again = [&](const u32x4& wx, int v) {
+        float x[E];
+        unpackv<TI>(wx, x);
+        const uint32_t bits = listed_bits<E>(map, v * BLK + tid);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s += bits >> e & 1u ? 0.f : ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
+      };
 #pragma unroll
       for (int v = 0; v < NV; ++v)
-        if (v == last_v) w[v] = x;
+        if (v < last_v) again(w[v], v);
+      again(wl, last_v);
+      s = wave_sum(s);
+      if (lane == 0) sh_s[wv] = s;
+      lds_barrier();  // 2, for the list too
     }
-    float m = kNegInf;
-    pin_all();
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (v <= last_v) {
-        float x[E];
-        unpackv<TI>(w[v], x);
-#pragma unroll
-        for (int e = 0; e < E; ++e) m = fmaxf(m, x[e]);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    m = wave_max(m);
-    if (lane == 0) sh_m[wv] = m;
-    lds_barrier();  // 1
-    const RowRef ref = row_ref(wave_max(lane < WK ? sh_m[lane] : kNegInf), p.scd);
-    float s = 0.f;
-    pin_all();
-    const int last_v2 = fresh(last_v);
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (v <= last_v2) {
-        float x[E];
-        unpackv<TI>(w[v], x);
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
-        const uint32_t bits = listed_bits<E>(map, v * BLK + tid);
-        if (bits)
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (bits >> e & 1u) x[e] = 0.f;
-        s += tree_sum(x);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    s = wave_sum(s);
-    if (lane == 0) sh_s[wv] = s;
-    lds_barrier();  // 2
     lds_barrier();  // 3
     const int64_t next = row + grid;
     const bool more = next < p.R;
     const Rv rn(more ? next : row, p.R, p.V);
-    const rsrc_t rsn = row_rsrc(more ? next : row);
+    const rsrc_t rsn = row_rsrc(more ? next : row, more);
+    const int last_n = more ? rn.ng - 1 : 0;
     const float cR = sh_cR;
-    pin_all();
-    const int last_v3 = fresh(last_v), last_n = fresh(more ? (rn.ng - 1) / BLK : -1);
-    if (grad != nullptr) {
-      const rsrc_t gr = make_rsrc(static_cast<uint8_t*>(grad) + row * int64_t(grow_bytes), grow_bytes);
+    const int last_v3 = fresh(grad != nullptr ? last_v : -1);
+    const rsrc_t gr = make_rsrc(static_cast<uint8_t*>(grad) + row * int64_t(grow_bytes), grow_bytes);
+    auto store = [&](const u32x4& wx, int v) {
+      const int gi = v * BLK + tid;
+      float x[E];
+      unpackv<TI>(wx, x);
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        if (v <= last_v3) {
-          const int gi = v * BLK + tid;
-          float x[E];
-          unpackv<TI>(w[v], x);
-#pragma unroll
-          for (int e = 0; e < E; ++e) x[e] = cR * ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
-          if constexpr (VEC) {
-            store_g<TG, E>(gr, uint32_t(gi) * (E * GS), x);  // dropped past the row
-          } else if (rv.whole(gi)) {
-            store_vec<TG, E>(grad, (rv.g0 + gi) * E, x);
-          } else if (gi < rv.ng) {
+      for (int e = 0; e < E; ++e) x[e] = cR * ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
+      if constexpr (VEC) {
+        store_g<TG, E>(gr, uint32_t(gi) * (E * GS), x);  // dropped past the row
+      } else if (rv.whole(gi)) {
+        store_vec<TG, E>(grad, (rv.g0 + gi) * E, x);
+      } else if (gi < rv.ng) {
 #pragma unroll 1
-            for (int e = 0; e < E; ++e) {
-              const int i = rv.index(gi, e);
-              float ge = x[0];
+        for (int e = 0; e < E; ++e) {
+          const int i = rv.index(gi, e);
+          float ge = x[0];
 #pragma unroll
-              for (int q = 1; q < E; ++q) ge = e == q ? x[q] : ge;
-              if (i >= 0 && i < p.V) TG::store1(grad, (rv.g0 + gi) * E + e, ge);
-            }
-          }
+          for (int q = 1; q < E; ++q) ge = e == q ? x[q] : ge;
+          if (i >= 0 && i < p.V) TG::store1(grad, (rv.g0 + gi) * E + e, ge);
         }
-        if (v <= last_n) load_vec(rsn, rn, v);
-        __builtin_amdgcn_sched_barrier(0);
       }
-    } else {
+    };
+    if (last_v3 >= 0) store(wl, last_v);
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
-        if (v <= last_n) load_vec(rsn, rn, v);
+    for (int v = 0; v < NV; ++v) {
+      if (v < last_v3) {
+        pin(w[v]);  // the packed vector was kept, not unpacked copies of it
+        store(w[v], v);
+      }
+      load_row_vec(rsn, rn, last_n, v);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   wait_vmem_all();
@@ -838,6 +844,7 @@ hipError_t fused_launch(const TopLossArgs& a, bool* used) {
 template <class TI, class TG, bool VEC, bool COUPLED>
 hipError_t fused_size(const TopLossArgs& a, bool* used) {
   const int ng = a.V / TI::kVec + (VEC ? 0 : 2);  // vectors that cover a row, at most
+  if (a.R * a.V < TI::kVec) return hipSuccess;  // less than a vector in all
   if (ng <= 1 * 64 * 18) return fused_launch<TI, TG, VEC, 1, 18, COUPLED>(a, used);
   if (ng <= 3 * 64 * 18) return fused_launch<TI, TG, VEC, 3, 18, COUPLED>(a, used);
   if (ng <= 7 * 64 * 18) return fused_launch<TI, TG, VEC, 7, 18, COUPLED>(a, used);
