@@ -261,7 +261,10 @@ __device__ __forceinline__ void write_row(const TopLossParams& p, int64_t r, con
 
 // ------------------------------------------------------- resident schedule
 // The bitmap reaches to the end of the last vectors that a workgroup holds.
-inline size_t fused_lds_bytes(int held, int k) { return size_t(bitmap_words(held) + 5 * k) * 4; }
+constexpr int stage_words(int held) { return (bitmap_words(held) + 3) & ~3; }  // before the staging buffer
+inline size_t fused_lds_bytes(int held, int staged, int k) {
+  return size_t(stage_words(held)) * 4 + size_t(staged) * 16 + size_t(k) * 20;
+}
 
 // WK waves hold the row, NV vectors a thread; the last wave does the list, the
 // windows and the coefficients beside their passes, so that neither's registers
@@ -277,23 +280,24 @@ inline size_t fused_lds_bytes(int held, int k) { return size_t(bitmap_words(held
 // its own sums, and only the step between 2 and 3 (about 3 us) has none.
 // The listed entries' gradient is stored over the others' after the next row's barrier 2,
 // when every holder has waited for its stores.
-template <class TI, class TG, bool VEC, int WK, int NV, bool COUPLED>
+template <class TI, class TG, bool VEC, int WK, int NV, int NS, bool COUPLED>
 __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p, int grid, void* __restrict__ grad) {
   using Rv = RowVecs<TI, VEC>;
   constexpr int E = Rv::E;
   constexpr int BLK = WK * kWave;  // threads that hold the row
-  constexpr int kWords = bitmap_words(NV * BLK * E);
+  constexpr int kWords = stage_words(NV * BLK * E);
   constexpr int GS = sizeof(typename TG::storage);
   extern __shared__ uint32_t sh_dyn[];
   __shared__ float sh_m[WK], sh_s[WK], sh_cR;
   __shared__ float sh_a[2][128];  // acceptances of the row's neighbours (COUPLED)
   uint32_t* const map = sh_dyn;
+  u32x4* const stage = reinterpret_cast<u32x4*>(map + kWords);  // NS vectors of a holder
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
   const int wv = __builtin_amdgcn_readfirstlane(tid / kWave);
 
   if (wv == WK) {
     // ------------------------------------------------------- the list
-    float* const lt = reinterpret_cast<float*>(map + kWords);  // target logits
+    float* const lt = reinterpret_cast<float*>(stage + NS * BLK);  // target logits
     float* const lz = lt + p.k;                                // the draft's
     int* const li = reinterpret_cast<int*>(lz + p.k);          // ids
     int* const done_id = li + p.k;                             // of the row before: ids
@@ -389,6 +393,14 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
   // row); lanes past a ragged row's last vector read that one.
   const uint32_t row_bytes = uint32_t(p.V) * sizeof(typename TI::storage), grow_bytes = uint32_t(p.V) * GS;
   u32x4 w[NV];
+  // the first NS vectors of a row go through LDS, straight from memory: their loads
+  // are issued as soon as the row before is summed, and run while its coefficients are made
+  auto stage_row = [&](const rsrc_t& rs) {
+#pragma unroll
+    for (int v = 0; v < NS; ++v)
+      bld16_lds(rs, stage + v * BLK + wv * kWave, uint32_t(tid) * 16u, uint32_t(v) * (BLK * 16u));
+  };
+  static_assert(VEC || NS == 0, "ragged rows are not staged");
   auto load_row_vec = [&](const rsrc_t& rs, const Rv& rv, int last, int v) {
     if constexpr (VEC)
       w[v] = bld16(rs, uint32_t(tid) * 16u, uint32_t(v) * (BLK * 16u));
@@ -407,8 +419,12 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
   {
     const Rv rv(int64_t(blockIdx.x), p.R, p.V);
     const rsrc_t rs = row_rsrc(blockIdx.x, true);
+    stage_row(rs);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) load_row_vec(rs, rv, rv.ng - 1, v);
+    for (int v = NS; v < NV; ++v) {
+      load_row_vec(rs, rv, rv.ng - 1, v);
+      __builtin_amdgcn_sched_barrier(0);  // in the order in which they are waited for
+    }
   }
   for (int64_t row = blockIdx.x; row < p.R; row += grid) {
     const Rv rv(row, p.R, p.V);
@@ -435,8 +451,14 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
     };
     if constexpr (!VEC)
       if (tid == 0 && !rv.whole(0)) w[0] = rv.edge(p.zd, 0, w[0]);
+    if constexpr (NS > 0) {
+      // the staged vectors are older than the NV - NS loads of the others
+      wait_vmem_le<NV - NS>();
+      __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
+      if (v < NS) w[v] = stage[v * BLK + tid];
       if (v < last_v) {
         pin(w[v]);
         fold(w[v], v);
@@ -454,6 +476,10 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
     pin(wl);
     fold(wl, last_v);
     wait_vmem_all();  // the stores of the row before are done
+    const int64_t next = row + grid;
+    const bool more = next < p.R;
+    const rsrc_t rsn = row_rsrc(more ? next : row, more);
+    stage_row(rsn);
     {
       const float M = wave_max(m);
       s = wave_sum(s * ex2(fmaxf(m * p.scd, -1e30f) - fmaxf(M * p.scd, -1e30f)));
@@ -484,10 +510,7 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
       lds_barrier();  // 2, for the list too
     }
     lds_barrier();  // 3
-    const int64_t next = row + grid;
-    const bool more = next < p.R;
     const Rv rn(more ? next : row, p.R, p.V);
-    const rsrc_t rsn = row_rsrc(more ? next : row, more);
     const int last_n = more ? rn.ng - 1 : 0;
     const float cR = sh_cR;
     const int last_v3 = fresh(grad != nullptr ? last_v : -1);
@@ -520,7 +543,7 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
         pin(w[v]);  // the packed vector was kept, not unpacked copies of it
         store(w[v], v);
       }
-      load_row_vec(rsn, rn, last_n, v);
+      if (v >= NS) load_row_vec(rsn, rn, last_n, v);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -804,13 +827,13 @@ hipError_t loss_launch(const TopLossArgs& a, bool waited) {
   return hipGetLastError();
 }
 
-template <class TI, class TG, bool VEC, int WK, int NV, bool COUPLED>
+template <class TI, class TG, bool VEC, int WK, int NV, int NS, bool COUPLED>
 hipError_t fused_launch(const TopLossArgs& a, bool* used) {
   constexpr int BLK = (WK + 1) * kWave;
-  auto kern = k_top_fused<TI, TG, VEC, WK, NV, COUPLED>;
+  auto kern = k_top_fused<TI, TG, VEC, WK, NV, NS, COUPLED>;
   const DevInfo di = device_info();
   if (di.cus == 0 || (COUPLED && a.coop && !di.coop)) return hipSuccess;
-  const size_t lds = fused_lds_bytes(NV * WK * kWave * TI::kVec, a.k);
+  const size_t lds = fused_lds_bytes(NV * WK * kWave * TI::kVec, NS * WK * kWave, a.k);
   int per_cu = 0;
   hipError_t e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kern, BLK, lds);
   if (e != hipSuccess) return e;
@@ -845,11 +868,12 @@ template <class TI, class TG, bool VEC, bool COUPLED>
 hipError_t fused_size(const TopLossArgs& a, bool* used) {
   const int ng = a.V / TI::kVec + (VEC ? 0 : 2);  // vectors that cover a row, at most
   if (a.R * a.V < TI::kVec) return hipSuccess;  // less than a vector in all
-  if (ng <= 1 * 64 * 18) return fused_launch<TI, TG, VEC, 1, 18, COUPLED>(a, used);
-  if (ng <= 3 * 64 * 18) return fused_launch<TI, TG, VEC, 3, 18, COUPLED>(a, used);
-  if (ng <= 7 * 64 * 18) return fused_launch<TI, TG, VEC, 7, 18, COUPLED>(a, used);
-  if (ng <= 15 * 64 * 18) return fused_launch<TI, TG, VEC, 15, 18, COUPLED>(a, used);
-  if (ng <= 15 * 64 * 20) return fused_launch<TI, TG, VEC, 15, 20, COUPLED>(a, used);
+  constexpr int NS = VEC ? 8 : 0;
+  if (ng <= 1 * 64 * 18) return fused_launch<TI, TG, VEC, 1, 18, 0, COUPLED>(a, used);
+  if (ng <= 3 * 64 * 18) return fused_launch<TI, TG, VEC, 3, 18, 0, COUPLED>(a, used);
+  if (ng <= 7 * 64 * 18) return fused_launch<TI, TG, VEC, 7, 18, 0, COUPLED>(a, used);
+  if (ng <= 15 * 64 * 18) return fused_launch<TI, TG, VEC, 15, 18, NS, COUPLED>(a, used);
+  if (ng <= 15 * 64 * 20) return fused_launch<TI, TG, VEC, 15, 20, NS, COUPLED>(a, used);
   return hipSuccess;
 }
 
