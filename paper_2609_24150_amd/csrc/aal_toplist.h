@@ -81,6 +81,15 @@ inline size_t top_loss_workspace_bytes(int64_t rows) {
 
 hipError_t launch_top_loss(const TopLossArgs& a);
 
+// The resident schedule, by element types and by whether V is a multiple of the 16-byte
+// vector; *used = false (and nothing enqueued) where no kernel holds the row.
+hipError_t launch_top_fused_bf16_whole(const TopLossArgs& a, bool* used);
+hipError_t launch_top_fused_bf16_ragged(const TopLossArgs& a, bool* used);
+hipError_t launch_top_fused_bf16_g32_whole(const TopLossArgs& a, bool* used);
+hipError_t launch_top_fused_bf16_g32_ragged(const TopLossArgs& a, bool* used);
+hipError_t launch_top_fused_f32_whole(const TopLossArgs& a, bool* used);
+hipError_t launch_top_fused_f32_ragged(const TopLossArgs& a, bool* used);
+
 // ------------------------------------------------------ logits processing
 struct LogitsRules {
   const int32_t* tokens;
