@@ -10,12 +10,19 @@
 //   dz = 0 where blocked, g / repetition or g * repetition at a history's token
 //   (by the sign of z + bias), else g
 //
-// One workgroup per row and slice of the vocabulary.  Its counters lie in LDS:
-// 16 bits an entry (the high one: in the prompt) for rows that generated up to
-// 32,767 tokens, 32 bits and half the slice at a time for longer ones or rows
-// with biases.  It counts the history's tokens that fall into the slice, then
-// streams the slice; a vector without counts, biases and blocked entries is
-// copied as it is.
+// One workgroup per row and slice of the vocabulary: it loads its first vectors, counts
+// the history's tokens that fall into the slice in LDS, and streams the slice. A
+// vector without counts, biases and blocked entries is copied as it is.
+//   forward   16 bits an entry, the high one for the prompt
+//   backward  one bit an entry: only whether the history holds it
+//   wide      32 bits, and 32 for the place of a bias, 4,096 entries at a time (8,192 without biases): rows that
+//             generated more than 32,767 tokens, rows with more than 256 biases
+// Up to 256 biases of a row are copied to LDS and marked by a bit an entry; an
+// entry with the bit looks its bias up in the copy, from the end.
+// A row whose penalties change nothing has no history.
+//
+// Bound by memory: 3,584 rows of 128,256 bf16 with histories of 1,024 and grammars: see the
+// figures at the launch.
 #include "aal_device.h"
 #include "aal_rowops.h"
 #include "aal_toplist.h"
@@ -23,9 +30,11 @@
 namespace aal {
 namespace {
 
-constexpr int kLpWords = 8192;       // counter words of a slice: 16,384 entries of 16 bits
+constexpr int kLpWords = 8192;       // counter words: 16,384 entries of 16 bits
+constexpr int kWideBias = kLpWords / 2;
 constexpr uint32_t kPrompt16 = 0x8000u, kPrompt32 = 0x80000000u;
 constexpr int kNarrowMost = 32767;   // generated tokens that 15 bits count
+constexpr int kBiasMost = 256;       // biases of a row in LDS
 
 struct LogitsParams {
   const void* src;   // forward: z; backward: the gradient that comes in
@@ -52,36 +61,44 @@ __device__ __forceinline__ uint32_t mask_bits(const uint32_t* m, int i, int word
   return uint32_t(((uint64_t(hi) << 32) | a) >> (i & 31)) & ((1u << E) - 1u);
 }
 
-template <class TI, bool VEC, bool BWD, int BLK>
-__global__ __launch_bounds__(BLK) void k_logits(LogitsParams p) {
+// U vectors of a thread are loaded at once.
+template <class TI, bool VEC, bool BWD, bool BIAS, int BLK, int U>
+__global__ __launch_bounds__(BLK, BWD ? 6 : 8) void k_logits(LogitsParams p) {
   using Rv = RowVecs<TI, VEC>;
   using TG = std::conditional_t<TI::kVec == 8, GBf16, GF32>;
   constexpr int E = Rv::E;
+  constexpr int kMostBits = BWD ? 65536 : 2 * kLpWords;  // entries at a time
   __shared__ __attribute__((aligned(16))) uint32_t sh_cnt[kLpWords];
-  __shared__ __attribute__((aligned(16))) uint32_t sh_pos[kLpWords];
+  __shared__ __attribute__((aligned(16))) uint32_t sh_biased[BIAS ? kMostBits / 32 : 4];  // a bit an entry
+  __shared__ int sh_bid[BIAS ? kBiasMost : 1];
+  __shared__ float sh_bval[BIAS ? kBiasMost : 1];
 
   const int64_t row = blockIdx.x;
   const Rv rv(row, p.rows, p.V);
   const int64_t e0 = row * int64_t(p.V);
   const int gs0 = int(blockIdx.y) * p.slice, gs1 = min(rv.ng, gs0 + p.slice);
+  if (gs0 >= gs1) return;
 
   // the row's rules; whatever the arrays hold, reads stay inside them
   int64_t h0 = 0;
   int nh = 0, np = 0;
   float rep = 1.f, freq = 0.f, pres = 0.f;
   if (p.r.tokens != nullptr) {
-    h0 = clamp64(p.r.hist_start[row], 0, p.r.n_tokens);
-    nh = int(clamp64(p.r.hist_len[row], 0, p.r.n_tokens - h0));
-    np = p.r.prompt_len != nullptr ? min(max(p.r.prompt_len[row], 0), nh) : 0;
     if (p.r.repetition != nullptr) rep = p.r.repetition[row];
-    if (p.r.frequency != nullptr) freq = p.r.frequency[row];
-    if (p.r.presence != nullptr) pres = p.r.presence[row];
+    if (!BWD && p.r.frequency != nullptr) freq = p.r.frequency[row];
+    if (!BWD && p.r.presence != nullptr) pres = p.r.presence[row];
+    if (rep != 1.f || freq != 0.f || pres != 0.f) {
+      h0 = clamp64(p.r.hist_start[row], 0, p.r.n_tokens);
+      nh = int(clamp64(p.r.hist_len[row], 0, p.r.n_tokens - h0));
+      if (!BWD && p.r.prompt_len != nullptr) np = min(max(p.r.prompt_len[row], 0), nh);
+    }
   }
   int64_t b0 = 0;
   int nb = 0;
-  if (p.r.bias_offsets != nullptr) {
+  if constexpr (BIAS) {
     b0 = clamp64(p.r.bias_offsets[row], 0, p.r.n_bias);
     nb = int(clamp64(p.r.bias_offsets[row + 1], b0, p.r.n_bias) - b0);
+    if (BWD && nh == 0) nb = 0;  // a bias alone leaves the gradient as it is
   }
   const uint32_t* mask = nullptr;
   const int words = (p.V + 31) / 32;
@@ -89,100 +106,193 @@ __global__ __launch_bounds__(BLK) void k_logits(LogitsParams p) {
     const int64_t m = p.r.mask_row != nullptr ? int64_t(p.r.mask_row[row]) : p.r.n_masks == 1 ? 0 : row;
     if (m >= 0 && m < p.r.n_masks) mask = p.r.mask + m * words;
   }
-  const bool wide = nb > 0 || nh - np > kNarrowMost;
+  const bool many = BIAS && nb > kBiasMost;
+  const bool wide = many || (!BWD && nh - np > kNarrowMost);
   const bool rules = nh > 0 || nb > 0;
-  const int step = wide ? kLpWords / E : 2 * kLpWords / E;  // vectors that the counters cover
+  uint32_t* const sh_pos = sh_cnt + kWideBias;
+  // vectors that the counters cover
+  const int step = (wide ? (many ? kWideBias : kLpWords) : kMostBits) / E;
 
   for (int gp0 = gs0; gp0 < gs1; gp0 += step) {
     const int gp1 = min(gs1, gp0 + step);
+    // the first vectors are on their way while the history is counted
+    u32x4 w[1][U];
+    rv.load({p.src}, gp0 + int(threadIdx.x), BLK, w);
     if (rules) {
       const int n = (gp1 - gp0) * E;  // entries of this part
-      const int used = wide ? n : (n + 1) / 2;
+      const int used = ((wide ? n : BWD ? (n + 31) / 32 : n / 2) + 3) / 4;
       __syncthreads();
+      const uint4 zero = make_uint4(0, 0, 0, 0);
       for (int i = threadIdx.x; i < used; i += BLK) {
-        sh_cnt[i] = 0;
-        if (nb > 0) sh_pos[i] = 0;
+        reinterpret_cast<uint4*>(sh_cnt)[i] = zero;
+        if (many) reinterpret_cast<uint4*>(sh_pos)[i] = zero;
       }
+      if (BIAS && nb > 0 && !many)
+        for (int i = threadIdx.x; i < (n + 127) / 128; i += BLK) reinterpret_cast<uint4*>(sh_biased)[i] = zero;
       __syncthreads();
       const int first = gp0 * E - rv.head;  // the entry of counter 0
-      for (int i = threadIdx.x; i < nh; i += BLK) {
-        const int t = p.r.tokens[h0 + i];
+      const int lo = max(first, 0), hi = min(first + n, p.V);  // the entries of this part
+      auto count = [&](int i, int t) {
+        if (t < lo || t >= hi) return;
         const int at = t - first;
-        if (t < 0 || t >= p.V || at < 0 || at >= n) continue;
         if (wide) {
           if (i < np) atomicOr(&sh_cnt[at], kPrompt32);
           else atomicAdd(&sh_cnt[at], 1u);
+        } else if (BWD) {
+          atomicOr(&sh_cnt[at >> 5], 1u << (at & 31));
         } else {
           const int sh = (at & 1) * 16;
           if (i < np) atomicOr(&sh_cnt[at >> 1], kPrompt16 << sh);
           else atomicAdd(&sh_cnt[at >> 1], 1u << sh);
         }
+      };
+      // four tokens of a thread at once: a wait for memory per 4 BLK tokens
+      int i = threadIdx.x;
+      for (; i + 3 * BLK < nh; i += 4 * BLK) {
+        int t[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) t[q] = p.r.tokens[h0 + i + q * BLK];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) count(i + q * BLK, t[q]);
       }
-      for (int i = threadIdx.x; i < nb; i += BLK) {
-        const int t = p.r.bias_ids[b0 + i];
-        const int at = t - first;
-        // of equal ids the last one counts
-        if (t >= 0 && t < p.V && at >= 0 && at < n) atomicMax(&sh_pos[at], uint32_t(i) + 1u);
-      }
+      for (; i < nh; i += BLK) count(i, p.r.tokens[h0 + i]);
+      if constexpr (BIAS)
+        for (int j = threadIdx.x; j < nb; j += BLK) {
+          const int t = p.r.bias_ids[b0 + j], at = t - first;
+          const bool in = t >= lo && t < hi;
+          if (many) {  // of equal ids the last one counts
+            if (in) atomicMax(&sh_pos[at], uint32_t(j) + 1u);
+          } else {
+            sh_bid[j] = t;
+            sh_bval[j] = p.r.bias_values[b0 + j];
+            if (in) atomicOr(&sh_biased[at >> 5], 1u << (at & 31));
+          }
+        }
       __syncthreads();
     }
-    for (int gi = gp0 + int(threadIdx.x); gi < gp1; gi += BLK) {
-      u32x4 w = rv.load(p.src, gi);
+    // the counters of a vector (bit 31: in the prompt), and a bit for each biased entry
+    auto counters = [&](int gi, uint32_t (&c)[E], uint32_t& biased) {
       const int at = (gi - gp0) * E;
-      uint32_t cnt[E], pos[E], any = 0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) cnt[e] = pos[e] = 0;
-      if (rules) {
+      uint32_t any = 0;
+      biased = 0;
+      if (wide) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          if (wide) {
-            cnt[e] = sh_cnt[at + e];
-            if (nb > 0) pos[e] = sh_pos[at + e];
-          } else {
-            const uint32_t c = sh_cnt[(at + e) >> 1] >> ((e & 1) * 16) & 0xffffu;
-            cnt[e] = (c & 0x7fffu) | (c & kPrompt16 ? kPrompt32 : 0u);
-          }
-          any |= cnt[e] | pos[e];
+          c[e] = sh_cnt[at + e];
+          any |= c[e];
+          if (many && sh_pos[at + e] != 0u) biased |= 1u << e;
+        }
+        if (BIAS && nb > 0 && !many) biased = sh_biased[at >> 5] >> (at & 31) & ((1u << E) - 1u);
+        return any;
+      }
+      if constexpr (BWD) {
+        any = sh_cnt[at >> 5] >> (at & 31) & ((1u << E) - 1u);
+#pragma unroll
+        for (int e = 0; e < E; ++e) c[e] = any >> e & 1u;
+      } else {
+        uint32_t two[E / 2];
+        __builtin_memcpy(two, __builtin_assume_aligned(sh_cnt + at / 2, E * 2), E * 2);
+#pragma unroll
+        for (int q = 0; q < E / 2; ++q) any |= two[q];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const uint32_t h = e & 1 ? two[e / 2] >> 16 : two[e / 2] & 0xffffu;
+          c[e] = (h & 0x7fffu) | ((h & kPrompt16) << 16);
         }
       }
-      float x[E];
-      TI::unpack(to_uint4(w), x);
-      if (any) {
+      if (BIAS && nb > 0) biased = sh_biased[at >> 5] >> (at & 31) & ((1u << E) - 1u);
+      return any;
+    };
+    auto bias_of = [&](int gi, int e) {
+      if (many) return p.r.bias_values[b0 + sh_pos[(gi - gp0) * E + e] - 1];
+      const int v = rv.index(gi, e);
+      int j = nb - 1;
+      while (j > 0 && sh_bid[j] != v) --j;
+      return sh_bval[j];
+    };
+    for (int base = gp0 + int(threadIdx.x); base < gp1; base += BLK * U) {
+      if (base >= gp0 + BLK * U) rv.load({p.src}, base, BLK, w);
+      // backward: the logits of the vectors with seen entries, all on their way at once
+      u32x4 zv[BWD ? U : 1];
+      const bool same = BWD && p.z_bf16 == (E == 8);
+      if constexpr (BWD)
+        if (rules && same) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          if ((cnt[e] | pos[e]) == 0) continue;
-          const int v = rv.index(gi, e);
-          float y = x[e];
-          if constexpr (BWD) y = p.z_bf16 ? Bf16::load1(p.z, e0 + v) : F32::load1(p.z, e0 + v);
-          if (pos[e]) y += p.r.bias_values[b0 + pos[e] - 1];
+          for (int u = 0; u < U; ++u) {
+            const int gi = base + u * BLK;
+            uint32_t c[E], biased;
+            zv[u] = Rv::none();
+            if (gi < gp1 && counters(gi, c, biased)) zv[u] = rv.load(p.z, gi);
+          }
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int gi = base + u * BLK;
+        if (gi >= gp1) break;
+        float x[E];
+        TI::unpack(to_uint4(w[0][u]), x);
+        if (rules) {
+          uint32_t c[E], biased;
+          const uint32_t any = counters(gi, c, biased);
           if constexpr (BWD) {
-            if (cnt[e]) x[e] = y > 0.f ? x[e] / rep : x[e] * rep;
-          } else {
-            if (cnt[e]) {
-              y = y > 0.f ? y / rep : y * rep;
-              const uint32_t c = cnt[e] & ~kPrompt32;
-              y -= freq * float(c) + (c ? pres : 0.f);
+            if (any) {
+              float y[E];
+              if (same) {
+                TI::unpack(to_uint4(zv[u]), y);
+              } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                  const int64_t at = e0 + (c[e] ? rv.index(gi, e) : 0);
+                  y[e] = p.z_bf16 ? Bf16::load1(p.z, at) : F32::load1(p.z, at);
+                }
+              }
+#pragma unroll
+              for (int e = 0; e < E; ++e) {
+                if (c[e] == 0u) continue;
+                if (BIAS && (biased >> e & 1u)) y[e] += bias_of(gi, e);
+                x[e] = y[e] > 0.f ? x[e] / rep : x[e] * rep;
+              }
             }
-            x[e] = y;
+          } else if (any | biased) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              float y = x[e];
+              if (BIAS && (biased >> e & 1u)) y += bias_of(gi, e);
+              if (c[e]) {
+                y = y > 0.f ? y / rep : y * rep;
+                const uint32_t n = c[e] & ~kPrompt32;
+                y -= freq * float(n) + (n ? pres : 0.f);
+              }
+              x[e] = y;
+            }
           }
         }
-      }
-      if (mask != nullptr) {
-        const uint32_t free = mask_bits<E>(mask, rv.index(gi, 0), words);
-        // by whole numbers: a blocked entry may hold anything, NaN too
-        constexpr uint32_t kBlocked = BWD ? 0u : 0xff800000u;
+        if (mask != nullptr) {
+          const uint32_t free = mask_bits<E>(mask, rv.index(gi, 0), words);
+          // by whole numbers: a blocked entry may hold anything, NaN too
+          constexpr uint32_t kBlocked = BWD ? 0u : 0xff800000u;
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          x[e] = __builtin_bit_cast(float, free >> e & 1u ? __builtin_bit_cast(uint32_t, x[e]) : kBlocked);
+          for (int e = 0; e < E; ++e)
+            x[e] = __builtin_bit_cast(float, free >> e & 1u ? __builtin_bit_cast(uint32_t, x[e]) : kBlocked);
+        }
+        rv.template store<TG>(p.out, gi, x);
       }
-      rv.template store<TG>(p.out, gi, x);
     }
   }
 }
 
-template <class TI, bool VEC, bool BWD>
+// Entries of a workgroup's slice: as many as the counters hold at once (backward, where
+// they hold a whole row, a quarter of 131,072), fewer where that makes fewer than
+// 1,024 workgroups, four a CU, but at least 4,096 or the history is read too often.
+template <bool BWD>
+int slice_entries(int64_t rows, int V) {
+  int n = BWD ? 32768 : 2 * kLpWords;
+  while (n > 4096 && rows * ((V + n - 1) / n) < 1024) n /= 2;
+  return n;
+}
+
+template <class TI, bool VEC, bool BWD, bool BIAS>
 hipError_t launch_vec(const LogitsArgs& a) {
-  constexpr int kBlk = 512;
   LogitsParams p{};
   p.src = BWD ? a.grad_out : a.z;
   p.z = a.z;
@@ -191,16 +301,21 @@ hipError_t launch_vec(const LogitsArgs& a) {
   p.rows = a.rows;
   p.V = a.V;
   p.r = a.rules;
-  const int ng = a.V / TI::kVec + 2;  // at most: a row may start and end inside a vector
-  p.slice = 2 * kLpWords / TI::kVec;
-  const unsigned slices = unsigned((ng + p.slice - 1) / p.slice);
-  k_logits<TI, VEC, BWD, kBlk><<<dim3(unsigned(a.rows), slices), kBlk, 0, a.stream>>>(p);
+  const int ng = a.V / TI::kVec + (VEC ? 0 : 2);  // at most: a row may start and end inside a vector
+  p.slice = slice_entries<BWD>(a.rows, a.V) / TI::kVec;
+  const dim3 grid(unsigned(a.rows), unsigned((ng + p.slice - 1) / p.slice));
+  if (ng <= 512)
+    k_logits<TI, VEC, BWD, BIAS, 128, 4><<<grid, 128, 0, a.stream>>>(p);
+  else
+    k_logits<TI, VEC, BWD, BIAS, 512, 4><<<grid, 512, 0, a.stream>>>(p);
   return hipGetLastError();
 }
 
 template <class TI, bool BWD>
 hipError_t launch_typed(const LogitsArgs& a) {
-  return a.V % TI::kVec == 0 ? launch_vec<TI, true, BWD>(a) : launch_vec<TI, false, BWD>(a);
+  const bool bias = a.rules.bias_offsets != nullptr;
+  if (a.V % TI::kVec == 0) return bias ? launch_vec<TI, true, BWD, true>(a) : launch_vec<TI, true, BWD, false>(a);
+  return bias ? launch_vec<TI, false, BWD, true>(a) : launch_vec<TI, false, BWD, false>(a);
 }
 
 }  // namespace
