@@ -15,10 +15,10 @@
 // vector without counts, biases and blocked entries is copied as it is.
 //   forward   16 bits an entry, the high one for the prompt
 //   backward  one bit an entry: only whether the history holds it
-//   wide      32 bits, and 32 for the place of a bias, 4,096 entries at a time (8,192 without biases): rows that
-//             generated more than 32,767 tokens, rows with more than 256 biases
-// Up to 256 biases of a row are copied to LDS and marked by a bit an entry; an
-// entry with the bit looks its bias up in the copy, from the end.
+//   wide      32 bits, and 32 more for the place of a bias, a part of the slice at a
+//             time: rows that generated more than 32,767 tokens or have more than 256 biases
+// Up to 256 biases of a row are marked by a bit an entry and found through a hash table in
+// LDS (a search of the list cost 16,760 rows of 16,609 with up to 100 biases 927 us).
 // A row whose penalties change nothing has no history.
 //
 // Bound by memory: 3,584 rows of 128,256 bf16 with histories of 1,024 and grammars: see the
@@ -30,11 +30,12 @@
 namespace aal {
 namespace {
 
-constexpr int kLpWords = 8192;       // counter words: 16,384 entries of 16 bits
-constexpr int kWideBias = kLpWords / 2;
+constexpr int kLpWords = 8192;       // counter words, at most: 16,384 entries of 16 bits
 constexpr uint32_t kPrompt16 = 0x8000u, kPrompt32 = 0x80000000u;
 constexpr int kNarrowMost = 32767;   // generated tokens that 15 bits count
 constexpr int kBiasMost = 256;       // biases of a row in LDS
+constexpr int kBiasSlots = 2 * kBiasMost;
+__device__ __forceinline__ int bias_slot(int v) { return int((uint32_t(v) * 2654435761u) >> 16) & (kBiasSlots - 1); }
 
 struct LogitsParams {
   const void* src;   // forward: z; backward: the gradient that comes in
@@ -44,6 +45,7 @@ struct LogitsParams {
   int64_t rows;
   int V;
   int slice;         // vectors of a workgroup
+  int words;         // counter words in LDS, a multiple of 8
   LogitsRules r;
 };
 
@@ -62,16 +64,18 @@ __device__ __forceinline__ uint32_t mask_bits(const uint32_t* m, int i, int word
 }
 
 // U vectors of a thread are loaded at once.
-template <class TI, bool VEC, bool BWD, bool BIAS, int BLK, int U>
-__global__ __launch_bounds__(BLK, BWD ? 6 : 8) void k_logits(LogitsParams p) {
+template <class TI, bool VEC, bool BWD, bool BIAS, int BLK, int U, int MINW>
+__global__ __launch_bounds__(BLK, MINW) void k_logits(LogitsParams p) {
   using Rv = RowVecs<TI, VEC>;
   using TG = std::conditional_t<TI::kVec == 8, GBf16, GF32>;
   constexpr int E = Rv::E;
-  constexpr int kMostBits = BWD ? 65536 : 2 * kLpWords;  // entries at a time
-  __shared__ __attribute__((aligned(16))) uint32_t sh_cnt[kLpWords];
-  __shared__ __attribute__((aligned(16))) uint32_t sh_biased[BIAS ? kMostBits / 32 : 4];  // a bit an entry
-  __shared__ int sh_bid[BIAS ? kBiasMost : 1];
-  __shared__ float sh_bval[BIAS ? kBiasMost : 1];
+  constexpr int kBiasRounds = (kBiasMost + BLK - 1) / BLK;
+  extern __shared__ __attribute__((aligned(16))) uint32_t sh_cnt[];  // p.words of them
+  uint32_t* const sh_biased = sh_cnt + p.words;                      // BIAS: a bit an entry
+  // the part's biases by entry (a hash table), and the place of the last one there
+  __shared__ int sh_bkey[BIAS ? kBiasSlots : 1];
+  __shared__ uint32_t sh_bpos[BIAS ? kBiasSlots : 1];
+  __shared__ float sh_bval[BIAS ? kBiasSlots : 1];
 
   const int64_t row = blockIdx.x;
   const Rv rv(row, p.rows, p.V);
@@ -109,9 +113,9 @@ __global__ __launch_bounds__(BLK, BWD ? 6 : 8) void k_logits(LogitsParams p) {
   const bool many = BIAS && nb > kBiasMost;
   const bool wide = many || (!BWD && nh - np > kNarrowMost);
   const bool rules = nh > 0 || nb > 0;
-  uint32_t* const sh_pos = sh_cnt + kWideBias;
+  uint32_t* const sh_pos = sh_cnt + p.words / 2;
   // vectors that the counters cover
-  const int step = (wide ? (many ? kWideBias : kLpWords) : kMostBits) / E;
+  const int step = wide ? (many ? p.words / 2 : p.words) / E : p.slice;
 
   for (int gp0 = gs0; gp0 < gs1; gp0 += step) {
     const int gp1 = min(gs1, gp0 + step);
@@ -127,8 +131,13 @@ __global__ __launch_bounds__(BLK, BWD ? 6 : 8) void k_logits(LogitsParams p) {
         reinterpret_cast<uint4*>(sh_cnt)[i] = zero;
         if (many) reinterpret_cast<uint4*>(sh_pos)[i] = zero;
       }
-      if (BIAS && nb > 0 && !many)
+      if (BIAS && nb > 0 && !many) {
         for (int i = threadIdx.x; i < (n + 127) / 128; i += BLK) reinterpret_cast<uint4*>(sh_biased)[i] = zero;
+        for (int i = threadIdx.x; i < kBiasSlots; i += BLK) {
+          sh_bkey[i] = -1;
+          sh_bpos[i] = 0;
+        }
+      }
       __syncthreads();
       const int first = gp0 * E - rv.head;  // the entry of counter 0
       const int lo = max(first, 0), hi = min(first + n, p.V);  // the entries of this part
@@ -156,18 +165,40 @@ __global__ __launch_bounds__(BLK, BWD ? 6 : 8) void k_logits(LogitsParams p) {
         for (int q = 0; q < 4; ++q) count(i + q * BLK, t[q]);
       }
       for (; i < nh; i += BLK) count(i, p.r.tokens[h0 + i]);
-      if constexpr (BIAS)
-        for (int j = threadIdx.x; j < nb; j += BLK) {
-          const int t = p.r.bias_ids[b0 + j], at = t - first;
-          const bool in = t >= lo && t < hi;
-          if (many) {  // of equal ids the last one counts
-            if (in) atomicMax(&sh_pos[at], uint32_t(j) + 1u);
-          } else {
-            sh_bid[j] = t;
-            sh_bval[j] = p.r.bias_values[b0 + j];
-            if (in) atomicOr(&sh_biased[at >> 5], 1u << (at & 31));
+      if constexpr (BIAS) {
+        // of equal ids the last one counts
+        if (many) {
+          for (int j = threadIdx.x; j < nb; j += BLK) {
+            const int t = p.r.bias_ids[b0 + j];
+            if (t >= lo && t < hi) atomicMax(&sh_pos[t - first], uint32_t(j) + 1u);
           }
+        } else {
+          int slot[kBiasRounds];
+          float value[kBiasRounds];
+#pragma unroll
+          for (int q = 0; q < kBiasRounds; ++q) {
+            const int j = int(threadIdx.x) + q * BLK;
+            slot[q] = -1;
+            if (j >= nb) continue;
+            const int t = p.r.bias_ids[b0 + j];
+            value[q] = p.r.bias_values[b0 + j];
+            if (t < lo || t >= hi) continue;
+            int h = bias_slot(t);
+            for (int n = 0; n < kBiasSlots; ++n) {  // never more than half full
+              const int was = atomicCAS(&sh_bkey[h], -1, t);
+              if (was == -1 || was == t) break;
+              h = (h + 1) & (kBiasSlots - 1);
+            }
+            slot[q] = h;
+            atomicMax(&sh_bpos[h], uint32_t(j) + 1u);
+            atomicOr(&sh_biased[(t - first) >> 5], 1u << ((t - first) & 31));
+          }
+          if (nb > 0) __syncthreads();
+#pragma unroll
+          for (int q = 0; q < kBiasRounds; ++q)
+            if (slot[q] >= 0 && sh_bpos[slot[q]] == uint32_t(threadIdx.x) + uint32_t(q * BLK) + 1u) sh_bval[slot[q]] = value[q];
         }
+      }
       __syncthreads();
     }
     // the counters of a vector (bit 31: in the prompt), and a bit for each biased entry
@@ -206,9 +237,9 @@ __global__ __launch_bounds__(BLK, BWD ? 6 : 8) void k_logits(LogitsParams p) {
     auto bias_of = [&](int gi, int e) {
       if (many) return p.r.bias_values[b0 + sh_pos[(gi - gp0) * E + e] - 1];
       const int v = rv.index(gi, e);
-      int j = nb - 1;
-      while (j > 0 && sh_bid[j] != v) --j;
-      return sh_bval[j];
+      int h = bias_slot(v);
+      for (int n = 0; n < kBiasSlots && sh_bkey[h] != v; ++n) h = (h + 1) & (kBiasSlots - 1);
+      return sh_bval[h];
     };
     for (int base = gp0 + int(threadIdx.x); base < gp1; base += BLK * U) {
       if (base >= gp0 + BLK * U) rv.load({p.src}, base, BLK, w);
@@ -302,12 +333,22 @@ hipError_t launch_vec(const LogitsArgs& a) {
   p.V = a.V;
   p.r = a.rules;
   const int ng = a.V / TI::kVec + (VEC ? 0 : 2);  // at most: a row may start and end inside a vector
-  p.slice = slice_entries<BWD>(a.rows, a.V) / TI::kVec;
-  const dim3 grid(unsigned(a.rows), unsigned((ng + p.slice - 1) / p.slice));
+  // slices of one size, to a KB
+  const int most = slice_entries<BWD>(a.rows, a.V) / TI::kVec, slices = (ng + most - 1) / most;
+  p.slice = ((ng + slices - 1) / slices + 63) / 64 * 64;
+  const dim3 grid(unsigned(a.rows), unsigned(slices));
+  // LDS by the slice, so that as many workgroups of short rows fit a CU as of long ones
+  const int entries = p.slice * TI::kVec;
+  p.words = (entries / 2 < kLpWords ? entries / 2 : kLpWords);
+  const size_t lds = size_t(p.words + (BIAS ? entries / 32 : 0)) * 4;
+  auto run = [&](auto kern, int blk) { kern<<<grid, blk, lds, a.stream>>>(p); };
+  constexpr int kMinWaves = !VEC && BIAS ? 4 : BWD ? 5 : BIAS || !VEC ? 6 : 8;
   if (ng <= 512)
-    k_logits<TI, VEC, BWD, BIAS, 128, 4><<<grid, 128, 0, a.stream>>>(p);
+    run(k_logits<TI, VEC, BWD, BIAS, 128, 4, kMinWaves>, 128);
+  else if (ng <= 1024)
+    run(k_logits<TI, VEC, BWD, BIAS, 256, 4, kMinWaves>, 256);
   else
-    k_logits<TI, VEC, BWD, BIAS, 512, 4><<<grid, 512, 0, a.stream>>>(p);
+    run(k_logits<TI, VEC, BWD, BIAS, 512, 4, kMinWaves>, 512);
   return hipGetLastError();
 }
 
