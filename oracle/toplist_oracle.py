@@ -22,6 +22,14 @@ def _lse(x: np.ndarray) -> float:
     return -math.inf if m == -math.inf else float(m + np.log(np.exp(x - m).sum()))
 
 
+def _softmax(x: np.ndarray) -> np.ndarray:
+    """Zeros where nothing is finite.  Not exp(x - lse): where all of x is -3e38 the lse rounds
+    to it and every entry would get 1."""
+    m = x.max()
+    e = np.exp(x - m) if m > -math.inf else np.zeros(len(x))
+    return e / e.sum() if m > -math.inf else e
+
+
 def top_logits(z, k: int, T: float = 1.0):
     """(values [R, k], ids [R, k], rest [R]): larger first, lower id first among equal ones."""
     z = np.asarray(z, np.float64)
@@ -56,13 +64,10 @@ def top_loss(z_draft, top, ids, rest, T_draft: float, T_target: float, weights, 
         ok = (ids[r] >= 0) & (ids[r] < V) & (top[r] > -math.inf)
         at, t = ids[r][ok], top[r][ok] / T_target
         tr = -math.inf if rest is None else float(np.asarray(rest, np.float64).reshape(R)[r])
-        norm = _lse(np.append(t, tr))
-        has = norm > -math.inf
-        p = np.exp(t - norm) if has else np.zeros(len(t))
-        pr = math.exp(tr - norm) if has and tr > -math.inf else 0.0
-        x = z[r] / T_draft
-        full = _lse(x)
-        q = np.exp(x - full) if full > -math.inf else np.zeros(V)
+        pp = _softmax(np.append(t, tr))
+        p, pr = pp[:-1], float(pp[-1])
+        has = pp.any()
+        q = _softmax(z[r] / T_draft)
         others = np.ones(V, bool)
         others[at] = False
         qr = float(q[others].sum()) if rest is not None else 0.0

@@ -78,6 +78,22 @@ struct TopkParams {
   float* rest;
 };
 
+// A reference of sums, 2^(z sc - msc) with the logit `m` at 1.  Entries below -1e30 / sc
+// differ by more than any exponential holds or not at all: a power of two that keeps the products
+// finite takes the place of sc where m is one of them.
+struct RowScale {
+  float m, sc, msc;
+};
+__device__ __forceinline__ RowScale row_scale(float m, float sc) {
+  const float s = m * sc < -1e30f ? 0x1p-64f : sc;
+  return {m, s, m == kNegInf ? 0.f : m * s};
+}
+// A sum against reference a, none of whose entries is above it, against b >= a.
+__device__ __forceinline__ float rescaled(float s, RowScale a, RowScale b) {
+  if (a.m == kNegInf) return 0.f;
+  return a.sc == b.sc ? s * ex2(a.msc - b.msc) : 0.f;
+}
+
 template <int WAVES>
 __device__ __forceinline__ float block_max(float v, float* sh) {
   v = wave_max(v);
@@ -134,13 +150,13 @@ __device__ __forceinline__ int bucket_of(uint64_t e, float t, float scale) {
   return 255 - min(255, int((key_logit<TI>(entry_key(e)) - t) * scale));
 }
 
-// Sorts the n candidates, all in [t, m], writes the first k and returns the sum of
-// 2^(z sc - msc) over the others (this thread's share).  Up to 64 are ranked by
+// Sorts the n candidates, all in [t, m], writes the first k, and returns the sum over
+// the others (this thread's share) against the k-th, whose scale is `at`.  Up to 64 are ranked by
 // counting; more go through 256 buckets and are ranked in theirs (lists of
 // 256 of 14,336 rows of 4,000: 207 us with counting alone).
 template <class TI, int BLK, class Sh>
-__device__ __forceinline__ float write_ranked(const TopkParams& p, int64_t row, int n, float t, float m, float sc,
-                                              float msc, Sh& sh) {
+__device__ __forceinline__ float write_ranked(const TopkParams& p, int64_t row, int n, float t, float m, RowScale& at,
+                                              Sh& sh) {
   const uint64_t* sorted = sh.sorted;
   if (n <= kWave) {
     if (int(threadIdx.x) < (n & 1)) sh.cand[n] = 0;  // below every candidate
@@ -196,6 +212,7 @@ __device__ __forceinline__ float write_ranked(const TopkParams& p, int64_t row, 
   }
   __syncthreads();
   const int64_t o0 = row * int64_t(p.k);
+  at = row_scale(key_logit<TI>(entry_key(sorted[p.k - 1])), p.sc);
   float s = 0.f;
   for (int j = threadIdx.x; j < n; j += BLK) {
     const uint64_t key = sorted[j];
@@ -204,7 +221,7 @@ __device__ __forceinline__ float write_ranked(const TopkParams& p, int64_t row, 
       const uint32_t b = key & 1u ? 0x80000000u : __builtin_bit_cast(uint32_t, key_logit<TI>(entry_key(key)));
       static_cast<typename TI::bits*>(p.top)[o0 + j] = typename TI::bits(key_bits<TI>() == 16 ? b >> 16 : b);
     } else {
-      s += ex2(__builtin_fmaf(key_logit<TI>(entry_key(key)), sc, -msc));
+      s += ex2(__builtin_fmaf(key_logit<TI>(entry_key(key)), at.sc, -at.msc));
     }
   }
   return s;
@@ -225,11 +242,10 @@ __device__ __forceinline__ void add_candidates(Sh& sh, const float (&x)[E], int 
 }
 
 // Any row: the k-th largest key digit by digit, then a pass in index order that
-// collects the larger entries and the first of its ties.  Returns this thread's share of the
-// others' sum of 2^(z sc - msc).
+// collects the larger entries and the first of its ties.  t becomes the k-th logit; returns this
+// thread's share of the others' sum against it.
 template <class TI, bool VEC, int BLK, class Sh>
-__device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row, float sc, float msc, Sh& sh,
-                                               float& t) {
+__device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row, Sh& sh, float& t) {
   using Rv = RowVecs<TI, VEC>;
   constexpr int E = Rv::E;
   constexpr int WV = BLK / kWave;
@@ -265,6 +281,7 @@ __device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row,
     need = sh.need;  // of the entries whose key starts with `prefix`
   }
   t = key_logit<TI>(prefix);
+  const RowScale at_t = row_scale(t, p.sc);
   if (tid == 0) sh.n = 0;
   uint32_t ties = 0;  // before this round
   float s = 0.f;
@@ -306,7 +323,7 @@ __device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row,
       if (key[e] > prefix || (tie && at < need))
         take |= 1u << e;
       else
-        s += ex2(__builtin_fmaf(x[e], sc, -msc));
+        s += ex2(__builtin_fmaf(x[e], at_t.sc, -at_t.msc));
       at += tie;
     }
     add_candidates<TI>(sh, x, rv.index(gi, 0), take);
@@ -315,25 +332,13 @@ __device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row,
   return s;
 }
 
-// The reference of a row's sums.  All entries of a row whose largest is below
-// -1e30 / sc differ by more than any exponential holds or not at all: any power of two that
-// keeps the products finite takes the place of sc there.
-struct RowScale {
-  float sc, msc;
-};
-__device__ __forceinline__ RowScale row_scale(float m, float sc) {
-  const float s = m * sc < -1e30f ? 0x1p-64f : sc;
-  return {s, m == kNegInf ? 0.f : m * s};
-}
-
 template <int WAVES, class Sh>
-__device__ __forceinline__ void write_rest(const TopkParams& p, int64_t row, float s, float m, RowScale rs,
-                                           Sh& sh) {
+__device__ __forceinline__ void write_rest(const TopkParams& p, int64_t row, float s, RowScale at, Sh& sh) {
   if (p.rest == nullptr) return;
   s = block_sum<WAVES>(s, sh.f);
   if (threadIdx.x != 0) return;
-  const float at = rs.sc == p.sc ? rs.msc * kLn2 : m * p.inv_t;
-  p.rest[row] = s > 0.f ? __builtin_fmaf(__log2f(s), kLn2, at) : kNegInf;
+  const float ref = at.sc == p.sc ? at.msc * kLn2 : at.m * p.inv_t;
+  p.rest[row] = s > 0.f ? __builtin_fmaf(__log2f(s), kLn2, ref) : kNegInf;
 }
 
 // Rows of up to 16 BLK logits: all of them in registers.
@@ -360,8 +365,8 @@ __global__ __launch_bounds__(BLK) void k_topk_short(TopkParams p) {
       m = fmaxf(m, x[u][e]);
     }
   m = block_max<WV>(m, sh.f);
-  const RowScale rs = row_scale(m, p.sc);
   float t = threshold<TI, WV>(y, p.k, m, sh.f);
+  RowScale rs = row_scale(t, p.sc), at;  // what is below t is summed against it
   float s = 0.f;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -380,11 +385,12 @@ __global__ __launch_bounds__(BLK) void k_topk_short(TopkParams p) {
   __syncthreads();
   int n = int(sh.n);
   if (n > CAP) {
-    s = select_slowly<TI, VEC, BLK>(p, row, rs.sc, rs.msc, sh, t);
+    s = select_slowly<TI, VEC, BLK>(p, row, sh, t);
+    rs = row_scale(t, p.sc);
     n = p.k;
   }
-  s += write_ranked<TI, BLK>(p, row, n, t, m, rs.sc, rs.msc, sh);
-  write_rest<WV>(p, row, s, m, rs, sh);
+  const float others = write_ranked<TI, BLK>(p, row, n, t, m, at, sh);
+  write_rest<WV>(p, row, rescaled(s, rs, at) + others, at, sh);
 }
 
 // The largest, or the sum, over the L lanes that share a line (L = 1, 2, 4).
@@ -452,11 +458,10 @@ __global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_)
     m = fmaxf(m, gm[g]);
   }
   m = block_max<WV>(m, sh.f);
-  const RowScale rs = row_scale(m, p.sc);
   int n = CAP + 1;
-  float s = 0.f, t = kNegInf;
-  if (rs.sc == p.sc) {
-    t = threshold<TI, WV>(gm, p.k, m, sh.f);
+  float s = 0.f, t = threshold<TI, WV>(gm, p.k, m, sh.f);
+  RowScale rs = row_scale(t, p.sc), at;  // what is below t is summed against it
+  if (rs.sc == p.sc || t == kNegInf) {
     // the groups that reach t, in an order that does not depend on timing; the sums of the others
     int mine = 0;
 #pragma unroll
@@ -474,16 +479,16 @@ __global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_)
     }
     if (lane == kWave - 1) sh.i[0][wv] = before;
     __syncthreads();
-    int at = before - mine, nq = 0;
+    int to = before - mine, nq = 0;
 #pragma unroll
     for (int i = 0; i < WV; ++i) {
-      if (i < wv) at += sh.i[0][i];
+      if (i < wv) to += sh.i[0][i];
       nq += sh.i[0][i];
     }
     if (nq <= CAP) {
 #pragma unroll
       for (int g = 0; g < NG; ++g)
-        if (g * rounds * U * BLK + mu * BLK + tid - mu < rv.ng && gm[g] >= t) sh.queue[at++] = uint16_t(g * BLK + tid);
+        if (g * rounds * U * BLK + mu * BLK + tid - mu < rv.ng && gm[g] >= t) sh.queue[to++] = uint16_t(g * BLK + tid);
       __syncthreads();
       const int per = rounds * U;  // vectors of a group
       for (int j = tid; j < nq * per; j += BLK) {
@@ -508,11 +513,12 @@ __global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_)
     }
   }
   if (n > CAP) {
-    s = select_slowly<TI, VEC, BLK>(p, row, rs.sc, rs.msc, sh, t);
+    s = select_slowly<TI, VEC, BLK>(p, row, sh, t);
+    rs = row_scale(t, p.sc);
     n = p.k;
   }
-  s += write_ranked<TI, BLK>(p, row, n, t, m, rs.sc, rs.msc, sh);
-  write_rest<WV>(p, row, s, m, rs, sh);
+  const float others = write_ranked<TI, BLK>(p, row, n, t, m, at, sh);
+  write_rest<WV>(p, row, rescaled(s, rs, at) + others, at, sh);
 }
 
 template <class TI, bool VEC, int U, int BLK, int NG, int CAP>

@@ -163,3 +163,30 @@ def test_refusals(A):
         A.aal_topk_logits(torch.zeros(1001, dtype=BF16, device="cuda")[1:].view(10, 100), 3)  # misaligned
     with pytest.raises(A.AalError):
         A.aal_topk_logits(z, 3, ws=torch.empty(8, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("V", [300, 5000, 40000])
+def test_the_types_lowest_value(A, V, dtype):
+    low = torch.finfo(dtype).min
+    z = rows_of("normal", 6, V, 13)
+    z[0, V // 3:] = low
+    z[1] = low
+    z[2] = low
+    z[2, 7] = 2.0
+    z[3, 3:] = -math.inf
+    z[4] = low
+    z[4, ::2] = -math.inf
+    z[5, :2] = low
+    check(A, z.to(dtype).cuda(), 50, 1.0)
+
+
+def test_lists_longer_than_what_is_finite(A):
+    # grammars that leave fewer tokens than the list has places, all over the row
+    for V in (900, 9000, 130000):
+        for n in (0, 1, 63, 64, 65, 300):
+            z = torch.full((3, V), -math.inf)
+            at = torch.randperm(V, generator=torch.Generator().manual_seed(n))[:n]
+            z[:, at] = torch.randn(3, n, generator=torch.Generator().manual_seed(V))
+            check(A, z.bfloat16().cuda(), 64, 1.0)
+            check(A, z.cuda(), 256, 1.0)

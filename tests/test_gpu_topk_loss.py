@@ -279,3 +279,61 @@ def test_the_longest_vocabulary(A):
     V = 1 << 19
     zd, top, ids, rest = make(1, 2, V, 9, BF16, 2)
     check(A, zd, top, ids, rest, 2, WEIGHTS["all"], WIN)
+
+
+@pytest.mark.parametrize("flags", [0, 1], ids=["default", "streaming"])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+def test_the_types_lowest_value(A, dtype, flags):
+    # masks of the lowest finite value: parts of a row, whole rows, whole rows but one entry, and lists
+    low = torch.finfo(dtype).min
+    for V in (400, 2003):
+        zd, top, ids, rest = make(4, 3, V, 8, dtype, V)
+        zd[0, :, V // 2:] = low
+        zd[1, 0] = low
+        zd[1, 1] = low
+        zd[1, 1, 5] = 1.0
+        top[2, 0, 3:] = low
+        top[2, 1] = low
+        rest[2, 1] = -math.inf
+        top[3, 0] = low  # all mass in the remainder
+        check(A, zd, top, ids, rest, 3, WEIGHTS["wtv"], WIN, flags=flags)
+        check(A, zd, top, ids, rest, 3, WEIGHTS["eal"], WIN, flags=flags)
+        # with KL: where the draft gives wanted entries nothing it is infinite or beyond fp32, so without those rows
+        keep = torch.tensor([2, 3], device="cuda")
+        check(A, zd[keep].contiguous(), top[keep].contiguous(), ids[keep].contiguous(), rest[keep].contiguous(), 3,
+              WEIGHTS["all"], WIN, flags=flags)
+    zd = torch.full((1, 2, 300), low, dtype=dtype, device="cuda")
+    zd[0, 1, ::2] = -math.inf
+    got = A.aal_topk_loss_fwd_bwd(zd, top[:1, :2].contiguous(), ids[:1, :2].clamp(0, 299).contiguous(), 2,
+                                  rest=rest[:1, :2].contiguous(), weights=WEIGHTS["wtv"], flags=flags)
+    assert torch.isfinite(got["grad"]).all() and math.isfinite(got["loss"].item())
+
+
+def test_a_poll_that_times_out(A, monkeypatch):
+    # the state a time-out leaves, set by the host: every wait ends at once, the loss reads NaN
+    zd, top, ids, rest = make(40, 7, 500, 8, F32, 3)
+    monkeypatch.setenv("AAL_TEST_PRESET_TIMEOUT", "1")
+    got = A.aal_topk_loss_fwd_bwd(zd, top, ids, 7, rest=rest, weights=WEIGHTS["wtv"])
+    torch.cuda.synchronize()
+    assert math.isnan(got["loss"].item())
+    monkeypatch.delenv("AAL_TEST_PRESET_TIMEOUT")
+    check(A, zd, top, ids, rest, 7, WEIGHTS["wtv"], WIN)
+
+
+@pytest.mark.parametrize("V", [600, 4000, 9000, 18000, 33000, 49000, 66000, 100000, 130000, 153000, 160000])
+def test_every_size_of_workgroup(A, V):
+    # one row length for each number of waves and vectors, whole vectors and ragged, over more than one round
+    for v, dtype in ((V, BF16), (V + 3, BF16), (V // 2 // 4 * 4, F32)):
+        zd, top, ids, rest = make(1, 3, v, 6, dtype, v)
+        n = 300
+        zd, top, ids, rest = (t.repeat(n, *([1] * (t.dim() - 1))) for t in (zd, top, ids, rest))
+        for weights, layout in ((WEIGHTS["all"], WIN), (WEIGHTS["kl"], SEQ)):
+            call = lambda f: A.aal_topk_loss_fwd_bwd(zd, top, ids, 3, rest=rest, weights=weights, layout=layout, flags=f)  # noqa: E731,B023
+            got, ref = call(0), call(A.AAL_FLAG_STREAMING)
+            torch.testing.assert_close(got["accept_tv"], ref["accept_tv"], rtol=4 * REL, atol=1e-6)
+            torch.testing.assert_close(got["loss"], ref["loss"], rtol=1e-4, atol=1e-6)
+            scale = ref["grad"].float().abs().amax().item()
+            torch.testing.assert_close(got["grad"].float(), ref["grad"].float(), rtol=2.0 ** -7, atol=20 * REL * scale)
+            # every copy of a window gets the same gradient (rows of whole vectors: sums in one order)
+            if v % (8 if dtype == BF16 else 4) == 0:
+                assert torch.equal(got["grad"][0], got["grad"][-1])
