@@ -62,13 +62,14 @@ SANITIZE_FLAGS = ["-O1", "-g", "-Xarch_host", "-fsanitize=address", "-Xarch_host
                   "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer"]
 
 
-def compile_api_sanitized(obj: str | None = None) -> str:
-    """Compile csrc/aal_api.hip with the host sanitizers into an object that a
-    driver links with host-side stand-ins for the kernel launchers."""
+def compile_api_sanitized(obj: str | None = None, source: str = "aal_api.hip") -> str:
+    """Compile a file of the C-ABI layer (csrc/aal_api.hip, csrc/aal_toplist_api.hip)
+    with the host sanitizers into an object that a driver links with host-side
+    stand-ins for the kernel launchers."""
     os.makedirs(BUILD, exist_ok=True)
-    obj = obj or os.path.join(BUILD, "aal_api_asan.o")
+    obj = obj or os.path.join(BUILD, source[:-4] + "_asan.o")
     flags = [f for f in COMMON_FLAGS if f != "-O3"] + SANITIZE_FLAGS
-    cmd = [hipcc(), *flags, "-c", os.path.join(CSRC, "aal_api.hip"), "-o", obj]
+    cmd = [hipcc(), *flags, "-c", os.path.join(CSRC, source), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"hipcc failed:\n{' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
