@@ -189,15 +189,22 @@ __global__ __launch_bounds__(kRowBlock) void k_top_grad(TopLossParams p, int spl
 
 // ------------------------------------------------------------------- loss
 constexpr int kLossBlock = 256;
+static_assert(kTopLossParts <= kLossBlock, "a part a thread");
 
-__device__ double block_sum_d(double v, double* sh) {
-  v = wave_sum_d(v);
-  if ((threadIdx.x & (kWave - 1)) == 0) sh[threadIdx.x / kWave] = v;
+// The sums of four values over the workgroup, to every thread.
+__device__ void block_sum4(double (&v)[4], double (*sh)[4]) {
+  for (int off = kWave / 2; off > 0; off >>= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += __shfl_xor(v[i], off, kWave);
   __syncthreads();
-  double t = 0.0;
-  for (int i = 0; i < kLossBlock / kWave; ++i) t += sh[i];
+  if ((threadIdx.x & (kWave - 1)) == 0)
+    for (int i = 0; i < 4; ++i) sh[threadIdx.x / kWave][i] = v[i];
   __syncthreads();
-  return t;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = 0.0;
+    for (int w = 0; w < kLossBlock / kWave; ++w) v[i] += sh[w][i];
+  }
 }
 
 // Every window's E and the loss: workgroup b sums the rows of its slice (a window
@@ -205,7 +212,7 @@ __device__ double block_sum_d(double v, double* sh) {
 __global__ __launch_bounds__(kLossBlock) void k_top_loss(TopLossParams p, int n, double* parts, float* loss,
                                                          float* terms, float* e_tv, float* e_eal,
                                                          const unsigned* err) {
-  __shared__ double sh[kLossBlock / kWave];
+  __shared__ double sh[kLossBlock / kWave][4];
   __shared__ int sh_last;
   const int64_t r0 = p.R * blockIdx.x / n, r1 = p.R * (int64_t(blockIdx.x) + 1) / n;
   double v[4] = {0.0, 0.0, 0.0, 0.0};  // sums of E_tv, E_eal, KL, TV
@@ -230,7 +237,7 @@ __global__ __launch_bounds__(kLossBlock) void k_top_loss(TopLossParams p, int n,
     v[2] += double(l.x);
     v[3] += double(l.y);
   }
-  for (int i = 0; i < 4; ++i) v[i] = block_sum_d(v[i], sh);
+  block_sum4(v, sh);
   if (n > 1) {
     if (threadIdx.x == 0) {
       for (int i = 0; i < 4; ++i)
@@ -239,12 +246,10 @@ __global__ __launch_bounds__(kLossBlock) void k_top_loss(TopLossParams p, int n,
     }
     __syncthreads();
     if (!sh_last) return;
-    for (int i = 0; i < 4; ++i) {
-      double s = 0.0;
-      for (int b = threadIdx.x; b < n; b += kLossBlock)
-        s += __hip_atomic_load(parts + 4 * b + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      v[i] = block_sum_d(s, sh);
-    }
+    // at most a part a thread
+    for (int i = 0; i < 4; ++i)
+      v[i] = int(threadIdx.x) < n ? __hip_atomic_load(parts + 4 * threadIdx.x + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+    block_sum4(v, sh);
   }
   if (threadIdx.x != 0) return;
   // a term whose weight is 0 reads 0
