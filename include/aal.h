@@ -534,9 +534,6 @@ aal_status_t aal_vp_grad(const void* z_draft, const void* z_target, aal_dtype_t 
 /* Longest list of a row's top logits. */
 #define AAL_TOPK_MAX 512
 
-/* Workspace bytes of aal_topk_logits (0 for invalid arguments). */
-size_t aal_topk_workspace_bytes(int64_t rows, int32_t V, int32_t k);
-
 /*
  * A row's k largest logits, their ids, and the log-sum-exp of all others: what
  * a data set keeps of a target's logits, and what aal_topk_loss_fwd_bwd reads.
@@ -551,11 +548,10 @@ size_t aal_topk_workspace_bytes(int64_t rows, int32_t V, int32_t k);
  * finite and > 0 (it bears on rest alone).
  * top_logits : [rows, k] of in_dtype, the logits themselves, in order.  top_ids : [rows, k].
  * rest : [rows] float, or NULL.
- * workspace : at least aal_topk_workspace_bytes(rows, V, k) bytes, 256-byte aligned.
  */
 aal_status_t aal_topk_logits(const void* z, aal_dtype_t in_dtype, int64_t rows, int32_t V, int32_t k,
                              float temperature, void* top_logits, int32_t* top_ids, float* rest,
-                             void* workspace, size_t workspace_bytes, hipStream_t stream);
+                             hipStream_t stream);
 
 /* Workspace bytes of aal_topk_loss_fwd_bwd for the given layout and sizes (0
  * for invalid arguments). */

@@ -26,7 +26,6 @@ from .api import (  # noqa: F401
     aal_topk_logits,
     aal_topk_loss_fwd_bwd,
     aal_topk_loss_workspace_bytes,
-    aal_topk_workspace_bytes,
     aal_vp_accept_partials,
     aal_vp_grad,
     aal_vp_merge_rows,

@@ -113,9 +113,8 @@ _SIGNATURES = {
         _vp, _vp, C.c_int32, C.c_int64, C.c_int32, C.c_int, C.c_float, _vp, _vp, _vp, _vp, _vp, _vp]),
     "aal_vp_sequence_scan": (C.c_int, [
         _vp, _vp, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int, C.c_float, _vp, _vp, _vp, _vp, _vp, _vp]),
-    "aal_topk_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int32, C.c_int32]),
     "aal_topk_logits": (C.c_int, [
-        _vp, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_float, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
+        _vp, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_float, _vp, _vp, _vp, _vp]),
     "aal_topk_loss_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int64, C.c_int32, C.c_int32]),
     "aal_topk_loss_fwd_bwd": (C.c_int, [
         _vp, C.c_int, _vp, C.c_int, _vp, _vp, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32,

@@ -444,6 +444,12 @@ def _guard(device, stream):
     return contextlib.nullcontext()
 
 
+def _raw_stream(device, stream) -> int:
+    """The handle of `stream`, or of the device's current one (torch.cuda.current_stream builds an
+    object for it, 2 us of a call that takes 10)."""
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
+
+
 def _device_array(t, name: str, dtype, numel: int | None, device):
     if t.dtype != dtype or t.device != device or not t.is_contiguous() or (numel is not None and t.numel() != numel):
         size = "" if numel is None else f" of {numel} entries"
@@ -459,12 +465,7 @@ def _check_rows(z: torch.Tensor, name: str):
     return z.numel() // V, V
 
 
-def aal_topk_workspace_bytes(rows: int, V: int, k: int) -> int:
-    return int(_lib.lib().aal_topk_workspace_bytes(int(rows), int(V), int(k)))
-
-
-def aal_topk_logits(z: torch.Tensor, k: int, temperature: float = 1.0, *, rest: bool = True,
-                    ws: torch.Tensor | None = None, stream=None) -> dict:
+def aal_topk_logits(z: torch.Tensor, k: int, temperature: float = 1.0, *, rest: bool = True, stream=None) -> dict:
     """The k largest logits of each row of z [..., V] (larger first, the lower
     id first among equal ones) and the log-sum-exp of all others at
     `temperature`: what a data set keeps of a target's logits.
@@ -481,11 +482,8 @@ def aal_topk_logits(z: torch.Tensor, k: int, temperature: float = 1.0, *, rest: 
             "ids": torch.empty(*lead, k, dtype=torch.int32, device=dev),
             "rest": torch.empty(lead, dtype=torch.float32, device=dev) if rest else None,
         }
-        if ws is None:
-            ws = torch.empty(aal_topk_workspace_bytes(rows, V, k), dtype=torch.uint8, device=dev)
         st = _lib.lib().aal_topk_logits(_ptr(z), code, rows, V, int(k), float(temperature), _ptr(out["logits"]),
-                                        _ptr(out["ids"]), _ptr(out["rest"]), _ptr(ws), ws.numel(),
-                                        _stream(dev, stream))
+                                        _ptr(out["ids"]), _ptr(out["rest"]), _raw_stream(dev, stream))
     _lib.check(st, "aal_topk_logits")
     return out
 
@@ -535,23 +533,24 @@ def aal_topk_loss_fwd_bwd(z_draft: torch.Tensor, top_logits: torch.Tensor, top_i
     gcode = _dtype_code(grad_dtype or z_draft.dtype) if grad else AAL_F32
     W = B if layout == AAL_LAYOUT_WINDOWS else B * max(0, S - K + 1)
     with _guard(dev, stream):
-        new = lambda n, dtype=torch.float32: torch.empty(n, dtype=dtype, device=dev)  # noqa: E731
-        out = {
-            "loss": new(1), "terms": new(4),
-            "E_tv": new(W) if outputs else None, "E_eal": new(W) if outputs else None,
-            "accept_tv": new(R) if outputs else None, "accept_eal": new(R) if outputs else None,
-            "xstar": new(R, torch.int32) if outputs else None,
-            "grad": new((B, S, V), grad_dtype or z_draft.dtype) if grad else None,
-        }
+        # the small outputs are pieces of one allocation (seven of them take 9 us)
+        sizes = (1, 4, W, W, R, R, R) if outputs else (1, 4, 0, 0, 0, 0, 0)
+        parts = torch.empty(sum(sizes), dtype=torch.float32, device=dev).split_with_sizes(sizes)
+        out = dict(zip(("loss", "terms", "E_tv", "E_eal", "accept_tv", "accept_eal", "xstar"), parts))
+        if outputs:
+            out["xstar"] = out["xstar"].view(torch.int32)
+        else:
+            out.update(E_tv=None, E_eal=None, accept_tv=None, accept_eal=None, xstar=None)
+        out["grad"] = torch.empty(B, S, V, dtype=grad_dtype or z_draft.dtype, device=dev) if grad else None
         if ws is None:
-            ws = new(aal_topk_loss_workspace_bytes(layout, B, S, K), torch.uint8)
+            ws = torch.empty(aal_topk_loss_workspace_bytes(layout, B, S, K), dtype=torch.uint8, device=dev)
         st = _lib.lib().aal_topk_loss_fwd_bwd(
             _ptr(z_draft), code, _ptr(top_logits), top_code, _ptr(top_ids), _ptr(rest), int(layout), B, S, int(K), V, k,
             float(temp_draft), float(temp_target), _lib.LossWeights(*(float(x) for x in weights)), _ptr(out["loss"]),
             _ptr(out["terms"]), _ptr(out["E_tv"]) if W and outputs else None,
             _ptr(out["E_eal"]) if W and outputs else None, _ptr(out["accept_tv"]), _ptr(out["accept_eal"]),
             _ptr(out["xstar"]), _ptr(out["grad"]), gcode, _ptr(grad_scale), int(flags), _ptr(ws), ws.numel(),
-            _stream(dev, stream))
+            _raw_stream(dev, stream))
     _lib.check(st, "aal_topk_loss_fwd_bwd")
     return out
 
@@ -636,7 +635,7 @@ def aal_logits_process(z: torch.Tensor, *, tokens: torch.Tensor | None = None, h
     with _guard(dev, stream):
         if out is None:
             out = torch.empty_like(z)
-        st = _lib.lib().aal_logits_process(_ptr(z), code, rows, V, C.byref(rules), _ptr(out), _stream(dev, stream))
+        st = _lib.lib().aal_logits_process(_ptr(z), code, rows, V, C.byref(rules), _ptr(out), _raw_stream(dev, stream))
     _lib.check(st, "aal_logits_process")
     return out
 
@@ -670,7 +669,7 @@ def aal_logits_process_bwd(grad_out: torch.Tensor, z: torch.Tensor, *, tokens: t
         if grad_z is None:
             grad_z = torch.empty_like(grad_out)
         st = _lib.lib().aal_logits_process_bwd(_ptr(grad_out), gcode, _ptr(z), code, rows, V, C.byref(rules),
-                                               _ptr(grad_z), _stream(dev, stream))
+                                               _ptr(grad_z), _raw_stream(dev, stream))
     _lib.check(st, "aal_logits_process_bwd")
     return grad_z
 

@@ -574,8 +574,6 @@ hipError_t launch_typed(const TopkArgs& a) {
 
 }  // namespace
 
-size_t topk_workspace_bytes(int64_t, int, int) { return 256; }
-
 hipError_t launch_topk(const TopkArgs& a) {
   return a.in == DType::kBf16 ? launch_typed<Bf16>(a) : launch_typed<F32>(a);
 }

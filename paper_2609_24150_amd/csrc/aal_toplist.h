@@ -17,11 +17,9 @@ struct TopkArgs {
   void* top;       // [rows, k] of the logits' type
   int32_t* ids;    // [rows, k]
   float* rest;     // [rows], may be null
-  uint8_t* ws;
   hipStream_t stream;
 };
 
-size_t topk_workspace_bytes(int64_t rows, int V, int k);
 hipError_t launch_topk(const TopkArgs& a);
 
 // ------------------------------------------- objectives against top lists

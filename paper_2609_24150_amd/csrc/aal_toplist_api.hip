@@ -77,14 +77,9 @@ aal::LogitsRules rules_of(const aal_logits_rules_t& r) {
 
 extern "C" {
 
-size_t aal_topk_workspace_bytes(int64_t rows, int32_t V, int32_t k) {
-  if (rows < 1 || rows >= (int64_t(1) << 31) || V < 1 || k < 1 || k > AAL_TOPK_MAX || k > V) return 0;
-  return aal::topk_workspace_bytes(rows, V, k);
-}
-
 aal_status_t aal_topk_logits(const void* z, aal_dtype_t in_dtype, int64_t rows, int32_t V, int32_t k,
-                             float temperature, void* top_logits, int32_t* top_ids, float* rest, void* workspace,
-                             size_t workspace_bytes, hipStream_t stream) {
+                             float temperature, void* top_logits, int32_t* top_ids, float* rest,
+                             hipStream_t stream) {
   clear_error();
   if (!z) return fail(AAL_ERR_ARG, "z must be non-NULL");
   if (!top_logits || !top_ids) return fail(AAL_ERR_ARG, "top_logits and top_ids must be non-NULL");
@@ -96,8 +91,6 @@ aal_status_t aal_topk_logits(const void* z, aal_dtype_t in_dtype, int64_t rows, 
   if (!positive_finite(temperature) || sc == 0.f)
     return fail(AAL_ERR_ARG, "temperature must be finite, > 0 and >= 1e-37");
   if (!aligned(z, 16)) return fail(AAL_ERR_ALIGN, "logit pointers must be 16-byte aligned");
-  if (aal_status_t s = check_workspace(workspace, workspace_bytes, aal::topk_workspace_bytes(rows, V, k)); s != AAL_OK)
-    return s;
   aal::TopkArgs a{};
   a.in = to_dtype(raw(in_dtype));
   a.z = z;
@@ -109,7 +102,6 @@ aal_status_t aal_topk_logits(const void* z, aal_dtype_t in_dtype, int64_t rows, 
   a.top = top_logits;
   a.ids = top_ids;
   a.rest = rest;
-  a.ws = static_cast<uint8_t*>(workspace);
   a.stream = stream;
   return launched(aal::launch_topk(a));
 }

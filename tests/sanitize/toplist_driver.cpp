@@ -21,11 +21,9 @@ static int g_failures = 0, g_calls = 0;
 
 namespace aal {
 
-size_t topk_workspace_bytes(int64_t, int, int) { return 512; }
-
 hipError_t launch_topk(const TopkArgs& a) {
   ++g_calls;
-  memset(a.ws, 0xA5, topk_workspace_bytes(a.rows, a.V, a.k));
+  CHECK(a.k >= 1 && a.k <= a.V && a.sc > 0.f);
   return hipSuccess;
 }
 
@@ -54,11 +52,7 @@ static int32_t* const DI = reinterpret_cast<int32_t*>(uintptr_t(0x30000));
 static int64_t* const DL = reinterpret_cast<int64_t*>(uintptr_t(0x40000));
 
 static aal_status_t topk(int64_t rows, int32_t V, int32_t k, int dt = AAL_BF16, float T = 1.f) {
-  const size_t n = aal_topk_workspace_bytes(rows, V, k);
-  void* ws = n ? aligned_alloc(256, n) : nullptr;
-  const aal_status_t s = aal_topk_logits(D, aal_dtype_t(dt), rows, V, k, T, D, DI, DF, ws, n, nullptr);
-  free(ws);
-  return s;
+  return aal_topk_logits(D, aal_dtype_t(dt), rows, V, k, T, D, DI, DF, nullptr);
 }
 
 static aal_status_t loss(int lay, int64_t B, int32_t S, int32_t K, int32_t V, int32_t k, int dt = AAL_BF16, uint32_t flags = 0) {

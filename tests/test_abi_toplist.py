@@ -20,8 +20,7 @@ def lib():
 
 
 SIGNATURES = '''
-size_t (*f1)(int64_t, int32_t, int32_t) = aal_topk_workspace_bytes;
-aal_status_t (*f2)(const void*, aal_dtype_t, int64_t, int32_t, int32_t, float, void*, int32_t*, float*, void*, size_t,
+aal_status_t (*f2)(const void*, aal_dtype_t, int64_t, int32_t, int32_t, float, void*, int32_t*, float*,
                    hipStream_t) = aal_topk_logits;
 size_t (*f3)(aal_layout_t, int64_t, int32_t, int32_t) = aal_topk_loss_workspace_bytes;
 aal_status_t (*f4)(const void*, aal_dtype_t, const void*, aal_dtype_t, const int32_t*, const float*, aal_layout_t,
@@ -51,11 +50,6 @@ def test_signatures(lib, tmp_path):
 
 def test_workspace_bytes(lib):
     L = lib.lib()
-    for rows, V, k in ((1, 1, 1), (7, 151936, 20), (14336, 128256, 64), (3, 512, 512)):
-        n = L.aal_topk_workspace_bytes(rows, V, k)
-        assert n > 0 and n % 256 == 0
-    for rows, V, k in ((0, 10, 1), (-1, 10, 1), (1, 0, 1), (1, 10, 0), (1, 10, 11), (1, 1000, 513), (1 << 31, 10, 1)):
-        assert L.aal_topk_workspace_bytes(rows, V, k) == 0
     a = L.aal_topk_loss_workspace_bytes(0, 2048, 0, 7)
     assert a > 0 and a % 256 == 0 and L.aal_topk_loss_workspace_bytes(1, 2, 5, 7) > 0
     for bad in ((2, 1, 1, 1), (0, 0, 0, 7), (1, 2, 0, 7), (0, 2, 0, 65), (0, 2, 0, 0), (1, 1 << 30, 2, 1)):
@@ -66,14 +60,14 @@ def test_workspace_bytes(lib):
     (dict(z=None), 1), (dict(top=None), 1), (dict(ids=None), 1), (dict(rows=0), 1), (dict(rows=1 << 31), 1),
     (dict(V=0), 1), (dict(V=(1 << 30) + 1), 1), (dict(k=0), 1), (dict(k=101), 1), (dict(V=1000, k=513), 1),
     (dict(T=0.0), 1), (dict(T=float("nan")), 1), (dict(T=float("inf")), 1), (dict(dt=2), 2), (dict(dt=-1), 2),
-    (dict(z=24), 3), (dict(ws=None), 4), (dict(ws=128), 3), (dict(wsb=0), 4),
+    (dict(z=24), 3),
 ])
 def test_topk_validation(lib, kw, code):
-    a = dict(z=16, dt=0, rows=4, V=100, k=5, T=1.0, top=16, ids=16, ws=256, wsb=1 << 40)
+    a = dict(z=16, dt=0, rows=4, V=100, k=5, T=1.0, top=16, ids=16)
     a.update(kw)
     L = lib.lib()
-    assert L.aal_topk_logits(a["z"], a["dt"], a["rows"], a["V"], a["k"], a["T"], a["top"], a["ids"], None, a["ws"],
-                             a["wsb"], None) == code
+    assert L.aal_topk_logits(a["z"], a["dt"], a["rows"], a["V"], a["k"], a["T"], a["top"], a["ids"], None,
+                             None) == code
     assert L.aal_last_error().decode() != ""
 
 
