@@ -42,7 +42,7 @@ struct LogitsParams {
   const void* z;
   int z_bf16;
   void* out;
-  int64_t rows;
+  int64_t rows, row0;  // all of them, the first one of the launch
   int V;
   int slice;         // vectors of a workgroup
   int words;         // counter words in LDS, a multiple of 8
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(BLK, MINW) void k_logits(LogitsParams p) {
   __shared__ uint32_t sh_bpos[BIAS ? kBiasSlots : 1];
   __shared__ float sh_bval[BIAS ? kBiasSlots : 1];
 
-  const int64_t row = blockIdx.x;
+  const int64_t row = p.row0 + blockIdx.x;
   const Rv rv(row, p.rows, p.V);
   const int64_t e0 = row * int64_t(p.V);
   const int gs0 = int(blockIdx.y) * p.slice, gs1 = min(rv.ng, gs0 + p.slice);
@@ -336,20 +336,21 @@ hipError_t launch_vec(const LogitsArgs& a) {
   // slices of one size, to a KB
   const int most = slice_entries<BWD>(a.rows, a.V) / TI::kVec, slices = (ng + most - 1) / most;
   p.slice = ((ng + slices - 1) / slices + 63) / 64 * 64;
-  const dim3 grid(unsigned(a.rows), unsigned(slices));
   // LDS by the slice, so that as many workgroups of short rows fit a CU as of long ones
   const int entries = p.slice * TI::kVec;
   p.words = (entries / 2 < kLpWords ? entries / 2 : kLpWords);
   const size_t lds = size_t(p.words + (BIAS ? entries / 32 : 0)) * 4;
-  auto run = [&](auto kern, int blk) { kern<<<grid, blk, lds, a.stream>>>(p); };
+  auto run = [&](auto kern, int blk) {
+    return for_row_parts(a.rows, [&](int64_t row0, unsigned n) {
+      p.row0 = row0;
+      kern<<<dim3(n, unsigned(slices)), blk, lds, a.stream>>>(p);
+      return hipGetLastError();
+    });
+  };
   constexpr int kMinWaves = !VEC && BIAS ? 4 : BWD ? 5 : BIAS || !VEC ? 6 : 8;
-  if (ng <= 512)
-    run(k_logits<TI, VEC, BWD, BIAS, 128, 4, kMinWaves>, 128);
-  else if (ng <= 1024)
-    run(k_logits<TI, VEC, BWD, BIAS, 256, 4, kMinWaves>, 256);
-  else
-    run(k_logits<TI, VEC, BWD, BIAS, 512, 4, kMinWaves>, 512);
-  return hipGetLastError();
+  if (ng <= 512) return run(k_logits<TI, VEC, BWD, BIAS, 128, 4, kMinWaves>, 128);
+  if (ng <= 1024) return run(k_logits<TI, VEC, BWD, BIAS, 256, 4, kMinWaves>, 256);
+  return run(k_logits<TI, VEC, BWD, BIAS, 512, 4, kMinWaves>, 512);
 }
 
 template <class TI, bool BWD>

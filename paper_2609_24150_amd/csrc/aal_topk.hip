@@ -70,7 +70,7 @@ struct TopkShared {
 
 struct TopkParams {
   const void* z;
-  int64_t rows;
+  int64_t rows, row0;  // all of them, the first one of the launch
   int V, k;
   float sc, inv_t;
   void* top;
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(BLK) void k_topk_short(TopkParams p) {
   constexpr int WV = BLK / kWave;
   constexpr int U = 16 / E + (VEC ? 0 : 1);  // a row may start and end inside a vector
   __shared__ TopkShared<CAP> sh;
-  const int64_t row = blockIdx.x;
+  const int64_t row = p.row0 + blockIdx.x;
   const Rv rv(row, p.rows, p.V);
   u32x4 w[1][U];
   rv.load({p.z}, int(threadIdx.x), BLK, w);
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_)
   constexpr int E = Rv::E;
   constexpr int WV = BLK / kWave;
   __shared__ TopkShared<CAP> sh;
-  const int64_t row = blockIdx.x;
+  const int64_t row = p.row0 + blockIdx.x;
   const Rv rv(row, p.rows, p.V);
   const int rounds = ONE ? 1 : rounds_;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave, mu = tid & (U - 1);
@@ -522,9 +522,8 @@ __global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_)
 }
 
 template <class TI, bool VEC, int U, int BLK, int NG, int CAP>
-void rows_launch(const TopkArgs& a, const TopkParams& p, int ng) {
+void rows_launch(const TopkArgs& a, const TopkParams& p, dim3 grid, int ng) {
   const int64_t round = int64_t(NG) * U * BLK;
-  const dim3 grid{unsigned(a.rows)};
   if (ng <= round)
     k_topk_rows<TI, VEC, U, BLK, NG, CAP, true><<<grid, BLK, 0, a.stream>>>(p, 1);
   else if constexpr (U * BLK == 2048)
@@ -539,9 +538,8 @@ void rows_launch(const TopkArgs& a, const TopkParams& p, int ng) {
 // 1,000, k = 8, 23 with all logits in registers.  256 threads of 16 groups and 1,024
 // of 4 are slower at 14,336 rows of 128,256 (k = 64: 588 and 640 against 578).
 template <class TI, bool VEC>
-hipError_t launch_vec(const TopkArgs& a) {
-  const TopkParams p{a.z, a.rows, a.V, a.k, a.sc, a.inv_t, a.top, a.ids, a.rest};
-  const dim3 grid{unsigned(a.rows)};
+hipError_t launch_vec(const TopkArgs& a, int64_t row0, dim3 grid) {
+  const TopkParams p{a.z, a.rows, row0, a.V, a.k, a.sc, a.inv_t, a.top, a.ids, a.rest};
   const int ng = a.V / TI::kVec + (VEC ? 0 : 2);  // vectors that cover a row, at most
   // lines of U vectors have to be several times k for few of them to reach the threshold
   auto lines = [&](int U) { return ng / U >= 3 * a.k; };
@@ -549,9 +547,9 @@ hipError_t launch_vec(const TopkArgs& a) {
   if (few && a.V <= 16 * 64)
     k_topk_short<TI, VEC, 64, 320><<<grid, 64, 0, a.stream>>>(p);
   else if (few && ng <= 1024 && lines(2))
-    rows_launch<TI, VEC, 2, 64, 8, 320>(a, p, ng);
+    rows_launch<TI, VEC, 2, 64, 8, 320>(a, p, grid, ng);
   else if (few && ng <= 2048 && lines(4))
-    rows_launch<TI, VEC, 4, 64, 8, 320>(a, p, ng);
+    rows_launch<TI, VEC, 4, 64, 8, 320>(a, p, grid, ng);
   else if (a.V <= 16 * 128)
     k_topk_short<TI, VEC, 128, 1024><<<grid, 128, 0, a.stream>>>(p);
   else if (a.V <= 16 * 256)
@@ -559,17 +557,19 @@ hipError_t launch_vec(const TopkArgs& a) {
   else if (a.V <= 16 * 512)
     k_topk_short<TI, VEC, 512, 1024><<<grid, 512, 0, a.stream>>>(p);
   else if (ng <= 4096 && !lines(4))
-    rows_launch<TI, VEC, 1, 512, 8, 1024>(a, p, ng);
+    rows_launch<TI, VEC, 1, 512, 8, 1024>(a, p, grid, ng);
   else if (ng <= 8192)
-    rows_launch<TI, VEC, 4, 256, 8, 1024>(a, p, ng);
+    rows_launch<TI, VEC, 4, 256, 8, 1024>(a, p, grid, ng);
   else
-    rows_launch<TI, VEC, 4, 512, 8, 1024>(a, p, ng);
+    rows_launch<TI, VEC, 4, 512, 8, 1024>(a, p, grid, ng);
   return hipGetLastError();
 }
 
 template <class TI>
 hipError_t launch_typed(const TopkArgs& a) {
-  return a.V % TI::kVec == 0 ? launch_vec<TI, true>(a) : launch_vec<TI, false>(a);
+  return for_row_parts(a.rows, [&](int64_t row0, unsigned n) {
+    return a.V % TI::kVec == 0 ? launch_vec<TI, true>(a, row0, dim3(n)) : launch_vec<TI, false>(a, row0, dim3(n));
+  });
 }
 
 }  // namespace

@@ -39,7 +39,7 @@ namespace {
 
 // -------------------------------------------------- multi-kernel schedule
 template <class TI, bool VEC, int U, int BLK>
-__global__ __launch_bounds__(BLK) void k_top_rows(TopLossParams p) {
+__global__ __launch_bounds__(BLK) void k_top_rows(TopLossParams p, int64_t row0) {
   using Rv = RowVecs<TI, VEC>;
   constexpr int E = Rv::E;
   extern __shared__ uint32_t sh_map[];
@@ -47,11 +47,11 @@ __global__ __launch_bounds__(BLK) void k_top_rows(TopLossParams p) {
   __shared__ int sh_id[kTopMax];
   __shared__ float sh_m[BLK / kWave], sh_s[BLK / kWave];
 
-  const int64_t row = blockIdx.x;
+  const int64_t row = row0 + blockIdx.x;
   const Rv rv(row, p.R, p.V);
   const int64_t e0 = row * int64_t(p.V), l0 = row * p.k;
   const int words = bitmap_words(p.V);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.counter = 0u;
+  if (row == 0 && threadIdx.x == 0) *p.counter = 0u;
   for (int i = threadIdx.x; i < words; i += BLK) sh_map[i] = 0;
   __syncthreads();
   for (int i = threadIdx.x; i < p.k; i += BLK) {
@@ -152,10 +152,10 @@ __global__ __launch_bounds__(kRowBlock) void k_top_scan(TopLossParams p) {
 }
 
 template <class TI, class TG, bool VEC, int U>
-__global__ __launch_bounds__(kRowBlock) void k_top_grad(TopLossParams p, int splits, void* __restrict__ grad) {
+__global__ __launch_bounds__(kRowBlock) void k_top_grad(TopLossParams p, int64_t row0, int splits, void* __restrict__ grad) {
   using Rv = RowVecs<TI, VEC>;
   constexpr int E = Rv::E;
-  const int64_t row = blockIdx.x;
+  const int64_t row = row0 + blockIdx.x;
   const Rv rv(row, p.R, p.V);
   const TopRow s = p.stats[row];
   const float sc = s.flags & kTopDeep ? kDeepScale : p.scd;
@@ -290,13 +290,17 @@ hipError_t launch_top_fused(const TopLossArgs& a, bool* used) {
 }
 
 template <class TI, class TG, bool VEC>
-void grad_launch(const TopLossArgs& a) {
+hipError_t grad_launch(const TopLossArgs& a) {
+  hipError_t e = hipSuccess;
   with_grad_shape(a.V, TI::kVec, [&](auto sh) {
     constexpr int U = decltype(sh)::kU;
     const unsigned splits = row_splits(a.R, a.V, TI::kVec, U);
-    k_top_grad<TI, TG, VEC, U><<<dim3(unsigned(a.R), splits), kRowBlock, 0, a.stream>>>(params_of(a), int(splits),
-                                                                                      a.grad);
+    e = for_row_parts(a.R, [&](int64_t row0, unsigned n) {
+      k_top_grad<TI, TG, VEC, U><<<dim3(n, splits), kRowBlock, 0, a.stream>>>(params_of(a), row0, int(splits), a.grad);
+      return hipGetLastError();
+    });
   });
+  return e;
 }
 
 template <class TI, bool VEC>
@@ -304,15 +308,17 @@ hipError_t launch_vec(const TopLossArgs& a) {
   hipError_t e = hipSuccess;
   with_row_shape<4>(a.R, a.V, TI::kVec, [&](auto sh) {
     using Sh = decltype(sh);
-    k_top_rows<TI, VEC, Sh::kU, Sh::kBlock>
-        <<<dim3(unsigned(a.R)), Sh::kBlock, size_t(bitmap_words(a.V)) * 4, a.stream>>>(params_of(a));
-    e = hipGetLastError();
+    e = for_row_parts(a.R, [&](int64_t row0, unsigned n) {
+      k_top_rows<TI, VEC, Sh::kU, Sh::kBlock>
+          <<<dim3(n), Sh::kBlock, size_t(bitmap_words(a.V)) * 4, a.stream>>>(params_of(a), row0);
+      return hipGetLastError();
+    });
   });
   if (e != hipSuccess) return e;
   k_top_scan<<<dim3(unsigned((a.R + kRowBlock - 1) / kRowBlock)), kRowBlock, 0, a.stream>>>(params_of(a));
   if ((e = loss_launch(a, false)) != hipSuccess) return e;
-  if (a.grad) a.gd == DType::kBf16 ? grad_launch<TI, GBf16, VEC>(a) : grad_launch<TI, GF32, VEC>(a);
-  return hipGetLastError();
+  if (a.grad == nullptr) return hipSuccess;
+  return a.gd == DType::kBf16 ? grad_launch<TI, GBf16, VEC>(a) : grad_launch<TI, GF32, VEC>(a);
 }
 
 template <class TI>

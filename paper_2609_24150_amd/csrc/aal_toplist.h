@@ -7,6 +7,17 @@
 
 namespace aal {
 
+// A launch holds fewer than 2^32 threads: kernels of a workgroup or more per row take 2^22 rows
+// of at most 512 threads at a time.
+constexpr int64_t kLaunchRows = int64_t(1) << 22;
+template <class F>
+hipError_t for_row_parts(int64_t rows, F&& launch) {
+  for (int64_t row0 = 0; row0 < rows; row0 += kLaunchRows)
+    if (hipError_t e = launch(row0, unsigned(rows - row0 < kLaunchRows ? rows - row0 : kLaunchRows)); e != hipSuccess)
+      return e;
+  return hipSuccess;
+}
+
 // ------------------------------------------------------------ extraction
 struct TopkArgs {
   DType in;

@@ -278,3 +278,19 @@ def test_refusals(A):
         A.aal_logits_process_bwd(z.half(), z, **rules)
     with pytest.raises(A.AalError):
         A.aal_logits_process(torch.zeros(301, device="cuda")[1:].view(3, 100), **rules)
+
+
+def test_more_rows_than_a_launch_holds(A):
+    rows, V = (1 << 22) + 9, 9
+    g = torch.Generator("cuda").manual_seed(5)
+    z = torch.randint(-8, 9, (rows, V), generator=g, device="cuda").float()
+    token = torch.randint(0, V, (rows,), generator=g, device="cuda")
+    rules = dict(tokens=token.int(), hist_start=torch.arange(rows, device="cuda"),
+                 hist_len=torch.ones(rows, dtype=torch.int32, device="cuda"),
+                 repetition=torch.full((rows,), 2.0, device="cuda"))
+    seen = torch.nn.functional.one_hot(token, V).bool()
+    half = seen & (z > 0)
+    factor = torch.where(half, 0.5, torch.where(seen, 2.0, 1.0))  # all exact
+    assert torch.equal(A.aal_logits_process(z, **rules), z * factor)
+    up = torch.randint(-8, 9, (rows, V), generator=g, device="cuda").float()
+    assert torch.equal(A.aal_logits_process_bwd(up, z, **rules), up * factor)

@@ -186,3 +186,13 @@ def test_lists_longer_than_what_is_finite(A):
             z[:, at] = torch.randn(3, n, generator=torch.Generator().manual_seed(V))
             check(A, z.bfloat16().cuda(), 64, 1.0)
             check(A, z.cuda(), 256, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+def test_more_rows_than_a_launch_holds(A, dtype):
+    rows, V, k = (1 << 22) + 9, 9, 2
+    z = torch.randn(rows, V, generator=torch.Generator("cuda").manual_seed(5), device="cuda").to(dtype)
+    out = A.aal_topk_logits(z, k)
+    vals, ids = z.double().sort(dim=1, descending=True, stable=True)
+    assert torch.equal(out["ids"].long(), ids[:, :k]) and torch.equal(out["logits"].double(), vals[:, :k])
+    assert (out["rest"] - vals[:, k:].logsumexp(1)).abs().max() <= REST_TOL

@@ -337,3 +337,26 @@ def test_every_size_of_workgroup(A, V):
             # every copy of a window gets the same gradient (rows of whole vectors: sums in one order)
             if v % (8 if dtype == BF16 else 4) == 0:
                 assert torch.equal(got["grad"][0], got["grad"][-1])
+
+
+@pytest.mark.parametrize("flags", [0, 1], ids=["default", "streaming"])
+def test_more_rows_than_a_launch_holds(A, flags):
+    """Windows of one row: a row's results do not depend on the others'.  The first rows and
+    those around row 2^22 against a call of their own, which the oracle checks."""
+    B, V, k = (1 << 22) + 9, 9, 2
+    g = torch.Generator("cuda").manual_seed(5)
+    zd = torch.randn(B, 1, V, generator=g, device="cuda")
+    t = A.aal_topk_logits(zd.view(B, V) + torch.randn(B, V, generator=g, device="cuda"), k)
+    top, ids, rest = t["logits"].view(B, 1, k), t["ids"].view(B, 1, k), t["rest"].view(B, 1)
+    whole = A.aal_topk_loss_fwd_bwd(
+        zd, top, ids, 1, rest=rest, weights=WEIGHTS["all"], layout=WIN, flags=flags,
+        grad_scale=torch.tensor([float(B)], device="cuda"))
+    for a in (0, (1 << 22) - 31):
+        s = slice(a, a + 40)
+        check(A, zd[s].clone(), top[s].clone(), ids[s].clone(), rest[s].clone(), 1, WEIGHTS["all"], WIN, flags=flags)
+        part = A.aal_topk_loss_fwd_bwd(zd[s].clone(), top[s].clone(), ids[s].clone(), 1, rest=rest[s].clone(),
+                                       weights=WEIGHTS["all"], layout=WIN, flags=flags,
+                                       grad_scale=torch.tensor([40.0], device="cuda"))
+        for n in ("accept_tv", "accept_eal", "xstar"):
+            torch.testing.assert_close(whole[n][s], part[n], rtol=4 * REL, atol=4 * REL)
+        torch.testing.assert_close(whole["grad"][s], part["grad"], rtol=24 * REL, atol=24 * REL)
