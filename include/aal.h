@@ -590,7 +590,10 @@ size_t aal_topk_loss_workspace_bytes(aal_layout_t layout, int64_t B, int32_t S, 
  * loss [1] is required; terms, e_tv, e_eal, accept_tv, accept_eal, xstar: as there, or NULL, and
  *     evaluated whatever the weights (a term whose weight is 0 reads 0).
  * grad_draft, grad_dtype, grad_scale, flags : as there.  AAL_FLAG_STREAMING forces the
- *     multi-kernel schedule.
+ *     multi-kernel schedule, which also takes rows of more than 153,600 bf16 or 76,800 fp32 logits and
+ *     fp32 logits with a bf16 gradient; the others stay in registers between their one read and
+ *     the write of their gradient.  With WTV or EAL weights the resident schedule's workgroups wait for each
+ *     other: see "Concurrency"; without them AAL_FLAG_COOPERATIVE has no effect.
  * workspace : at least aal_topk_loss_workspace_bytes(layout, B, S, K) bytes, 256-byte aligned.
  */
 aal_status_t aal_topk_loss_fwd_bwd(const void* z_draft, aal_dtype_t in_dtype, const void* top_logits,

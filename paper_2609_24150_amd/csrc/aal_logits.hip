@@ -21,8 +21,9 @@
 // LDS (a search of the list cost 16,760 rows of 16,609 with up to 100 biases 927 us).
 // A row whose penalties change nothing has no history.
 //
-// Bound by memory: 3,584 rows of 128,256 bf16 with histories of 1,024 and grammars: see the
-// figures at the launch.
+// Bound by memory: 3,584 rows of 128,256 bf16, each with a prompt and up to 7 windows' tokens of
+// history and a grammar mask: forward 344 us, 5.3 TB/s, 95% of what a lone read and write take;
+// backward, which reads a third array where the history has entries, 395 us, 83%.
 #include "aal_device.h"
 #include "aal_rowops.h"
 #include "aal_toplist.h"
