@@ -28,8 +28,12 @@ inline size_t fused_lds_bytes(int held, int staged, int k) {
 // its own sums, and only the step between 2 and 3 (about 3 us) has none.
 // The listed entries' gradient is stored over the others' after the next row's barrier 2,
 // when every holder has waited for its stores.
+// With seven holders the registers are held to what lets two workgroups run on a CU: 7,168 rows of
+// 65,536 bf16, WTV, 398 us against 465 with one.  Ragged rows through the buffer resources
+// and LDS too, their ends alone apart: 7,168 rows of 50,001, 331 us against 408 with an address
+// and a condition for every vector, whose registers left one workgroup a CU.
 template <class TI, class TG, bool VEC, int WK, int NV, int NS, bool COUPLED>
-__global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p, int grid, void* __restrict__ grad) {
+__global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused(TopLossParams p, int grid, void* __restrict__ grad) {
   using Rv = RowVecs<TI, VEC>;
   constexpr int E = Rv::E;
   constexpr int BLK = WK * kWave;  // threads that hold the row
@@ -143,10 +147,10 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
   // -------------------------------------------------------- the row
   // Every load is issued unconditionally, so that a vector's registers have one
   // definition a row (with conditions the compiler kept old and new vectors side by side
-  // and spilled 63 registers).  Rows of whole vectors go through buffer resources, which
-  // read zeros and store nothing past their end (0 bytes where there is no next
-  // row); lanes past a ragged row's last vector read that one.
-  const uint32_t row_bytes = uint32_t(p.V) * sizeof(typename TI::storage), grow_bytes = uint32_t(p.V) * GS;
+  // and spilled 63 registers).  Rows go through buffer resources of the vectors that cover
+  // them, which read zeros past their end (0 bytes where there is no next row; without the
+  // vector that reaches past the array, which is loaded on its own).
+  constexpr uint32_t kDropped = 0x7fffff00u;  // an offset past every row
   u32x4 w[NV];
   // the first NS vectors of a row go through LDS, straight from memory: their loads
   // are issued as soon as the row before is summed, and run while its coefficients are made
@@ -155,15 +159,10 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
     for (int v = 0; v < NS; ++v)
       bld16_lds(rs, stage + v * BLK + wv * kWave, uint32_t(tid) * 16u, uint32_t(v) * (BLK * 16u));
   };
-  static_assert(VEC || NS == 0, "ragged rows are not staged");
-  auto load_row_vec = [&](const rsrc_t& rs, const Rv& rv, int last, int v) {
-    if constexpr (VEC)
-      w[v] = bld16(rs, uint32_t(tid) * 16u, uint32_t(v) * (BLK * 16u));
-    else
-      w[v] = rv.raw(p.zd, min(v * BLK + tid, last));
-  };
+  auto load_row_vec = [&](const rsrc_t& rs, int v) { w[v] = bld16(rs, uint32_t(tid) * 16u, uint32_t(v) * (BLK * 16u)); };
   auto row_rsrc = [&](int64_t r, bool there) {
-    return make_rsrc(static_cast<const uint8_t*>(p.zd) + r * int64_t(row_bytes), there ? row_bytes : 0u);
+    const Rv rv(r, p.R, p.V);
+    return make_rsrc(static_cast<const uint8_t*>(p.zd) + rv.g0 * 16, there ? uint32_t(rv.nfull) * 16u : 0u);
   };
   // a wave-uniform number that the compiler takes as new, so that it makes the
   // conditions that follow from it where they are used, not once for every vector
@@ -172,12 +171,11 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
     return x;
   };
   {
-    const Rv rv(int64_t(blockIdx.x), p.R, p.V);
     const rsrc_t rs = row_rsrc(blockIdx.x, true);
     stage_row(rs);
 #pragma unroll
     for (int v = NS; v < NV; ++v) {
-      load_row_vec(rs, rv, rv.ng - 1, v);
+      load_row_vec(rs, v);
       __builtin_amdgcn_sched_barrier(0);  // in the order in which they are waited for
     }
   }
@@ -204,16 +202,14 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
           if (bits >> e & 1u) x[e] = 0.f;
       s = __builtin_fmaf(s, keep, tree_sum(x));
     };
-    if constexpr (!VEC)
-      if (tid == 0 && !rv.whole(0)) w[0] = rv.edge(p.zd, 0, w[0]);
-    if constexpr (NS > 0) {
-      // the staged vectors are older than the NV - NS loads of the others
-      wait_vmem_le<NV - NS>();
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    // the staged vectors are older than the NV - NS loads of the others
+    wait_vmem_le<NV - NS>();
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       if (v < NS) w[v] = stage[v * BLK + tid];
+      if constexpr (!VEC)
+        if (v == 0 && tid == 0 && rv.ng > 1 && !rv.whole(0)) w[0] = rv.edge(p.zd, 0, w[0]);
       if (v < last_v) {
         pin(w[v]);
         fold(w[v], v);
@@ -227,7 +223,10 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
       if (v == last_v) wl = w[v];
     if (tid > last_t) wl = Rv::none();
     if constexpr (!VEC)
-      if (tid == last_t && rv.ng > 1 && !rv.whole(rv.ng - 1)) wl = rv.edge(p.zd, rv.ng - 1, wl);
+      if (tid == last_t && !rv.whole(rv.ng - 1)) {
+        if (rv.ng > rv.nfull) wl = rv.raw(p.zd, rv.ng - 1);
+        wl = rv.edge(p.zd, rv.ng - 1, wl);
+      }
     pin(wl);
     fold(wl, last_v);
     wait_vmem_all();  // the stores of the row before are done
@@ -265,40 +264,38 @@ __global__ __launch_bounds__((WK + 1) * kWave) void k_top_fused(TopLossParams p,
       lds_barrier();  // 2, for the list too
     }
     lds_barrier();  // 3
-    const Rv rn(more ? next : row, p.R, p.V);
-    const int last_n = more ? rn.ng - 1 : 0;
     const float cR = sh_cR;
     const int last_v3 = fresh(grad != nullptr ? last_v : -1);
-    const rsrc_t gr = make_rsrc(static_cast<uint8_t*>(grad) + row * int64_t(grow_bytes), grow_bytes);
-    auto store = [&](const u32x4& wx, int v) {
+    // the vectors inside the row by 16 bytes, dropped past its last one; of a ragged row's first and
+    // last vector the row's elements one by one
+    const rsrc_t gr = make_rsrc(static_cast<uint8_t*>(grad) + rv.g0 * (E * GS), uint32_t(rv.nfull) * (E * GS));
+    auto store = [&](const u32x4& wx, int v, bool ends) {
       const int gi = v * BLK + tid;
       float x[E];
       unpackv<TI>(wx, x);
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] = cR * ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
-      if constexpr (VEC) {
-        store_g<TG, E>(gr, uint32_t(gi) * (E * GS), x);  // dropped past the row
-      } else if (rv.whole(gi)) {
-        store_vec<TG, E>(grad, (rv.g0 + gi) * E, x);
-      } else if (gi < rv.ng) {
+      store_g<TG, E>(gr, VEC || !ends || rv.whole(gi) ? uint32_t(gi) * (E * GS) : kDropped, x);
+      if constexpr (!VEC)
+        if (ends && gi < rv.ng && !rv.whole(gi)) {
 #pragma unroll 1
-        for (int e = 0; e < E; ++e) {
-          const int i = rv.index(gi, e);
-          float ge = x[0];
+          for (int e = 0; e < E; ++e) {
+            const int i = rv.index(gi, e);
+            float ge = x[0];
 #pragma unroll
-          for (int q = 1; q < E; ++q) ge = e == q ? x[q] : ge;
-          if (i >= 0 && i < p.V) TG::store1(grad, (rv.g0 + gi) * E + e, ge);
+            for (int q = 1; q < E; ++q) ge = e == q ? x[q] : ge;
+            if (i >= 0 && i < p.V) TG::store1(grad, (rv.g0 + gi) * E + e, ge);
+          }
         }
-      }
     };
-    if (last_v3 >= 0) store(wl, last_v);
+    if (last_v3 >= 0) store(wl, last_v, true);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       if (v < last_v3) {
         pin(w[v]);  // the packed vector was kept, not unpacked copies of it
-        store(w[v], v);
+        store(w[v], v, v == 0);
       }
-      if (v >= NS) load_row_vec(rsn, rn, last_n, v);
+      if (v >= NS) load_row_vec(rsn, v);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -362,7 +359,7 @@ hipError_t fused_size(const TopLossArgs& a, bool* used) {
   const int ng = a.V / TI::kVec + (VEC ? 0 : 2);  // vectors that cover a row, at most
   if (a.R * a.V < TI::kVec) return hipSuccess;    // less than a vector in all
 #define AAL_FUSED(WK, NV, NS) \
-  if (ng <= WK * kWave * NV) return fused_launch<TI, TG, VEC, WK, NV, VEC ? NS : 0, COUPLED>(a, used)
+  if (ng <= WK * kWave * NV) return fused_launch<TI, TG, VEC, WK, NV, NS, COUPLED>(a, used)
   AAL_FUSED(1, 9, 4);
   AAL_FUSED(2, 9, 4);
   AAL_FUSED(3, 12, 4);
