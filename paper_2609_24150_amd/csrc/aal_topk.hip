@@ -284,7 +284,7 @@ __device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row,
   t = key_logit<TI>(prefix);
   const RowScale at_t = row_scale(t, p.sc);
   if (tid == 0) sh.n = 0;
-  uint32_t ties = 0;  // before this round
+  uint32_t ties = 0;  // before this pass
   float s = 0.f;
   for (int base = 0; base < rv.ng; base += BLK) {
     const int gi = base + tid;

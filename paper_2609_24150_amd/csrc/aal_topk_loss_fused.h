@@ -351,9 +351,9 @@ hipError_t fused_launch(const TopLossArgs& a, bool* used) {
 // WK, NV and NS by the vectors that cover a row: the fewest vectors a thread that
 // hold it in as many workgroups as 16 to 24 wavefronts of a CU make.  us per WTV call with
 // lists of 64: 14,336 rows of 32,000 bf16 386 with 7 x 9 (3 workgroups a CU), 470 with 7 x 18, 510 in the
-// multi-kernel schedule; of 50,000, 626 with 7 x 14, 758 with 7 x 20; of 16,032, 213 with 3 x 12, 235 with
-// 3 x 18, 241 with 7 x 9; of 8,000, 123 with 2 x 9, 132 with 1 x 18.  More vectors a thread than
-// the row has cost loads that read nothing.
+// multi-kernel schedule; of 50,000, 626 with 7 x 14, 758 with 7 x 20 (one workgroup a CU then); of
+// 16,032, 213 with 3 x 12, 235 with 3 x 18, 241 with 7 x 9; of 8,000, 123 with 2 x 9, 132 with
+// 1 x 18.  More vectors a thread than the row has cost loads that read nothing.
 template <class TI, class TG, bool VEC, bool COUPLED>
 hipError_t fused_size(const TopLossArgs& a, bool* used) {
   const int ng = a.V / TI::kVec + (VEC ? 0 : 2);  // vectors that cover a row, at most
