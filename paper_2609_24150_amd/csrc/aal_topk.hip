@@ -12,8 +12,10 @@
 // numbers that order as logits, one ballot count per line and step, in every
 // wave for its share of k.  The lines that reach t are read again (k = 64 of
 // 128,256: 2% of the row), their entries from t on sorted.  The remainder is
-// the sum of the lines below t and of the entries not taken: never a
-// difference of sums, so it keeps its digits where the list has nearly all mass.
+// the sum of the lines below t and of the entries not taken: never a difference of sums, so it
+// keeps its digits where the list has nearly all mass.  Its reference is the first entry not
+// taken or, where no candidate is left over, t, unless the others lie so far below
+// t that exponentials against it vanish: those are summed again, against the largest of them.
 // k_topk_short, for rows of up to 16 logits per thread, bisects over the logits.
 // Where ties or clusters put more entries at t than the candidates' list holds
 // (rows of few distinct values, rows with fewer than k finite ones), the
@@ -152,9 +154,9 @@ __device__ __forceinline__ int bucket_of(uint64_t e, float t, float scale) {
 }
 
 // Sorts the n candidates, all in [t, m], writes the first k, and returns the sum over
-// the others (this thread's share) against the k-th, whose scale is `at`.  Up to 64 are ranked by
-// counting; more go through 256 buckets and are ranked in theirs (lists of
-// 256 of 14,336 rows of 4,000: 207 us with counting alone).
+// the others (this thread's share) against the first of them, whose scale is `at` (t's where
+// there is none).  Up to 64 are ranked by counting; more go through 256 buckets and are
+// ranked in theirs (lists of 256 of 14,336 rows of 4,000: 207 us with counting alone).
 template <class TI, int BLK, class Sh>
 __device__ __forceinline__ float write_ranked(const TopkParams& p, int64_t row, int n, float t, float m, RowScale& at,
                                               Sh& sh) {
@@ -213,7 +215,7 @@ __device__ __forceinline__ float write_ranked(const TopkParams& p, int64_t row, 
   }
   __syncthreads();
   const int64_t o0 = row * int64_t(p.k);
-  at = row_scale(key_logit<TI>(entry_key(sorted[p.k - 1])), p.sc);
+  at = row_scale(n > p.k ? key_logit<TI>(entry_key(sorted[p.k])) : t, p.sc);
   float s = 0.f;
   for (int j = threadIdx.x; j < n; j += BLK) {
     const uint64_t key = sorted[j];
@@ -244,9 +246,10 @@ __device__ __forceinline__ void add_candidates(Sh& sh, const float (&x)[E], int 
 
 // Any row: the k-th largest key digit by digit, then a pass in index order that
 // collects the larger entries and the first of its ties.  t becomes the k-th logit; returns this
-// thread's share of the others' sum against it.
+// thread's share of the others' sum against it, which is the reference of choice where some of
+// its ties are left over (`tied`).
 template <class TI, bool VEC, int BLK, class Sh>
-__device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row, Sh& sh, float& t) {
+__device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row, Sh& sh, float& t, bool& tied) {
   using Rv = RowVecs<TI, VEC>;
   constexpr int E = Rv::E;
   constexpr int WV = BLK / kWave;
@@ -282,6 +285,7 @@ __device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row,
     need = sh.need;  // of the entries whose key starts with `prefix`
   }
   t = key_logit<TI>(prefix);
+  tied = sh.hist[sh.digit] > need;
   const RowScale at_t = row_scale(t, p.sc);
   if (tid == 0) sh.n = 0;
   uint32_t ties = 0;  // before this pass
@@ -333,10 +337,39 @@ __device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row,
   return s;
 }
 
-template <int WAVES, class Sh>
-__device__ __forceinline__ void write_rest(const TopkParams& p, int64_t row, float s, RowScale at, Sh& sh) {
+// The remainder, whose sum against `at` has this thread's share s.  `low`: all of it lies below t.
+// Exponentials against t are flushed below 2^-126: 2^30 entries of that size make 2^-96,
+// the last digits of a sum of 2^-72.  A smaller one is taken again, over the row, against the
+// largest entry below t.
+template <class TI, bool VEC, int BLK, class Sh>
+__device__ __forceinline__ void write_rest(const TopkParams& p, int64_t row, float s, RowScale at, bool low, float t,
+                                           Sh& sh) {
+  constexpr int WV = BLK / kWave;
   if (p.rest == nullptr) return;
-  s = block_sum<WAVES>(s, sh.f);
+  s = block_sum<WV>(s, sh.f);
+  if (low && s < 0x1p-72f && t != kNegInf) {
+    using Rv = RowVecs<TI, VEC>;
+    constexpr int E = Rv::E;
+    const Rv rv(row, p.rows, p.V);
+    float m = kNegInf;
+    for (int gi = threadIdx.x; gi < rv.ng; gi += BLK) {
+      float x[E];
+      TI::unpack(to_uint4(rv.load(p.z, gi)), x);
+#pragma unroll
+      for (int e = 0; e < E; ++e) m = fmaxf(m, x[e] < t ? x[e] : kNegInf);
+    }
+    m = block_max<WV>(m, sh.f);
+    at = row_scale(m, p.sc);
+    s = 0.f;
+    if (m != kNegInf)
+      for (int gi = threadIdx.x; gi < rv.ng; gi += BLK) {
+        float x[E];
+        TI::unpack(to_uint4(rv.load(p.z, gi)), x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s += x[e] < t ? ex2(__builtin_fmaf(x[e], at.sc, -at.msc)) : 0.f;
+      }
+    s = block_sum<WV>(s, sh.f);
+  }
   if (threadIdx.x != 0) return;
   const float ref = at.sc == p.sc ? at.msc * kLn2 : at.m * p.inv_t;
   p.rest[row] = s > 0.f ? __builtin_fmaf(__log2f(s), kLn2, ref) : kNegInf;
@@ -385,13 +418,14 @@ __global__ __launch_bounds__(BLK) void k_topk_short(TopkParams p) {
   }
   __syncthreads();
   int n = int(sh.n);
+  bool tied = false;
   if (n > CAP) {
-    s = select_slowly<TI, VEC, BLK>(p, row, sh, t);
+    s = select_slowly<TI, VEC, BLK>(p, row, sh, t, tied);
     rs = row_scale(t, p.sc);
     n = p.k;
   }
   const float others = write_ranked<TI, BLK>(p, row, n, t, m, at, sh);
-  write_rest<WV>(p, row, rescaled(s, rs, at) + others, at, sh);
+  write_rest<TI, VEC, BLK>(p, row, rescaled(s, rs, at) + others, at, n == p.k && !tied, t, sh);
 }
 
 // The largest, or the sum, over the L lanes that share a line (L = 1, 2, 4).
@@ -513,13 +547,14 @@ __global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_)
       n = int(sh.n);
     }
   }
+  bool tied = false;
   if (n > CAP) {
-    s = select_slowly<TI, VEC, BLK>(p, row, sh, t);
+    s = select_slowly<TI, VEC, BLK>(p, row, sh, t, tied);
     rs = row_scale(t, p.sc);
     n = p.k;
   }
   const float others = write_ranked<TI, BLK>(p, row, n, t, m, at, sh);
-  write_rest<WV>(p, row, rescaled(s, rs, at) + others, at, sh);
+  write_rest<TI, VEC, BLK>(p, row, rescaled(s, rs, at) + others, at, n == p.k && !tied, t, sh);
 }
 
 template <class TI, bool VEC, int U, int BLK, int NG, int CAP>
