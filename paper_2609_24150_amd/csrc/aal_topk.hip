@@ -81,20 +81,29 @@ struct TopkParams {
   float* rest;
 };
 
-// A reference of sums, 2^(z sc - msc) with the logit `m` at 1.  Entries below -1e30 / sc
-// differ by more than any exponential holds or not at all: a power of two that keeps the products
-// finite takes the place of sc where m is one of them.
+// A reference of sums: entries count 2^(z sc - msc), the logit `m` 1.  msc is m sc rounded, by up
+// to 2^-25 of it, which cancels between entries but is an exponent: beyond 2^27 (8) sums
+// could overflow or vanish.  A reference that large ("steep": a masked row, a temperature
+// near zero) takes the difference before the product, and a sum that is not yet against the
+// row's reference is against at least -2^27, from where a larger one loses nothing.
+constexpr float kSteep = 0x1p27f;
 struct RowScale {
   float m, sc, msc;
+  bool steep;
 };
 __device__ __forceinline__ RowScale row_scale(float m, float sc) {
-  const float s = m * sc < -1e30f ? 0x1p-64f : sc;
-  return {m, s, m == kNegInf ? 0.f : m * s};
+  const float msc = m == kNegInf ? 0.f : m * sc;
+  return {m, sc, msc, fabsf(msc) > kSteep};
 }
+__device__ __forceinline__ float log2_of(const RowScale& r, float z) {
+  return r.steep ? (z - r.m) * r.sc : __builtin_fmaf(z, r.sc, -r.msc);
+}
+// The reference of a thread's own sum whose largest logit is m.
+__device__ __forceinline__ float own_ref(float m, float sc) { return fmaxf(m * sc, -kSteep); }
 // A sum against reference a, none of whose entries is above it, against b >= a.
-__device__ __forceinline__ float rescaled(float s, RowScale a, RowScale b) {
+__device__ __forceinline__ float rescaled(float s, const RowScale& a, const RowScale& b) {
   if (a.m == kNegInf) return 0.f;
-  return a.sc == b.sc ? s * ex2(a.msc - b.msc) : 0.f;
+  return s * ex2(a.steep || b.steep ? (a.m - b.m) * a.sc : a.msc - b.msc);
 }
 
 template <int WAVES>
@@ -224,7 +233,7 @@ __device__ __forceinline__ float write_ranked(const TopkParams& p, int64_t row, 
       const uint32_t b = key & 1u ? 0x80000000u : __builtin_bit_cast(uint32_t, key_logit<TI>(entry_key(key)));
       static_cast<typename TI::bits*>(p.top)[o0 + j] = typename TI::bits(key_bits<TI>() == 16 ? b >> 16 : b);
     } else {
-      s += ex2(__builtin_fmaf(key_logit<TI>(entry_key(key)), at.sc, -at.msc));
+      s += ex2(log2_of(at, key_logit<TI>(entry_key(key))));
     }
   }
   return s;
@@ -328,7 +337,7 @@ __device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row,
       if (key[e] > prefix || (tie && at < need))
         take |= 1u << e;
       else
-        s += ex2(__builtin_fmaf(x[e], at_t.sc, -at_t.msc));
+        s += ex2(log2_of(at_t, x[e]));
       at += tie;
     }
     add_candidates<TI>(sh, x, rv.index(gi, 0), take);
@@ -339,39 +348,41 @@ __device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row,
 
 // The remainder, whose sum against `at` has this thread's share s.  `low`: all of it lies below t.
 // Exponentials against t are flushed below 2^-126: 2^30 entries of that size make 2^-96,
-// the last digits of a sum of 2^-72.  A smaller one is taken again, over the row, against the
-// largest entry below t.
+// the last digits of a sum of 2^-72.  Where there is less, what is below t is summed again, over the
+// row, against the largest of it.  `again`: s lacks what is below t, which a steep t is no reference for.
 template <class TI, bool VEC, int BLK, class Sh>
-__device__ __forceinline__ void write_rest(const TopkParams& p, int64_t row, float s, RowScale at, bool low, float t,
-                                           Sh& sh) {
+__device__ __forceinline__ void write_rest(const TopkParams& p, int64_t row, float s, RowScale at, bool low, bool again,
+                                           float t, Sh& sh) {
   constexpr int WV = BLK / kWave;
   if (p.rest == nullptr) return;
   s = block_sum<WV>(s, sh.f);
-  if (low && s < 0x1p-72f && t != kNegInf) {
+  if (again || (low && s < 0x1p-72f && t != kNegInf)) {
     using Rv = RowVecs<TI, VEC>;
     constexpr int E = Rv::E;
     const Rv rv(row, p.rows, p.V);
-    float m = kNegInf;
-    for (int gi = threadIdx.x; gi < rv.ng; gi += BLK) {
-      float x[E];
-      TI::unpack(to_uint4(rv.load(p.z, gi)), x);
-#pragma unroll
-      for (int e = 0; e < E; ++e) m = fmaxf(m, x[e] < t ? x[e] : kNegInf);
-    }
-    m = block_max<WV>(m, sh.f);
-    at = row_scale(m, p.sc);
-    s = 0.f;
-    if (m != kNegInf)
+    if (low) {
+      float m = kNegInf;
       for (int gi = threadIdx.x; gi < rv.ng; gi += BLK) {
         float x[E];
         TI::unpack(to_uint4(rv.load(p.z, gi)), x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) s += x[e] < t ? ex2(__builtin_fmaf(x[e], at.sc, -at.msc)) : 0.f;
+        for (int e = 0; e < E; ++e) m = fmaxf(m, x[e] < t ? x[e] : kNegInf);
       }
-    s = block_sum<WV>(s, sh.f);
+      at = row_scale(block_max<WV>(m, sh.f), p.sc);
+      s = 0.f;
+    }
+    float more = 0.f;
+    if (at.m != kNegInf)
+      for (int gi = threadIdx.x; gi < rv.ng; gi += BLK) {
+        float x[E];
+        TI::unpack(to_uint4(rv.load(p.z, gi)), x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) more += x[e] < t ? ex2(log2_of(at, x[e])) : 0.f;
+      }
+    s += block_sum<WV>(more, sh.f);
   }
   if (threadIdx.x != 0) return;
-  const float ref = at.sc == p.sc ? at.msc * kLn2 : at.m * p.inv_t;
+  const float ref = at.steep ? at.m * p.inv_t : at.msc * kLn2;
   p.rest[row] = s > 0.f ? __builtin_fmaf(__log2f(s), kLn2, ref) : kNegInf;
 }
 
@@ -401,6 +412,7 @@ __global__ __launch_bounds__(BLK) void k_topk_short(TopkParams p) {
   m = block_max<WV>(m, sh.f);
   float t = threshold<TI, WV>(y, p.k, m, sh.f);
   RowScale rs = row_scale(t, p.sc), at;  // what is below t is summed against it
+  bool tied = false, again = rs.steep;
   float s = 0.f;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -418,14 +430,14 @@ __global__ __launch_bounds__(BLK) void k_topk_short(TopkParams p) {
   }
   __syncthreads();
   int n = int(sh.n);
-  bool tied = false;
   if (n > CAP) {
     s = select_slowly<TI, VEC, BLK>(p, row, sh, t, tied);
     rs = row_scale(t, p.sc);
+    again = false;
     n = p.k;
   }
   const float others = write_ranked<TI, BLK>(p, row, n, t, m, at, sh);
-  write_rest<TI, VEC, BLK>(p, row, rescaled(s, rs, at) + others, at, n == p.k && !tied, t, sh);
+  write_rest<TI, VEC, BLK>(p, row, again ? others : rescaled(s, rs, at) + others, at, n == p.k && !tied, again, t, sh);
 }
 
 // The largest, or the sum, over the L lanes that share a line (L = 1, 2, 4).
@@ -454,7 +466,7 @@ __global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_)
   const Rv rv(row, p.rows, p.V);
   const int rounds = ONE ? 1 : rounds_;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave, mu = tid & (U - 1);
-  float gm[NG], gs[NG];  // of each group: the largest, the sum of 2^(z sc - max(largest sc, -1e30))
+  float gm[NG], gs[NG];  // of each group: the largest, the sum of 2^(z sc - own_ref(largest))
   float m = kNegInf;
   if (tid == 0) sh.n = 0;
 #pragma unroll
@@ -474,7 +486,7 @@ __global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_)
 #pragma unroll
         for (int e = 1; e < E; ++e) um = fmaxf(um, x[u][e]);
         um = line_max<U>(um);
-        const float at = fmaxf(um * p.sc, -1e30f);
+        const float at = own_ref(um, p.sc);
 #pragma unroll
         for (int e = 0; e < E; ++e) x[u][e] = ex2(__builtin_fmaf(x[u][e], p.sc, -at));
         const float us = line_sum<U>(tree_sum(x[u]));
@@ -485,8 +497,8 @@ __global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_)
         gm[g] = lm;
         gs[g] = ls;
       } else {
-        const float nm = fmaxf(gm[g], lm), at = fmaxf(nm * p.sc, -1e30f);
-        gs[g] = gs[g] * ex2(fmaxf(gm[g] * p.sc, -1e30f) - at) + ls * ex2(fmaxf(lm * p.sc, -1e30f) - at);
+        const float nm = fmaxf(gm[g], lm), at = own_ref(nm, p.sc);
+        gs[g] = gs[g] * ex2(own_ref(gm[g], p.sc) - at) + ls * ex2(own_ref(lm, p.sc) - at);
         gm[g] = nm;
       }
     }
@@ -496,65 +508,64 @@ __global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_)
   int n = CAP + 1;
   float s = 0.f, t = threshold<TI, WV>(gm, p.k, m, sh.f);
   RowScale rs = row_scale(t, p.sc), at;  // what is below t is summed against it
-  if (rs.sc == p.sc || t == kNegInf) {
-    // the groups that reach t, in an order that does not depend on timing; the sums of the others
-    int mine = 0;
+  bool tied = false, again = rs.steep;
+  // the groups that reach t, in an order that does not depend on timing; the sums of the others
+  int mine = 0;
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      if (g * rounds * U * BLK + mu * BLK + tid - mu >= rv.ng) continue;
-      if (gm[g] >= t)
-        ++mine;
-      else
-        s += gs[g] * ex2(fmaxf(gm[g] * p.sc, -1e30f) - rs.msc);
-    }
-    int before = mine;
-    for (int off = 1; off < kWave; off <<= 1) {
-      const int o = __shfl_up(before, off, kWave);
-      if (lane >= off) before += o;
-    }
-    if (lane == kWave - 1) sh.i[0][wv] = before;
-    __syncthreads();
-    int to = before - mine, nq = 0;
-#pragma unroll
-    for (int i = 0; i < WV; ++i) {
-      if (i < wv) to += sh.i[0][i];
-      nq += sh.i[0][i];
-    }
-    if (nq <= CAP) {
-#pragma unroll
-      for (int g = 0; g < NG; ++g)
-        if (g * rounds * U * BLK + mu * BLK + tid - mu < rv.ng && gm[g] >= t) sh.queue[to++] = uint16_t(g * BLK + tid);
-      __syncthreads();
-      const int per = rounds * U;  // vectors of a group
-      for (int j = tid; j < nq * per; j += BLK) {
-        const int q = sh.queue[j / per], sub = j % per, qt = q % BLK, qu = qt % U;
-        const int gi = (((q / BLK) * rounds + sub / U) * U + qu) * BLK + qt - qu + sub % U;
-        if (gi >= rv.ng) continue;
-        float x[E];
-        TI::unpack(to_uint4(rv.load(p.z, gi)), x);
-        uint32_t take = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int v = rv.index(gi, e);
-          if (x[e] >= t)
-            take |= VEC || (v >= 0 && v < p.V) ? 1u << e : 0u;
-          else
-            s += ex2(__builtin_fmaf(x[e], rs.sc, -rs.msc));
-        }
-        add_candidates<TI>(sh, x, rv.index(gi, 0), take);
-      }
-      __syncthreads();
-      n = int(sh.n);
-    }
+  for (int g = 0; g < NG; ++g) {
+    if (g * rounds * U * BLK + mu * BLK + tid - mu >= rv.ng) continue;
+    if (gm[g] >= t)
+      ++mine;
+    else
+      s += gs[g] * ex2(own_ref(gm[g], p.sc) - rs.msc);
   }
-  bool tied = false;
+  int before = mine;
+  for (int off = 1; off < kWave; off <<= 1) {
+    const int o = __shfl_up(before, off, kWave);
+    if (lane >= off) before += o;
+  }
+  if (lane == kWave - 1) sh.i[0][wv] = before;
+  __syncthreads();
+  int to = before - mine, nq = 0;
+#pragma unroll
+  for (int i = 0; i < WV; ++i) {
+    if (i < wv) to += sh.i[0][i];
+    nq += sh.i[0][i];
+  }
+  if (nq <= CAP) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+      if (g * rounds * U * BLK + mu * BLK + tid - mu < rv.ng && gm[g] >= t) sh.queue[to++] = uint16_t(g * BLK + tid);
+    __syncthreads();
+    const int per = rounds * U;  // vectors of a group
+    for (int j = tid; j < nq * per; j += BLK) {
+      const int q = sh.queue[j / per], sub = j % per, qt = q % BLK, qu = qt % U;
+      const int gi = (((q / BLK) * rounds + sub / U) * U + qu) * BLK + qt - qu + sub % U;
+      if (gi >= rv.ng) continue;
+      float x[E];
+      TI::unpack(to_uint4(rv.load(p.z, gi)), x);
+      uint32_t take = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int v = rv.index(gi, e);
+        if (x[e] >= t)
+          take |= VEC || (v >= 0 && v < p.V) ? 1u << e : 0u;
+        else
+          s += ex2(__builtin_fmaf(x[e], rs.sc, -rs.msc));
+      }
+      add_candidates<TI>(sh, x, rv.index(gi, 0), take);
+    }
+    __syncthreads();
+    n = int(sh.n);
+  }
   if (n > CAP) {
     s = select_slowly<TI, VEC, BLK>(p, row, sh, t, tied);
     rs = row_scale(t, p.sc);
+    again = false;
     n = p.k;
   }
   const float others = write_ranked<TI, BLK>(p, row, n, t, m, at, sh);
-  write_rest<TI, VEC, BLK>(p, row, rescaled(s, rs, at) + others, at, n == p.k && !tied, t, sh);
+  write_rest<TI, VEC, BLK>(p, row, again ? others : rescaled(s, rs, at) + others, at, n == p.k && !tied, again, t, sh);
 }
 
 template <class TI, bool VEC, int U, int BLK, int NG, int CAP>

@@ -84,3 +84,24 @@ def test_ties_far_above_and_below(A, V, k, dtype):
         z[1, V - n:] = 120.0
         z[1, 5] = 119.0
         check(A, z.to(dtype), k, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("V,k", SHAPES)
+def test_finite_masks_of_every_size(A, V, k, dtype):
+    # what fp32 rounds off a product with log2(e) is an exponent of up to 2^-25 of it: hundreds here
+    for fill in (-1e8, -2e8, -1e9, -1e10, -3e10, -1e12, -1e20, -1e25, -7e29, -1e31):
+        z = torch.full((5, V), fill)
+        for r, n in enumerate((k + V // 9, k, 1, k + 1, 0)):
+            at = torch.randperm(V, generator=torch.Generator().manual_seed(r + 3))[:min(n, V)]
+            z[r, at] = normal(1, len(at), r)[0]
+        z[4, V // 2:] = fill / 3
+        check(A, z.to(dtype), k, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("V,k", [(300, 8), (1003, 20), (3000, 64), (20000, 256), (128256, 64)])
+def test_temperatures_near_zero(A, V, k, dtype):
+    for temperature in (1e-7, 1e-8, 1e-9, 1e-12, 1e-20, 1e-30, 1e-36):
+        for shift in (-9.0, 0.0, 9.0):
+            check(A, (normal(3, V, V) + shift).to(dtype), k, temperature)
