@@ -77,7 +77,8 @@ __device__ __forceinline__ uint32_t listed_bits(const uint32_t* map, int gi) {
 // one that is no part of it), in three steps: the target alone, the listed draft
 // logits against the row's reference, and the sums with the draft's unlisted mass.
 struct ListTarget {
-  float tmax, D, inv_zt, lzt, pr;  // p_i = inv_zt 2^((t - tmax) sct); lzt = log2 of that sum's inverse
+  float tmax, inv_zt, lzt;  // p_i = inv_zt 2^((t - tmax) sct); lzt = log2 of that sum's inverse
+  float pr, lpr;               // p_r and its log2, which is exact where p_r is denormal
   int star;
   bool has;
 };
@@ -118,6 +119,7 @@ __device__ ListTarget list_target(const TopLossParams& p, int64_t row, const flo
   o.inv_zt = o.has ? f / zt : 0.f;
   o.lzt = o.has ? -__log2f(zt) - fmaxf(D, 0.f) : 0.f;
   o.pr = o.has ? g / zt : 0.f;
+  o.lpr = o.has ? fminf(D, 0.f) - __log2f(zt) : 0.f;
   return o;
 }
 __device__ __forceinline__ float list_draft(const TopLossParams& p, const float* sh_t, const float* sh_z, RowRef ref) {
@@ -153,7 +155,7 @@ __device__ TopRow list_row(const TopLossParams& p, const ListTarget& o, const fl
   r.a_eal = v[3];
   const bool below = qr < o.pr;
   r.qlt = v[1] + (below ? qr : 0.f);
-  r.kl = (v[2] + (o.pr > 0.f ? o.pr * (__log2f(o.pr) - __log2f(qr)) : 0.f)) * kLn2;
+  r.kl = (v[2] + (o.pr > 0.f ? o.pr * (o.lpr - __log2f(qr)) : 0.f)) * kLn2;
   r.share = qr > 0.f ? o.pr / qr : 0.f;
   r.xstar = o.star == INT_MAX ? -1 : o.star;
   r.flags = (o.has ? kTopHas : 0) | (below ? kTopRestBelow : 0) | (ref.deep ? kTopDeep : 0);

@@ -1,0 +1,87 @@
+"""aal_topk_loss_fwd_bwd where list and remainder are far apart, on the draft's side and on
+the target's, and at temperatures near zero, against the fp64 oracle.
+
+Tolerances.  With |z / T| <= 200 an exponent z sc - m sc is off by at most 290 2^-24 (the
+rounding of sc) + 290 2^-24 (the fused multiply-add), ln 2 times that is 2.4e-5, exp2 and the sums
+add less than 1e-6: every q and p, and sums of them, are within REL = 2.5e-5 of their value, and
+a logarithm of one within REL plus 2^-23 of its size (up to 200: 2.4e-5), so 5e-5 = 2 REL.
+From these, acceptances are within 2 REL, E within 2 REL K^2, KL (logarithms weighted with
+p, which sum to 1; differences of two of them) within 4 REL + 2 REL KL, gradient entries within 6 REL
+times the oracle's `bound`, and bf16 ones 2^-8 of their size besides.  Values below 1e-37, which fp32
+holds in fewer bits or not at all, are compared to that.  Rows where some q is within 1e-3 of its p are left out of the
+comparison of gradients."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import toplist_oracle as T
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+REL = 2.5e-5
+TINY = 1e-37
+WIN, SEQ = 0, 1
+WEIGHTS = {"wtv": (1.0, 0.0, 0.0, 0.0), "eal": (0.0, 1.0, 0.0, 0.0), "kl": (0.0, 0.0, 1.0, 0.0),
+           "tv": (0.0, 0.0, 0.0, 1.0), "kl+eal": (0.0, 0.1, 1.0, 0.0), "all": (0.5, 0.1, 1.0, 0.3)}
+
+
+@pytest.fixture(scope="module")
+def A():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_24150_amd as lib
+    return lib
+
+
+def check(A, zd, top, ids, rest, K, weights, flags=0, T_d=1.0, T_t=1.0):
+    """Windows [N, K, V], tensors on the host."""
+    N, _, V = zd.shape
+    cuda = lambda t: None if t is None else t.cuda()  # noqa: E731
+    host = lambda t: t.detach().cpu().double().numpy()  # noqa: E731
+    got = A.aal_topk_loss_fwd_bwd(zd.cuda(), top.cuda(), ids.cuda(), K, rest=cuda(rest), weights=weights, temp_draft=T_d,
+                                  temp_target=T_t, flags=flags)
+    ref = T.top_loss(host(zd), host(top), ids.numpy(), None if rest is None else host(rest), T_d, T_t, weights, WIN,
+                     N, K, K)
+    for n in ("accept_tv", "accept_eal"):
+        np.testing.assert_allclose(host(got[n]), ref[n], rtol=2 * REL, atol=TINY, err_msg=n)
+    for n in ("E_tv", "E_eal"):
+        np.testing.assert_allclose(host(got[n]), ref[n], rtol=2 * REL * K * K, atol=TINY, err_msg=n)
+    assert np.array_equal(got["xstar"].cpu().numpy(), ref["xstar"])
+    kl = ref["terms"][2]
+    tol = np.array([2 * REL * K ** 3, 2 * REL * K ** 3, 4 * REL + 2 * REL * abs(kl), 4 * REL])
+    assert np.isfinite(host(got["terms"])).all() and math.isfinite(kl), (host(got["terms"]), ref["terms"])
+    assert (np.abs(host(got["terms"]) - ref["terms"]) <= tol).all(), (host(got["terms"]), ref["terms"])
+    assert abs(got["loss"].item() - ref["loss"]) <= (np.abs(weights) * tol).sum() + 1e-6 * abs(ref["loss"])
+    g = host(got["grad"]).reshape(-1, V)
+    assert np.isfinite(g).all()
+    clear = ref["near"] > 1e-3
+    assert clear.any()
+    tol = 6 * REL * ref["bound"] + TINY + (2.0 ** -8 * np.abs(ref["grad"]) if got["grad"].dtype == BF16 else 0.0)
+    off = np.abs(g - ref["grad"]) > tol
+    assert not off[clear].any(), (np.argwhere(off & clear[:, None])[:5], g[off][:5], ref["grad"][off][:5])
+    return got, ref
+
+
+def make(V, k, gap, dtype, seed, N=3, K=3):
+    """Lists whose target keeps a fair share in the remainder; draft rows that put all but the list `gap` lower."""
+    g = torch.Generator().manual_seed(seed)
+    ids = torch.stack([torch.randperm(V, generator=g)[:k] for _ in range(N * K)]).view(N, K, k)
+    top = (torch.randn(N, K, k, generator=g) + 2).to(dtype)
+    rest = torch.randn(N, K, generator=g) + 2.0
+    zd = torch.randn(N, K, V, generator=g) - gap
+    zd.scatter_(2, ids, torch.randn(N, K, k, generator=g))
+    return zd.to(dtype), top, ids.int(), rest
+
+
+@pytest.mark.parametrize("flags", [0, 1], ids=["default", "streaming"])
+@pytest.mark.parametrize("weights", sorted(WEIGHTS))
+def test_targets_with_little_or_nearly_all_in_the_remainder(A, weights, flags):
+    for k in (1, 8, 64, 500):
+        for gap in (60.0, 80.0, 84.0, 85.5, 86.5, 87.0, 87.3, 90.0, 120.0, -60.0, -80.0, -84.0, -87.0, -90.0, -120.0):
+            zd, top, ids, rest = make(900, k, 1.0, F32, k + 7)
+            top = torch.zeros_like(top)  # all alike: the sum of the list is k
+            rest = torch.full_like(rest, -gap)
+            check(A, zd, top, ids, rest, 3, WEIGHTS[weights], flags)
