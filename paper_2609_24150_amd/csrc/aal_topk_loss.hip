@@ -30,8 +30,9 @@
 // Both end with k_top_loss: every window's E, the four terms and the weighted
 // loss, in a fixed order of summation.
 //
-// The listed entries are kept out of the unlisted sum by a bitmap of the
-// vocabulary in LDS, so that q_r is a sum and not a difference.  A row whose largest logit
+// The listed entries are kept out of the unlisted sum and its reference by a bitmap of the
+// vocabulary in LDS, so that q_r is a sum and not a difference, and KL and its gradient hold
+// where the draft's unlisted logits lie so far below the list that q_r is 0 in fp32.  A row whose largest logit
 // is below -1e30 / sc ("deep": filled with the type's lowest value) has entries that are
 // equal or further apart than any exponential holds: 2^-64 takes the place of sc
 // there, so that the products stay finite.
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(BLK) void k_top_rows(TopLossParams p, int64_t row0)
     if (in) atomicOr(&sh_map[(id + rv.head) >> 5], 1u << ((id + rv.head) & 31));
   }
   __syncthreads();
-  // the largest logit of all entries, the sum over the unlisted ones against
+  // the largest unlisted logit, the sum over the unlisted ones against
   // max(largest sc, -1e30) so far
   float m = kNegInf, s = 0.f;
   for (int base = threadIdx.x; base < rv.ng; base += BLK * U) {
@@ -77,23 +78,24 @@ __global__ __launch_bounds__(BLK) void k_top_rows(TopLossParams p, int64_t row0)
     rv.unpack(w[0], x);
     float cm = m;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      const int gi = base + u * BLK;
+      const uint32_t bits = gi < rv.ng ? listed_bits<E>(sh_map, gi) : 0u;
+      if (bits)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (bits >> e & 1u) x[u][e] = kNegInf;
 #pragma unroll
       for (int e = 0; e < E; ++e) cm = fmaxf(cm, x[u][e]);
+    }
     const float at = fmaxf(cm * p.scd, -1e30f);
     s *= ex2(fmaxf(m * p.scd, -1e30f) - at);
     m = cm;
     float c[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int gi = base + u * BLK;
-      const uint32_t bits = gi < rv.ng ? listed_bits<E>(sh_map, gi) : 0u;
 #pragma unroll
       for (int e = 0; e < E; ++e) x[u][e] = ex2(__builtin_fmaf(x[u][e], p.scd, -at));
-      if (bits)
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (bits >> e & 1u) x[u][e] = 0.f;
       c[u] = tree_sum(x[u]);
     }
     s += tree_sum(c);
@@ -123,8 +125,7 @@ __global__ __launch_bounds__(BLK) void k_top_rows(TopLossParams p, int64_t row0)
   __syncthreads();
   if (threadIdx.x < kWave) {
     s = wave_sum(lane < BLK / kWave ? sh_s[lane] : 0.f);
-    const TopRow o = list_row(p, list_target(p, row, sh_t, sh_id), sh_t, sh_z, sh_id, ref,
-                              list_draft(p, sh_t, sh_z, ref), s);
+    const TopRow o = list_row(p, list_target(p, row, sh_t, sh_id), sh_t, sh_z, sh_id, list_draft(p, sh_t, sh_z), ref, s);
     if (lane == 0) {
       p.stats[row] = o;
       publish(p.slots + 2 * row, o.a_tv, 1u);
@@ -161,7 +162,7 @@ __global__ __launch_bounds__(kRowBlock) void k_top_grad(TopLossParams p, int64_t
   const int64_t row = row0 + blockIdx.x;
   const Rv rv(row, p.R, p.V);
   const TopRow s = p.stats[row];
-  const float sc = s.flags & kTopDeep ? kDeepScale : p.scd;
+  const RowRef ref = row_ref(s.mu, p.scd), list = row_ref(s.ml, p.scd);
   const int64_t e0 = row * int64_t(p.V), l0 = row * p.k;
   for (int base = blockIdx.y * kRowBlock * U + threadIdx.x; base < rv.ng; base += splits * kRowBlock * U) {
     u32x4 w[1][U];
@@ -173,7 +174,7 @@ __global__ __launch_bounds__(kRowBlock) void k_top_grad(TopLossParams p, int64_t
       float x[E], g[E];
       TI::unpack(to_uint4(w[0][u]), x);
 #pragma unroll
-      for (int e = 0; e < E; ++e) g[e] = s.cR * ex2(__builtin_fmaf(x[e], sc, -s.msc));
+      for (int e = 0; e < E; ++e) g[e] = s.cR * ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
       rv.template store<TG>(grad, gi, g);
     }
   }
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(kRowBlock) void k_top_grad(TopLossParams p, int64_t
     if (((id + rv.head) / E / (kRowBlock * U)) % splits != int(blockIdx.y)) continue;
     const float t = load_top(p, l0 + i);
     if (t == kNegInf) continue;
-    const float q = ex2(__builtin_fmaf(TI::load1(p.zd, e0 + id), sc, -s.msc)) * s.inv_s;
+    const float q = ex2(listed_log2(list, TI::load1(p.zd, e0 + id), p.scd)) * s.ql;
     TG::store1(grad, e0 + id, listed_grad(s, q, listed_p(s, t, p.sct), id));
   }
 }

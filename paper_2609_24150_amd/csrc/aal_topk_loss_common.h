@@ -74,11 +74,21 @@ __device__ __forceinline__ uint32_t listed_bits(const uint32_t* map, int gi) {
 }
 
 // What one wave makes of a row's list, its entries' t and z in LDS (t = -inf marks
-// one that is no part of it), in three steps: the target alone, the listed draft
-// logits against the row's reference, and the sums with the draft's unlisted mass.
+// one that is no part of it), in three steps: the target alone, the draft's listed
+// logits alone, and both with the draft's unlisted mass.  List and remainder have a reference and a
+// sum each, on the target's side and on the draft's, so that neither vanishes however far it lies
+// below the other; they are joined through the log2 of one reference over the other.
+struct Join {
+  float f, g, up, dn;  // what takes values of the list and of the remainder to the larger reference, and -log2 of f, log2 of g
+};
+__device__ __forceinline__ Join join(float D) {
+  const float up = fmaxf(D, 0.f), dn = fminf(D, 0.f);
+  return {ex2(-up), ex2(dn), up, dn};
+}
 struct ListTarget {
-  float tmax, inv_zt, lzt;  // p_i = inv_zt 2^((t - tmax) sct); lzt = log2 of that sum's inverse
-  float pr, lpr;               // p_r and its log2, which is exact where p_r is denormal
+  float tmax, inv_zt;  // p_i = inv_zt 2^((t - tmax) sct)
+  float pr;
+  float iz, up, dn;    // log2 p_i = (t - tmax) sct + log2 iz - up, log2 p_r = log2 iz + dn
   int star;
   bool has;
 };
@@ -105,41 +115,51 @@ __device__ ListTarget list_target(const TopLossParams& p, int64_t row, const flo
   for (int i = lane; i < p.k; i += kWave)
     if (sh_t[i] != kNegInf) st += ex2((sh_t[i] - o.tmax) * p.sct);
   st = wave_sum(st);
-  // the remainder against the list's largest, in log2: the larger of the two is the reference
-  float D = 0.f, f = 1.f, g = 0.f;  // list terms times f, the remainder's g
-  if (!any) {
-    f = 0.f;
-    g = rest != kNegInf ? 1.f : 0.f;
-  } else if (rest != kNegInf) {
-    D = float(double(rest) * 1.4426950408889634 - double(o.tmax) * double(p.sct));
-    f = ex2(-fmaxf(D, 0.f));
-    g = ex2(fminf(D, 0.f));
-  }
-  const float zt = __builtin_fmaf(st, f, g);
-  o.inv_zt = o.has ? f / zt : 0.f;
-  o.lzt = o.has ? -__log2f(zt) - fmaxf(D, 0.f) : 0.f;
-  o.pr = o.has ? g / zt : 0.f;
-  o.lpr = o.has ? fminf(D, 0.f) - __log2f(zt) : 0.f;
+  // the remainder, one entry, against the list's largest
+  Join j = join(any && rest != kNegInf ? float(double(rest) * 1.4426950408889634 - double(o.tmax) * double(p.sct)) : 0.f);
+  if (!any) j.f = 0.f;
+  if (rest == kNegInf) j.g = 0.f;
+  const float zt = __builtin_fmaf(st, j.f, j.g);
+  o.iz = o.has ? 1.f / zt : 0.f;
+  o.inv_zt = j.f * o.iz;
+  o.pr = j.g * o.iz;
+  o.up = j.up;
+  o.dn = j.dn;
   return o;
 }
-__device__ __forceinline__ float list_draft(const TopLossParams& p, const float* sh_t, const float* sh_z, RowRef ref) {
-  float sz = 0.f;
-  for (int i = threadIdx.x & (kWave - 1); i < p.k; i += kWave)
-    if (sh_t[i] != kNegInf) sz += ex2(listed_log2(ref, sh_z[i], p.scd));
-  return wave_sum(sz);
+struct ListDraft {
+  RowRef ref;
+  float s;
+};
+__device__ __forceinline__ ListDraft list_draft(const TopLossParams& p, const float* sh_t, const float* sh_z) {
+  const int lane = threadIdx.x & (kWave - 1);
+  float m = kNegInf, s = 0.f;
+  for (int i = lane; i < p.k; i += kWave)
+    if (sh_t[i] != kNegInf) m = fmaxf(m, sh_z[i]);
+  const RowRef ref = row_ref(wave_max(m), p.scd);
+  for (int i = lane; i < p.k; i += kWave)
+    if (sh_t[i] != kNegInf) s += ex2(listed_log2(ref, sh_z[i], p.scd));
+  return {ref, wave_sum(s)};
 }
+// u, su: the unlisted entries' reference and their sum against it.
 __device__ TopRow list_row(const TopLossParams& p, const ListTarget& o, const float* sh_t, const float* sh_z,
-                           const int* sh_id, RowRef ref, float sz, float su) {
-  const float zd = sz + su, inv_s = zd > 0.f ? 1.f / zd : 0.f;
-  // log2 of the sums' ratio (a draft row without a finite entry has q = 0 everywhere)
-  const float dl = (zd > 0.f ? __log2f(zd) : 0.f) + o.lzt;
-  const float qr = p.rest != nullptr ? su * inv_s : 0.f;
+                           const int* sh_id, const ListDraft& l, const RowRef& u, float su) {
+  float D = u.deep || l.ref.deep ? (u.m - l.ref.m) * p.scd : u.msc - l.ref.msc;
+  if (u.m == kNegInf) D = l.ref.m == kNegInf ? 0.f : kNegInf;
+  else if (l.ref.m == kNegInf) D = -kNegInf;
+  const Join j = join(D);
+  const float zd = l.s * j.f + su * j.g, iz = zd > 0.f ? 1.f / zd : 0.f;  // 0: a draft row without a finite entry
+  const float ql = j.f * iz, qu = j.g * iz, qr = p.rest != nullptr ? su * qu : 0.f;
+  // log2 p - log2 q of a listed entry is (lt - lz) + dl, of the remainder lr: one logarithm each, of sums
+  const float zz = zd * o.iz;
+  const float dl = (zz > 0.f ? __log2f(zz) : 0.f) + (j.up - o.up);
+  const float lr = su > 0.f ? __log2f(zz / su) + (o.dn - j.dn) : -kNegInf;
   float v[4] = {0.f, 0.f, 0.f, 0.f};  // sums of min(p, q), q where q < p, p log2(p / q), q at x*
   for (int i = threadIdx.x & (kWave - 1); i < p.k; i += kWave) {
     const float t = sh_t[i];
     if (t == kNegInf) continue;
-    const float lt = (t - o.tmax) * p.sct, lz = listed_log2(ref, sh_z[i], p.scd);
-    const float pv = ex2(lt) * o.inv_zt, qv = ex2(lz) * inv_s;
+    const float lt = (t - o.tmax) * p.sct, lz = listed_log2(l.ref, sh_z[i], p.scd);
+    const float pv = ex2(lt) * o.inv_zt, qv = ex2(lz) * ql;
     v[0] += fminf(pv, qv);
     v[1] += qv < pv ? qv : 0.f;
     v[2] += pv > 0.f ? pv * ((lt - lz) + dl) : 0.f;
@@ -147,18 +167,20 @@ __device__ TopRow list_row(const TopLossParams& p, const ListTarget& o, const fl
   }
   wave_sum_n(v);
   TopRow r{};
-  r.msc = ref.msc;
-  r.inv_s = inv_s;
+  r.mu = u.m;
+  r.ml = l.ref.m;
+  r.qu = qu;
+  r.ql = ql;
   r.tmax = o.tmax;
   r.inv_zt = o.inv_zt;
   r.a_tv = v[0] + fminf(o.pr, qr);
   r.a_eal = v[3];
   const bool below = qr < o.pr;
   r.qlt = v[1] + (below ? qr : 0.f);
-  r.kl = (v[2] + (o.pr > 0.f ? o.pr * (o.lpr - __log2f(qr)) : 0.f)) * kLn2;
-  r.share = qr > 0.f ? o.pr / qr : 0.f;
+  r.kl = (v[2] + (o.pr > 0.f ? o.pr * lr : 0.f)) * kLn2;
+  r.pu = su > 0.f ? o.pr / su : 0.f;
   r.xstar = o.star == INT_MAX ? -1 : o.star;
-  r.flags = (o.has ? kTopHas : 0) | (below ? kTopRestBelow : 0) | (ref.deep ? kTopDeep : 0);
+  r.flags = (o.has ? kTopHas : 0) | (below ? kTopRestBelow : 0);
   return r;
 }
 
@@ -216,8 +238,9 @@ __device__ __forceinline__ void row_coefs(TopRow& o, const TopLossParams& p, dou
   const double c_eal = -f * p.f_eal * d_eal * double(o.a_eal);
   const double c_kl = (o.flags & kTopHas) ? f * p.f_kl : 0.0;
   const double q_lt = double(o.qlt);
-  o.cR = float((c_tv * (((o.flags & kTopRestBelow) ? 1.0 : 0.0) - q_lt) - c_eal + c_kl * (1.0 - double(o.share))) *
-               double(o.inv_s));
+  // (p_r q_v / q_r of the KL term as p_r over the unlisted sum: q_r may be 0 in fp32)
+  o.cR = float((c_tv * (((o.flags & kTopRestBelow) ? 1.0 : 0.0) - q_lt) - c_eal + c_kl) * double(o.qu) -
+               c_kl * double(o.pu));
   o.cA = float(c_tv * (1.0 - q_lt) - c_eal + c_kl);
   o.cB = float(-c_tv * q_lt - c_eal + c_kl);
   o.cP = float(c_kl);

@@ -18,11 +18,11 @@ inline size_t fused_lds_bytes(int held, int staged, int k) {
 // windows and the coefficients beside their passes, so that neither's registers
 // add to the other's.  Three barriers a row:
 //   holders                                                list
-//   gradient of the row before, this row's loads           finishes the row before last; this list, bitmap, p
-//   1
+//   gradient of the row before, this row's loads           finishes the row before last; this list, bitmap
+//   1                                                      the listed alone: p's sum, the draft's
 //   each vector as it arrives: largest, sum of the unlisted
 //   2
-//                                                          q, acceptances, neighbours, coefficients
+//                                                          p and q, acceptances, neighbours, coefficients
 //   3
 // So the loads of a row run under the gradient pass of the one before and under
 // its own sums, and only the step between 2 and 3 (about 3 us) has none.
@@ -82,13 +82,14 @@ __global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused
       wait_lds_all();
       lds_barrier();  // 1
       const ListTarget lt_row = list_target(p, row, lt, li);
+      const ListDraft ld_row = list_draft(p, lt, lz);
       const RowWindows rw = row_windows(row, p.layout, p.S, p.K);
       lds_barrier();  // 2
       const float wm = lane < WK ? sh_m[lane] : kNegInf;
       const RowRef ref = row_ref(wave_max(wm), p.scd);
       if (ref.deep) lds_barrier();
       const float su = wave_sum(lane < WK ? sh_s[lane] * (ref.deep ? 1.f : ex2(fmaxf(wm * p.scd, -1e30f) - ref.msc)) : 0.f);
-      TopRow o = list_row(p, lt_row, lt, lz, li, ref, list_draft(p, lt, lz, ref), su);
+      TopRow o = list_row(p, lt_row, lt, lz, li, ld_row, ref, su);
       if (lane == 0) {
         publish(p.slots + 2 * row, o.a_tv, 1u);
         publish(p.slots + 2 * row + 1, o.a_eal, 1u);
@@ -132,7 +133,7 @@ __global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused
         const int id = li[i];
         done_id[i] = id;
         if (id < 0) continue;
-        const float q = ex2(listed_log2(ref, lz[i], p.scd)) * o.inv_s;
+        const float q = ex2(listed_log2(ld_row.ref, lz[i], p.scd)) * o.ql;
         done_g[i] = listed_grad(o, q, listed_p(o, lt[i], p.sct), id);
         map[(id + head) >> 5] = 0;
       }
@@ -183,10 +184,15 @@ __global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused
     const Rv rv(row, p.R, p.V);
     const int last_v = fresh((rv.ng - 1) / BLK), last_t = fresh((rv.ng - 1) % BLK);
     lds_barrier();  // 1
-    float m = kNegInf, s = 0.f;  // s against max(m sc, -1e30)
+    float m = kNegInf, s = 0.f;  // of the unlisted entries; s against max(m sc, -1e30)
     auto fold = [&](const u32x4& wx, int v) {
       float x[E];
       unpackv<TI>(wx, x);
+      const uint32_t bits = listed_bits<E>(map, v * BLK + tid);
+      if (bits)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (bits >> e & 1u) x[e] = kNegInf;
       float cm = m;
 #pragma unroll
       for (int e = 0; e < E; ++e) cm = fmaxf(cm, x[e]);
@@ -195,11 +201,6 @@ __global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused
       m = cm;
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] = ex2(__builtin_fmaf(x[e], p.scd, -at));
-      const uint32_t bits = listed_bits<E>(map, v * BLK + tid);
-      if (bits)
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (bits >> e & 1u) x[e] = 0.f;
       s = __builtin_fmaf(s, keep, tree_sum(x));
     };
     // the staged vectors are older than the NV - NS loads of the others

@@ -34,22 +34,23 @@ struct TopkArgs {
 hipError_t launch_topk(const TopkArgs& a);
 
 // ------------------------------------------- objectives against top lists
-// Per-row results of the row pass and coefficients of the gradient.  64 bytes.
+// Per-row results of the row pass and coefficients of the gradient.  72 bytes.
 struct TopRow {
-  float msc, inv_s;   // draft: fl(max * sc), 1 / sum of 2^(z*sc - msc)
+  float mu, ml;       // draft: largest unlisted and listed logit, the references of 2^(z*sc - m*sc)
+  float qu, ql;       // and what takes a value against them to q
   float tmax, inv_zt; // target: largest logit of the list, p_i = inv_zt 2^((t - tmax)*sct)
   float a_tv, a_eal;  // acceptances
   float qlt;          // sum of q over the entries (the remainder among them) with q < p
   float kl;           // KL(p || q) in nats
-  float share;        // p_rest / q_rest, 0 where q_rest = 0
+  float pu;           // p_rest / sum of the unlisted values against mu, 0 where there are none
   int32_t xstar;      // greedy token of the list, -1 for an empty one
-  int32_t flags;      // kTopHas: the row has a target; kTopRestBelow: q_rest < p_rest; kTopDeep: see aal_topk_loss.hip
-  float cR;           // unlisted entries: g = cR 2^(z*sc - msc)
+  int32_t flags;      // kTopHas: the row has a target; kTopRestBelow: q_rest < p_rest
+  float cR;           // unlisted entries: g = cR 2^(z*sc - mu*sc)
   float cA, cB;       // listed entries: g = q (q < p ? cA : cB) - cP p + cX [v = x*]
   float cP, cX;
 };
-static_assert(sizeof(TopRow) == 64, "TopRow layout");
-constexpr int kTopHas = 1, kTopRestBelow = 2, kTopDeep = 4;
+static_assert(sizeof(TopRow) == 72, "TopRow layout");
+constexpr int kTopHas = 1, kTopRestBelow = 2;
 
 struct TopLossArgs {
   DType in, td, gd;        // draft logits, listed logits, gradient

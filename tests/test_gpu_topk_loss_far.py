@@ -10,6 +10,7 @@ p, which sum to 1; differences of two of them) within 4 REL + 2 REL KL, gradient
 times the oracle's `bound`, and bf16 ones 2^-8 of their size besides.  Values below 1e-37, which fp32
 holds in fewer bits or not at all, are compared to that.  Rows where some q is within 1e-3 of its p are left out of the
 comparison of gradients."""
+import itertools
 import math
 
 import numpy as np
@@ -74,6 +75,45 @@ def make(V, k, gap, dtype, seed, N=3, K=3):
     zd = torch.randn(N, K, V, generator=g) - gap
     zd.scatter_(2, ids, torch.randn(N, K, k, generator=g))
     return zd.to(dtype), top, ids.int(), rest
+
+
+@pytest.mark.parametrize("flags", [0, 1], ids=["default", "streaming"])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("weights", sorted(WEIGHTS))
+@pytest.mark.parametrize("gap", [50.0, 80.0, 88.0, 92.0, 100.0, 150.0])
+def test_drafts_that_leave_the_remainder_little(A, gap, weights, dtype, flags):
+    for V, k in ((90, 64), (700, 8), (4099, 1), (33000, 100)):
+        zd, top, ids, rest = make(V, k, gap, dtype, V)
+        check(A, zd, top, ids, rest, 3, WEIGHTS[weights], flags)
+    zd, top, ids, rest = make(1003, 20, gap / 2, dtype, 5)
+    check(A, zd, top, ids, rest, 3, WEIGHTS[weights], flags, T_d=0.5)
+
+
+@pytest.mark.parametrize("flags", [0, 1], ids=["default", "streaming"])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("weights", sorted(WEIGHTS))
+@pytest.mark.parametrize("gap", [50.0, 88.0, 120.0])
+def test_drafts_that_leave_the_list_little(A, gap, weights, dtype, flags):
+    for V, k in ((90, 64), (700, 8), (33000, 100)):
+        zd, top, ids, rest = make(V, k, -gap, dtype, V + 1)
+        check(A, zd, top, ids, rest, 3, WEIGHTS[weights], flags)
+
+
+@pytest.mark.parametrize("flags", [0, 1], ids=["default", "streaming"])
+@pytest.mark.parametrize("weights", sorted(WEIGHTS))
+def test_a_remainder_of_one_entry(A, weights, flags):
+    """One finite entry beside the list, where the draft's share of it is near what fp32 holds."""
+    for k in (1, 8, 64, 500):
+        for gap, more in itertools.product((80.0, 84.0, 86.0, 87.0, 87.3, 87.5, 88.0, 90.0, 103.0), (0.0, 8.0)):
+            zd, top, ids, rest = make(900, k, 0.0, F32, k)
+            rest = rest + more
+            for n in range(3):
+                for j in range(3):
+                    zd[n, j] = -math.inf
+                    zd[n, j, ids[n, j].long()] = 0.0
+                    free = next(v for v in range(900) if v not in set(ids[n, j].tolist()))
+                    zd[n, j, free] = -gap
+            check(A, zd, top, ids, rest, 3, WEIGHTS[weights], flags)
 
 
 @pytest.mark.parametrize("flags", [0, 1], ids=["default", "streaming"])
