@@ -174,6 +174,10 @@ __global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused
   {
     const rsrc_t rs = row_rsrc(blockIdx.x, true);
     stage_row(rs);
+    // The row's first wait is for all but the NV - NS youngest loads, so none of those may go
+    // before one into LDS: nothing else orders them, and the last staged vectors would be read
+    // before they are there.
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int v = NS; v < NV; ++v) {
       load_row_vec(rs, v);
