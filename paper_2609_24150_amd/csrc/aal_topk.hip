@@ -25,6 +25,7 @@
 // us, 6.2 TB/s, 89% of what a lone read of them takes (k = 8 94%, k = 256 75%: sorting).
 // Few rows are bound by the arithmetic of the CU that each has to itself: 7 of 151,936, 18 us.
 #include "aal_device.h"
+#include "aal_row_ref.h"
 #include "aal_rowops.h"
 #include "aal_toplist.h"
 
@@ -81,27 +82,8 @@ struct TopkParams {
   float* rest;
 };
 
-// A reference of sums: entries count 2^(z sc - msc), the logit `m` 1.  msc is m sc rounded, by up
-// to 2^-25 of it, which cancels between entries but is an exponent: beyond 2^27 (8) sums
-// could overflow or vanish.  A reference that large ("steep": a masked row, a temperature
-// near zero) takes the difference before the product, and a sum that is not yet against the
-// row's reference is against at least -2^27, from where a larger one loses nothing.
-constexpr float kSteep = 0x1p27f;
-struct RowScale {
-  float m, sc, msc;
-  bool steep;
-};
-__device__ __forceinline__ RowScale row_scale(float m, float sc) {
-  const float msc = m == kNegInf ? 0.f : m * sc;
-  return {m, sc, msc, fabsf(msc) > kSteep};
-}
-__device__ __forceinline__ float log2_of(const RowScale& r, float z) {
-  return r.steep ? (z - r.m) * r.sc : __builtin_fmaf(z, r.sc, -r.msc);
-}
-// The reference of a thread's own sum whose largest logit is m.
-__device__ __forceinline__ float own_ref(float m, float sc) { return fmaxf(m * sc, -kSteep); }
 // A sum against reference a, none of whose entries is above it, against b >= a.
-__device__ __forceinline__ float rescaled(float s, const RowScale& a, const RowScale& b) {
+__device__ __forceinline__ float rescaled(float s, const RowRef& a, const RowRef& b) {
   if (a.m == kNegInf) return 0.f;
   return s * ex2(a.steep || b.steep ? (a.m - b.m) * a.sc : a.msc - b.msc);
 }
@@ -167,7 +149,7 @@ __device__ __forceinline__ int bucket_of(uint64_t e, float t, float scale) {
 // there is none).  Up to 64 are ranked by counting; more go through 256 buckets and are
 // ranked in theirs (lists of 256 of 14,336 rows of 4,000: 207 us with counting alone).
 template <class TI, int BLK, class Sh>
-__device__ __forceinline__ float write_ranked(const TopkParams& p, int64_t row, int n, float t, float m, RowScale& at,
+__device__ __forceinline__ float write_ranked(const TopkParams& p, int64_t row, int n, float t, float m, RowRef& at,
                                               Sh& sh) {
   const uint64_t* sorted = sh.sorted;
   if (n <= kWave) {
@@ -224,7 +206,7 @@ __device__ __forceinline__ float write_ranked(const TopkParams& p, int64_t row, 
   }
   __syncthreads();
   const int64_t o0 = row * int64_t(p.k);
-  at = row_scale(n > p.k ? key_logit<TI>(entry_key(sorted[p.k])) : t, p.sc);
+  at = row_ref(n > p.k ? key_logit<TI>(entry_key(sorted[p.k])) : t, p.sc);
   float s = 0.f;
   for (int j = threadIdx.x; j < n; j += BLK) {
     const uint64_t key = sorted[j];
@@ -295,7 +277,7 @@ __device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row,
   }
   t = key_logit<TI>(prefix);
   tied = sh.hist[sh.digit] > need;
-  const RowScale at_t = row_scale(t, p.sc);
+  const RowRef at_t = row_ref(t, p.sc);
   if (tid == 0) sh.n = 0;
   uint32_t ties = 0;  // before this pass
   float s = 0.f;
@@ -351,7 +333,7 @@ __device__ __forceinline__ float select_slowly(const TopkParams& p, int64_t row,
 // the last digits of a sum of 2^-72.  Where there is less, what is below t is summed again, over the
 // row, against the largest of it.  `again`: s lacks what is below t, which a steep t is no reference for.
 template <class TI, bool VEC, int BLK, class Sh>
-__device__ __forceinline__ void write_rest(const TopkParams& p, int64_t row, float s, RowScale at, bool low, bool again,
+__device__ __forceinline__ void write_rest(const TopkParams& p, int64_t row, float s, RowRef at, bool low, bool again,
                                            float t, Sh& sh) {
   constexpr int WV = BLK / kWave;
   if (p.rest == nullptr) return;
@@ -368,7 +350,7 @@ __device__ __forceinline__ void write_rest(const TopkParams& p, int64_t row, flo
 #pragma unroll
         for (int e = 0; e < E; ++e) m = fmaxf(m, x[e] < t ? x[e] : kNegInf);
       }
-      at = row_scale(block_max<WV>(m, sh.f), p.sc);
+      at = row_ref(block_max<WV>(m, sh.f), p.sc);
       s = 0.f;
     }
     float more = 0.f;
@@ -411,7 +393,7 @@ __global__ __launch_bounds__(BLK) void k_topk_short(TopkParams p) {
     }
   m = block_max<WV>(m, sh.f);
   float t = threshold<TI, WV>(y, p.k, m, sh.f);
-  RowScale rs = row_scale(t, p.sc), at;  // what is below t is summed against it
+  RowRef rs = row_ref(t, p.sc), at;  // what is below t is summed against it
   bool tied = false, again = rs.steep;
   float s = 0.f;
 #pragma unroll
@@ -432,7 +414,7 @@ __global__ __launch_bounds__(BLK) void k_topk_short(TopkParams p) {
   int n = int(sh.n);
   if (n > CAP) {
     s = select_slowly<TI, VEC, BLK>(p, row, sh, t, tied);
-    rs = row_scale(t, p.sc);
+    rs = row_ref(t, p.sc);
     again = false;
     n = p.k;
   }
@@ -507,7 +489,7 @@ __global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_)
   m = block_max<WV>(m, sh.f);
   int n = CAP + 1;
   float s = 0.f, t = threshold<TI, WV>(gm, p.k, m, sh.f);
-  RowScale rs = row_scale(t, p.sc), at;  // what is below t is summed against it
+  RowRef rs = row_ref(t, p.sc), at;  // what is below t is summed against it
   bool tied = false, again = rs.steep;
   // the groups that reach t, in an order that does not depend on timing; the sums of the others
   int mine = 0;
@@ -560,7 +542,7 @@ __global__ __launch_bounds__(BLK, 8) void k_topk_rows(TopkParams p, int rounds_)
   }
   if (n > CAP) {
     s = select_slowly<TI, VEC, BLK>(p, row, sh, t, tied);
-    rs = row_scale(t, p.sc);
+    rs = row_ref(t, p.sc);
     again = false;
     n = p.k;
   }

@@ -32,10 +32,7 @@
 //
 // The listed entries are kept out of the unlisted sum and its reference by a bitmap of the
 // vocabulary in LDS, so that q_r is a sum and not a difference, and KL and its gradient hold
-// where the draft's unlisted logits lie so far below the list that q_r is 0 in fp32.  A row whose largest logit
-// is below -1e30 / sc ("deep": filled with the type's lowest value) has entries that are
-// equal or further apart than any exponential holds: 2^-64 takes the place of sc
-// there, so that the products stay finite.
+// where the draft's unlisted logits lie so far below the list that q_r is 0 in fp32.
 #include "aal_topk_loss_common.h"
 
 namespace aal {
@@ -68,8 +65,7 @@ __global__ __launch_bounds__(BLK) void k_top_rows(TopLossParams p, int64_t row0)
     if (in) atomicOr(&sh_map[(id + rv.head) >> 5], 1u << ((id + rv.head) & 31));
   }
   __syncthreads();
-  // the largest unlisted logit, the sum over the unlisted ones against
-  // max(largest sc, -1e30) so far
+  // the largest unlisted logit, the sum over the unlisted ones against its own_ref so far
   float m = kNegInf, s = 0.f;
   for (int base = threadIdx.x; base < rv.ng; base += BLK * U) {
     u32x4 w[1][U];
@@ -88,8 +84,8 @@ __global__ __launch_bounds__(BLK) void k_top_rows(TopLossParams p, int64_t row0)
 #pragma unroll
       for (int e = 0; e < E; ++e) cm = fmaxf(cm, x[u][e]);
     }
-    const float at = fmaxf(cm * p.scd, -1e30f);
-    s *= ex2(fmaxf(m * p.scd, -1e30f) - at);
+    const float at = own_ref(cm, p.scd);
+    s *= ex2(own_ref(m, p.scd) - at);
     m = cm;
     float c[U];
 #pragma unroll
@@ -107,7 +103,7 @@ __global__ __launch_bounds__(BLK) void k_top_rows(TopLossParams p, int64_t row0)
   float bm = sh_m[0];
   for (int i = 1; i < BLK / kWave; ++i) bm = fmaxf(bm, sh_m[i]);
   const RowRef ref = row_ref(bm, p.scd);
-  if (ref.deep) {
+  if (ref.steep) {
     s = 0.f;
     for (int gi = threadIdx.x; gi < rv.ng; gi += BLK) {
       float x[E];
@@ -115,10 +111,10 @@ __global__ __launch_bounds__(BLK) void k_top_rows(TopLossParams p, int64_t row0)
       const uint32_t bits = listed_bits<E>(sh_map, gi);
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (!(bits >> e & 1u)) s += ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
+        if (!(bits >> e & 1u)) s += ex2(log2_of(ref, x[e]));
     }
   } else {
-    s *= ex2(fmaxf(m * p.scd, -1e30f) - ref.msc);
+    s *= ex2(own_ref(m, p.scd) - ref.msc);
   }
   s = wave_sum(s);
   if (lane == 0) sh_s[wv] = s;
@@ -174,7 +170,7 @@ __global__ __launch_bounds__(kRowBlock) void k_top_grad(TopLossParams p, int64_t
       float x[E], g[E];
       TI::unpack(to_uint4(w[0][u]), x);
 #pragma unroll
-      for (int e = 0; e < E; ++e) g[e] = s.cR * ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
+      for (int e = 0; e < E; ++e) g[e] = s.cR * ex2(log2_of(ref, x[e]));
       rv.template store<TG>(grad, gi, g);
     }
   }
@@ -186,7 +182,7 @@ __global__ __launch_bounds__(kRowBlock) void k_top_grad(TopLossParams p, int64_t
     if (((id + rv.head) / E / (kRowBlock * U)) % splits != int(blockIdx.y)) continue;
     const float t = load_top(p, l0 + i);
     if (t == kNegInf) continue;
-    const float q = ex2(listed_log2(list, TI::load1(p.zd, e0 + id), p.scd)) * s.ql;
+    const float q = ex2(log2_of(list, TI::load1(p.zd, e0 + id))) * s.ql;
     TG::store1(grad, e0 + id, listed_grad(s, q, listed_p(s, t, p.sct), id));
   }
 }

@@ -5,6 +5,7 @@
 
 #include "aal_device.h"
 #include "aal_resident_common.h"
+#include "aal_row_ref.h"
 #include "aal_rowops.h"
 #include "aal_toplist.h"
 
@@ -16,7 +17,6 @@ namespace {
 constexpr int kTopMax = 512;
 constexpr float kLn2 = 0.693147180559945309417f;
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kDeepScale = 0x1p-64f;
 
 struct TopLossParams {
   const void* zd;
@@ -47,21 +47,6 @@ struct TopLossParams {
 
 __device__ __forceinline__ float load_top(const TopLossParams& p, int64_t i) {
   return p.top_bf16 ? Bf16::load1(p.top, i) : F32::load1(p.top, i);
-}
-
-// The reference of a draft row's sums: 2^(z sc - msc).
-struct RowRef {
-  float m, sc, msc;
-  bool deep;
-};
-__device__ __forceinline__ RowRef row_ref(float m, float sc) {
-  const bool deep = m * sc < -1e30f && m != kNegInf;
-  const float s = deep ? kDeepScale : sc;
-  return {m, s, m == kNegInf ? 0.f : m * s, deep};
-}
-// log2 of q's numerator at a listed entry (exact where a deep row's is huge)
-__device__ __forceinline__ float listed_log2(const RowRef& r, float z, float sc) {
-  return r.deep ? (z - r.m) * sc : __builtin_fmaf(z, r.sc, -r.msc);
 }
 
 // The bitmap of a row's listed ids, one bit per element counted from the row's
@@ -138,13 +123,13 @@ __device__ __forceinline__ ListDraft list_draft(const TopLossParams& p, const fl
     if (sh_t[i] != kNegInf) m = fmaxf(m, sh_z[i]);
   const RowRef ref = row_ref(wave_max(m), p.scd);
   for (int i = lane; i < p.k; i += kWave)
-    if (sh_t[i] != kNegInf) s += ex2(listed_log2(ref, sh_z[i], p.scd));
+    if (sh_t[i] != kNegInf) s += ex2(log2_of(ref, sh_z[i]));
   return {ref, wave_sum(s)};
 }
 // u, su: the unlisted entries' reference and their sum against it.
 __device__ TopRow list_row(const TopLossParams& p, const ListTarget& o, const float* sh_t, const float* sh_z,
                            const int* sh_id, const ListDraft& l, const RowRef& u, float su) {
-  float D = u.deep || l.ref.deep ? (u.m - l.ref.m) * p.scd : u.msc - l.ref.msc;
+  float D = u.steep || l.ref.steep ? (u.m - l.ref.m) * p.scd : u.msc - l.ref.msc;
   if (u.m == kNegInf) D = l.ref.m == kNegInf ? 0.f : kNegInf;
   else if (l.ref.m == kNegInf) D = -kNegInf;
   const Join j = join(D);
@@ -158,7 +143,7 @@ __device__ TopRow list_row(const TopLossParams& p, const ListTarget& o, const fl
   for (int i = threadIdx.x & (kWave - 1); i < p.k; i += kWave) {
     const float t = sh_t[i];
     if (t == kNegInf) continue;
-    const float lt = (t - o.tmax) * p.sct, lz = listed_log2(l.ref, sh_z[i], p.scd);
+    const float lt = (t - o.tmax) * p.sct, lz = log2_of(l.ref, sh_z[i]);
     const float pv = ex2(lt) * o.inv_zt, qv = ex2(lz) * ql;
     v[0] += fminf(pv, qv);
     v[1] += qv < pv ? qv : 0.f;

@@ -14,6 +14,15 @@ inline size_t fused_lds_bytes(int held, int staged, int k) {
   return size_t(stage_words(held)) * 4 + size_t(staged) * 16 + size_t(k) * 20;
 }
 
+template <class TI, int E>
+__device__ __forceinline__ u32x4 packv(const float (&x)[E]) {
+  if constexpr (E == 8)
+    return u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+  else
+    return u32x4{__builtin_bit_cast(uint32_t, x[0]), __builtin_bit_cast(uint32_t, x[1]),
+                 __builtin_bit_cast(uint32_t, x[2]), __builtin_bit_cast(uint32_t, x[3])};
+}
+
 // WK waves hold the row, NV vectors a thread; the last wave does the list, the
 // windows and the coefficients beside their passes, so that neither's registers
 // add to the other's.  Three barriers a row:
@@ -32,8 +41,12 @@ inline size_t fused_lds_bytes(int held, int staged, int k) {
 // 65,536 bf16, WTV, 398 us against 465 with one.  Ragged rows through the buffer resources
 // and LDS too, their ends alone apart: 7,168 rows of 50,001, 331 us against 408 with an address
 // and a condition for every vector, whose registers left one workgroup a CU.
+// With nine vectors and a bf16 gradient, to 80 for 24 waves: one more left 20 (the same with an
+// fp32 gradient, which takes 89 to 94, costs 14,336 rows of 32,000 783 us against 689).
+template <class TG, int WK, int NV>
+constexpr int kMinWaves = NV == 9 && sizeof(typename TG::storage) == 2 ? 6 : WK == 7 ? 4 : 1;
 template <class TI, class TG, bool VEC, int WK, int NV, int NS, bool COUPLED>
-__global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused(TopLossParams p, int grid, void* __restrict__ grad) {
+__global__ __launch_bounds__((WK + 1) * kWave, (kMinWaves<TG, WK, NV>)) void k_top_fused(TopLossParams p, int grid, void* __restrict__ grad) {
   using Rv = RowVecs<TI, VEC>;
   constexpr int E = Rv::E;
   constexpr int BLK = WK * kWave;  // threads that hold the row
@@ -87,8 +100,8 @@ __global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused
       lds_barrier();  // 2
       const float wm = lane < WK ? sh_m[lane] : kNegInf;
       const RowRef ref = row_ref(wave_max(wm), p.scd);
-      if (ref.deep) lds_barrier();
-      const float su = wave_sum(lane < WK ? sh_s[lane] * (ref.deep ? 1.f : ex2(fmaxf(wm * p.scd, -1e30f) - ref.msc)) : 0.f);
+      if (ref.steep) lds_barrier();
+      const float su = wave_sum(lane < WK ? sh_s[lane] * (ref.steep ? 1.f : ex2(own_ref(wm, p.scd) - ref.msc)) : 0.f);
       TopRow o = list_row(p, lt_row, lt, lz, li, ld_row, ref, su);
       if (lane == 0) {
         publish(p.slots + 2 * row, o.a_tv, 1u);
@@ -133,7 +146,7 @@ __global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused
         const int id = li[i];
         done_id[i] = id;
         if (id < 0) continue;
-        const float q = ex2(listed_log2(ld_row.ref, lz[i], p.scd)) * o.ql;
+        const float q = ex2(log2_of(ld_row.ref, lz[i])) * o.ql;
         done_g[i] = listed_grad(o, q, listed_p(o, lt[i], p.sct), id);
         map[(id + head) >> 5] = 0;
       }
@@ -188,7 +201,7 @@ __global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused
     const Rv rv(row, p.R, p.V);
     const int last_v = fresh((rv.ng - 1) / BLK), last_t = fresh((rv.ng - 1) % BLK);
     lds_barrier();  // 1
-    float m = kNegInf, s = 0.f;  // of the unlisted entries; s against max(m sc, -1e30)
+    float m = kNegInf, s = 0.f;  // of the unlisted entries; s against own_ref(m)
     auto fold = [&](const u32x4& wx, int v) {
       float x[E];
       unpackv<TI>(wx, x);
@@ -200,8 +213,8 @@ __global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused
       float cm = m;
 #pragma unroll
       for (int e = 0; e < E; ++e) cm = fmaxf(cm, x[e]);
-      const float at = fmaxf(cm * p.scd, -1e30f);
-      const float keep = ex2(fmaxf(m * p.scd, -1e30f) - at);
+      const float at = own_ref(cm, p.scd);
+      const float keep = ex2(own_ref(m, p.scd) - at);
       m = cm;
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] = ex2(__builtin_fmaf(x[e], p.scd, -at));
@@ -241,7 +254,7 @@ __global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused
     stage_row(rsn);
     {
       const float M = wave_max(m);
-      s = wave_sum(s * ex2(fmaxf(m * p.scd, -1e30f) - fmaxf(M * p.scd, -1e30f)));
+      s = wave_sum(s * ex2(own_ref(m, p.scd) - own_ref(M, p.scd)));
       if (lane == 0) {
         sh_m[wv] = M;
         sh_s[wv] = s;
@@ -251,14 +264,21 @@ __global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused
     lds_barrier();  // 2
     m = wave_max(lane < WK ? sh_m[lane] : kNegInf);
     const RowRef ref = row_ref(m, p.scd);
-    if (ref.deep) {  // nothing was above -1e30: the sum again, at its scale
+    const float msc = ref.steep ? 0.f : ref.msc;
+    if (ref.steep) {
+      // the sum again, from differences to the reference, which take the logits' place: exact in their type
+      // up to half the reference, and far below every exponential beyond
       s = 0.f;
-      auto again = [&](const u32x4& wx, int v) {
+      auto again = [&](u32x4& wx, int v) {
         float x[E];
         unpackv<TI>(wx, x);
         const uint32_t bits = listed_bits<E>(map, v * BLK + tid);
 #pragma unroll
-        for (int e = 0; e < E; ++e) s += bits >> e & 1u ? 0.f : ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
+        for (int e = 0; e < E; ++e) {
+          x[e] -= ref.m;
+          s += bits >> e & 1u ? 0.f : ex2(x[e] * p.scd);
+        }
+        wx = packv<TI>(x);
       };
 #pragma unroll
       for (int v = 0; v < NV; ++v)
@@ -279,7 +299,7 @@ __global__ __launch_bounds__((WK + 1) * kWave, WK == 7 ? 4 : 1) void k_top_fused
       float x[E];
       unpackv<TI>(wx, x);
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = cR * ex2(__builtin_fmaf(x[e], ref.sc, -ref.msc));
+      for (int e = 0; e < E; ++e) x[e] = cR * ex2(__builtin_fmaf(x[e], p.scd, -msc));
       store_g<TG, E>(gr, VEC || !ends || rv.whole(gi) ? uint32_t(gi) * (E * GS) : kDropped, x);
       if constexpr (!VEC)
         if (ends && gi < rv.ng && !rv.whole(gi)) {

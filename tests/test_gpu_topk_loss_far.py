@@ -125,3 +125,42 @@ def test_targets_with_little_or_nearly_all_in_the_remainder(A, weights, flags):
             top = torch.zeros_like(top)  # all alike: the sum of the list is k
             rest = torch.full_like(rest, -gap)
             check(A, zd, top, ids, rest, 3, WEIGHTS[weights], flags)
+
+
+@pytest.mark.parametrize("flags", [0, 1], ids=["default", "streaming"])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("T_d", [1e-28, 1e-30, 1e-33, 1e-36, 1e-37])
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+def test_temperatures_near_zero(A, T_d, sign, dtype, flags):
+    # q is 1 at the row's largest logit, listed or not, and 0 elsewhere (two equal ones: a half each)
+    for V in (90, 1000, 5003):
+        zd, top, ids, rest = make(V, 8, 0.0, dtype, V + 2)
+        zd = sign * (1 + zd.abs() * 8)
+        zd[0, 0, 3] = zd[0, 0].max()
+        listed = ids[1, 1, 2].item()
+        zd[1, 1, listed] = zd[1, 1].max() * (2.0 if sign > 0 else 0.5)
+        for weights in ("wtv", "eal", "tv"):
+            check(A, zd, top, ids, rest, 3, WEIGHTS[weights], flags, T_d=T_d)
+
+
+@pytest.mark.parametrize("flags", [0, 1], ids=["default", "streaming"])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("fill", [-1e8, -2e8, -1e9, -1e10, -3e10, -1e12, -1e20, -1e25, -7e29, -1e31])
+def test_finite_masks_of_every_size(A, fill, dtype, flags):
+    # what fp32 rounds off a product with log2(e) is an exponent of up to 2^-25 of it: hundreds here
+    for V in (300, 1003, 9000, 33001):
+        zd, top, ids, rest = make(V, 8, 0.0, dtype, V + 3, N=4)
+        g = torch.Generator().manual_seed(V)
+        zd = torch.where(torch.rand(zd.shape, generator=g) < 0.9, torch.full_like(zd, fill), zd)
+        # a share of the row left on both sides, so that KL is one that fp64 holds
+        zd.scatter_(2, ids.long(), torch.randn(ids.shape, generator=g).to(dtype))
+        check(A, zd, top, ids, rest, 3, WEIGHTS["all"], flags)
+        # all but the list masked, all of the list masked, whole rows, and rows with two fills
+        zd[0] = fill
+        zd[0].scatter_(1, ids[0].long(), torch.randn(ids[0].shape, generator=g).to(dtype))
+        zd[1].scatter_(1, ids[1].long(), fill)
+        zd[2] = fill
+        zd[3, :, V // 2:] = fill / 3
+        zd[3, :, : V // 2] = fill
+        for weights in ("wtv", "eal", "tv"):
+            check(A, zd, top, ids, rest, 3, WEIGHTS[weights], flags)
