@@ -142,30 +142,32 @@ __global__ __launch_bounds__(BLK, MINW) void k_logits(LogitsParams p) {
       __syncthreads();
       const int first = gp0 * E - rv.head;  // the entry of counter 0
       const int lo = max(first, 0), hi = min(first + n, p.V);  // the entries of this part
-      auto count = [&](int i, int t) {
+      auto count = [&](uint32_t i, int t) {
         if (t < lo || t >= hi) return;
         const int at = t - first;
         if (wide) {
-          if (i < np) atomicOr(&sh_cnt[at], kPrompt32);
+          if (i < uint32_t(np)) atomicOr(&sh_cnt[at], kPrompt32);
           else atomicAdd(&sh_cnt[at], 1u);
         } else if (BWD) {
           atomicOr(&sh_cnt[at >> 5], 1u << (at & 31));
         } else {
           const int sh = (at & 1) * 16;
-          if (i < np) atomicOr(&sh_cnt[at >> 1], kPrompt16 << sh);
+          if (i < uint32_t(np)) atomicOr(&sh_cnt[at >> 1], kPrompt16 << sh);
           else atomicAdd(&sh_cnt[at >> 1], 1u << sh);
         }
       };
-      // four tokens of a thread at once: a wait for memory per 4 BLK tokens
-      int i = threadIdx.x;
-      for (; i + 3 * BLK < nh; i += 4 * BLK) {
+      // four tokens of a thread at once: a wait for memory per 4 BLK tokens (unsigned: the index
+      // of the next ones passes 2^31 in a history of nearly that length)
+      const uint32_t tokens = uint32_t(nh);
+      uint32_t i = threadIdx.x;
+      for (; i + 3 * BLK < tokens; i += 4 * BLK) {
         int t[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) t[q] = p.r.tokens[h0 + i + q * BLK];
 #pragma unroll
         for (int q = 0; q < 4; ++q) count(i + q * BLK, t[q]);
       }
-      for (; i < nh; i += BLK) count(i, p.r.tokens[h0 + i]);
+      for (; i < tokens; i += BLK) count(i, p.r.tokens[h0 + i]);
       if constexpr (BIAS) {
         // of equal ids the last one counts
         if (many) {
