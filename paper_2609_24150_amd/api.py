@@ -529,6 +529,10 @@ def aal_topk_loss_fwd_bwd(z_draft: torch.Tensor, top_logits: torch.Tensor, top_i
         _device_array(rest, "rest", torch.float32, R, dev)
     if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.device != dev):
         raise TypeError("grad_scale must be a float32 device tensor")
+    if grad_scale is not None and grad_scale.numel() == 0:
+        raise ValueError("grad_scale must have an element")
+    if ws is not None and (ws.device != dev or not ws.is_contiguous()):
+        raise ValueError(f"ws must be a contiguous tensor on {dev}")
     code, top_code = _dtype_code(z_draft.dtype), _dtype_code(top_logits.dtype)
     gcode = _dtype_code(grad_dtype or z_draft.dtype) if grad else AAL_F32
     W = B if layout == AAL_LAYOUT_WINDOWS else B * max(0, S - K + 1)
