@@ -339,7 +339,9 @@ hipError_t launch_vec(const LogitsArgs& a) {
   // slices of one size, to a KB
   const int most = slice_entries<BWD>(a.rows, a.V) / TI::kVec, slices = (ng + most - 1) / most;
   p.slice = ((ng + slices - 1) / slices + 63) / 64 * 64;
-  // LDS by the slice, so that as many workgroups of short rows fit a CU as of long ones
+  // LDS by the slice, so that as many workgroups of short rows fit a CU as of long ones: of the forward's
+  // counters in both directions (the backward's bits need less, but its registers, not
+  // LDS, say how many workgroups fit)
   const int entries = p.slice * TI::kVec;
   p.words = (entries / 2 < kLpWords ? entries / 2 : kLpWords);
   const size_t lds = size_t(p.words + (BIAS ? entries / 32 : 0)) * 4;

@@ -32,7 +32,6 @@
 namespace aal {
 namespace {
 
-constexpr int kTopkMax = 512;
 constexpr float kLn2 = 0.693147180559945309417f;
 
 // A whole number that orders as the logits do, -0 as +0: 16 bits for bf16

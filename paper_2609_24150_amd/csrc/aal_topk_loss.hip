@@ -257,10 +257,11 @@ __global__ __launch_bounds__(kLossBlock) void k_top_loss(TopLossParams p, int n,
   const double t1 = p.W > 0 && p.w_eal != 0.f ? -v[1] / double(p.W) : 0.0;
   const double t2 = p.w_kl != 0.f ? v[2] / double(p.R) : 0.0;
   const double t3 = p.W > 0 && p.w_tv != 0.f ? v[3] / (double(p.W) * p.K) : 0.0;
-  // a set error word (a poll of the resident schedule timed out): NaN
-  loss[0] = (err != nullptr && *err != 0u) ? __builtin_nanf("")
-                                           : float(double(p.w_wtv) * t0 + double(p.w_eal) * t1 +
-                                                   double(p.w_kl) * t2 + double(p.w_tv) * t3);
+  const float l = float(double(p.w_wtv) * t0 + double(p.w_eal) * t1 + double(p.w_kl) * t2 + double(p.w_tv) * t3);
+  // a set error word (a poll of the resident schedule timed out): NaN, by its bits, since the build
+  // takes floating-point values for anything else
+  const uint32_t bits = err != nullptr && *err != 0u ? 0x7fc00000u : __builtin_bit_cast(uint32_t, l);
+  loss[0] = __builtin_bit_cast(float, bits);
   if (terms) {
     terms[0] = float(t0);
     terms[1] = float(t1);

@@ -16,7 +16,6 @@ namespace {
 
 constexpr int kTopMax = 512;
 constexpr float kLn2 = 0.693147180559945309417f;
-constexpr float kLog2e = 1.44269504088896340736f;
 
 struct TopLossParams {
   const void* zd;

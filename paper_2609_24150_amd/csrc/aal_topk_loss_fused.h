@@ -378,7 +378,9 @@ hipError_t fused_launch(const TopLossArgs& a, bool* used) {
 // lists of 64: 14,336 rows of 32,000 bf16 386 with 7 x 9 (3 workgroups a CU), 470 with 7 x 18, 510 in the
 // multi-kernel schedule; of 50,000, 626 with 7 x 14, 758 with 7 x 20 (one workgroup a CU then); of
 // 16,032, 213 with 3 x 12, 235 with 3 x 18, 241 with 7 x 9; of 8,000, 123 with 2 x 9, 132 with
-// 1 x 18.  More vectors a thread than the row has cost loads that read nothing.
+// 1 x 18.  More vectors a thread than the row has cost loads that read nothing: rows of 50,176, the
+// most that 7 x 14 holds, 7,168 of them, 310; of 50,257 with 7 x 19 344 (multi-kernel 457).  Rows of
+// 1,000 are no slower in either schedule, 50 and 48.
 template <class TI, class TG, bool VEC, bool COUPLED>
 hipError_t fused_size(const TopLossArgs& a, bool* used) {
   const int ng = a.V / TI::kVec + (VEC ? 0 : 2);  // vectors that cover a row, at most
