@@ -33,7 +33,9 @@
  * Alignment.  Logit and gradient pointers must be 16-byte aligned, the
  *   workspace 256-byte aligned; otherwise AAL_ERR_ALIGN.
  * Inputs.  Logits must be finite or -inf (a vocabulary mask); every row needs
- *   at least one finite entry.  NaN inputs give unspecified results.
+ *   at least one finite entry.  NaN inputs give unspecified results.  Except in
+ *   the calls on top logits, |z| / temperature must stay under 1e8 (a finite mask
+ *   of -1e10 can make sums NaN); those take any finite logits.
  * Errors.  Arguments are validated before anything is enqueued; on a
  *   validation error nothing is written.  A failed kernel launch returns
  *   AAL_ERR_HIP.  aal_last_error() gives a per-thread description of the last

@@ -25,7 +25,7 @@
 //               the row's coefficients.
 //   k_top_grad  one constant times 2^x for every entry, then the listed ones.
 // Bound by memory and, with WTV or EAL terms, by the wait between a row's sums and its
-// coefficients: 14,336 rows of 128,256 bf16, lists of 64, WTV: 1,582 us, 83% of the rate of a
+// coefficients: 14,336 rows of 128,256 bf16, lists of 64, WTV: 1,589 us, 83% of the rate of a
 // lone read and write; KL alone, which waits for nobody, 1,412 us, 93%.
 // Both end with k_top_loss: every window's E, the four terms and the weighted
 // loss, in a fixed order of summation.

@@ -39,7 +39,7 @@ __device__ __forceinline__ u32x4 packv(const float (&x)[E]) {
 // when every holder has waited for its stores.
 // With seven holders the registers are held to what lets two workgroups run on a CU: 7,168 rows of
 // 65,536 bf16, WTV, 398 us against 465 with one.  Ragged rows through the buffer resources
-// and LDS too, their ends alone apart: 7,168 rows of 50,001, 331 us against 408 with an address
+// and LDS too, their ends alone apart: 7,168 rows of 50,001, 334 us against 408 with an address
 // and a condition for every vector, whose registers left one workgroup a CU.
 // With nine vectors and a bf16 gradient, to 80 for 24 waves: one more left 20 (the same with an
 // fp32 gradient, which takes 89 to 94, costs 14,336 rows of 32,000 783 us against 689).
