@@ -667,6 +667,131 @@ aal_status_t aal_logits_process_bwd(const void* grad_out, aal_dtype_t grad_dtype
                                     aal_dtype_t in_dtype, int64_t rows, int32_t V,
                                     const aal_logits_rules_t* rules, void* grad_z, hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * A language-model head in 8-bit floating point: what makes the logits that the calls
+ * above take, and takes the gradients that they give.  OCP formats: e4m3 (largest value 448,
+ * no infinity) and e5m2 (57344).  Scales belong to blocks of AAL_FP8_BLOCK values along the
+ * inner dimension and of 1 or 128 rows, as floats or as e8m0 bytes (2^(byte - 127), 255 NaN). */
+#define AAL_FP8_BLOCK 128
+typedef enum { AAL_FP8_E4M3 = 0, AAL_FP8_E5M2 = 1 } aal_fp8_t;
+typedef enum { AAL_SCALE_F32 = 0, AAL_SCALE_E8M0 = 1 } aal_scale_t;
+
+/*
+ * Quantisation with a power of two for each block:
+ *
+ *   s = 2^e, e the least with max |x| 2^-e <= the format's largest value, in [-126, 126]; 1 for a block of zeros
+ *   q = x / s rounded to nearest even
+ *
+ * x : [rows, cols] of in_dtype, row stride ld_x elements (any alignment of its type).  Values that are not
+ *     finite bear on no scale; they become NaN in e4m3 and keep their infinity in e5m2.
+ * block_rows : 1 (a scale for each row's 128 columns) or 128 (one for 128 x 128).
+ * q : [rows, cols] of format, row stride ld_q bytes, with scale [ceil(cols / 128)][ceil(rows / block_rows)]
+ *     of scale_type (the rows' scales of a block of columns one after the other); or both NULL.
+ * qt : the same of x transposed, in one pass over x: [cols, rows], row stride ld_qt bytes, with
+ *     scale_t [ceil(rows / 128)][ceil(cols / block_rows)], its blocks along x's rows; or both NULL.
+ * q and qt 16-byte aligned, ld_q and ld_qt multiples of 16 (bytes behind a row's values are left as
+ * they are).  1 <= rows < 2^31, 1 <= cols <= 2^30.  Outputs must not overlap x.
+ */
+aal_status_t aal_fp8_quantize(const void* x, aal_dtype_t in_dtype, int64_t rows, int64_t cols, int64_t ld_x,
+                              aal_fp8_t format, aal_scale_t scale_type, int32_t block_rows, void* q, int64_t ld_q,
+                              void* scale, void* qt, int64_t ld_qt, void* scale_t, hipStream_t stream);
+
+/* One operand of a product: [rows, K] 8-bit values, K along the row.
+ *   values       16-byte aligned; ld bytes from row to row, a multiple of 16, at least K (what lies
+ *                behind a row's K values bears on nothing)
+ *   scale        of scale_type; row block r's scale of column block j is scale[r * scale_row + j * scale_block]
+ *   block_rows   1 or 128 */
+typedef struct {
+  const void* values;
+  const void* scale;
+  int64_t ld;
+  int64_t scale_row;
+  int64_t scale_block;
+  int32_t format;     /* aal_fp8_t   */
+  int32_t scale_type; /* aal_scale_t */
+  int32_t block_rows;
+} aal_fp8_operand_t;
+
+/* Workspace bytes of aal_fp8_matmul for these sizes (0 for invalid ones, or where it needs none). */
+size_t aal_fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
+/*
+ * c[m, n] = sum_j sa[m, j] sb[n, j] sum_{k in block j} a[m, k] b[n, k],   blocks of 128 of K
+ *
+ * in fp32, rounded once to c_dtype.  a : M rows, b : N rows, in host memory (read before the call
+ * returns); both scales of one type, formats as they are.  c : [M, N] contiguous, 16-byte aligned, no overlap
+ * with an operand.  1 <= M, N, K < 2^31.
+ * workspace : at least aal_fp8_matmul_workspace_bytes(M, N, K) bytes, 256-byte aligned (NULL where that is 0).
+ */
+aal_status_t aal_fp8_matmul(const aal_fp8_operand_t* a, const aal_fp8_operand_t* b, int64_t M, int64_t N, int64_t K,
+                            void* c, aal_dtype_t c_dtype, void* workspace, size_t workspace_bytes,
+                            hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Beam search over logits. */
+#define AAL_BEAM_MAX 64         /* most beams of a request */
+#define AAL_BEAM_SELECT_MAX 128 /* most chosen of them     */
+
+/* Outputs of aal_beam_select, [B, n] device arrays each; any but parents and tokens may be NULL. */
+typedef struct {
+  float* scores;     /* total of the chosen candidate                              */
+  float* rank;       /* total / length^length_penalty, what they are ordered by    */
+  int32_t* parents;  /* beam that it goes on from, -1 where there is no candidate  */
+  int32_t* tokens;
+  uint8_t* finished; /* 1: the parent had ended, the token is eos, or no candidate */
+  int32_t* lengths;  /* the parent's, and 1 more unless it had ended               */
+} aal_beam_out_t;
+
+/* Workspace bytes of aal_beam_select (0 for invalid sizes). */
+size_t aal_beam_select_workspace_bytes(aal_dtype_t in_dtype, int64_t B, int32_t W, int32_t V, int32_t n);
+
+/*
+ * The n best continuations of B requests with W beams each:
+ *
+ *   total[w, v] = scores[w] + z[w, v] / T - lse_w,   lse_w = ln sum_v exp(z[w, v] / T)
+ *   rank[w, v]  = total[w, v] / (lengths[w] + 1)^length_penalty
+ *   a beam that has ended stands for itself alone: token pad, total scores[w], rank total / lengths[w]^length_penalty
+ *   order       : larger rank first; among equal ones the lower beam, the larger logit, the lower token
+ *
+ * Totals and ranks are formed in 64 bits, the exponentials of all but each part's n largest logits in 32.
+ * Candidates of total -inf (a masked token, a beam of score -inf) are never chosen; where
+ * candidates run out, scores and rank are -inf, parents -1, tokens pad, finished 1, lengths 0.
+ * z : [B, W, V] of in_dtype, 16-byte aligned, finite or -inf (a beam's whole row may be -inf).  Rows of
+ *     beams that have ended, or whose score is -inf, are not read.
+ * scores : [B, W] finite or -inf.  finished : [B, W] bytes, nonzero for a beam that has ended, or NULL.
+ * lengths : [B, W], at least 0 (1 for a beam that has ended), or NULL, which counts as 0 and asks for a
+ *     length_penalty of 0.  temperature finite, > 0 and >= 1e-37; length_penalty finite.
+ * 1 <= W <= AAL_BEAM_MAX, 1 <= n <= min(AAL_BEAM_SELECT_MAX, W * V), B * W < 2^31, 1 <= V <= 2^18.
+ * out : host memory, read before the call returns.  eos: a token, or -1 for none.
+ * workspace : aal_beam_select_workspace_bytes(...) bytes, 256-byte aligned.
+ */
+aal_status_t aal_beam_select(const void* z, aal_dtype_t in_dtype, int64_t B, int32_t W, int32_t V, int32_t n,
+                             float temperature, const float* scores, const uint8_t* finished, const int32_t* lengths,
+                             float length_penalty, int32_t eos, int32_t pad, const aal_beam_out_t* out,
+                             void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* One array that is kept for each beam: B requests x W (out: n) beams x segments x segment_bytes,
+ * all strides in bytes.  dst NULL: in place. */
+typedef struct {
+  const void* src;
+  void* dst;
+  int64_t src_request, src_beam, src_segment;
+  int64_t dst_request, dst_beam, dst_segment;
+  int64_t segments, segment_bytes;
+} aal_beam_state_t;
+
+/*
+ * dst[b, j] = src[b, parents[b, j]] for every state, j < n: caches, histories and other
+ * states after a selection.  In place, src[b, j] becomes what src[b, parents[b, j]] was before the call, and
+ * beams that keep their slot move no byte.  A parent outside [0, W) leaves its slot as it was.
+ * states : host memory [n_states], read before the call returns; 0 <= n_states.  parents : device [B, n].
+ * In place asks for n = W <= AAL_BEAM_MAX (src is written); otherwise 1 <= n <= AAL_BEAM_SELECT_MAX, and a
+ * dst overlaps no src.  The slots of a state must not overlap each other.  Any alignment; states whose addresses,
+ * strides and sizes are multiples of 16 (or 4) bytes move in such pieces.
+ */
+aal_status_t aal_beam_reorder(const aal_beam_state_t* states, int32_t n_states, int64_t B, int32_t W, int32_t n,
+                              const int32_t* parents, hipStream_t stream);
+
 /*
  * Measurement aid, not part of the method: streams 1 to 3 device buffers of
  * `bytes` bytes each (src0, then src1 and src2 when non-NULL) with 16-byte

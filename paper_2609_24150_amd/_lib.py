@@ -30,6 +30,13 @@ VP_PART_BYTES = 32
 VP_ACC_BYTES = 8
 VP_ROW_BYTES = 32
 AAL_TOPK_MAX = 512
+AAL_FP8_BLOCK = 128
+AAL_FP8_E4M3 = 0
+AAL_FP8_E5M2 = 1
+AAL_SCALE_F32 = 0
+AAL_SCALE_E8M0 = 1
+AAL_BEAM_MAX = 64
+AAL_BEAM_SELECT_MAX = 128
 
 
 class LossWeights(C.Structure):
@@ -50,6 +57,25 @@ class GrpoParams(C.Structure):
     """aal_grpo_params_t (passed by value)."""
     _fields_ = [("eps", C.c_float), ("adv_clip", C.c_float), ("eps_clip", C.c_float),
                 ("rho_min", C.c_float), ("rho_max", C.c_float)]
+
+
+class Fp8Operand(C.Structure):
+    """aal_fp8_operand_t (passed by address)."""
+    _fields_ = [("values", C.c_void_p), ("scale", C.c_void_p), ("ld", C.c_int64), ("scale_row", C.c_int64),
+                ("scale_block", C.c_int64), ("format", C.c_int32), ("scale_type", C.c_int32), ("block_rows", C.c_int32)]
+
+
+class BeamOut(C.Structure):
+    """aal_beam_out_t (passed by address)."""
+    _fields_ = [("scores", C.c_void_p), ("rank", C.c_void_p), ("parents", C.c_void_p), ("tokens", C.c_void_p),
+                ("finished", C.c_void_p), ("lengths", C.c_void_p)]
+
+
+class BeamState(C.Structure):
+    """aal_beam_state_t (an array of them passed by address)."""
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("src_request", C.c_int64), ("src_beam", C.c_int64),
+                ("src_segment", C.c_int64), ("dst_request", C.c_int64), ("dst_beam", C.c_int64),
+                ("dst_segment", C.c_int64), ("segments", C.c_int64), ("segment_bytes", C.c_int64)]
 
 
 _vp = C.c_void_p
@@ -124,6 +150,19 @@ _SIGNATURES = {
         _vp, C.c_int, C.c_int64, C.c_int32, C.POINTER(LogitsRules), _vp, _vp]),
     "aal_logits_process_bwd": (C.c_int, [
         _vp, C.c_int, _vp, C.c_int, C.c_int64, C.c_int32, C.POINTER(LogitsRules), _vp, _vp]),
+    "aal_fp8_quantize": (C.c_int, [
+        _vp, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_int32, _vp, C.c_int64, _vp,
+        _vp, C.c_int64, _vp, _vp]),
+    "aal_fp8_matmul_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
+    "aal_fp8_matmul": (C.c_int, [
+        C.POINTER(Fp8Operand), C.POINTER(Fp8Operand), C.c_int64, C.c_int64, C.c_int64, _vp, C.c_int, _vp, C.c_size_t,
+        _vp]),
+    "aal_beam_select_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_int32]),
+    "aal_beam_select": (C.c_int, [
+        _vp, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, _vp, _vp, _vp, C.c_float, C.c_int32,
+        C.c_int32, C.POINTER(BeamOut), _vp, C.c_size_t, _vp]),
+    "aal_beam_reorder": (C.c_int, [
+        C.POINTER(BeamState), C.c_int32, C.c_int64, C.c_int32, C.c_int32, _vp, _vp]),
     "aal_stream_probe": (C.c_int, [_vp, _vp, _vp, _vp, C.c_size_t, _vp, _vp]),
     "aal_vp_grad": (C.c_int, [
         _vp, _vp, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_int, C.c_float, C.c_float, _vp, _vp, C.c_int,

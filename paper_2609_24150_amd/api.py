@@ -13,10 +13,12 @@ import torch
 from . import _lib
 from ._lib import (  # noqa: F401
     AAL_BF16, AAL_F32, AAL_FLAG_COOPERATIVE, AAL_FLAG_STREAMING, AAL_LAYOUT_SEQUENCES, AAL_LAYOUT_WINDOWS,
-    AAL_TOPK_MAX, AAL_VP_EAL, AAL_VP_WTV,
+    AAL_BEAM_MAX, AAL_BEAM_SELECT_MAX, AAL_FP8_BLOCK, AAL_TOPK_MAX, AAL_VP_EAL, AAL_VP_WTV,
 )
 
 _DT = {torch.bfloat16: AAL_BF16, torch.float32: AAL_F32}
+_FP8 = {torch.float8_e4m3fn: _lib.AAL_FP8_E4M3, torch.float8_e5m2: _lib.AAL_FP8_E5M2}
+_SCALE = {torch.float32: _lib.AAL_SCALE_F32, torch.float8_e8m0fnu: _lib.AAL_SCALE_E8M0}
 
 
 def _dtype_code(t: torch.dtype) -> int:
@@ -676,6 +678,315 @@ def aal_logits_process_bwd(grad_out: torch.Tensor, z: torch.Tensor, *, tokens: t
                                                _ptr(grad_z), _raw_stream(dev, stream))
     _lib.check(st, "aal_logits_process_bwd")
     return grad_z
+
+
+# ----------------------------------------------------------------------------
+# A language-model head in 8-bit floating point.
+
+def _code(table: dict, t: torch.dtype, name: str) -> int:
+    if t not in table:
+        raise TypeError(f"unsupported {name} {t}; use one of {', '.join(str(k) for k in table)}")
+    return table[t]
+
+
+def _pitch(n: int) -> int:
+    return (n + 15) // 16 * 16
+
+
+def aal_fp8_quantize(x: torch.Tensor, *, block_rows: int = 1, rows: bool = True, columns: bool = False,
+                     dtype: torch.dtype = torch.float8_e4m3fn, scale_dtype: torch.dtype = torch.float32,
+                     stream=None) -> dict:
+    """x [R, C] in 8-bit floating point, over a power of two for each block of
+    block_rows x 128 (block_rows 1 or 128): the least that brings the block's
+    largest finite value into the format's range, 1 for a block of zeros.
+
+    x: bf16 or fp32, its columns contiguous, its rows at any distance.  dtype: float8_e4m3fn or float8_e5m2;
+    scale_dtype: float32 or float8_e8m0fnu.  rows: quantise x, its blocks along the columns; columns:
+    quantise x transposed, its blocks along x's rows (both in one pass over x).
+
+    Returns a dict: q [R, C] and scale [ceil(R / block_rows), ceil(C / 128)], qt [C, R] and
+    scale_t [ceil(C / block_rows), ceil(R / 128)] (None where not asked for).  q and qt are views
+    whose rows start at multiples of 16 bytes, as aal_fp8_matmul takes them."""
+    if x.dim() != 2 or x.numel() == 0:
+        raise ValueError("x must be [R, C] with at least one entry")
+    R, Cn = x.shape
+    if not x.is_cuda or (Cn > 1 and x.stride(1) != 1) or (R > 1 and x.stride(0) < Cn):
+        raise ValueError("x must be a device tensor of contiguous rows")
+    if not (rows or columns):
+        raise ValueError("rows or columns must be asked for")
+    if block_rows not in (1, AAL_FP8_BLOCK):
+        raise ValueError(f"block_rows must be 1 or {AAL_FP8_BLOCK}")
+    code, fmt, st = _dtype_code(x.dtype), _code(_FP8, dtype, "dtype"), _code(_SCALE, scale_dtype, "scale_dtype")
+    dev = x.device
+    out = {"q": None, "scale": None, "qt": None, "scale_t": None}
+    with _guard(dev, stream):
+        for want, q, s, n, m in ((rows, "q", "scale", R, Cn), (columns, "qt", "scale_t", Cn, R)):
+            if want:
+                out[q] = torch.empty(n, _pitch(m), dtype=dtype, device=dev)
+                out[s] = torch.empty((m + AAL_FP8_BLOCK - 1) // AAL_FP8_BLOCK, (n + block_rows - 1) // block_rows,
+                                     dtype=scale_dtype, device=dev)
+        st = _lib.lib().aal_fp8_quantize(_ptr(x), code, R, Cn, x.stride(0) if R > 1 else Cn, fmt, st, int(block_rows),
+                                         _ptr(out["q"]), _pitch(Cn), _ptr(out["scale"]), _ptr(out["qt"]), _pitch(R),
+                                         _ptr(out["scale_t"]), _raw_stream(dev, stream))
+    _lib.check(st, "aal_fp8_quantize")
+    if rows:
+        out["q"], out["scale"] = out["q"][:, :Cn], out["scale"].t()
+    if columns:
+        out["qt"], out["scale_t"] = out["qt"][:, :R], out["scale_t"].t()
+    return out
+
+
+def _fp8_operand(v: torch.Tensor, s: torch.Tensor, name: str, dev) -> _lib.Fp8Operand:
+    if v.dim() != 2 or v.numel() == 0 or s.dim() != 2:
+        raise ValueError(f"{name} must be [rows, K] with a 2-d scale")
+    R, K = v.shape
+    if not v.is_cuda or v.device != dev or s.device != dev:
+        raise ValueError(f"{name} and its scale must be on one device with the others")
+    ld = v.stride(0) if R > 1 else _pitch(K)
+    if (K > 1 and v.stride(1) != 1) or ld < K or ld % 16 or v.data_ptr() % 16:
+        raise ValueError(f"{name}: values must be contiguous in a row, rows at multiples of 16 bytes")
+    if v.untyped_storage().nbytes() - v.storage_offset() < R * ld:
+        raise ValueError(f"{name}: the last row's memory must reach to its full stride")
+    blocks = (K + AAL_FP8_BLOCK - 1) // AAL_FP8_BLOCK
+    square = (R + AAL_FP8_BLOCK - 1) // AAL_FP8_BLOCK
+    if s.shape[1] != blocks or s.shape[0] not in (R, square):
+        raise ValueError(f"{name}: its scale must be [{R} or {square}, {blocks}]; got {tuple(s.shape)}")
+    return _lib.Fp8Operand(v.data_ptr(), s.data_ptr(), ld, s.stride(0), s.stride(1), _code(_FP8, v.dtype, "dtype"),
+                           _code(_SCALE, s.dtype, "scale dtype"), 1 if s.shape[0] == R else AAL_FP8_BLOCK)
+
+
+def aal_fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, *,
+                   out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
+                   ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """a [M, K] times the transpose of b [N, K], 8-bit values with a scale for
+    each block of 128 along K and of 1 or 128 rows (which of them, the scale's
+    shape tells): a_scale [M or ceil(M / 128), ceil(K / 128)], b_scale alike, both
+    float32 or both float8_e8m0fnu, any strides.  Values: float8_e4m3fn or float8_e5m2, rows at multiples
+    of 16 bytes (as aal_fp8_quantize makes them).  Sums are fp32, rounded once to out_dtype (bf16
+    or fp32).
+
+    Returns out, [M, N]."""
+    dev = a.device
+    oa, ob = _fp8_operand(a, a_scale, "a", dev), _fp8_operand(b, b_scale, "b", dev)
+    (M, K), N = a.shape, b.shape[0]
+    if b.shape[1] != K:
+        raise ValueError(f"a and b must agree in K; got {K} and {b.shape[1]}")
+    if oa.scale_type != ob.scale_type:
+        raise TypeError("a_scale and b_scale must be of one dtype")
+    if out is not None:
+        if out.shape != (M, N):
+            raise ValueError(f"out must be [{M}, {N}]")
+        _device_array(out, "out", out.dtype, M * N, dev)
+        out_dtype = out.dtype
+    code = _dtype_code(out_dtype)
+    need = aal_fp8_matmul_workspace_bytes(M, N, K)
+    if ws is not None and (ws.device != dev or not ws.is_contiguous()):
+        raise ValueError(f"ws must be a contiguous tensor on {dev}")
+    with _guard(dev, stream):
+        if out is None:
+            out = torch.empty(M, N, dtype=out_dtype, device=dev)
+        if ws is None and need:
+            ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        st = _lib.lib().aal_fp8_matmul(C.byref(oa), C.byref(ob), M, N, K, _ptr(out), code, _ptr(ws),
+                                       0 if ws is None else ws.numel() * ws.element_size(), _raw_stream(dev, stream))
+    _lib.check(st, "aal_fp8_matmul")
+    return out
+
+
+def aal_fp8_matmul_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(_lib.lib().aal_fp8_matmul_workspace_bytes(int(M), int(N), int(K)))
+
+
+def _check_head(head: dict, *names: str):
+    for name in names:
+        if head.get(name) is None:
+            raise ValueError(f"head must hold {name}: aal_fp8_quantize(W, block_rows=128, columns=True)")
+
+
+def aal_head_logits(x: torch.Tensor, head: dict, *, out_dtype: torch.dtype | None = None, stream=None) -> torch.Tensor:
+    """Logits of hidden states x [..., D] (bf16 or fp32) through a head whose
+    weights [V, D] are held in 8 bits: head["q"] and head["scale"], as from
+    aal_fp8_quantize(W, block_rows=128, columns=True).  x is quantised here, in
+    blocks of 1 x 128, to e4m3 with scales of the head's type.
+
+    Returns [..., V] of out_dtype (x's dtype if None)."""
+    _check_head(head, "q", "scale")
+    D = x.shape[-1] if x.dim() else 0
+    if x.dim() < 1 or x.numel() == 0 or head["q"].shape[-1] != D:
+        raise ValueError(f"x must be [..., {head['q'].shape[-1]}] with at least one row")
+    flat = x.reshape(-1, D)
+    r = aal_fp8_quantize(flat, scale_dtype=head["scale"].dtype, stream=stream)
+    z = aal_fp8_matmul(r["q"], r["scale"], head["q"], head["scale"], out_dtype=out_dtype or x.dtype, stream=stream)
+    return z.view(*x.shape[:-1], z.shape[1])
+
+
+def aal_head_logits_bwd(grad: torch.Tensor, x: torch.Tensor, head: dict, *, x_grad: bool = True,
+                        weight_grad: bool = True, weight_dtype: torch.dtype = torch.float32, stream=None) -> dict:
+    """The gradients through aal_head_logits, from grad [..., V] (with respect
+    to the logits) and its x [..., D]: both products in 8 bits as well, grad and
+    x quantised to e4m3 in blocks of 128 along the dimension that is summed over
+    (x's gradient: V, against head["qt"] and head["scale_t"]; the weights': the rows).
+
+    Returns a dict: grad_x [..., D] of x's dtype and grad_w [V, D] of
+    weight_dtype (None where not asked for)."""
+    if not (x_grad or weight_grad):
+        raise ValueError("x_grad or weight_grad must be asked for")
+    if x_grad:
+        _check_head(head, "qt", "scale_t")
+    if x.dim() < 1 or x.numel() == 0 or grad.dim() < 1 or grad.shape[:-1] != x.shape[:-1] or grad.numel() == 0:
+        raise ValueError("grad must be [..., V] and x [..., D] of the same rows, one at least")
+    D, V = x.shape[-1], grad.shape[-1]
+    if x_grad and tuple(head["qt"].shape) != (D, V):
+        raise ValueError(f"grad and x do not fit a head of {tuple(head['qt'].shape)[::-1]}")
+    scale = (head["scale_t"] if x_grad else head["scale"]).dtype
+    g = aal_fp8_quantize(grad.reshape(-1, V), rows=x_grad, columns=weight_grad, scale_dtype=scale, stream=stream)
+    out = {"grad_x": None, "grad_w": None}
+    if x_grad:
+        out["grad_x"] = aal_fp8_matmul(g["q"], g["scale"], head["qt"], head["scale_t"], out_dtype=x.dtype,
+                                       stream=stream).view(x.shape)
+    if weight_grad:
+        xt = aal_fp8_quantize(x.reshape(-1, D), rows=False, columns=True, scale_dtype=scale, stream=stream)
+        out["grad_w"] = aal_fp8_matmul(g["qt"], g["scale_t"], xt["qt"], xt["scale_t"], out_dtype=weight_dtype,
+                                       stream=stream)
+    return out
+
+
+# ----------------------------------------------------------------------------
+# Beam search.
+
+def aal_beam_select_workspace_bytes(dtype: torch.dtype, B: int, W: int, V: int, n: int) -> int:
+    return int(_lib.lib().aal_beam_select_workspace_bytes(_dtype_code(dtype), int(B), int(W), int(V), int(n)))
+
+
+def aal_beam_select(z: torch.Tensor, scores: torch.Tensor, n: int, *, temperature: float = 1.0,
+                    finished: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                    length_penalty: float = 0.0, eos: int = -1, pad: int = 0, ws: torch.Tensor | None = None,
+                    stream=None) -> dict:
+    """The n best continuations of each request's beams, over all its beams and
+    the vocabulary.
+
+    z [B, W, V]: logits (bf16 or fp32).  scores [B, W] float32: the beams' cumulative
+    log-probabilities, -inf for one that is not to go on.  finished [B, W] bool: beams that have
+    ended, each of which stands for itself with token pad and its own score.  lengths [B, W] int32: tokens so
+    far.  Candidates are ordered by (score + log softmax(z / temperature)) / (lengths + 1) **
+    length_penalty; among equal ones the lower beam, the larger logit, the lower token come first.
+
+    Returns a dict of [B, n]: scores and rank float32, parents and tokens int32, finished bool, lengths
+    int32.  Where a request has fewer candidates: -inf, -inf, -1, pad, True, 0."""
+    if z.dim() != 3 or z.numel() == 0 or not z.is_cuda or not z.is_contiguous():
+        raise ValueError("z must be a contiguous [B, W, V] device tensor with at least one entry")
+    B, W, V = z.shape
+    code, dev = _dtype_code(z.dtype), z.device
+    if W > AAL_BEAM_MAX:
+        raise ValueError(f"at most {AAL_BEAM_MAX} beams; got {W}")
+    if not 1 <= n <= min(AAL_BEAM_SELECT_MAX, W * V):
+        raise ValueError(f"n must be in [1, min({AAL_BEAM_SELECT_MAX}, W * V)]; got {n}")
+    for t, name, dtype in ((scores, "scores", torch.float32), (finished, "finished", torch.bool),
+                           (lengths, "lengths", torch.int32)):
+        if t is not None:
+            if t.shape != (B, W):
+                raise ValueError(f"{name} must be [{B}, {W}]")
+            _device_array(t, name, dtype, B * W, dev)
+    if ws is not None and (ws.device != dev or not ws.is_contiguous()):
+        raise ValueError(f"ws must be a contiguous tensor on {dev}")
+    with _guard(dev, stream):
+        # the outputs are pieces of one allocation
+        words = torch.empty(5 * B * n, dtype=torch.int32, device=dev).split(B * n)
+        out = {"scores": words[0].view(torch.float32).view(B, n), "rank": words[1].view(torch.float32).view(B, n),
+               "parents": words[2].view(B, n), "tokens": words[3].view(B, n),
+               "finished": torch.empty(B, n, dtype=torch.bool, device=dev), "lengths": words[4].view(B, n)}
+        if ws is None:
+            ws = torch.empty(aal_beam_select_workspace_bytes(z.dtype, B, W, V, n), dtype=torch.uint8, device=dev)
+        o = _lib.BeamOut(*(_ptr(out[k]) for k in ("scores", "rank", "parents", "tokens", "finished", "lengths")))
+        st = _lib.lib().aal_beam_select(
+            _ptr(z), code, B, W, V, int(n), float(temperature), _ptr(scores), _ptr(finished), _ptr(lengths),
+            float(length_penalty), int(eos), int(pad), C.byref(o), _ptr(ws), ws.numel() * ws.element_size(),
+            _raw_stream(dev, stream))
+    _lib.check(st, "aal_beam_select")
+    return out
+
+
+def _segments(t: torch.Tensor):
+    """t's memory behind its first two dimensions: (segments, elements of one, elements from one to the next)."""
+    size, step = 1, 1  # of the contiguous end
+    dims = [(n, s) for n, s in zip(t.shape[2:], t.stride()[2:]) if n != 1]
+    while dims and dims[-1][1] == size:
+        size *= dims.pop()[0]
+    count, step = 1, 0
+    for n, s in reversed(dims):
+        if count == 1:
+            count, step = n, s
+        elif s == step * count:
+            count *= n
+        else:
+            return None
+    return count, size, step
+
+
+def _apart(t: torch.Tensor) -> bool:
+    """Whether no two of t's entries share memory (dimensions nested by their strides)."""
+    end = 1
+    for step, n in sorted((s, n) for n, s in zip(t.shape, t.stride()) if n > 1):
+        if step < end:
+            return False
+        end += step * (n - 1)
+    return True
+
+
+def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) -> list:
+    """Each state's beams after a selection: state[b, j] becomes what
+    state[b, parents[b, j]] was, for tensors [B, W, ...] of any dtype (caches,
+    token histories, last states), all in one call.
+
+    parents: [B, n] int32, as from aal_beam_select; a parent outside [0, W) leaves its slot as it
+    was.  out: None, for in place (n = W; beams that keep their slot move nothing), or tensors
+    [B, n, ...] that overlap no state.  Behind its first two dimensions a state may be any view that is
+    contiguous pieces at one distance (state[:, :, :, t0:t1] of a [B, W, heads, length, dim] cache).
+
+    Returns out, or the states."""
+    states = list(states)
+    outs = states if out is None else list(out)
+    if parents.dim() != 2 or parents.numel() == 0:
+        raise ValueError("parents must be [B, n]")
+    B, n = parents.shape
+    dev = parents.device
+    if not parents.is_cuda:
+        raise ValueError("parents must be a device tensor")
+    _device_array(parents, "parents", torch.int32, B * n, dev)
+    if len(outs) != len(states):
+        raise ValueError("out must have a tensor for each state")
+    if not states:
+        return outs
+    W = states[0].shape[1] if states[0].dim() >= 2 else 0
+    if not 1 <= n <= AAL_BEAM_SELECT_MAX or (out is None and (n != W or n > AAL_BEAM_MAX)):
+        raise ValueError(f"n must be in [1, {AAL_BEAM_SELECT_MAX}], in place W and at most {AAL_BEAM_MAX}; got {n}")
+    table = (_lib.BeamState * len(states))()
+    for i, (s, o) in enumerate(zip(states, outs)):
+        if s.dim() < 2 or s.shape[:2] != (B, W) or s.device != dev:
+            raise ValueError(f"states must be [{B}, {W}, ...] on {dev}; got {tuple(s.shape)} on {s.device}")
+        cut = _segments(s)
+        if cut is None:
+            raise ValueError("a state must be contiguous pieces at one distance behind its first two dimensions")
+        e = s.element_size()
+        count, size, step = cut
+        row = table[i]
+        row.src, row.dst = s.data_ptr(), None
+        row.src_request, row.src_beam, row.src_segment = s.stride(0) * e, s.stride(1) * e, step * e
+        row.segments, row.segment_bytes = count, size * e
+        if not _apart(o):
+            raise ValueError("the entries of what is written must not share memory")
+        if out is not None:
+            if o.shape != (B, n, *s.shape[2:]) or o.dtype != s.dtype or o.device != dev:
+                raise ValueError(f"out must be [{B}, {n}, ...] of the states' shapes and dtypes on {dev}")
+            to = _segments(o)
+            if to is None or to[:2] != (count, size):
+                raise ValueError("an output must be the same contiguous pieces as its state")
+            row.dst = o.data_ptr()
+            row.dst_request, row.dst_beam, row.dst_segment = o.stride(0) * e, o.stride(1) * e, to[2] * e
+    with _guard(dev, stream):
+        st = _lib.lib().aal_beam_reorder(table, len(states), B, W, n, _ptr(parents), _raw_stream(dev, stream))
+    _lib.check(st, "aal_beam_reorder")
+    return outs
 
 
 def aal_stream_probe(srcs, dst: torch.Tensor | None = None, flag: torch.Tensor | None = None, stream=None):

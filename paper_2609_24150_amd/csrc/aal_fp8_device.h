@@ -1,0 +1,98 @@
+// Device-side pieces of the 8-bit operators.
+#pragma once
+
+#include "aal_device.h"
+#include "aal_fp8.h"
+
+namespace aal {
+namespace {
+
+typedef u32x4 u32x4_e2 __attribute__((aligned(2)));  // a vector at any element
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// 2^e, e in [-126, 127].
+__device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, uint32_t(e + 127) << 23); }
+
+// The exponent of a block's scale: the least e with amax 2^-e <= the format's largest value,
+// 1.75 2^8 or 1.75 2^15; amax as its bits.
+template <Fp8 F>
+__device__ __forceinline__ int scale_exponent(uint32_t amax) {
+  if (amax == 0u) return 0;
+  const int e = int(amax >> 23) - 127 - (F == Fp8::kE4M3 ? 8 : 15) + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return max(e, -126);
+}
+
+// |x| as bits, 0 where x is not finite.
+__device__ __forceinline__ uint32_t finite_bits(float x) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
+  return b < 0x7f800000u ? b : 0u;
+}
+
+// Four values to 8 bits each, to nearest even.
+template <Fp8 F>
+__device__ __forceinline__ uint32_t pack_fp8(float a, float b, float c, float d) {
+  int w = 0;
+  if constexpr (F == Fp8::kE4M3) {
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, w, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+  } else {
+    w = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, w, false);
+    w = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, w, true);
+  }
+  return uint32_t(w);
+}
+
+// A scale of either type as a float.
+template <Scale S>
+__device__ __forceinline__ float load_scale(const void* s, int64_t i) {
+  if constexpr (S == Scale::kF32) {
+    return static_cast<const float*>(s)[i];
+  } else {
+    const uint32_t b = static_cast<const uint8_t*>(s)[i];
+    return __builtin_bit_cast(float, b == 0u ? 0x400000u : b == 255u ? 0x7fc00000u : b << 23);
+  }
+}
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// Eight 8-bit values (two words) in bf16, which holds them all: four more significant bits, more exponents.
+template <int F>
+__device__ __forceinline__ bf16x8 widen(int lo, int hi) {
+  typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+  u4 w;
+  if constexpr (F == 0) {
+    w.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false));
+    w.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true));
+    w.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false));
+    w.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true));
+  } else {
+    w.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, 1.f, false));
+    w.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, 1.f, true));
+    w.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, 1.f, false));
+    w.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, 1.f, true));
+  }
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+// t += x y over 64 values of the inner dimension, 32 x 32 results, 32 bytes of a row per lane.
+//
+// The matrix unit aligns the products of eight neighbouring 8-bit values to the largest of them and
+// cuts what lies 2^-13 below its power of two (measured; sums of the eights are fp32): 1.5e-5 of a sum of
+// random values, root mean square.  A result that is rounded to bf16 (1.7e-3) does not feel that, one in fp32
+// would: WIDE goes through bf16, whose products and sums are exact to fp32 (7e-9), at half the rate.
+template <bool WIDE, int FX, int FY>
+__device__ __forceinline__ f32x16 dot64(const i32x8& x, const i32x8& y, f32x16 t) {
+  if constexpr (!WIDE) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, t, FX, FY, 0, 127, 0, 127);
+  } else {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen<FX>(x[2 * s], x[2 * s + 1]), widen<FY>(y[2 * s], y[2 * s + 1]), t, 0,
+                                                  0, 0);
+    return t;
+  }
+}
+
+}  // namespace
+}  // namespace aal

@@ -1,0 +1,244 @@
+// Quantisation to 8-bit floating point with a power of two for each block of
+// 128 (aal_fp8_quantize):
+//
+//   s = 2^e, e the least with max |x| 2^-e <= the format's largest value;  q = x / s to nearest even
+//
+// The division is exact, so q is rounded once.  A power of two costs a floating format no digit
+// (values near a block's largest keep all of theirs) and is what the matrix instructions apply
+// by themselves.
+//
+// Bound by memory: k_quant_rows, for blocks of 1 x 128 in the order of x, takes a block per 16 lanes, whose
+// largest value is found by four lane exchanges; k_quant_tile takes tiles of 128 x 128 into registers,
+// 8 x 8 values per thread, for blocks of 128 x 128 and for the transposed order: a
+// thread's 8 rows are the 8 bytes that it writes of a transposed row, which goes through LDS
+// to leave in whole lines.
+#include "aal_fp8_device.h"
+
+#include <type_traits>
+
+namespace aal {
+namespace {
+
+struct QuantParams {
+  const void* x;
+  int64_t rows, cols, ld;
+  uint8_t* q;
+  int64_t ld_q;
+  void* scale;
+  uint8_t* qt;
+  int64_t ld_qt;
+  void* scale_t;
+  int64_t first;  // row of workgroups that the launch starts with
+};
+
+// The 8 values of row r from column c on, 0 behind the row's end.
+template <class TI>
+__device__ __forceinline__ void load8(const QuantParams& p, int64_t r, int64_t c, float (&x)[8]) {
+  const typename TI::storage* at = static_cast<const typename TI::storage*>(p.x) + r * p.ld + c;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = 0.f;
+  if (r >= p.rows) return;
+  if (c + 8 <= p.cols) {
+    constexpr int E = TI::kVec;
+#pragma unroll
+    for (int u = 0; u < 8 / E; ++u) {
+      float y[E];
+      TI::unpack(to_uint4(__builtin_nontemporal_load(reinterpret_cast<const u32x4_e2*>(at + u * E))), y);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[u * E + e] = y[e];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c + e < p.cols) x[e] = TI::load1(at, e);
+  }
+}
+
+// 8 bytes at `to`, of which n lie inside the row.
+__device__ __forceinline__ void store8(uint8_t* to, uint32_t lo, uint32_t hi, int64_t n) {
+  if (n >= 8) {
+    const u32x2 w = {lo, hi};
+    *reinterpret_cast<u32x2*>(to) = w;
+  } else {
+    const uint64_t w = uint64_t(hi) << 32 | lo;
+    for (int e = 0; e < int(n); ++e) to[e] = uint8_t(w >> (8 * e));
+  }
+}
+
+template <Scale S>
+__device__ __forceinline__ void store_scale(void* to, int64_t i, int e) {
+  if constexpr (S == Scale::kF32)
+    static_cast<float*>(to)[i] = power_of_two(e);
+  else
+    static_cast<uint8_t*>(to)[i] = uint8_t(e + 127);
+}
+
+// The largest over the 16 lanes of a row of the wave.
+__device__ __forceinline__ uint32_t row16_max(uint32_t v) {
+  v = max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0xB1, 0xF, 0xF, true)));
+  v = max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x4E, 0xF, 0xF, true)));
+  v = max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x141, 0xF, 0xF, true)));
+  return max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x140, 0xF, 0xF, true)));
+}
+
+// A workgroup takes 16 rows of 512 columns, a wave four rows of them.
+template <class TI, Fp8 F, Scale S>
+__global__ __launch_bounds__(256) void k_quant_rows(QuantParams p, int col_groups) {
+  constexpr int R = 4;
+  __shared__ int se[4][16];
+  const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
+  const int64_t rg = p.first + blockIdx.x / col_groups, cg = blockIdx.x % col_groups;
+  const int64_t r0 = rg * 16 + wv * R, c = cg * 512 + lane * 8;
+  float x[R][8];
+#pragma unroll
+  for (int i = 0; i < R; ++i) load8<TI>(p, r0 + i, c, x[i]);
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = max(m, finite_bits(x[i][e]));
+    const int e = scale_exponent<F>(row16_max(m));
+    const float inv = power_of_two(-e);
+    if ((lane & 15) == 0) se[lane / 16][wv * R + i] = e;
+    if (r0 + i < p.rows && c < p.cols)
+      store8(p.q + (r0 + i) * p.ld_q + c, pack_fp8<F>(x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv),
+             pack_fp8<F>(x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv), p.cols - c);
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const int64_t j = cg * 4 + threadIdx.x / 16, r = rg * 16 + threadIdx.x % 16;
+    if (j * kFp8Block < p.cols && r < p.rows) store_scale<S>(p.scale, j * p.rows + r, se[threadIdx.x / 16][threadIdx.x % 16]);
+  }
+}
+
+// A workgroup takes a tile of 128 x 128: 16 threads for the columns, 16 groups of 8 rows.
+template <class TI, Fp8 F, Scale S, bool SQUARE>
+__global__ __launch_bounds__(256) void k_quant_tile(QuantParams p, int col_blocks) {
+  constexpr int kPitch = 136;
+  __shared__ uint32_t part[4][kFp8Block];
+  __shared__ int ce[kFp8Block];
+  alignas(16) __shared__ uint8_t turn[kFp8Block * kPitch];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
+  const int64_t rb = p.first + blockIdx.x / col_blocks, cb = blockIdx.x % col_blocks;
+  const int rl = tid / 16 * 8, cl = tid % 16 * 8;  // in the tile
+  const int64_t r0 = rb * kFp8Block + rl, c0 = cb * kFp8Block + cl;
+  const int64_t row_blocks = (p.rows + kFp8Block - 1) / kFp8Block;
+  float x[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) load8<TI>(p, r0 + i, c0, x[i]);
+  int er[8], ec[8];
+  if constexpr (SQUARE) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = max(m, finite_bits(x[i][e]));
+    m = row16_max(m);
+    m = max(m, uint32_t(__shfl_xor(int(m), 16, kWave)));
+    m = max(m, uint32_t(__shfl_xor(int(m), 32, kWave)));
+    if (lane == 0) part[wv][0] = m;
+    __syncthreads();
+    m = max(max(part[0][0], part[1][0]), max(part[2][0], part[3][0]));
+    const int e = scale_exponent<F>(m);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) er[i] = ec[i] = e;
+    if (tid == 0) {
+      if (p.q) store_scale<S>(p.scale, cb * row_blocks + rb, e);
+      if (p.qt) store_scale<S>(p.scale_t, rb * col_blocks + cb, e);
+    }
+  } else {
+    if (p.q) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = max(m, finite_bits(x[i][e]));
+        er[i] = scale_exponent<F>(row16_max(m));
+        if (cl == 0 && r0 + i < p.rows) store_scale<S>(p.scale, cb * p.rows + r0 + i, er[i]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = max(m, finite_bits(x[i][e]));
+      m = max(m, uint32_t(__shfl_xor(int(m), 16, kWave)));
+      m = max(m, uint32_t(__shfl_xor(int(m), 32, kWave)));
+      if (lane < 16) part[wv][cl + e] = m;
+    }
+    __syncthreads();
+    if (tid < kFp8Block) {
+      const int e = scale_exponent<F>(max(max(part[0][tid], part[1][tid]), max(part[2][tid], part[3][tid])));
+      ce[tid] = e;
+      const int64_t c = cb * kFp8Block + tid;
+      if (c < p.cols) store_scale<S>(p.scale_t, rb * p.cols + c, e);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ec[e] = ce[cl + e];
+  }
+  if (p.q) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (r0 + i >= p.rows || c0 >= p.cols) continue;
+      const float inv = power_of_two(-er[i]);
+      store8(p.q + (r0 + i) * p.ld_q + c0,
+             pack_fp8<F>(x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv),
+             pack_fp8<F>(x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv), p.cols - c0);
+    }
+  }
+  if (p.qt == nullptr) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float inv = power_of_two(-ec[e]);
+    const u32x2 w = {pack_fp8<F>(x[0][e] * inv, x[1][e] * inv, x[2][e] * inv, x[3][e] * inv),
+                     pack_fp8<F>(x[4][e] * inv, x[5][e] * inv, x[6][e] * inv, x[7][e] * inv)};
+    *reinterpret_cast<u32x2*>(&turn[(cl + e) * kPitch + rl]) = w;
+  }
+  __syncthreads();
+  // 16 threads write a transposed row's 128 bytes
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int c = tid / 16 + i * 16, r = tid % 16 * 8;
+    const int64_t gc = cb * kFp8Block + c, gr = rb * kFp8Block + r;
+    if (gc >= p.cols || gr >= p.rows) continue;
+    const u32x2 w = *reinterpret_cast<const u32x2*>(&turn[c * kPitch + r]);
+    store8(p.qt + gc * p.ld_qt + gr, w.x, w.y, p.rows - gr);
+  }
+}
+
+template <class TI, Fp8 F, Scale S>
+hipError_t launch_typed(const QuantizeArgs& a) {
+  QuantParams p{a.x, a.rows, a.cols, a.ld, a.q, a.ld_q, a.scale, a.qt, a.ld_qt, a.scale_t, 0};
+  const bool tiles = a.block_rows != 1 || a.qt != nullptr;
+  const int64_t down = tiles ? (a.rows + 127) / 128 : (a.rows + 15) / 16;
+  const int64_t across = tiles ? (a.cols + 127) / 128 : (a.cols + 511) / 512;
+  // a launch holds fewer than 2^32 threads: up to 2^23 workgroups (cols <= 2^30: a row of them fits)
+  const int64_t most = (int64_t(1) << 23) / across;
+  for (; p.first < down; p.first += most) {
+    const dim3 grid(unsigned((down - p.first < most ? down - p.first : most) * across));
+    if (!tiles)
+      k_quant_rows<TI, F, S><<<grid, 256, 0, a.stream>>>(p, int(across));
+    else if (a.block_rows == 1)
+      k_quant_tile<TI, F, S, false><<<grid, 256, 0, a.stream>>>(p, int(across));
+    else
+      k_quant_tile<TI, F, S, true><<<grid, 256, 0, a.stream>>>(p, int(across));
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_quantize(const QuantizeArgs& a) {
+  auto with = [&](auto in, auto st) {
+    using TI = decltype(in);
+    constexpr Scale S = decltype(st)::value;
+    return a.format == Fp8::kE4M3 ? launch_typed<TI, Fp8::kE4M3, S>(a) : launch_typed<TI, Fp8::kE5M2, S>(a);
+  };
+  using F = std::integral_constant<Scale, Scale::kF32>;
+  using E = std::integral_constant<Scale, Scale::kE8M0>;
+  if (a.in == DType::kBf16) return a.st == Scale::kF32 ? with(Bf16{}, F{}) : with(Bf16{}, E{});
+  return a.st == Scale::kF32 ? with(F32{}, F{}) : with(F32{}, E{});
+}
+
+}  // namespace aal
