@@ -698,7 +698,7 @@ aal_status_t aal_fp8_quantize(const void* x, aal_dtype_t in_dtype, int64_t rows,
 
 /* One operand of a product: [rows, K] 8-bit values, K along the row.
  *   values       16-byte aligned; ld bytes from row to row, a multiple of 16, at least K (what lies
- *                behind a row's K values bears on nothing)
+ *                behind a row's K values bears on nothing, and is memory in the last row too)
  *   scale        of scale_type; row block r's scale of column block j is scale[r * scale_row + j * scale_block]
  *   block_rows   1 or 128 */
 typedef struct {

@@ -1,92 +1,91 @@
-// The product of two operands in 8-bit floating point with a scale for each
-// block of 128 (aal_fp8_matmul):
-//
-//   c[m, n] = sum_j sa[m, j] sb[n, j] sum_{k in block j} a[m, k] b[n, k]
-//
-// One wavefront for each 32 x 32 piece of c: a block of 128 is two matrix instructions of 32 x 32 x 64, their
-// result is scaled and added in fp32.  The rows of b go down the matrix tile and those of a
-// across, so that a lane holds four consecutive columns of one row of c.
-#include "aal_fp8_device.h"
+// The product of 8-bit operands (aal_fp8_matmul): how it is cut, and the sum of
+// the parts where the inner dimension is.  The kernels are in aal_fp8_matmul.h.
+#include "aal_fp8_matmul.h"
 
-#include <type_traits>
+#include <algorithm>
 
 namespace aal {
+extern template hipError_t launch_matmul_formats<0, 0>(const MatmulArgs&, const MatmulParams&, const MatmulPlan&);
+extern template hipError_t launch_matmul_formats<0, 1>(const MatmulArgs&, const MatmulParams&, const MatmulPlan&);
+extern template hipError_t launch_matmul_formats<1, 0>(const MatmulArgs&, const MatmulParams&, const MatmulPlan&);
+extern template hipError_t launch_matmul_formats<1, 1>(const MatmulArgs&, const MatmulParams&, const MatmulPlan&);
+
 namespace {
 
-// Bytes [at, at + 32) of a row of K values at `row` (null: none), 0 where they lie outside.
-__device__ __forceinline__ i32x8 load32(const uint8_t* row, int64_t at, int64_t K) {
-  i32x8 r = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (row == nullptr || at >= K) return r;
-  const int64_t n = K - at;
-  const u32x4 lo = *reinterpret_cast<const u32x4*>(row + at);
-  u32x4 hi = {0, 0, 0, 0};
-  if (n > 16) hi = *reinterpret_cast<const u32x4*>(row + at + 16);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r[i] = int(lo[i]);
-    r[i + 4] = int(hi[i]);
-  }
-  if (n < 32) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int bytes = int(n) - 4 * i;
-      if (bytes < 4) r[i] = bytes <= 0 ? 0 : int(uint32_t(r[i]) & ((1u << (8 * bytes)) - 1u));
-    }
-  }
-  return r;
+constexpr int kCus = 256;
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+MatmulPlan plan_of(int64_t M, int64_t N, int64_t K) {
+  const int64_t blocks = up(K, kFp8Block);
+  auto splits = [&](int64_t groups, int64_t want, int64_t least) {
+    // parts of at least `least` blocks, as many as bring the launch to `want` workgroups
+    const int64_t s = std::min(want / std::max<int64_t>(groups, 1), blocks / least);
+    return int(std::max<int64_t>(1, std::min<int64_t>(s, 64)));
+  };
+  if (M <= 32) return {0, splits(up(N, 64), 4 * kCus, 16)};
+  const int64_t large = up(M, 256) * up(N, 256), small = up(M, 128) * up(N, 128);
+  const int sl = splits(large, kCus, 8), ss = splits(small, 2 * kCus, 8);
+  // turns of the chip times the work of a tile; small tiles take more LDS traffic per result
+  const double tl = double(up(large * sl, kCus)) * 4.0 / sl, ts = double(up(small * ss, 2 * kCus)) * 2.0 * 1.25 / ss;
+  return tl <= ts ? MatmulPlan{2, sl} : MatmulPlan{1, ss};
 }
 
-template <int FA, int FB, Scale S, class TC>
-__global__ __launch_bounds__(64) void k_matmul(MatmulArgs p, int64_t tiles_n) {
-  const int lane = threadIdx.x, l = lane & 31, h = lane >> 5;
-  const int64_t m = blockIdx.x / tiles_n * 32 + l, n = blockIdx.x % tiles_n * 32;
-  const uint8_t* ra = m < p.M ? p.a.v + m * p.a.ld : nullptr;
-  const uint8_t* rb = n + l < p.N ? p.b.v + (n + l) * p.b.ld : nullptr;
-  f32x16 sum = {};
-  for (int64_t j = 0; j * kFp8Block < p.K; ++j) {
-    f32x16 t = {};
+__global__ __launch_bounds__(256) void k_join(const float* part, int64_t n, int splits, void* c, int out_bf16) {
+  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  const int e = int(min(int64_t(4), n - i));
+  for (int k = 0; k < splits; ++k)
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int64_t at = j * kFp8Block + u * 64 + h * 32;
-      t = dot64<std::is_same_v<TC, GF32>, FB, FA>(load32(rb, at, p.K), load32(ra, at, p.K), t);
-    }
-    const float sa = m < p.M ? load_scale<S>(p.a.s, m / p.a.block_rows * p.a.s_row + j * p.a.s_block) : 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int64_t c = n + (i / 4) * 8 + h * 4 + i % 4;
-      const float sb = c < p.N ? load_scale<S>(p.b.s, c / p.b.block_rows * p.b.s_row + j * p.b.s_block) : 0.f;
-      sum[i] = __builtin_fmaf(t[i], sa * sb, sum[i]);
-    }
-  }
-  if (m >= p.M) return;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int64_t c = n + (i / 4) * 8 + h * 4 + i % 4;
-    if (c < p.N) TC::store1(p.c, m * p.N + c, sum[i]);
-  }
-}
-
-template <int FA, int FB, Scale S, class TC>
-hipError_t launch_typed(const MatmulArgs& a) {
-  const int64_t tn = (a.N + 31) / 32, tm = (a.M + 31) / 32;
-  k_matmul<FA, FB, S, TC><<<dim3(unsigned(tn * tm)), 64, 0, a.stream>>>(a, tn);
-  return hipGetLastError();
-}
-
-template <Scale S, class TC>
-hipError_t with_formats(const MatmulArgs& a) {
-  if (a.a.format == 0) return a.b.format == 0 ? launch_typed<0, 0, S, TC>(a) : launch_typed<0, 1, S, TC>(a);
-  return a.b.format == 0 ? launch_typed<1, 0, S, TC>(a) : launch_typed<1, 1, S, TC>(a);
+    for (int u = 0; u < 4; ++u)
+      if (u < e) s[u] += part[k * n + i + u];
+  store4(c, i, s[0], s[1], s[2], s[3], n - i, out_bf16);
 }
 
 }  // namespace
 
-size_t matmul_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }
+size_t matmul_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+  const MatmulPlan plan = plan_of(M, N, K);
+  return plan.splits > 1 ? align256(size_t(plan.splits) * size_t(M) * size_t(N) * sizeof(float)) : 0;
+}
 
 hipError_t launch_matmul(const MatmulArgs& a) {
-  if (a.st == Scale::kF32)
-    return a.out == DType::kBf16 ? with_formats<Scale::kF32, GBf16>(a) : with_formats<Scale::kF32, GF32>(a);
-  return a.out == DType::kBf16 ? with_formats<Scale::kE8M0, GBf16>(a) : with_formats<Scale::kE8M0, GF32>(a);
+  const MatmulPlan plan = plan_of(a.M, a.N, a.K);
+  MatmulParams p{};
+  p.a = a.a.v;
+  p.b = a.b.v;
+  p.sa = a.a.s;
+  p.sb = a.b.s;
+  p.sa_row = a.a.s_row;
+  p.sa_block = a.a.s_block;
+  p.sb_row = a.b.s_row;
+  p.sb_block = a.b.s_block;
+  p.M = a.M;
+  p.N = a.N;
+  p.ld_a = int(a.a.ld);
+  p.ld_b = int(a.b.ld);
+  p.K = int(a.K);
+  p.blocks = int(up(a.K, kFp8Block));
+  p.per_split = int(up(p.blocks, plan.splits));
+  p.ra = a.a.block_rows == 1 ? 0 : 7;
+  p.rb = a.b.block_rows == 1 ? 0 : 7;
+  p.e8m0 = a.st == Scale::kE8M0;
+  const int64_t bm = plan.kind == 0 ? 32 : plan.kind == 1 ? 128 : 256, bn = plan.kind == 0 ? 64 : bm;
+  p.tiles_m = int(up(a.M, bm));
+  p.tiles_n = int(up(a.N, bn));
+  p.c = a.c;
+  p.part = static_cast<float*>(a.ws);
+  p.out_bf16 = a.out == DType::kBf16;
+  hipError_t e;
+  if (a.a.format == 0)
+    e = a.b.format == 0 ? launch_matmul_formats<0, 0>(a, p, plan) : launch_matmul_formats<0, 1>(a, p, plan);
+  else
+    e = a.b.format == 0 ? launch_matmul_formats<1, 0>(a, p, plan) : launch_matmul_formats<1, 1>(a, p, plan);
+  if (e != hipSuccess || plan.splits == 1) return e;
+  const int64_t n = a.M * a.N;
+  k_join<<<dim3(unsigned(up(n, 1024))), 256, 0, a.stream>>>(p.part, n, plan.splits, a.c, p.out_bf16);
+  return hipGetLastError();
 }
 
 }  // namespace aal

@@ -1,0 +1,6 @@
+// The product's kernels for a in e4m3 and b in e5m2.
+#include "aal_fp8_matmul.h"
+
+namespace aal {
+template hipError_t launch_matmul_formats<0, 1>(const MatmulArgs&, const MatmulParams&, const MatmulPlan&);
+}  // namespace aal

@@ -5,9 +5,14 @@
 
 namespace {
 
-constexpr int64_t kMostSize = int64_t(1) << 31;  // sizes are below it
+constexpr int64_t kMostSize = int64_t(1) << 31;   // sizes are below it
+constexpr int64_t kMostRows = int64_t(1) << 28;   // of an operand
+constexpr int64_t kMostInner = int64_t(1) << 24;  // 256 rows' bytes are below 2^32
 
 bool size_in_range(int64_t n) { return n >= 1 && n < kMostSize; }
+bool product_sizes(int64_t M, int64_t N, int64_t K) {
+  return M >= 1 && M <= kMostRows && N >= 1 && N <= kMostRows && M * N < (int64_t(1) << 37) && K >= 1 && K < kMostInner;
+}
 bool valid_format(int f) { return f == AAL_FP8_E4M3 || f == AAL_FP8_E5M2; }
 bool valid_scale(int s) { return s == AAL_SCALE_F32 || s == AAL_SCALE_E8M0; }
 
@@ -22,7 +27,7 @@ aal_status_t check_operand(const aal_fp8_operand_t* o, const char* name, int64_t
   if (!valid_scale(o->scale_type)) return fail(AAL_ERR_DTYPE, "%s: unknown scale_type %d", name, o->scale_type);
   if (o->block_rows != 1 && o->block_rows != 128)
     return fail(AAL_ERR_ARG, "%s: block_rows must be 1 or 128 (got %d)", name, o->block_rows);
-  if (o->ld < K || o->ld >= kMostSize) return fail(AAL_ERR_ARG, "%s: ld must be at least K and below 2^31", name);
+  if (o->ld < K || o->ld >= kMostInner) return fail(AAL_ERR_ARG, "%s: ld must be at least K and below 2^24", name);
   if (o->ld % 16 != 0 || !aligned(o->values, 16))
     return fail(AAL_ERR_ALIGN, "%s: values must be 16-byte aligned, ld a multiple of 16", name);
   if (o->scale_type == AAL_SCALE_F32 && !aligned(o->scale, 4)) return fail(AAL_ERR_ALIGN, "%s: scale must be 4-byte aligned", name);
@@ -79,7 +84,7 @@ aal_status_t aal_fp8_quantize(const void* x, aal_dtype_t in_dtype, int64_t rows,
 }
 
 size_t aal_fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-  return size_in_range(M) && size_in_range(N) && size_in_range(K) ? aal::matmul_workspace_bytes(M, N, K) : 0;
+  return product_sizes(M, N, K) ? aal::matmul_workspace_bytes(M, N, K) : 0;
 }
 
 aal_status_t aal_fp8_matmul(const aal_fp8_operand_t* a, const aal_fp8_operand_t* b, int64_t M, int64_t N, int64_t K,
@@ -87,8 +92,8 @@ aal_status_t aal_fp8_matmul(const aal_fp8_operand_t* a, const aal_fp8_operand_t*
                             hipStream_t stream) {
   clear_error();
   if (!c) return fail(AAL_ERR_ARG, "c must be non-NULL");
-  if (!size_in_range(M) || !size_in_range(N) || !size_in_range(K))
-    return fail(AAL_ERR_ARG, "M, N and K must be in [1, 2^31)");
+  if (!product_sizes(M, N, K))
+    return fail(AAL_ERR_ARG, "M and N must be in [1, 2^28], M * N below 2^37, K in [1, 2^24)");
   if (aal_status_t s = check_operand(a, "a", K); s != AAL_OK) return s;
   if (aal_status_t s = check_operand(b, "b", K); s != AAL_OK) return s;
   if (a->scale_type != b->scale_type) return fail(AAL_ERR_DTYPE, "the scales of a and b must be of one type");
