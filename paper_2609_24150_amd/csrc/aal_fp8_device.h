@@ -75,20 +75,21 @@ __device__ __forceinline__ bf16x8 widen(int lo, int hi) {
   return __builtin_bit_cast(bf16x8, w);
 }
 
-// t += x y over 64 values of the inner dimension, 32 x 32 results, 32 bytes of a row per lane.
+// x y over 128 values of the inner dimension, 16 x 16 results, 32 bytes of a row per lane.
 //
 // The matrix unit aligns the products of eight neighbouring 8-bit values to the largest of them and
 // cuts what lies 2^-13 below its power of two (measured; sums of the eights are fp32): 1.5e-5 of a sum of
 // random values, root mean square.  A result that is rounded to bf16 (1.7e-3) does not feel that, one in fp32
 // would: WIDE goes through bf16, whose products and sums are exact to fp32 (7e-9), at half the rate.
 template <bool WIDE, int FX, int FY>
-__device__ __forceinline__ f32x16 dot64(const i32x8& x, const i32x8& y, f32x16 t) {
+__device__ __forceinline__ f32x4 dot128(const i32x8& x, const i32x8& y) {
+  f32x4 t = {0.f, 0.f, 0.f, 0.f};
   if constexpr (!WIDE) {
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, t, FX, FY, 0, 127, 0, 127);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, t, FX, FY, 0, 0, 0, 0);
   } else {
 #pragma unroll
     for (int s = 0; s < 4; ++s)
-      t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen<FX>(x[2 * s], x[2 * s + 1]), widen<FY>(y[2 * s], y[2 * s + 1]), t, 0,
+      t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FX>(x[2 * s], x[2 * s + 1]), widen<FY>(y[2 * s], y[2 * s + 1]), t, 0,
                                                   0, 0);
     return t;
   }

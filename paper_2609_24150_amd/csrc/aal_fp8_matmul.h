@@ -44,10 +44,28 @@ hipError_t launch_matmul_formats(const MatmulArgs& a, const MatmulParams& p, con
 namespace {
 
 typedef __attribute__((address_space(3))) void lds_t;
-typedef __amdgpu_buffer_rsrc_t rsrc_t;
 
-__device__ __forceinline__ float scale_at(const void* s, int64_t i, int e8m0) {
-  return e8m0 ? load_scale<Scale::kE8M0>(s, i) : load_scale<Scale::kF32>(s, i);
+// A scale as it is stored, and as a float: apart, so that its load is not waited for at once.
+__device__ __forceinline__ uint32_t raw_scale(const void* s, int64_t i, int e8m0) {
+  return e8m0 ? static_cast<const uint8_t*>(s)[i] : static_cast<const uint32_t*>(s)[i];
+}
+__device__ __forceinline__ float scale_of(uint32_t raw, int e8m0) {
+  const uint32_t e = raw == 0u ? 0x400000u : raw == 255u ? 0x7fc00000u : raw << 23;
+  return __builtin_bit_cast(float, e8m0 ? e : raw);
+}
+
+// 16 bytes per lane from base + voff (0 from `bytes` on) into LDS, lane l's at `to` + 16 l.  In assembly, since the
+// compiler takes every later LDS read for one of these bytes and waits; nothing here has a result
+// to wait for but LDS, which stage_barrier() does.
+__device__ __forceinline__ void load_lds(u32x4 rsrc, uint32_t voff, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "m0");
+}
+__device__ __forceinline__ u32x4 buffer_of(const uint8_t* base, uint32_t bytes) {
+  const uint64_t b = reinterpret_cast<uint64_t>(base);
+  u32x4 r = {uint32_t(b), uint32_t(b >> 32), bytes, 0x00020000u};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = uint32_t(__builtin_amdgcn_readfirstlane(int(r[i])));
+  return r;
 }
 
 // Four consecutive results of a row, of which n exist.
@@ -81,17 +99,18 @@ __device__ __forceinline__ void stage_barrier() {
 }
 
 // ------------------------------------------------------------------ tiles
-// A workgroup of WN x WM waves makes 32 TN WN x 32 TM WM results.  Both operands' rows of a block, 128 bytes
+// A workgroup of WN x WM waves makes 16 TN WN x 16 TM WM results.  Both operands' rows of a block, 128 bytes
 // each, are loaded straight into LDS, the next block's while one is being multiplied; 16-byte pieces
 // of row r stand at place (piece ^ r % 8), so that the 8 lanes that read at a time meet no bank twice.
 template <bool WIDE, int FA, int FB, bool SQUARE, int TN, int TM, int WN, int WM>
-__global__ __launch_bounds__(64 * WN * WM) void k_tiles(MatmulParams p) {
-  constexpr int NT = 64 * WN * WM, BN = 32 * TN * WN, BM = 32 * TM * WM, RP = NT / 8;  // RP: rows of a round of loads
-  static_assert(BN <= NT && BM <= NT, "one scale of either side per thread");
+__global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
+  constexpr int NT = 64 * WN * WM, BN = 16 * TN * WN, BM = 16 * TM * WM, RP = NT / 8;  // RP: rows of a round of loads
+  static_assert(BN + BM == NT, "one scale per thread");
+  static_assert(!SQUARE || 128 % (16 * TN) == 0, "a wave's columns have one scale");
   __shared__ __attribute__((aligned(16))) uint8_t tile[2][(BN + BM) * 128];
   __shared__ __attribute__((aligned(16))) float scales[2][BN + BM];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l = lane & 31, h = lane >> 5;
+  const int l = lane & 15, h = lane >> 4;
   // Workgroups go round over the 8 XCDs: each takes a stretch of tiles of its own, in which
   // groups of 8 tiles down run through all of those across, so that its L2 serves both operands' panels.
   const int total = p.tiles_m * p.tiles_n, id = blockIdx.x, x = id & 7, q = total >> 3, rest = total & 7;
@@ -100,38 +119,29 @@ __global__ __launch_bounds__(64 * WN * WM) void k_tiles(MatmulParams p) {
   const int in = at - group * 8 * p.tiles_n, tm = first + in % rows, tn = in / rows;
   const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
   const int left_m = int(min(int64_t(BM), p.M - m0)), left_n = int(min(int64_t(BN), p.N - n0));
-  // rows behind the last one repeat it: what they give is not stored
-  const rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p.a) + m0 * p.ld_a, short(0),
-                                                      int(uint32_t(left_m) * uint32_t(p.ld_a)), 0x00020000);
-  const rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p.b) + n0 * p.ld_b, short(0),
-                                                      int(uint32_t(left_n) * uint32_t(p.ld_b)), 0x00020000);
+  // rows behind the last one lie outside the buffers and are zeros
+  const u32x4 ra = buffer_of(p.a + m0 * p.ld_a, uint32_t(left_m) * uint32_t(p.ld_a));
+  const u32x4 rb = buffer_of(p.b + n0 * p.ld_b, uint32_t(left_n) * uint32_t(p.ld_b));
   const int row = tid >> 3, piece = ((tid & 7) ^ (row & 7)) << 4;
-  uint32_t va[BM / RP], vb[BN / RP];
-#pragma unroll
-  for (int i = 0; i < BM / RP; ++i) va[i] = uint32_t(min(row + i * RP, left_m - 1)) * uint32_t(p.ld_a) + piece;
-#pragma unroll
-  for (int i = 0; i < BN / RP; ++i) vb[i] = uint32_t(min(row + i * RP, left_n - 1)) * uint32_t(p.ld_b) + piece;
+  const uint32_t va = uint32_t(row) * uint32_t(p.ld_a) + piece, vb = uint32_t(row) * uint32_t(p.ld_b) + piece;
   const int j0 = blockIdx.y * p.per_split, j1 = min(p.blocks, j0 + p.per_split);
+  const uint32_t lds0 = uint32_t(reinterpret_cast<uintptr_t>((lds_t*)&tile[0][0])) + wave * 1024;
   auto load = [&](int j, int to) {
-    const uint32_t k = uint32_t(j) * 128u;
+    const uint32_t k = uint32_t(j) * 128u, base = lds0 + uint32_t(to) * ((BN + BM) * 128);
 #pragma unroll
-    for (int i = 0; i < BN / RP; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_t*)&tile[to][(i * RP + wave * 8) * 128], 16, int(vb[i] + k), 0, 0, 0);
+    for (int i = 0; i < BN / RP; ++i) load_lds(rb, vb + (uint32_t(i * RP) * uint32_t(p.ld_b) + k), base + i * RP * 128);
 #pragma unroll
-    for (int i = 0; i < BM / RP; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_t*)&tile[to][(BN + i * RP + wave * 8) * 128], 16, int(va[i] + k), 0, 0,
-                                               0);
+    for (int i = 0; i < BM / RP; ++i) load_lds(ra, va + (uint32_t(i * RP) * uint32_t(p.ld_a) + k), base + (BN + i * RP) * 128);
   };
-  const int64_t sn = (n0 + min(tid, left_n - 1)) >> p.rb, sm = (m0 + min(tid, left_m - 1)) >> p.ra;
-  float next_n = 0.f, next_m = 0.f;
-  auto load_scales = [&](int j) {
-    if (tid < BN) next_n = scale_at(p.sb, sn * p.sb_row + j * p.sb_block, p.e8m0);
-    if (tid < BM) next_m = scale_at(p.sa, sm * p.sa_row + j * p.sa_block, p.e8m0);
-  };
-  auto put_scales = [&](int to) {
-    if (tid < BN) scales[to][tid] = next_n;
-    if (tid < BM) scales[to][BN + tid] = next_m;
-  };
+  // a thread has one scale: of the first BN threads one of b's rows, of the others one of a's
+  const bool is_b = wave < BN / 64;
+  const void* scale_base = is_b ? p.sb : p.sa;
+  const int64_t scale_step = is_b ? p.sb_block : p.sa_block;
+  const int64_t scale_row = is_b ? ((n0 + min(tid, left_n - 1)) >> p.rb) * p.sb_row
+                                 : ((m0 + min(tid - BN, left_m - 1)) >> p.ra) * p.sa_row;
+  uint32_t next = 0;
+  auto load_scales = [&](int j) { next = raw_scale(scale_base, scale_row + j * scale_step, p.e8m0); };
+  auto put_scales = [&](int to) { scales[to][tid] = scale_of(next, p.e8m0); };
   // K ends inside the last block: zeros for what lies behind it
   auto clear_tail = [&](int to) {
     const int rem = p.K & 127;
@@ -150,15 +160,15 @@ __global__ __launch_bounds__(64 * WN * WM) void k_tiles(MatmulParams p) {
     }
   };
   const int wn = wave % WN, wm = wave / WN;
-  f32x16 acc[TN][TM];
+  f32x4 acc[TN][TM];
 #pragma unroll
   for (int i = 0; i < TN; ++i)
 #pragma unroll
-    for (int j = 0; j < TM; ++j) acc[i][j] = f32x16{};
-  auto fragment = [&](const uint8_t* base, int r, int u) {
-    const u32x4 lo = *reinterpret_cast<const u32x4*>(base + r * 128 + (((4 * u + 2 * h) ^ (l & 7)) << 4));
-    const u32x4 hi = *reinterpret_cast<const u32x4*>(base + r * 128 + (((4 * u + 2 * h + 1) ^ (l & 7)) << 4));
-    return i32x8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
+    for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int lo = ((2 * h) ^ (l & 7)) << 4, hi = ((2 * h + 1) ^ (l & 7)) << 4;
+  auto fragment = [&](const uint8_t* at) {
+    const u32x4 a = *reinterpret_cast<const u32x4*>(at + lo), b = *reinterpret_cast<const u32x4*>(at + hi);
+    return i32x8{int(a.x), int(a.y), int(a.z), int(a.w), int(b.x), int(b.y), int(b.z), int(b.w)};
   };
   load_scales(j0);
   load(j0, 0);
@@ -175,39 +185,41 @@ __global__ __launch_bounds__(64 * WN * WM) void k_tiles(MatmulParams p) {
       load_scales(j + 1);
       load(j + 1, cur ^ 1);
     }
-    const uint8_t* tb = tile[cur];
-    const uint8_t* ta = tile[cur] + BN * 128;
+    const uint8_t* tb = tile[cur] + (wn * TN * 16 + l) * 128;
+    const uint8_t* ta = tile[cur] + (BN + wm * TM * 16 + l) * 128;
     const float* sc = scales[cur];
-    i32x8 xa[TM][2];
+    i32x8 xa[TM];
     float fa[TM];
+    auto add = [&](int n, int m, const f32x4& t, const f32x4& fb) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[n][m][i] = __builtin_fmaf(t[i], SQUARE ? fa[m] : fa[m] * fb[i], acc[n][m][i]);
+      // here, not where the compiler would rather have all of them: 128 registers of products
+      asm volatile("" : "+v"(acc[n][m]));
+    };
 #pragma unroll
     for (int m = 0; m < TM; ++m) {
-      const int r = (wm * TM + m) * 32 + l;
-      fa[m] = sc[BN + r];
-      xa[m][0] = fragment(ta, r, 0);
-      xa[m][1] = fragment(ta, r, 1);
+      fa[m] = sc[BN + (wm * TM + m) * 16 + l];
+      if constexpr (SQUARE) fa[m] *= sc[wn * TN * 16];
+      xa[m] = fragment(ta + m * 16 * 128);
     }
+    // a row of products is added while the next one is in the matrix unit
+    i32x8 xb = fragment(tb);
+    f32x4 t[TM], fb{}, fp{};
 #pragma unroll
-    for (int n = 0; n < TN; ++n) {
-      const int r0 = (wn * TN + n) * 32;
-      const i32x8 xb0 = fragment(tb, r0 + l, 0), xb1 = fragment(tb, r0 + l, 1);
-      f32x4 fb[4];
-      float fb1 = 0.f;
-      if constexpr (SQUARE) {
-        fb1 = sc[r0];
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) fb[i] = *reinterpret_cast<const f32x4*>(&sc[r0 + i * 8 + h * 4]);
-      }
+    for (int n = 0; n <= TN; ++n) {
+      const i32x8 x = xb;
+      if (n + 1 < TN) xb = fragment(tb + (n + 1) * 16 * 128);
+      if constexpr (!SQUARE)
+        if (n < TN) fb = *reinterpret_cast<const f32x4*>(&sc[(wn * TN + n) * 16 + h * 4]);
 #pragma unroll
       for (int m = 0; m < TM; ++m) {
-        f32x16 t = dot64<WIDE, FB, FA>(xb0, xa[m][0], f32x16{});
-        t = dot64<WIDE, FB, FA>(xb1, xa[m][1], t);
-        const float f = fa[m] * fb1;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          acc[n][m][i] = __builtin_fmaf(t[i], SQUARE ? f : fa[m] * fb[i / 4][i % 4], acc[n][m][i]);
+        f32x4 u{};
+        if (n < TN) u = dot128<WIDE, FB, FA>(x, xa[m]);
+        if (n > 0) add(n - 1, m, t[m], fp);
+        t[m] = u;
+        if constexpr (!WIDE) __builtin_amdgcn_sched_barrier(0);
       }
+      fp = fb;
     }
     if (more) {
       put_scales(cur ^ 1);
@@ -223,92 +235,103 @@ __global__ __launch_bounds__(64 * WN * WM) void k_tiles(MatmulParams p) {
   const bool bf16 = whole && p.out_bf16;
 #pragma unroll
   for (int m = 0; m < TM; ++m) {
-    const int64_t gm = m0 + (wm * TM + m) * 32 + l;
+    const int64_t gm = m0 + (wm * TM + m) * 16 + l;
     if (gm >= p.M) continue;
 #pragma unroll
-    for (int n = 0; n < TN; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t gn = n0 + (wn * TN + n) * 32 + i * 8 + h * 4;
-        if (gn < p.N)
-          store4(c, gm * p.N + gn, acc[n][m][4 * i], acc[n][m][4 * i + 1], acc[n][m][4 * i + 2], acc[n][m][4 * i + 3],
-                 p.N - gn, bf16);
-      }
+    for (int n = 0; n < TN; ++n) {
+      const int64_t gn = n0 + (wn * TN + n) * 16 + h * 4;
+      if (gn < p.N) store4(c, gm * p.N + gn, acc[n][m][0], acc[n][m][1], acc[n][m][2], acc[n][m][3], p.N - gn, bf16);
+    }
   }
 }
 
 // --------------------------------------------------------------- few rows
-// Up to 32 rows of a.  A workgroup takes 64 rows of b, its four waves every fourth block each; b goes from
+// Up to 16 TM rows of a.  A workgroup takes 64 rows of b, its four waves every fourth block each; b goes from
 // memory to registers, since nothing else reads it, the next block's on its way while one is being multiplied.
-template <bool WIDE, int FA, int FB, bool SQUARE>
-__global__ __launch_bounds__(256) void k_few_rows(MatmulParams p) {
-  __shared__ float sums[4][32][65];
+template <bool WIDE, int FA, int FB, bool SQUARE, int TM>
+__global__ __launch_bounds__(256, 2) void k_few_rows(MatmulParams p) {
+  constexpr int TN = 4;
+  __shared__ float sums[4][16 * TM][16 * TN + 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l = lane & 31, h = lane >> 5;
-  const int64_t n0 = int64_t(blockIdx.x) * 64;
+  const int l = lane & 15, h = lane >> 4;
+  const int64_t n0 = int64_t(blockIdx.x) * (16 * TN);
   const int j0 = blockIdx.y * p.per_split, j1 = min(p.blocks, j0 + p.per_split);
-  const int64_t m = min(int64_t(l), p.M - 1);
-  const uint8_t* ra = p.a + m * p.ld_a;
-  const uint8_t* rb[2];
-  int64_t sn[2];
+  // rows behind the last one repeat it: what they give is not stored
+  const uint8_t* ra[TM];
+  const uint8_t* rb[TN];
+  int64_t sm[TM], sn[TN];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int64_t n = min(n0 + t * 32 + l, p.N - 1);
+  for (int t = 0; t < TM; ++t) {
+    const int64_t m = min(int64_t(t * 16 + l), p.M - 1);
+    ra[t] = p.a + m * p.ld_a;
+    sm[t] = (m >> p.ra) * p.sa_row;
+  }
+#pragma unroll
+  for (int t = 0; t < TN; ++t) {
+    const int64_t n = min(n0 + t * 16 + l, p.N - 1);
     rb[t] = p.b + n * p.ld_b;
-    sn[t] = (SQUARE ? min(n0 + t * 32, p.N - 1) : n) >> p.rb;
+    sn[t] = (n >> p.rb) * p.sb_row;
   }
   struct Block {
-    u32x4 a[4], b[2][4];
-    float fa, fb[2];
+    u32x4 a[TM][2], b[TN][2];
+    uint32_t fa[TM], fb[SQUARE ? 1 : TN];
   };
-  // a lane's 64 bytes of a row: 16-byte pieces h, 2 + h, 4 + h and 6 + h, the same of either operand
+  // a lane's 32 bytes of a row: 16-byte pieces h and 4 + h, the same of either operand
   auto load = [&](int j, Block& r) {
-    const int64_t k = int64_t(j) * 128 + h * 16;
+    const int k = j * 128 + h * 16;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool in = k + i * 32 < p.K;
+    for (int i = 0; i < 2; ++i) {
+      const bool in = k + i * 64 < p.K;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-        r.b[t][i] = in ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(rb[t] + k + i * 32)) : u32x4{0, 0, 0, 0};
-      r.a[i] = in ? *reinterpret_cast<const u32x4*>(ra + k + i * 32) : u32x4{0, 0, 0, 0};
+      for (int t = 0; t < TN; ++t)
+        r.b[t][i] = in ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(rb[t] + k + i * 64)) : u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int t = 0; t < TM; ++t) r.a[t][i] = in ? *reinterpret_cast<const u32x4*>(ra[t] + k + i * 64) : u32x4{0, 0, 0, 0};
     }
-    r.fa = scale_at(p.sa, (m >> p.ra) * p.sa_row + j * p.sa_block, p.e8m0);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) r.fb[t] = scale_at(p.sb, sn[t] * p.sb_row + j * p.sb_block, p.e8m0);
+    for (int t = 0; t < TM; ++t) r.fa[t] = raw_scale(p.sa, sm[t] + j * p.sa_block, p.e8m0);
+#pragma unroll
+    for (int t = 0; t < (SQUARE ? 1 : TN); ++t) r.fb[t] = raw_scale(p.sb, sn[t] + j * p.sb_block, p.e8m0);
   };
   // bytes behind K, which only the last block has
-  auto clear = [&](u32x4& v, int64_t k) {
+  auto clear = [&](u32x4& v, int k) {
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const int64_t n = p.K - k - 4 * w;
+      const int n = p.K - k - 4 * w;
       v[w] = n >= 4 ? v[w] : n <= 0 ? 0u : v[w] & ((1u << (8 * n)) - 1u);
     }
   };
-  auto join = [](const u32x4& lo, const u32x4& hi) {
-    return i32x8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
+  auto join = [](const u32x4& a, const u32x4& b) {
+    return i32x8{int(a.x), int(a.y), int(a.z), int(a.w), int(b.x), int(b.y), int(b.z), int(b.w)};
   };
-  f32x16 acc[2] = {};
+  f32x4 acc[TN][TM];
+#pragma unroll
+  for (int n = 0; n < TN; ++n)
+#pragma unroll
+    for (int m = 0; m < TM; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
   auto multiply = [&](int j, Block& r) {
     if ((p.K & 127) && j == p.blocks - 1) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t k = int64_t(j) * 128 + h * 16 + i * 32;
-        clear(r.a[i], k);
-        clear(r.b[0][i], k);
-        clear(r.b[1][i], k);
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int t = 0; t < TM; ++t) clear(r.a[t][i], j * 128 + h * 16 + i * 64);
+#pragma unroll
+        for (int t = 0; t < TN; ++t) clear(r.b[t][i], j * 128 + h * 16 + i * 64);
       }
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      f32x16 s = dot64<WIDE, FB, FA>(join(r.b[t][0], r.b[t][1]), join(r.a[0], r.a[1]), f32x16{});
-      s = dot64<WIDE, FB, FA>(join(r.b[t][2], r.b[t][3]), join(r.a[2], r.a[3]), s);
-      const float f = r.fa * r.fb[t];
+    for (int n = 0; n < TN; ++n) {
+      // with a scale for each row of b: the lane that has row l's gives it to those that hold its result
+      const float fb = scale_of(r.fb[SQUARE ? 0 : n], p.e8m0);
+      float fi[4];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if constexpr (SQUARE)
-          acc[t][i] = __builtin_fmaf(s[i], f, acc[t][i]);
-        else
-          acc[t][i] = __builtin_fmaf(s[i], r.fa * __shfl(r.fb[t], (i / 4) * 8 + h * 4 + i % 4, 64), acc[t][i]);
+      for (int i = 0; i < 4; ++i) fi[i] = SQUARE ? fb : __shfl(fb, h * 4 + i, kWave);
+#pragma unroll
+      for (int m = 0; m < TM; ++m) {
+        const f32x4 t = dot128<WIDE, FB, FA>(join(r.b[n][0], r.b[n][1]), join(r.a[m][0], r.a[m][1]));
+        const float fa = scale_of(r.fa[m], p.e8m0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[n][m][i] = __builtin_fmaf(t[i], fa * fi[i], acc[n][m][i]);
       }
     }
   };
@@ -325,18 +348,19 @@ __global__ __launch_bounds__(256) void k_few_rows(MatmulParams p) {
     j += 4;
   }
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int n = 0; n < TN; ++n)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sums[wave][l][t * 32 + (i / 4) * 8 + h * 4 + i % 4] = acc[t][i];
+    for (int m = 0; m < TM; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sums[wave][m * 16 + l][n * 16 + h * 4 + i] = acc[n][m][i];
   __syncthreads();
   const bool whole = gridDim.y == 1;
   void* c = whole ? p.c : p.part + int64_t(blockIdx.y) * p.M * p.N;
   const bool bf16 = whole && p.out_bf16;
-  const int64_t n = n0 + (tid & 63);
+  const int64_t n = n0 + lane;
   if (n >= p.N) return;
-  for (int r = tid >> 6; r < p.M; r += 4) {
-    const int i = tid & 63;
-    const float s = (sums[0][r][i] + sums[1][r][i]) + (sums[2][r][i] + sums[3][r][i]);
+  for (int r = wave; r < p.M; r += 4) {
+    const float s = (sums[0][r][lane] + sums[1][r][lane]) + (sums[2][r][lane] + sums[3][r][lane]);
     if (bf16)
       GBf16::store1(c, int64_t(r) * p.N + n, s);
     else
@@ -347,12 +371,14 @@ __global__ __launch_bounds__(256) void k_few_rows(MatmulParams p) {
 template <bool WIDE, int FA, int FB, bool SQUARE>
 hipError_t launch_square(const MatmulParams& p, const MatmulPlan& plan, hipStream_t stream) {
   const dim3 grid(unsigned(int64_t(p.tiles_m) * p.tiles_n), unsigned(plan.splits));
-  if (plan.kind == 0)
-    k_few_rows<WIDE, FA, FB, SQUARE><<<grid, 256, 0, stream>>>(p);
+  if (plan.kind == 0 && p.M <= 16)
+    k_few_rows<WIDE, FA, FB, SQUARE, 1><<<grid, 256, 0, stream>>>(p);
+  else if (plan.kind == 0)
+    k_few_rows<WIDE, FA, FB, SQUARE, 2><<<grid, 256, 0, stream>>>(p);
   else if (plan.kind == 1)
-    k_tiles<WIDE, FA, FB, SQUARE, 2, 2, 2, 2><<<grid, 256, 0, stream>>>(p);
-  else
-    k_tiles<WIDE, FA, FB, SQUARE, 4, 2, 2, 4><<<grid, 512, 0, stream>>>(p);
+    k_tiles<WIDE, FA, FB, SQUARE, 4, 4, 2, 2><<<grid, 256, 0, stream>>>(p);
+  else if constexpr (!WIDE)
+    k_tiles<WIDE, FA, FB, SQUARE, 8, 4, 2, 4><<<grid, 512, 0, stream>>>(p);
   return hipGetLastError();
 }
 

@@ -16,7 +16,7 @@ constexpr int kCus = 256;
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-MatmulPlan plan_of(int64_t M, int64_t N, int64_t K) {
+MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, bool wide) {
   const int64_t blocks = up(K, kFp8Block);
   auto splits = [&](int64_t groups, int64_t want, int64_t least) {
     // parts of at least `least` blocks, as many as bring the launch to `want` workgroups
@@ -28,7 +28,7 @@ MatmulPlan plan_of(int64_t M, int64_t N, int64_t K) {
   const int sl = splits(large, kCus, 8), ss = splits(small, 2 * kCus, 8);
   // turns of the chip times the work of a tile; small tiles take more LDS traffic per result
   const double tl = double(up(large * sl, kCus)) * 4.0 / sl, ts = double(up(small * ss, 2 * kCus)) * 2.0 * 1.25 / ss;
-  return tl <= ts ? MatmulPlan{2, sl} : MatmulPlan{1, ss};
+  return tl <= ts && !wide ? MatmulPlan{2, sl} : MatmulPlan{1, ss};
 }
 
 __global__ __launch_bounds__(256) void k_join(const float* part, int64_t n, int splits, void* c, int out_bf16) {
@@ -46,12 +46,12 @@ __global__ __launch_bounds__(256) void k_join(const float* part, int64_t n, int 
 }  // namespace
 
 size_t matmul_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-  const MatmulPlan plan = plan_of(M, N, K);
-  return plan.splits > 1 ? align256(size_t(plan.splits) * size_t(M) * size_t(N) * sizeof(float)) : 0;
+  const int splits = std::max(plan_of(M, N, K, false).splits, plan_of(M, N, K, true).splits);
+  return splits > 1 ? align256(size_t(splits) * size_t(M) * size_t(N) * sizeof(float)) : 0;
 }
 
 hipError_t launch_matmul(const MatmulArgs& a) {
-  const MatmulPlan plan = plan_of(a.M, a.N, a.K);
+  const MatmulPlan plan = plan_of(a.M, a.N, a.K, a.out == DType::kF32);
   MatmulParams p{};
   p.a = a.a.v;
   p.b = a.b.v;
