@@ -21,9 +21,12 @@
 namespace aal {
 namespace {
 
-constexpr int kCand = 512;      // candidates of a part that fit
-constexpr int kMergeMost = 64;  // candidates per thread of the merge
-constexpr int kSurvivors = 1024;
+constexpr int kCand = 512;   // candidates of a part that fit
+constexpr int kQueue = 256;  // and vectors that hold some
+constexpr int kLists = 2048 + kBeamMax;  // a request's parts, and its beams: 64 rows of 2^18 fp32 in parts of 8,192
+constexpr int kMerge = 512;       // threads of the merge
+constexpr int kWork = 4096;       // candidates of a request that may reach the bound
+constexpr int kSurvivors = 1024;  // candidates of a request that reach the bound
 
 struct BeamParams {
   const void* z;
@@ -60,47 +63,65 @@ __device__ __forceinline__ int block_count(int wave_value, int* sh) {
 
 typedef u32x4 u32x4_e2 __attribute__((aligned(2)));  // a vector at any element
 
+// A value that all lanes have, as one of the wave.
+__device__ __forceinline__ float uniform(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
+
+// The vector stays packed here: unpacked copies are not kept for later.
+__device__ __forceinline__ void pin(u32x4& x) { asm volatile("" : "+v"(x)); }
+
+// Vectors stay packed, 32 registers of them, and are unpacked where they are used: eight workgroups
+// of 256 a CU, whose selections run under the others' loads and sums.
 template <class TI, int BLK, int U>
-__global__ __launch_bounds__(BLK) void k_beam_parts(BeamParams p) {
+__global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
   constexpr int E = TI::kVec, WV = BLK / kWave;
   constexpr int kShift = 32 - key_bits<TI>();
-  __shared__ uint64_t cand[kCand], sorted[kCand];
+  __shared__ __attribute__((aligned(16))) uint64_t cand[kCand];
+  __shared__ uint64_t sorted[kCand];
   __shared__ double dsum[WV];
   __shared__ float fsh[WV];
   __shared__ int ish[WV];
-  __shared__ int count;
+  __shared__ __attribute__((aligned(16))) u32x4 queue[kQueue];
+  __shared__ int place[kQueue];
+  __shared__ int count, vectors;
   const int64_t row = p.row0 + blockIdx.x / p.parts;
   const int part = blockIdx.x % p.parts, tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
   if ((p.finished && p.finished[row]) || p.scores[row] == kNegInf) return;
   const int s0 = part * p.part_len, len = min(p.part_len, p.V - s0);
   const typename TI::storage* base = static_cast<const typename TI::storage*>(p.z) + row * int64_t(p.V) + s0;
-  float x[U][E], gm[U], m = kNegInf;
-  if (tid == 0) count = 0;
+  if (tid == 0) count = vectors = 0;
   u32x4 raw[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int at = (u * BLK + tid) * E;
-    if (at + E <= len) raw[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_e2*>(base + at));
-  }
+  float gm[U], m = kNegInf;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int at = (u * BLK + tid) * E;
     if (at + E <= len) {
-      TI::unpack(to_uint4(raw[u]), x[u]);
+      raw[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_e2*>(base + at));
     } else {
+      typename TI::storage v[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[u][e] = at + e < len ? TI::load1(base, at + e) : kNegInf;
+      for (int e = 0; e < E; ++e) v[e] = at + e < len ? base[at + e] : TI::neg_inf();
+      __builtin_memcpy(&raw[u], v, 16);
     }
-    gm[u] = x[u][0];
+  }
 #pragma unroll
-    for (int e = 1; e < E; ++e) gm[u] = fmaxf(gm[u], x[u][e]);
+  for (int u = 0; u < U; ++u) {
+    float x[E];
+    TI::unpack(to_uint4(raw[u]), x);
+    gm[u] = x[0];
+#pragma unroll
+    for (int e = 1; e < E; ++e) gm[u] = fmaxf(gm[u], x[e]);
     m = fmaxf(m, gm[u]);
   }
+#pragma unroll
+  for (int u = 0; u < U; ++u) pin(raw[u]);
   m = wave_max(m);
   if (lane == 0) fsh[wv] = m;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < WV; ++i) m = fmaxf(m, fsh[i]);
+  m = uniform(m);
   __syncthreads();
   const int64_t slot = row * int64_t(p.parts) + part;
   uint64_t* list = p.list + slot * p.n;
@@ -110,22 +131,34 @@ __global__ __launch_bounds__(BLK) void k_beam_parts(BeamParams p) {
     return;
   }
   // at least n logits reach t, or all finite ones do
-  float t = threshold<TI, WV>(gm, p.n, m, fsh);
+  float t = uniform(threshold<TI, WV>(gm, p.n, m, fsh));
+  // the vectors that hold some, then their entries, each by a thread of its own
   auto collect = [&](float from, bool strict) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (!(gm[u] >= from)) continue;
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if ((strict ? x[u][e] > from : x[u][e] >= from) && x[u][e] != kNegInf) {
-          const int at = atomicAdd(&count, 1);
-          if (at < kCand) cand[at] = entry_of(order_key<TI>(x[u][e]), s0 + (u * BLK + tid) * E + e);
+    for (int u = 0; u < U; ++u)
+      if (gm[u] >= from && gm[u] != kNegInf) {
+        const int at = atomicAdd(&vectors, 1);
+        if (at < kQueue) {
+          queue[at] = raw[u];
+          place[at] = s0 + (u * BLK + tid) * E;
         }
+      }
+    __syncthreads();
+    const int q = vectors;
+    for (int i = tid; i < min(q, kQueue) * E; i += BLK) {
+      const int e = i % E;
+      const float x = TI::load1(&queue[i / E], e);
+      if ((strict ? x > from : x >= from) && x != kNegInf) {
+        const int at = atomicAdd(&count, 1);
+        if (at < kCand) cand[at] = entry_of(order_key<TI>(x), place[i / E] + e);
+      }
     }
+    __syncthreads();
+    return q > kQueue ? kCand + 1 : count;
   };
-  collect(t, false);
-  __syncthreads();
-  int c = count, left_ties = 0;
+  int c = collect(t, false), left_ties = 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) pin(raw[u]);
   if (c > kCand) {
     // ties or clusters: the n-th largest logit itself, and the first of its ties
     uint32_t lo = order_key<TI>(kNegInf) >> kShift, hi = (order_key<TI>(m) >> kShift) + 1u;
@@ -134,24 +167,27 @@ __global__ __launch_bounds__(BLK) void k_beam_parts(BeamParams p) {
       const float f = key_logit<TI>(mid << kShift);
       int reach = 0;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u) {
+        float x[E];
+        TI::unpack(to_uint4(raw[u]), x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) reach += __popcll(__builtin_amdgcn_ballot_w64(x[u][e] >= f));
+        for (int e = 0; e < E; ++e) reach += __popcll(__builtin_amdgcn_ballot_w64(x[e] >= f));
+      }
       (block_count<WV>(reach, ish) >= p.n ? lo : hi) = mid;
     }
-    t = key_logit<TI>(lo << kShift);
-    if (tid == 0) count = 0;
+    t = uniform(key_logit<TI>(lo << kShift));
+    if (tid == 0) count = vectors = 0;
     __syncthreads();
-    collect(t, true);
-    __syncthreads();
-    c = count;
+    c = collect(t, true);
     if (t != kNegInf) {
       int ties = 0;  // before this vector's turn
 #pragma unroll
       for (int u = 0; u < U; ++u) {
+        float x[E];
+        TI::unpack(to_uint4(raw[u]), x);
         int mine = 0;
 #pragma unroll
-        for (int e = 0; e < E; ++e) mine += x[u][e] == t;
+        for (int e = 0; e < E; ++e) mine += x[e] == t;
         int before = mine;
         for (int off = 1; off < kWave; off <<= 1) {
           const int o = __shfl_up(before, off, kWave);
@@ -168,7 +204,7 @@ __global__ __launch_bounds__(BLK) void k_beam_parts(BeamParams p) {
         }
 #pragma unroll
         for (int e = 0; e < E; ++e)
-          if (x[u][e] == t) {
+          if (x[e] == t) {
             if (at < p.n) cand[at] = entry_of(order_key<TI>(t), s0 + (u * BLK + tid) * E + e);
             ++at;
           }
@@ -182,32 +218,45 @@ __global__ __launch_bounds__(BLK) void k_beam_parts(BeamParams p) {
   for (int i = tid; i < c; i += BLK) {
     const uint64_t mine = cand[i];
     int rank = 0;
+#pragma unroll 8
     for (int j = 0; j < c; ++j) rank += cand[j] > mine;
     sorted[rank] = mine;
   }
-  // the others' sum, while the list is being sorted
+  // The others' sum of 2^((z - m) sc), sc in two pieces.  z sc_hi - ref takes one rounding, and so does adding
+  // z sc_lo; what ref, m sc rounded, is off by is a factor of the whole sum and joins it in 64 bits.
+  // References beyond 2^27 take the difference first.
+  const float ref = m * p.sc_hi;
+  const bool steep = fabsf(ref) > 0x1p27f;
   auto weight = [&](float z) {
-    const float d = z - m;
-    return ex2(__builtin_fmaf(d, p.sc_hi, d * p.sc_lo));
+    if (steep) {
+      const float d = z - m;
+      return ex2(__builtin_fmaf(d, p.sc_hi, d * p.sc_lo));
+    }
+    return ex2(__builtin_fmaf(z, p.sc_lo, __builtin_fmaf(z, p.sc_hi, -ref)));
   };
   float s = 0.f;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    float us = 0.f;
+    float x[E], us = 0.f;
+    TI::unpack(to_uint4(raw[u]), x);
+    if (__builtin_amdgcn_ballot_w64(gm[u] >= t) != 0) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) us += x[u][e] < t ? weight(x[u][e]) : 0.f;
+      for (int e = 0; e < E; ++e) us += x[e] < t ? weight(x[e]) : 0.f;
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) us += weight(x[e]);
+    }
     s += us;
   }
   if (tid == 0 && left_ties) s += float(left_ties) * weight(t);
   __syncthreads();
   double total = double(s);
-  for (int i = tid; i < max(c, p.n); i += BLK) {
-    if (i < p.n) {
-      list[i] = i < c ? sorted[i] : 0;
-      if (i < c) total += exp((double(entry_logit<TI>(sorted[i])) - double(m)) * p.inv_t);
-    } else {
-      total += double(weight(entry_logit<TI>(sorted[i])));
-    }
+  for (int i = tid; i < c; i += BLK)
+    if (i >= p.n) total += double(weight(entry_logit<TI>(sorted[i])));
+  if (!steep) total *= exp2(double(ref) - double(m) * (double(p.sc_hi) + double(p.sc_lo)));
+  for (int i = tid; i < p.n; i += BLK) {
+    list[i] = i < c ? sorted[i] : 0;
+    if (i < c) total += exp((double(entry_logit<TI>(sorted[i])) - double(m)) * p.inv_t);
   }
   total = wave_sum_d(total);
   if (lane == 0) dsum[wv] = total;
@@ -223,96 +272,163 @@ __device__ __forceinline__ bool before(double ra, int ba, uint64_t ea, double rb
   return ra > rb || (ra == rb && (ba < bb || (ba == bb && ea > eb)));
 }
 
-// NT threads with up to NPT candidates each: a request's lists and, behind them, the beams that have ended.
-template <class TI, int NT, int NPT>
-__global__ __launch_bounds__(NT) void k_beam_merge(BeamParams p, int64_t b0) {
-  constexpr int WV = NT / kWave;
-  __shared__ double lse[kBeamMax], factor[kBeamMax], score[kBeamMax];
+// The lists of a request and, behind them, the beams that have ended as lists of one.
+//
+// Of lists in order, the r-th largest of their entries number i is reached by r i candidates at least: with r i >= n a
+// bound below which nothing is chosen.  A wave each finds it for i = 1, 2, 4, ..., in 32 bits, which keep ranks'
+// order up to ties; the largest bound leaves little more than n candidates, which are ranked by counting.
+template <class TI>
+__global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0) {
+  constexpr int NT = kMerge, WV = NT / kWave, R = 4;
+  static_assert(WV == 8, "a wave for each i up to 128");
+  __shared__ double lse[kBeamMax], factor[kBeamMax], inverse[kBeamMax], score[kBeamMax];
   __shared__ int state[kBeamMax];  // 0 goes on, 1 has ended, 2 has score -inf
   __shared__ double srank[kSurvivors];
   __shared__ uint64_t sentry[kSurvivors];
   __shared__ int sbeam[kSurvivors];
-  __shared__ int ish[WV];
-  __shared__ int count;
+  __shared__ uint32_t heads[WV][kLists];
+  __shared__ uint32_t work[kWork];
+  __shared__ uint32_t bound;
+  __shared__ int count, items;
   const int64_t b = b0 + blockIdx.x, row0 = b * p.W;
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
-  if (tid == 0) count = 0;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int per = p.parts * p.n, C = p.W * per, L = p.W * p.parts;
+  const uint64_t* lists = p.list + row0 * per;
+  // the first lists' entries number i, before anything is known of their beams: one way to memory less to wait for
+  const int number = 1 << wv;
+  uint64_t early[R];
+#pragma unroll
+  for (int q = 0; q < R; ++q) {
+    const int k = q * kWave + lane;
+    early[q] = number <= p.n && k < L ? lists[k * p.n + number - 1] : 0;
+  }
+  if (tid == 0) {
+    count = items = 0;
+    bound = 1u;
+  }
   for (int w = wv; w < p.W; w += WV) {
     const float sw = p.scores[row0 + w];
     const bool done = p.finished && p.finished[row0 + w];
+    const int len = p.lengths ? p.lengths[row0 + w] : 0;
     const int st = sw == kNegInf ? 2 : done ? 1 : 0;
+    const BeamPart* part = p.part + (row0 + w) * p.parts;  // unspecified where the beam does not go on
+    float m = kNegInf;
+    for (int i = lane; i < p.parts; i += kWave) m = fmaxf(m, part[i].m);
+    m = wave_max(m);
     double l = 0.0;
-    if (st == 0) {
-      const BeamPart* part = p.part + (row0 + w) * p.parts;
-      float m = kNegInf;
-      for (int i = lane; i < p.parts; i += kWave) m = fmaxf(m, part[i].m);
-      m = wave_max(m);
+    if (st == 0 && m != kNegInf) {
       double s = 0.0;
       for (int i = lane; i < p.parts; i += kWave)
         if (part[i].m != kNegInf) s += part[i].s * exp((double(part[i].m) - double(m)) * p.inv_t);
-      s = wave_sum_d(s);
-      if (m != kNegInf) l = double(m) * p.inv_t + log(s);
+      l = double(m) * p.inv_t + log(wave_sum_d(s));
     }
     if (lane == 0) {
-      const int len = p.lengths ? p.lengths[row0 + w] : 0;
       lse[w] = l;
       score[w] = double(sw);
       state[w] = st;
       factor[w] = p.alpha != 0.0 ? pow(double(len + (st == 0)), p.alpha) : 1.0;
+      inverse[w] = 1.0 / factor[w];
     }
   }
   __syncthreads();
-  const int per = p.parts * p.n, C = p.W * per;
   auto total_of = [&](int w, uint64_t e) {
     return state[w] == 1 ? score[w] : double(entry_logit<TI>(e)) * p.inv_t - lse[w] + score[w];
+  };
+  auto rank_of = [&](int w, uint64_t e) {
+    const double t = total_of(w, e);
+    return p.alpha != 0.0 ? t / factor[w] : t;
+  };
+  // the rank without its division, in 32 bits; never below the next lower key than rank_of()'s
+  auto key_of = [&](int w, uint64_t e) { return order_key<F32>(float(total_of(w, e) * inverse[w])); };
+  auto head = [&](int k, uint64_t e) {
+    const int w = k / p.parts;
+    return k < L && e != 0 && state[w] == 0 ? key_of(w, e) : 0u;
+  };
+  if (number <= p.n) {
+    uint32_t key[R], ended = 0, top = 0;
+    if (wv == 0 && lane < p.W && state[lane] == 1) ended = key_of(lane, 1);
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      const int k = q * kWave + lane;
+      key[q] = head(k, early[q]);
+      if (k < L) heads[wv][k] = key[q];
+      top = max(top, key[q]);
+    }
+    for (int k = R * kWave + lane; k < L; k += kWave) {
+      const uint32_t more = head(k, lists[k * p.n + number - 1]);
+      heads[wv][k] = more;
+      top = max(top, more);
+    }
+    top = max(top, ended);
+    for (int off = 32; off > 0; off >>= 1) top = max(top, uint32_t(__shfl_xor(int(top), off, kWave)));
+    top = uint32_t(__builtin_amdgcn_readfirstlane(int(top)));
+    const int r = (p.n + number - 1) / number, enough = r + r / 8;
+    uint32_t lo = 0u, hi = top + 1u;  // lo is reached by r or is 0
+    while (hi > lo + 1u) {
+      const uint32_t mid = lo + (hi - lo) / 2;
+      int c = __popcll(__builtin_amdgcn_ballot_w64(ended >= mid));
+#pragma unroll
+      for (int q = 0; q < R; ++q) c += __popcll(__builtin_amdgcn_ballot_w64(key[q] >= mid));
+      for (int k = R * kWave; k < L; k += kWave)
+        c += __popcll(__builtin_amdgcn_ballot_w64(k + lane < L && heads[wv][k + lane] >= mid));
+      if (c >= r) {
+        lo = mid;
+        if (c <= enough) break;
+      } else {
+        hi = mid;
+      }
+    }
+    if (lane == 0) atomicMax(&bound, lo);
+  }
+  __syncthreads();
+  const uint32_t least = bound > 2u ? bound - 2u : 1u;  // two keys less: what multiplying may be off by
+  // of a list whose entries 1, 2, 4, ..., 2^(j - 1) reach the bound, the first 2^j - 1 may
+  for (int l = tid; l < L; l += NT) {
+    int j = 0;
+    while ((1 << j) <= p.n && heads[j][l] >= least) ++j;
+    const int most = min(p.n, (1 << j) - 1);
+    if (most == 0) continue;
+    int at = atomicAdd(&items, most);
+    for (int i = 0; i < most; ++i, ++at)
+      if (at < kWork) work[at] = uint32_t(l) << 8 | uint32_t(i);
+  }
+  __syncthreads();
+  auto consider = [&](int w, uint64_t e) {
+    if (e == 0 || key_of(w, e) < least) return;
+    const int at = atomicAdd(&count, 1);
+    if (at < kSurvivors) {
+      srank[at] = rank_of(w, e);
+      sentry[at] = e;
+      sbeam[at] = w;
+    }
   };
   // candidate i's beam and entry; false where there is none
   auto candidate = [&](int i, int& w, uint64_t& e) {
     if (i < C) {
       w = i / per;
       if (state[w] != 0) return false;
-      e = p.list[row0 * per + i];
+      e = lists[i];
       return e != 0;
     }
     w = i - C;
     e = 1;
     return w < p.W && state[w] == 1;
   };
-  auto rank_of = [&](int w, uint64_t e) {
-    const double t = total_of(w, e);
-    return p.alpha != 0.0 ? t / factor[w] : t;
-  };
-  // ranks in 32 bits keep their order, up to ties: enough to leave most candidates out
-  uint32_t key[NPT];
-#pragma unroll
-  for (int k = 0; k < NPT; ++k) {
-    int w;
-    uint64_t e;
-    key[k] = candidate(k * NT + tid, w, e) ? order_key<F32>(float(rank_of(w, e))) : 0u;
-  }
-  auto reached = [&](uint32_t t) {
-    int c = 0;
-#pragma unroll
-    for (int k = 0; k < NPT; ++k) c += __popcll(__builtin_amdgcn_ballot_w64(key[k] >= t));
-    return block_count<WV>(c, ish);
-  };
-  uint32_t lo = 1u;
-  const int most = p.n + p.n / 4 + 32;
-  int c = reached(lo);
-  if (c > most) {
-    uint32_t hi = 0xffffffffu;
-    while (hi > lo + 1u) {
-      const uint32_t mid = lo + (hi - lo) / 2;
-      const int r = reached(mid);
-      if (r >= p.n) {
-        lo = mid;
-        c = r;
-        if (r <= most) break;
-      } else {
-        hi = mid;
-      }
+  if (items <= kWork) {
+    for (int i = tid; i < items; i += NT) {
+      const int l = int(work[i] >> 8);
+      consider(l / p.parts, lists[l * p.n + int(work[i] & 255u)]);
+    }
+    if (tid < p.W && state[tid] == 1) consider(tid, 1);
+  } else {
+    for (int i = tid; i < C + p.W; i += NT) {
+      int w;
+      uint64_t e;
+      if (candidate(i, w, e)) consider(w, e);
     }
   }
+  __syncthreads();
+  const int c = count;
   const int64_t o = b * p.n;
   auto write = [&](int j, int w, uint64_t e, double rank) {
     const bool done = state[w] == 1;
@@ -324,42 +440,32 @@ __global__ __launch_bounds__(NT) void k_beam_merge(BeamParams p, int64_t b0) {
     if (p.out.finished) p.out.finished[o + j] = done || token == p.eos;
     if (p.out.lengths) p.out.lengths[o + j] = (p.lengths ? p.lengths[row0 + w] : 0) + !done;
   };
-  int found = c;
   if (c <= kSurvivors) {
-#pragma unroll
-    for (int k = 0; k < NPT; ++k) {
-      if (key[k] < lo) continue;
-      int w;
-      uint64_t e;
-      candidate(k * NT + tid, w, e);
-      const int at = atomicAdd(&count, 1);
-      srank[at] = rank_of(w, e);
-      sentry[at] = e;
-      sbeam[at] = w;
-    }
-    __syncthreads();
-    for (int i = tid; i < c; i += NT) {
+    // as many threads to a survivor as there are
+    const int g = c <= NT / 8 ? 8 : c <= NT / 4 ? 4 : c <= NT / 2 ? 2 : 1;
+    for (int i = tid / g; i < c; i += NT / g) {
       const double r = srank[i];
       const uint64_t e = sentry[i];
       const int w = sbeam[i];
       int at = 0;
-      for (int j = 0; j < c; ++j) at += before(srank[j], sbeam[j], sentry[j], r, w, e);
-      if (at < p.n) write(at, w, e, r);
+#pragma unroll 4
+      for (int j = tid % g; j < c; j += g) at += before(srank[j], sbeam[j], sentry[j], r, w, e);
+      for (int off = 1; off < g; off <<= 1) at += __shfl_xor(at, off, kWave);
+      if (tid % g == 0 && at < p.n) write(at, w, e, r);
     }
   } else {
-    // too many ranks that 32 bits do not tell apart: one after the other
+    // too many that the bound does not tell apart (rows of equal logits): one after the other
     double lr = __builtin_huge_val();
     int lw = -1;
     uint64_t le = 0;
-    for (found = 0; found < p.n; ++found) {
+    for (int found = 0; found < p.n; ++found) {
       double br = -__builtin_huge_val();
       int bw = kBeamMax;
       uint64_t be = 0;
-#pragma unroll 1
-      for (int k = 0; k < NPT; ++k) {
+      for (int i = tid; i < C + p.W; i += NT) {
         int w;
         uint64_t e;
-        if (!candidate(k * NT + tid, w, e)) continue;
+        if (!candidate(i, w, e)) continue;
         const double r = rank_of(w, e);
         if (before(lr, lw, le, r, w, e) && before(r, w, e, br, bw, be)) {
           br = r;
@@ -396,7 +502,7 @@ __global__ __launch_bounds__(NT) void k_beam_merge(BeamParams p, int64_t b0) {
       if (tid == 0) write(found, bw, be, br);
     }
   }
-  for (int j = min(found, p.n) + tid; j < p.n; j += NT) {
+  for (int j = min(c, p.n) + tid; j < p.n; j += NT) {
     p.out.parents[o + j] = -1;
     p.out.tokens[o + j] = p.pad;
     if (p.out.scores) p.out.scores[o + j] = kNegInf;
@@ -406,29 +512,24 @@ __global__ __launch_bounds__(NT) void k_beam_merge(BeamParams p, int64_t b0) {
   }
 }
 
-// How rows are cut: threads and vectors per thread of a part's workgroup, parts of a row.
+// How rows are cut: vectors per thread of a part's workgroup, parts of a row.  As long
+// as 1,024 workgroups remain.
 struct Cut {
-  int block, u, parts, len;
+  int u, parts, len;
 };
-Cut cut_rows(DType in, int64_t B, int W, int V, int n) {
+Cut cut_rows(DType in, int64_t B, int W, int V) {
   const int E = in == DType::kBf16 ? 8 : 4;
-  auto of = [&](int block, int u) {
-    const int most = block * u * E, parts = (V + most - 1) / most;
+  for (int u = 8;; u /= 2) {
+    const int most = 256 * u * E, parts = (V + most - 1) / most;
     const int len = ((V + parts - 1) / parts + E - 1) / E * E;
-    return Cut{block, u, (V + len - 1) / len, len};
-  };
-  // as long as 1,024 workgroups remain; no more candidates than the merge takes
-  for (int u = 8; u >= 1; u /= 2) {
-    const Cut c = of(256, u), half = u > 1 ? of(256, u / 2) : c;
-    if (int64_t(W) * c.parts * n + W > kMergeMost * 256) return of(1024, 8);
-    if (u == 1 || B * W * c.parts >= 1024 || int64_t(W) * half.parts * n + W > kMergeMost * 256) return c;
+    const Cut c{u, (V + len - 1) / len, len};
+    if (u == 1 || B * W * c.parts >= 1024 || 2 * W * c.parts + kBeamMax > kLists) return c;
   }
-  return of(1024, 8);
 }
 
 template <class TI>
 hipError_t launch_typed(const BeamArgs& a) {
-  const Cut c = cut_rows(a.in, a.B, a.W, a.V, a.n);
+  const Cut c = cut_rows(a.in, a.B, a.W, a.V);
   BeamParams p{};
   p.z = a.z;
   p.rows = a.B * a.W;
@@ -456,9 +557,7 @@ hipError_t launch_typed(const BeamArgs& a) {
   const int64_t most = (int64_t(1) << 21) / c.parts;
   for (; p.row0 < p.rows; p.row0 += most) {
     const dim3 grid(unsigned((p.rows - p.row0 < most ? p.rows - p.row0 : most) * c.parts));
-    if (c.block == 1024)
-      k_beam_parts<TI, 1024, 8><<<grid, 1024, 0, a.stream>>>(p);
-    else if (c.u == 8)
+    if (c.u == 8)
       k_beam_parts<TI, 256, 8><<<grid, 256, 0, a.stream>>>(p);
     else if (c.u == 4)
       k_beam_parts<TI, 256, 4><<<grid, 256, 0, a.stream>>>(p);
@@ -467,27 +566,15 @@ hipError_t launch_typed(const BeamArgs& a) {
     else
       k_beam_parts<TI, 256, 1><<<grid, 256, 0, a.stream>>>(p);
   }
-  const int64_t cands = int64_t(a.W) * c.parts * a.n + a.W;
-  for (int64_t b0 = 0; b0 < a.B; b0 += int64_t(1) << 21) {
-    const dim3 grid(unsigned(a.B - b0 < (int64_t(1) << 21) ? a.B - b0 : int64_t(1) << 21));
-    if (cands <= 256)
-      k_beam_merge<TI, 256, 1><<<grid, 256, 0, a.stream>>>(p, b0);
-    else if (cands <= 1024)
-      k_beam_merge<TI, 256, 4><<<grid, 256, 0, a.stream>>>(p, b0);
-    else if (cands <= 4096)
-      k_beam_merge<TI, 1024, 4><<<grid, 1024, 0, a.stream>>>(p, b0);
-    else if (cands <= 16384)
-      k_beam_merge<TI, 1024, 16><<<grid, 1024, 0, a.stream>>>(p, b0);
-    else
-      k_beam_merge<TI, 1024, kMergeMost + 1><<<grid, 1024, 0, a.stream>>>(p, b0);
-  }
+  for (int64_t b0 = 0; b0 < a.B; b0 += int64_t(1) << 21)
+    k_beam_merge<TI><<<dim3(unsigned(a.B - b0 < (int64_t(1) << 21) ? a.B - b0 : int64_t(1) << 21)), kMerge, 0, a.stream>>>(p, b0);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t beam_workspace_bytes(DType in, int64_t B, int W, int V, int n) {
-  const Cut c = cut_rows(in, B, W, V, n);
+  const Cut c = cut_rows(in, B, W, V);
   const size_t slots = size_t(B) * size_t(W) * size_t(c.parts);
   return align256(slots * sizeof(BeamPart)) + align256(slots * size_t(n) * sizeof(uint64_t));
 }
