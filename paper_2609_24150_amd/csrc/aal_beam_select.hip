@@ -50,6 +50,28 @@ __device__ __forceinline__ int entry_token(uint64_t e) { return int(0xffffffffu 
 template <class TI>
 __device__ __forceinline__ float entry_logit(uint64_t e) { return key_logit<TI>(uint32_t(e >> 32)); }
 
+// The same within a part (its elements have 14 bits), of a type that compares fast: 30 bits, or a double of
+// 46 bits behind a one.
+template <class TI>
+struct LocalKey {
+  using type = uint32_t;
+  static __device__ __forceinline__ type of(uint32_t key, int at) { return key >> 2 | (0x3fffu - uint32_t(at)); }
+  static __device__ __forceinline__ uint64_t entry(type k, int s0) {
+    return entry_of((k << 2) & 0xffff0000u, s0 + int(0x3fffu - (k & 0x3fffu)));
+  }
+};
+template <>
+struct LocalKey<F32> {
+  using type = double;
+  static __device__ __forceinline__ type of(uint32_t key, int at) {
+    return __builtin_bit_cast(double, 0x3ff0000000000000u | uint64_t(key) << 14 | uint64_t(0x3fffu - uint32_t(at)));
+  }
+  static __device__ __forceinline__ uint64_t entry(type k, int s0) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, k);
+    return entry_of(uint32_t(b >> 14), s0 + int(0x3fffu - (uint32_t(b) & 0x3fffu)));
+  }
+};
+
 template <int WAVES>
 __device__ __forceinline__ int block_count(int wave_value, int* sh) {
   __syncthreads();
@@ -77,7 +99,8 @@ template <class TI, int BLK, int U>
 __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
   constexpr int E = TI::kVec, WV = BLK / kWave;
   constexpr int kShift = 32 - key_bits<TI>();
-  __shared__ __attribute__((aligned(16))) uint64_t cand[kCand];
+  using Key = LocalKey<TI>;
+  __shared__ __attribute__((aligned(16))) typename Key::type cand[kCand];
   __shared__ uint64_t sorted[kCand];
   __shared__ double dsum[WV];
   __shared__ float fsh[WV];
@@ -93,18 +116,18 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
   if (tid == 0) count = vectors = 0;
   u32x4 raw[U];
   float gm[U], m = kNegInf;
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
+  auto vector = [&](int u) {
     const int at = (u * BLK + tid) * E;
-    if (at + E <= len) {
-      raw[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_e2*>(base + at));
-    } else {
-      typename TI::storage v[E];
+    if (at + E <= len) return u32x4(__builtin_nontemporal_load(reinterpret_cast<const u32x4_e2*>(base + at)));
+    typename TI::storage v[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = at + e < len ? base[at + e] : TI::neg_inf();
-      __builtin_memcpy(&raw[u], v, 16);
-    }
-  }
+    for (int e = 0; e < E; ++e) v[e] = at + e < len ? base[at + e] : TI::neg_inf();
+    u32x4 w;
+    __builtin_memcpy(&w, v, 16);
+    return w;
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u) raw[u] = vector(u);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     float x[E];
@@ -133,14 +156,14 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
   // at least n logits reach t, or all finite ones do
   float t = uniform(threshold<TI, WV>(gm, p.n, m, fsh));
   // the vectors that hold some, then their entries, each by a thread of its own
-  auto collect = [&](float from, bool strict) {
+  auto collect = [&](float from) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (gm[u] >= from && gm[u] != kNegInf) {
         const int at = atomicAdd(&vectors, 1);
         if (at < kQueue) {
           queue[at] = raw[u];
-          place[at] = s0 + (u * BLK + tid) * E;
+          place[at] = (u * BLK + tid) * E;
         }
       }
     __syncthreads();
@@ -148,79 +171,90 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
     for (int i = tid; i < min(q, kQueue) * E; i += BLK) {
       const int e = i % E;
       const float x = TI::load1(&queue[i / E], e);
-      if ((strict ? x > from : x >= from) && x != kNegInf) {
+      if (x >= from && x != kNegInf) {
         const int at = atomicAdd(&count, 1);
-        if (at < kCand) cand[at] = entry_of(order_key<TI>(x), place[i / E] + e);
+        if (at < kCand) cand[at] = Key::of(order_key<TI>(x), place[i / E] + e);
       }
     }
     __syncthreads();
     return q > kQueue ? kCand + 1 : count;
   };
-  int c = collect(t, false), left_ties = 0;
+  int c = collect(t), left_ties = 0;
 #pragma unroll
   for (int u = 0; u < U; ++u) pin(raw[u]);
   if (c > kCand) {
-    // ties or clusters: the n-th largest logit itself, and the first of its ties
+    // ties or clusters: the n-th largest logit itself, what lies above it and the first of its ties; the
+    // part is read again, so that the common way keeps its registers
     uint32_t lo = order_key<TI>(kNegInf) >> kShift, hi = (order_key<TI>(m) >> kShift) + 1u;
     while (hi > lo + 1u) {
       const uint32_t mid = lo + (hi - lo) / 2;
       const float f = key_logit<TI>(mid << kShift);
       int reach = 0;
-#pragma unroll
+#pragma unroll 1
       for (int u = 0; u < U; ++u) {
         float x[E];
-        TI::unpack(to_uint4(raw[u]), x);
+        TI::unpack(to_uint4(vector(u)), x);
 #pragma unroll
         for (int e = 0; e < E; ++e) reach += __popcll(__builtin_amdgcn_ballot_w64(x[e] >= f));
       }
       (block_count<WV>(reach, ish) >= p.n ? lo : hi) = mid;
     }
     t = uniform(key_logit<TI>(lo << kShift));
-    if (tid == 0) count = vectors = 0;
+    if (tid == 0) count = 0;
     __syncthreads();
-    c = collect(t, true);
-    if (t != kNegInf) {
-      int ties = 0;  // before this vector's turn
+    int ties = 0;  // before this vector's turn
+#pragma unroll 1
+    for (int u = 0; u < U; ++u) {
+      float x[E];
+      TI::unpack(to_uint4(vector(u)), x);
+      int mine = 0;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float x[E];
-        TI::unpack(to_uint4(raw[u]), x);
-        int mine = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) mine += x[e] == t;
-        int before = mine;
-        for (int off = 1; off < kWave; off <<= 1) {
-          const int o = __shfl_up(before, off, kWave);
-          if (lane >= off) before += o;
-        }
-        __syncthreads();
-        if (lane == kWave - 1) ish[wv] = before;
-        __syncthreads();
-        int at = c + ties + before - mine;
-#pragma unroll
-        for (int i = 0; i < WV; ++i) {
-          if (i < wv) at += ish[i];
-          ties += ish[i];
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (x[e] == t) {
-            if (at < p.n) cand[at] = entry_of(order_key<TI>(t), s0 + (u * BLK + tid) * E + e);
-            ++at;
-          }
+      for (int e = 0; e < E; ++e) {
+        mine += x[e] == t;
+        if (x[e] > t) cand[atomicAdd(&count, 1)] = Key::of(order_key<TI>(x[e]), (u * BLK + tid) * E + e);  // under n of them
       }
-      const int taken = min(p.n - c, ties);
-      left_ties = ties - taken;
-      c += taken;
+      int before = mine;
+      for (int off = 1; off < kWave; off <<= 1) {
+        const int o = __shfl_up(before, off, kWave);
+        if (lane >= off) before += o;
+      }
+      __syncthreads();
+      if (lane == kWave - 1) ish[wv] = before;
+      __syncthreads();
+      int at = ties + before - mine;
+#pragma unroll
+      for (int i = 0; i < WV; ++i) {
+        if (i < wv) at += ish[i];
+        ties += ish[i];
+      }
+      // the first n ties, from the end of the list down
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (x[e] == t) {
+          if (at < p.n) cand[kCand - 1 - at] = Key::of(order_key<TI>(t), (u * BLK + tid) * E + e);
+          ++at;
+        }
     }
+    __syncthreads();
+    c = count;
+    const int taken = t != kNegInf ? min(p.n - c, ties) : 0;
+    left_ties = t != kNegInf ? ties - taken : 0;
+    typename Key::type tie{};
+    if (tid < taken) tie = cand[kCand - 1 - tid];
+    __syncthreads();
+    if (tid < taken) cand[c + tid] = tie;
+    c += taken;
     __syncthreads();
   }
   for (int i = tid; i < c; i += BLK) {
-    const uint64_t mine = cand[i];
+    const auto mine = cand[i];
     int rank = 0;
-#pragma unroll 8
-    for (int j = 0; j < c; ++j) rank += cand[j] > mine;
-    sorted[rank] = mine;
+    int j = 0;
+    for (; j + 8 <= c; j += 8)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) rank += cand[j + k] > mine;
+    for (; j < c; ++j) rank += cand[j] > mine;
+    sorted[rank] = Key::entry(mine, s0);
   }
   // The others' sum of 2^((z - m) sc), sc in two pieces.  z sc_hi - ref takes one rounding, and so does adding
   // z sc_lo; what ref, m sc rounded, is off by is a factor of the whole sum and joins it in 64 bits.
@@ -268,8 +302,21 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
   }
 }
 
-__device__ __forceinline__ bool before(double ra, int ba, uint64_t ea, double rb, int bb, uint64_t eb) {
-  return ra > rb || (ra == rb && (ba < bb || (ba == bb && ea > eb)));
+// What orders candidates of equal rank, the larger first: the lower beam, then the larger entry (a token has 18 bits).
+__device__ __forceinline__ uint64_t tie_of(int w, uint64_t e) {
+  return uint64_t(kBeamMax - 1 - w) << 50 | (e >> 32) << 18 | (uint32_t(e) & 0x3ffffu);
+}
+__device__ __forceinline__ int tie_beam(uint64_t t) { return kBeamMax - 1 - int(t >> 50); }
+__device__ __forceinline__ uint64_t tie_entry(uint64_t t) {
+  return (t >> 18) << 32 | 0xfffc0000u | (uint32_t(t) & 0x3ffffu);
+}
+struct alignas(16) Candidate {
+  double rank;
+  uint64_t tie;
+};
+// without branches: both are read at once
+__device__ __forceinline__ bool before(const Candidate& a, const Candidate& b) {
+  return (a.rank > b.rank) | ((a.rank == b.rank) & (a.tie > b.tie));
 }
 
 // The lists of a request and, behind them, the beams that have ended as lists of one.
@@ -283,9 +330,10 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
   static_assert(WV == 8, "a wave for each i up to 128");
   __shared__ double lse[kBeamMax], factor[kBeamMax], inverse[kBeamMax], score[kBeamMax];
   __shared__ int state[kBeamMax];  // 0 goes on, 1 has ended, 2 has score -inf
-  __shared__ double srank[kSurvivors];
-  __shared__ uint64_t sentry[kSurvivors];
-  __shared__ int sbeam[kSurvivors];
+  __shared__ Candidate chosen[kSurvivors];
+  __shared__ __attribute__((aligned(16))) uint32_t keys[kSurvivors];
+  __shared__ int taken[kSurvivors];
+  __shared__ uint16_t place[kSurvivors];
   __shared__ uint32_t heads[WV][kLists];
   __shared__ uint32_t work[kWork];
   __shared__ uint32_t bound;
@@ -306,24 +354,27 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
     count = items = 0;
     bound = 1u;
   }
-  for (int w = wv; w < p.W; w += WV) {
+  // as many lanes to a beam as its parts ask for and the workgroup has
+  int g = 1;
+  while (g < kWave && g < p.parts && 2 * g * p.W <= NT) g <<= 1;
+  for (int w0 = 0; w0 < p.W; w0 += NT / g) {
+    const int w = w0 + tid / g, sub = tid % g;
+    if (w >= p.W) continue;
     const float sw = p.scores[row0 + w];
     const bool done = p.finished && p.finished[row0 + w];
     const int len = p.lengths ? p.lengths[row0 + w] : 0;
     const int st = sw == kNegInf ? 2 : done ? 1 : 0;
     const BeamPart* part = p.part + (row0 + w) * p.parts;  // unspecified where the beam does not go on
     float m = kNegInf;
-    for (int i = lane; i < p.parts; i += kWave) m = fmaxf(m, part[i].m);
-    m = wave_max(m);
-    double l = 0.0;
-    if (st == 0 && m != kNegInf) {
-      double s = 0.0;
-      for (int i = lane; i < p.parts; i += kWave)
+    for (int i = sub; i < p.parts; i += g) m = fmaxf(m, part[i].m);
+    for (int off = 1; off < g; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
+    double s = 0.0;
+    if (st == 0 && m != kNegInf)
+      for (int i = sub; i < p.parts; i += g)
         if (part[i].m != kNegInf) s += part[i].s * exp((double(part[i].m) - double(m)) * p.inv_t);
-      l = double(m) * p.inv_t + log(wave_sum_d(s));
-    }
-    if (lane == 0) {
-      lse[w] = l;
+    for (int off = 1; off < g; off <<= 1) s += __shfl_xor(s, off, kWave);
+    if (sub == 0) {
+      lse[w] = st == 0 && m != kNegInf ? double(m) * p.inv_t + log(s) : 0.0;
       score[w] = double(sw);
       state[w] = st;
       factor[w] = p.alpha != 0.0 ? pow(double(len + (st == 0)), p.alpha) : 1.0;
@@ -340,8 +391,10 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
   };
   // the rank without its division, in 32 bits; never below the next lower key than rank_of()'s
   auto key_of = [&](int w, uint64_t e) { return order_key<F32>(float(total_of(w, e) * inverse[w])); };
+  const float per_list = 1.f / float(p.parts);
+  auto beam_of = [&](int k) { return int((float(k) + 0.5f) * per_list); };  // k / parts: k is under 2^12
   auto head = [&](int k, uint64_t e) {
-    const int w = k / p.parts;
+    const int w = beam_of(k);
     return k < L && e != 0 && state[w] == 0 ? key_of(w, e) : 0u;
   };
   if (number <= p.n) {
@@ -386,21 +439,17 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
   for (int l = tid; l < L; l += NT) {
     int j = 0;
     while ((1 << j) <= p.n && heads[j][l] >= least) ++j;
-    const int most = min(p.n, (1 << j) - 1);
-    if (most == 0) continue;
-    int at = atomicAdd(&items, most);
-    for (int i = 0; i < most; ++i, ++at)
-      if (at < kWork) work[at] = uint32_t(l) << 8 | uint32_t(i);
+    if (j == 0) continue;
+    const int eights = (min(p.n, (1 << j) - 1) + 7) / 8;
+    int at = atomicAdd(&items, eights);
+    for (int i = 0; i < eights; ++i, ++at)
+      if (at < kWork) work[at] = uint32_t(l) << 4 | uint32_t(i);
   }
   __syncthreads();
   auto consider = [&](int w, uint64_t e) {
     if (e == 0 || key_of(w, e) < least) return;
     const int at = atomicAdd(&count, 1);
-    if (at < kSurvivors) {
-      srank[at] = rank_of(w, e);
-      sentry[at] = e;
-      sbeam[at] = w;
-    }
+    if (at < kSurvivors) chosen[at] = {rank_of(w, e), tie_of(w, e)};
   };
   // candidate i's beam and entry; false where there is none
   auto candidate = [&](int i, int& w, uint64_t& e) {
@@ -415,9 +464,9 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
     return w < p.W && state[w] == 1;
   };
   if (items <= kWork) {
-    for (int i = tid; i < items; i += NT) {
-      const int l = int(work[i] >> 8);
-      consider(l / p.parts, lists[l * p.n + int(work[i] & 255u)]);
+    for (int i = tid; i < items * 8; i += NT) {
+      const int l = int(work[i / 8] >> 4), k = int(work[i / 8] & 15u) * 8 + i % 8, w = beam_of(l);
+      if (k < p.n && state[w] == 0) consider(w, lists[l * p.n + k]);
     }
     if (tid < p.W && state[tid] == 1) consider(tid, 1);
   } else {
@@ -430,76 +479,77 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
   __syncthreads();
   const int c = count;
   const int64_t o = b * p.n;
-  auto write = [&](int j, int w, uint64_t e, double rank) {
+  auto write = [&](int j, const Candidate& c) {
+    const int w = tie_beam(c.tie);
+    const uint64_t e = tie_entry(c.tie);
     const bool done = state[w] == 1;
     const int token = done ? p.pad : entry_token(e);
     p.out.parents[o + j] = w;
     p.out.tokens[o + j] = token;
     if (p.out.scores) p.out.scores[o + j] = float(total_of(w, e));
-    if (p.out.rank) p.out.rank[o + j] = float(rank);
+    if (p.out.rank) p.out.rank[o + j] = float(c.rank);
     if (p.out.finished) p.out.finished[o + j] = done || token == p.eos;
     if (p.out.lengths) p.out.lengths[o + j] = (p.lengths ? p.lengths[row0 + w] : 0) + !done;
   };
   if (c <= kSurvivors) {
-    // as many threads to a survivor as there are
+    // counted by their 32-bit keys; those that share one, by what they are
+    for (int i = tid; i < c; i += NT) keys[i] = order_key<F32>(float(chosen[i].rank));
+    for (int i = c + tid; i < ((c + 7) & ~7); i += NT) keys[i] = 0u;
+    for (int i = tid; i < c; i += NT) taken[i] = 0;
+    __syncthreads();
+    // as many threads to one as there are
     const int g = c <= NT / 8 ? 8 : c <= NT / 4 ? 4 : c <= NT / 2 ? 2 : 1;
     for (int i = tid / g; i < c; i += NT / g) {
-      const double r = srank[i];
-      const uint64_t e = sentry[i];
-      const int w = sbeam[i];
+      const uint32_t mine = keys[i];
       int at = 0;
-#pragma unroll 4
-      for (int j = tid % g; j < c; j += g) at += before(srank[j], sbeam[j], sentry[j], r, w, e);
+      for (int j = tid % g * 8; j < c; j += g * 8)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) at += keys[j + k] > mine;
       for (int off = 1; off < g; off <<= 1) at += __shfl_xor(at, off, kWave);
-      if (tid % g == 0 && at < p.n) write(at, w, e, r);
+      if (tid % g == 0) {
+        place[i] = uint16_t(at);
+        atomicAdd(&taken[at], 1);
+      }
+    }
+    __syncthreads();
+    for (int i = tid; i < c; i += NT) {
+      const Candidate mine = chosen[i];
+      int at = place[i];
+      if (at >= p.n) continue;
+      if (taken[at] > 1) {
+        const uint32_t key = keys[i];
+        for (int j = 0; j < c; j += 8) {
+          uint32_t same = 0;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) same |= keys[j + k] == key ? 1u << k : 0u;
+          for (; same; same &= same - 1u) at += before(chosen[j + __builtin_ctz(same)], mine);
+        }
+      }
+      if (at < p.n) write(at, mine);
     }
   } else {
     // too many that the bound does not tell apart (rows of equal logits): one after the other
-    double lr = __builtin_huge_val();
-    int lw = -1;
-    uint64_t le = 0;
+    Candidate last{__builtin_huge_val(), ~uint64_t(0)};
     for (int found = 0; found < p.n; ++found) {
-      double br = -__builtin_huge_val();
-      int bw = kBeamMax;
-      uint64_t be = 0;
+      Candidate best{-__builtin_huge_val(), 0};
       for (int i = tid; i < C + p.W; i += NT) {
         int w;
         uint64_t e;
         if (!candidate(i, w, e)) continue;
-        const double r = rank_of(w, e);
-        if (before(lr, lw, le, r, w, e) && before(r, w, e, br, bw, be)) {
-          br = r;
-          bw = w;
-          be = e;
-        }
+        const Candidate c{rank_of(w, e), tie_of(w, e)};
+        if (before(last, c) && before(c, best)) best = c;
       }
       for (int off = 32; off > 0; off >>= 1) {
-        const double r = __shfl_xor(br, off, kWave);
-        const int w = __shfl_xor(bw, off, kWave);
-        const uint64_t e = uint64_t(__shfl_xor((unsigned long long)be, off, kWave));
-        if (before(r, w, e, br, bw, be)) {
-          br = r;
-          bw = w;
-          be = e;
-        }
+        const Candidate c{__shfl_xor(best.rank, off, kWave), uint64_t(__shfl_xor((unsigned long long)best.tie, off, kWave))};
+        if (before(c, best)) best = c;
       }
       __syncthreads();
-      if (lane == 0) {
-        srank[wv] = br;
-        sbeam[wv] = bw;
-        sentry[wv] = be;
-      }
+      if (lane == 0) chosen[wv] = best;
       __syncthreads();
       for (int i = 0; i < WV; ++i)
-        if (before(srank[i], sbeam[i], sentry[i], br, bw, be)) {
-          br = srank[i];
-          bw = sbeam[i];
-          be = sentry[i];
-        }
-      lr = br;
-      lw = bw;
-      le = be;
-      if (tid == 0) write(found, bw, be, br);
+        if (before(chosen[i], best)) best = chosen[i];
+      last = best;
+      if (tid == 0) write(found, best);
     }
   }
   for (int j = min(c, p.n) + tid; j < p.n; j += NT) {
