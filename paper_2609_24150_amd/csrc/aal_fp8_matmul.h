@@ -30,6 +30,7 @@ struct MatmulParams {
   int ld_a, ld_b, K;
   int blocks;        // of 128 of K
   int per_split;     // blocks of a part
+  int splits;        // parts, none of them empty
   int ra, rb;        // rows of a scale's block, as shifts: 0 or 7
   int e8m0;
   int tiles_m, tiles_n;
@@ -59,6 +60,10 @@ __device__ __forceinline__ float scale_of(uint32_t raw, int e8m0) {
 // to wait for but LDS, which stage_barrier() does.
 __device__ __forceinline__ void load_lds(u32x4 rsrc, uint32_t voff, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "m0");
+}
+// The same for what is read once.
+__device__ __forceinline__ void load_lds_once(u32x4 rsrc, uint32_t voff, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(voff), "s"(rsrc) : "m0");
 }
 __device__ __forceinline__ u32x4 buffer_of(const uint8_t* base, uint32_t bytes) {
   const uint64_t b = reinterpret_cast<uint64_t>(base);
@@ -246,131 +251,117 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
 }
 
 // --------------------------------------------------------------- few rows
-// Up to 16 TM rows of a.  A workgroup takes 64 rows of b, its four waves every fourth block each; b goes from
-// memory to registers, since nothing else reads it, the next block's on its way while one is being multiplied.
+// Up to 16 TM rows of a: b is read once and bounds the time.  A workgroup of four waves takes 128 rows of b and at
+// most kFewBlocks blocks, which run through a ring of kRing stages in LDS, two of them on their way while one is
+// being multiplied.  All its scales are in LDS before that, so that the loop waits for the stages alone.
+constexpr int kFewBlocks = 32, kRing = 3;
+
+template <int N>
+__device__ __forceinline__ void ring_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
 template <bool WIDE, int FA, int FB, bool SQUARE, int TM>
 __global__ __launch_bounds__(256, 2) void k_few_rows(MatmulParams p) {
-  constexpr int TN = 4;
-  __shared__ float sums[4][16 * TM][16 * TN + 1];
+  constexpr int BN = 128, BM = 32, RP = 32, kLoads = (BN + BM) / RP, SN = SQUARE ? 1 : BN;
+  static_assert(kRing == 3, "one stage is waited for while another is on its way");
+  __shared__ __attribute__((aligned(16))) uint8_t tile[kRing][(BN + BM) * 128];
+  __shared__ float scale_m[kFewBlocks][BM];
+  __shared__ __attribute__((aligned(16))) float scale_n[kFewBlocks][SN];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l = lane & 15, h = lane >> 4;
-  const int64_t n0 = int64_t(blockIdx.x) * (16 * TN);
+  const int64_t n0 = int64_t(blockIdx.x) * BN;
+  const int left_n = int(min(int64_t(BN), p.N - n0)), M = int(p.M);
   const int j0 = blockIdx.y * p.per_split, j1 = min(p.blocks, j0 + p.per_split);
-  // rows behind the last one repeat it: what they give is not stored
-  const uint8_t* ra[TM];
-  const uint8_t* rb[TN];
-  int64_t sm[TM], sn[TN];
+  const u32x4 ra = buffer_of(p.a, uint32_t(M) * uint32_t(p.ld_a));
+  const u32x4 rb = buffer_of(p.b + n0 * p.ld_b, uint32_t(left_n) * uint32_t(p.ld_b));
+  const int row = tid >> 3, piece = ((tid & 7) ^ (row & 7)) << 4;
+  const uint32_t va = uint32_t(row) * uint32_t(p.ld_a) + piece, vb = uint32_t(row) * uint32_t(p.ld_b) + piece;
+  const uint32_t lds0 = uint32_t(reinterpret_cast<uintptr_t>((lds_t*)&tile[0][0])) + wave * 1024;
+  // workgroups start at blocks of their own: rows of one length would have them all at the same memory channels
+  const int count = j1 - j0, turn = int(blockIdx.x % uint32_t(count));
+  auto block = [&](int i) { return i + turn < count ? j0 + i + turn : j0 + i + turn - count; };
+  auto load = [&](int i, int to) {
+    const uint32_t k = uint32_t(block(i)) * 128u, base = lds0 + uint32_t(to) * ((BN + BM) * 128);
 #pragma unroll
-  for (int t = 0; t < TM; ++t) {
-    const int64_t m = min(int64_t(t * 16 + l), p.M - 1);
-    ra[t] = p.a + m * p.ld_a;
-    sm[t] = (m >> p.ra) * p.sa_row;
+    for (int r = 0; r < BN / RP; ++r) load_lds_once(rb, vb + (uint32_t(r * RP) * uint32_t(p.ld_b) + k), base + r * RP * 128);
+    load_lds(ra, va + k, base + BN * 128);
+  };
+  for (int i = tid; i < (j1 - j0) * BM; i += 256) {
+    const int j = i / BM, m = min(i % BM, M - 1);
+    scale_m[j][i % BM] = scale_of(raw_scale(p.sa, int64_t(m >> p.ra) * p.sa_row + (j0 + j) * p.sa_block, p.e8m0), p.e8m0);
   }
-#pragma unroll
-  for (int t = 0; t < TN; ++t) {
-    const int64_t n = min(n0 + t * 16 + l, p.N - 1);
-    rb[t] = p.b + n * p.ld_b;
-    sn[t] = (n >> p.rb) * p.sb_row;
+  for (int i = tid; i < (j1 - j0) * SN; i += 256) {
+    const int j = i / SN, n = min(i % SN, left_n - 1);
+    scale_n[j][i % SN] = scale_of(raw_scale(p.sb, ((n0 + n) >> p.rb) * p.sb_row + (j0 + j) * p.sb_block, p.e8m0), p.e8m0);
   }
-  struct Block {
-    u32x4 a[TM][2], b[TN][2];
-    uint32_t fa[TM], fb[SQUARE ? 1 : TN];
-  };
-  // a lane's 32 bytes of a row: 16-byte pieces h and 4 + h, the same of either operand
-  auto load = [&](int j, Block& r) {
-    const int k = j * 128 + h * 16;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const bool in = k + i * 64 < p.K;
-#pragma unroll
-      for (int t = 0; t < TN; ++t)
-        r.b[t][i] = in ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(rb[t] + k + i * 64)) : u32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int t = 0; t < TM; ++t) r.a[t][i] = in ? *reinterpret_cast<const u32x4*>(ra[t] + k + i * 64) : u32x4{0, 0, 0, 0};
-    }
-#pragma unroll
-    for (int t = 0; t < TM; ++t) r.fa[t] = raw_scale(p.sa, sm[t] + j * p.sa_block, p.e8m0);
-#pragma unroll
-    for (int t = 0; t < (SQUARE ? 1 : TN); ++t) r.fb[t] = raw_scale(p.sb, sn[t] + j * p.sb_block, p.e8m0);
-  };
-  // bytes behind K, which only the last block has
-  auto clear = [&](u32x4& v, int k) {
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const int n = p.K - k - 4 * w;
-      v[w] = n >= 4 ? v[w] : n <= 0 ? 0u : v[w] & ((1u << (8 * n)) - 1u);
-    }
-  };
-  auto join = [](const u32x4& a, const u32x4& b) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  load(0, 0);
+  if (count > 1) load(1, 1);
+  const int lo = ((2 * h) ^ (l & 7)) << 4, hi = ((2 * h + 1) ^ (l & 7)) << 4;
+  auto fragment = [&](const uint8_t* at) {
+    const u32x4 a = *reinterpret_cast<const u32x4*>(at + lo), b = *reinterpret_cast<const u32x4*>(at + hi);
     return i32x8{int(a.x), int(a.y), int(a.z), int(a.w), int(b.x), int(b.y), int(b.z), int(b.w)};
   };
-  f32x4 acc[TN][TM];
+  f32x4 acc[2][TM];
 #pragma unroll
-  for (int n = 0; n < TN; ++n)
+  for (int n = 0; n < 2; ++n)
 #pragma unroll
     for (int m = 0; m < TM; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto multiply = [&](int j, Block& r) {
+  int at = 0;  // i's stage
+  for (int i = 0; i < count; ++i) {
+    const int j = block(i);
+    if (i + 1 < count)
+      ring_barrier<kLoads>();
+    else
+      ring_barrier<0>();
+    if (i + 2 < count) load(i + 2, at == 0 ? 2 : at - 1);
+    uint8_t* stage = tile[at];
     if ((p.K & 127) && j == p.blocks - 1) {
+      // K ends inside the block: zeros for what lies behind it
+      for (int r = tid; r < BN + BM; r += 256)
+        for (int b = p.K & 127; b < 128; ++b) stage[r * 128 + (((b >> 4) ^ (r & 7)) << 4) + (b & 15)] = 0;
+      __syncthreads();
+    }
+    const uint8_t* tb = stage + (wave * 32 + l) * 128;
+    const uint8_t* ta = stage + (BN + l) * 128;
+    const i32x8 xb[2] = {fragment(tb), fragment(tb + 16 * 128)};
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+    for (int m = 0; m < TM; ++m) {
+      const i32x8 xa = fragment(ta + m * 16 * 128);
+      const float fa = scale_m[j - j0][m * 16 + l];
 #pragma unroll
-        for (int t = 0; t < TM; ++t) clear(r.a[t][i], j * 128 + h * 16 + i * 64);
+      for (int n = 0; n < 2; ++n) {
+        const f32x4 t = dot128<WIDE, FB, FA>(xb[n], xa);
+        f32x4 fb;
+        if constexpr (SQUARE)
+          fb = f32x4{1.f, 1.f, 1.f, 1.f} * scale_n[j - j0][0];
+        else
+          fb = *reinterpret_cast<const f32x4*>(&scale_n[j - j0][wave * 32 + n * 16 + h * 4]);
 #pragma unroll
-        for (int t = 0; t < TN; ++t) clear(r.b[t][i], j * 128 + h * 16 + i * 64);
+        for (int i = 0; i < 4; ++i) acc[n][m][i] = __builtin_fmaf(t[i], fa * fb[i], acc[n][m][i]);
       }
     }
-#pragma unroll
-    for (int n = 0; n < TN; ++n) {
-      // with a scale for each row of b: the lane that has row l's gives it to those that hold its result
-      const float fb = scale_of(r.fb[SQUARE ? 0 : n], p.e8m0);
-      float fi[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) fi[i] = SQUARE ? fb : __shfl(fb, h * 4 + i, kWave);
-#pragma unroll
-      for (int m = 0; m < TM; ++m) {
-        const f32x4 t = dot128<WIDE, FB, FA>(join(r.b[n][0], r.b[n][1]), join(r.a[m][0], r.a[m][1]));
-        const float fa = scale_of(r.fa[m], p.e8m0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[n][m][i] = __builtin_fmaf(t[i], fa * fi[i], acc[n][m][i]);
-      }
-    }
-  };
-  Block one, two;
-  int j = j0 + wave;
-  if (j < j1) load(j, one);
-  while (j < j1) {
-    if (j + 4 < j1) load(j + 4, two);
-    multiply(j, one);
-    j += 4;
-    if (j >= j1) break;
-    if (j + 4 < j1) load(j + 4, one);
-    multiply(j, two);
-    j += 4;
+    at = at == 2 ? 0 : at + 1;
   }
-#pragma unroll
-  for (int n = 0; n < TN; ++n)
-#pragma unroll
-    for (int m = 0; m < TM; ++m)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sums[wave][m * 16 + l][n * 16 + h * 4 + i] = acc[n][m][i];
-  __syncthreads();
   const bool whole = gridDim.y == 1;
   void* c = whole ? p.c : p.part + int64_t(blockIdx.y) * p.M * p.N;
   const bool bf16 = whole && p.out_bf16;
-  const int64_t n = n0 + lane;
-  if (n >= p.N) return;
-  for (int r = wave; r < p.M; r += 4) {
-    const float s = (sums[0][r][lane] + sums[1][r][lane]) + (sums[2][r][lane] + sums[3][r][lane]);
-    if (bf16)
-      GBf16::store1(c, int64_t(r) * p.N + n, s);
-    else
-      GF32::store1(c, int64_t(r) * p.N + n, s);
+#pragma unroll
+  for (int m = 0; m < TM; ++m) {
+    const int64_t gm = m * 16 + l;
+    if (gm >= p.M) continue;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const int64_t gn = n0 + wave * 32 + n * 16 + h * 4;
+      if (gn < p.N) store4(c, gm * p.N + gn, acc[n][m][0], acc[n][m][1], acc[n][m][2], acc[n][m][3], p.N - gn, bf16);
+    }
   }
 }
 
 template <bool WIDE, int FA, int FB, bool SQUARE>
 hipError_t launch_square(const MatmulParams& p, const MatmulPlan& plan, hipStream_t stream) {
-  const dim3 grid(unsigned(int64_t(p.tiles_m) * p.tiles_n), unsigned(plan.splits));
+  const dim3 grid(unsigned(int64_t(p.tiles_m) * p.tiles_n), unsigned(p.splits));
   if (plan.kind == 0 && p.M <= 16)
     k_few_rows<WIDE, FA, FB, SQUARE, 1><<<grid, 256, 0, stream>>>(p);
   else if (plan.kind == 0)

@@ -23,7 +23,7 @@ MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, bool wide) {
     const int64_t s = std::min(want / std::max<int64_t>(groups, 1), blocks / least);
     return int(std::max<int64_t>(1, std::min<int64_t>(s, 64)));
   };
-  if (M <= 32) return {0, splits(up(N, 64), 4 * kCus, 16)};
+  if (M <= 32) return {0, int(std::max<int64_t>(up(blocks, kFewBlocks), splits(up(N, 128), 4 * kCus, 8)))};
   const int64_t large = up(M, 256) * up(N, 256), small = up(M, 128) * up(N, 128);
   const int sl = splits(large, kCus, 8), ss = splits(small, 2 * kCus, 8);
   // turns of the chip times the work of a tile; small tiles take more LDS traffic per result
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void k_join(const float* part, int64_t n, int 
 }  // namespace
 
 size_t matmul_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-  const int splits = std::max(plan_of(M, N, K, false).splits, plan_of(M, N, K, true).splits);
+  const int splits = std::max(plan_of(M, N, K, false).splits, plan_of(M, N, K, true).splits);  // an upper bound
   return splits > 1 ? align256(size_t(splits) * size_t(M) * size_t(N) * sizeof(float)) : 0;
 }
 
@@ -68,10 +68,11 @@ hipError_t launch_matmul(const MatmulArgs& a) {
   p.K = int(a.K);
   p.blocks = int(up(a.K, kFp8Block));
   p.per_split = int(up(p.blocks, plan.splits));
+  p.splits = int(up(p.blocks, p.per_split));
   p.ra = a.a.block_rows == 1 ? 0 : 7;
   p.rb = a.b.block_rows == 1 ? 0 : 7;
   p.e8m0 = a.st == Scale::kE8M0;
-  const int64_t bm = plan.kind == 0 ? 32 : plan.kind == 1 ? 128 : 256, bn = plan.kind == 0 ? 64 : bm;
+  const int64_t bm = plan.kind == 0 ? 32 : plan.kind == 1 ? 128 : 256, bn = plan.kind == 0 ? 128 : bm;
   p.tiles_m = int(up(a.M, bm));
   p.tiles_n = int(up(a.N, bn));
   p.c = a.c;
@@ -82,9 +83,9 @@ hipError_t launch_matmul(const MatmulArgs& a) {
     e = a.b.format == 0 ? launch_matmul_formats<0, 0>(a, p, plan) : launch_matmul_formats<0, 1>(a, p, plan);
   else
     e = a.b.format == 0 ? launch_matmul_formats<1, 0>(a, p, plan) : launch_matmul_formats<1, 1>(a, p, plan);
-  if (e != hipSuccess || plan.splits == 1) return e;
+  if (e != hipSuccess || p.splits == 1) return e;
   const int64_t n = a.M * a.N;
-  k_join<<<dim3(unsigned(up(n, 1024))), 256, 0, a.stream>>>(p.part, n, plan.splits, a.c, p.out_bf16);
+  k_join<<<dim3(unsigned(up(n, 1024))), 256, 0, a.stream>>>(p.part, n, p.splits, a.c, p.out_bf16);
   return hipGetLastError();
 }
 
