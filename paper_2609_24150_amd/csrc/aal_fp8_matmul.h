@@ -13,6 +13,8 @@
 
 namespace aal {
 
+constexpr unsigned kCus = 256;  // of an MI355X: workgroups of tiles of 256 x 256 that run at once, of 128 x 128 twice as many
+
 // How a product is cut (plan_of): few rows of a, or tiles of 128 or 256 in both directions; the inner
 // dimension in `splits` parts, whose sums are joined by a second kernel.
 struct MatmulPlan {
@@ -103,10 +105,18 @@ __device__ __forceinline__ void stage_barrier() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// A stage in LDS has the 128 bytes of each row side by side, the 16-byte piece i of row r at place i ^ r / 2 % 8: they are
+// loaded as whole lines, and the 16 lanes that read at a time, rows l of pieces h and h + 1, meet none of the 64 banks
+// twice.  A lane multiplies pieces h and h + 4 of its row, which are no neighbours in K, but the same of either operand.
+// (Pieces 2 h and 2 h + 1 met four banks twice in every read, a third of LDS's time; an order without any swizzle that
+// loads half lines took 5.6 ms for 8,192 x 128,256 x 4,096 instead of 4.4.)
+__device__ __forceinline__ int place_in_stage(int row, int byte) {
+  return row * 128 + (((byte >> 4) ^ ((row >> 1) & 7)) << 4) + (byte & 15);
+}
+
 // ------------------------------------------------------------------ tiles
 // A workgroup of WN x WM waves makes 16 TN WN x 16 TM WM results.  Both operands' rows of a block, 128 bytes
-// each, are loaded straight into LDS, the next block's while one is being multiplied; 16-byte pieces
-// of row r stand at place (piece ^ r % 8), so that the 8 lanes that read at a time meet no bank twice.
+// each, are loaded straight into LDS, the next block's while one is being multiplied.
 template <bool WIDE, int FA, int FB, bool SQUARE, int TN, int TM, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
   constexpr int NT = 64 * WN * WM, BN = 16 * TN * WN, BM = 16 * TM * WM, RP = NT / 8;  // RP: rows of a round of loads
@@ -116,49 +126,61 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
   __shared__ __attribute__((aligned(16))) float scales[2][BN + BM];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l = lane & 15, h = lane >> 4;
-  // Workgroups go round over the 8 XCDs: each takes a stretch of tiles of its own, in which
-  // groups of 8 tiles down run through all of those across, so that its L2 serves both operands' panels.
-  const int total = p.tiles_m * p.tiles_n, id = blockIdx.x, x = id & 7, q = total >> 3, rest = total & 7;
-  const int at = x * q + min(x, rest) + (id >> 3);
-  const int group = at / (8 * p.tiles_n), first = group * 8, rows = min(8, p.tiles_m - first);
-  const int in = at - group * 8 * p.tiles_n, tm = first + in % rows, tn = in / rows;
-  const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
-  const int left_m = int(min(int64_t(BM), p.M - m0)), left_n = int(min(int64_t(BN), p.N - n0));
-  // rows behind the last one lie outside the buffers and are zeros
-  const u32x4 ra = buffer_of(p.a + m0 * p.ld_a, uint32_t(left_m) * uint32_t(p.ld_a));
-  const u32x4 rb = buffer_of(p.b + n0 * p.ld_b, uint32_t(left_n) * uint32_t(p.ld_b));
-  const int row = tid >> 3, piece = ((tid & 7) ^ (row & 7)) << 4;
-  const uint32_t va = uint32_t(row) * uint32_t(p.ld_a) + piece, vb = uint32_t(row) * uint32_t(p.ld_b) + piece;
-  const int j0 = blockIdx.y * p.per_split, j1 = min(p.blocks, j0 + p.per_split);
-  const uint32_t lds0 = uint32_t(reinterpret_cast<uintptr_t>((lds_t*)&tile[0][0])) + wave * 1024;
-  auto load = [&](int j, int to) {
-    const uint32_t k = uint32_t(j) * 128u, base = lds0 + uint32_t(to) * ((BN + BM) * 128);
-#pragma unroll
-    for (int i = 0; i < BN / RP; ++i) load_lds(rb, vb + (uint32_t(i * RP) * uint32_t(p.ld_b) + k), base + i * RP * 128);
-#pragma unroll
-    for (int i = 0; i < BM / RP; ++i) load_lds(ra, va + (uint32_t(i * RP) * uint32_t(p.ld_a) + k), base + (BN + i * RP) * 128);
+  // A tile of c, and the blocks of a part of K.  Workgroups go round over the 8 XCDs: each XCD takes a stretch of
+  // tiles of its own, in which groups of 8 tiles down run through all of those across, so that its L2 serves
+  // both operands' panels.
+  struct Place {
+    int down, across, split, j0, j1;
   };
+  struct Sources {
+    u32x4 ra, rb;
+    int64_t scale;
+  };
+  const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.splits;
   // a thread has one scale: of the first BN threads one of b's rows, of the others one of a's
   const bool is_b = wave < BN / 64;
   const void* scale_base = is_b ? p.sb : p.sa;
   const int64_t scale_step = is_b ? p.sb_block : p.sa_block;
-  const int64_t scale_row = is_b ? ((n0 + min(tid, left_n - 1)) >> p.rb) * p.sb_row
-                                 : ((m0 + min(tid - BN, left_m - 1)) >> p.ra) * p.sa_row;
+  auto place_of = [&](int id) {
+    const int x = id & 7, q = total >> 3, rest = total & 7, seq = x * q + min(x, rest) + (id >> 3);
+    const int split = seq / tiles, at = seq - split * tiles;
+    const int group = at / (8 * p.tiles_n), first = group * 8, rows = min(8, p.tiles_m - first);
+    const int in = at - group * 8 * p.tiles_n, across = in / rows, j0 = split * p.per_split;
+    return Place{first + in - across * rows, across, split, j0, min(p.blocks, j0 + p.per_split)};
+  };
+  auto sources_of = [&](const Place& t) {
+    const int64_t m0 = int64_t(t.down) * BM, n0 = int64_t(t.across) * BN;
+    const int left_m = int(min(int64_t(BM), p.M - m0)), left_n = int(min(int64_t(BN), p.N - n0));
+    // rows behind the last one lie outside the buffers and are zeros
+    return Sources{buffer_of(p.a + m0 * p.ld_a, uint32_t(left_m) * uint32_t(p.ld_a)),
+                   buffer_of(p.b + n0 * p.ld_b, uint32_t(left_n) * uint32_t(p.ld_b)),
+                   is_b ? ((n0 + min(tid, left_n - 1)) >> p.rb) * p.sb_row
+                        : ((m0 + min(tid - BN, left_m - 1)) >> p.ra) * p.sa_row};
+  };
+  const int row = tid >> 3, piece = ((tid & 7) ^ ((row >> 1) & 7)) << 4;
+  const uint32_t va = uint32_t(row) * uint32_t(p.ld_a) + piece, vb = uint32_t(row) * uint32_t(p.ld_b) + piece;
+  const uint32_t lds0 = uint32_t(reinterpret_cast<uintptr_t>((lds_t*)&tile[0][0])) + wave * 1024;
+  auto load = [&](const Sources& t, int j, int to) {
+    const uint32_t k = uint32_t(j) * 128u, base = lds0 + uint32_t(to) * ((BN + BM) * 128);
+#pragma unroll
+    for (int i = 0; i < BN / RP; ++i) load_lds(t.rb, vb + (uint32_t(i * RP) * uint32_t(p.ld_b) + k), base + i * RP * 128);
+#pragma unroll
+    for (int i = 0; i < BM / RP; ++i) load_lds(t.ra, va + (uint32_t(i * RP) * uint32_t(p.ld_a) + k), base + (BN + i * RP) * 128);
+  };
   uint32_t next = 0;
-  auto load_scales = [&](int j) { next = raw_scale(scale_base, scale_row + j * scale_step, p.e8m0); };
+  auto load_scales = [&](const Sources& t, int j) { next = raw_scale(scale_base, t.scale + j * scale_step, p.e8m0); };
   auto put_scales = [&](int to) { scales[to][tid] = scale_of(next, p.e8m0); };
   // K ends inside the last block: zeros for what lies behind it
   auto clear_tail = [&](int to) {
     const int rem = p.K & 127;
     for (int r = tid; r < BN + BM; r += NT) {
-      uint8_t* at = &tile[to][r * 128];
       for (int b = rem; b < 128;) {
-        uint8_t* w = at + (((b >> 4) ^ (r & 7)) << 4);
+        uint8_t* at = &tile[to][place_in_stage(r, b)];
         if ((b & 15) == 0) {
-          *reinterpret_cast<u32x4*>(w) = u32x4{0, 0, 0, 0};
+          *reinterpret_cast<u32x4*>(at) = u32x4{0, 0, 0, 0};
           b += 16;
         } else {
-          w[b & 15] = 0;
+          *at = 0;
           ++b;
         }
       }
@@ -170,25 +192,41 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
   for (int i = 0; i < TN; ++i)
 #pragma unroll
     for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int lo = ((2 * h) ^ (l & 7)) << 4, hi = ((2 * h + 1) ^ (l & 7)) << 4;
+  const int front = (h ^ (l >> 1)) << 4, back = ((h + 4) ^ (l >> 1)) << 4;
   auto fragment = [&](const uint8_t* at) {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(at + lo), b = *reinterpret_cast<const u32x4*>(at + hi);
+    const u32x4 a = *reinterpret_cast<const u32x4*>(at + front), b = *reinterpret_cast<const u32x4*>(at + back);
     return i32x8{int(a.x), int(a.y), int(a.z), int(a.w), int(b.x), int(b.y), int(b.z), int(b.w)};
   };
-  load_scales(j0);
-  load(j0, 0);
+  // The blocks of all tiles that the workgroup takes follow each other without a break: a tile's first ones are
+  // loaded under the last ones of the tile before, and its results are stored under the next tile's.
+  int id = blockIdx.x, cur = 0;
+  Place t = place_of(id);
+  Sources from = sources_of(t);
+  load_scales(from, t.j0);
+  load(from, t.j0, 0);
   put_scales(0);
   stage_barrier();
-  if ((p.K & 127) && j0 == p.blocks - 1) {
+  if ((p.K & 127) && t.j0 == p.blocks - 1) {
     clear_tail(0);
     stage_barrier();
   }
-  for (int j = j0; j < j1; ++j) {
-    const int cur = (j - j0) & 1;
-    const bool more = j + 1 < j1;
+  for (int j = t.j0;;) {
+    const bool last = j + 1 == t.j1;
+    int next_j = j + 1;
+    bool more = true;
+    Place then = t;
+    if (last) {
+      id += gridDim.x;
+      more = id < total;
+      if (more) {
+        then = place_of(id);
+        from = sources_of(then);
+        next_j = then.j0;
+      }
+    }
     if (more) {
-      load_scales(j + 1);
-      load(j + 1, cur ^ 1);
+      load_scales(from, next_j);
+      load(from, next_j, cur ^ 1);
     }
     const uint8_t* tb = tile[cur] + (wn * TN * 16 + l) * 128;
     const uint8_t* ta = tile[cur] + (BN + wm * TM * 16 + l) * 128;
@@ -205,23 +243,23 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
     for (int m = 0; m < TM; ++m) {
       fa[m] = sc[BN + (wm * TM + m) * 16 + l];
       if constexpr (SQUARE) fa[m] *= sc[wn * TN * 16];
-      xa[m] = fragment(ta + m * 16 * 128);
+      xa[m] = fragment(ta + m * 2048);
     }
     // a row of products is added while the next one is in the matrix unit
     i32x8 xb = fragment(tb);
-    f32x4 t[TM], fb{}, fp{};
+    f32x4 made[TM], fb{}, fp{};
 #pragma unroll
     for (int n = 0; n <= TN; ++n) {
       const i32x8 x = xb;
-      if (n + 1 < TN) xb = fragment(tb + (n + 1) * 16 * 128);
+      if (n + 1 < TN) xb = fragment(tb + (n + 1) * 2048);
       if constexpr (!SQUARE)
         if (n < TN) fb = *reinterpret_cast<const f32x4*>(&sc[(wn * TN + n) * 16 + h * 4]);
 #pragma unroll
       for (int m = 0; m < TM; ++m) {
         f32x4 u{};
         if (n < TN) u = dot128<WIDE, FB, FA>(x, xa[m]);
-        if (n > 0) add(n - 1, m, t[m], fp);
-        t[m] = u;
+        if (n > 0) add(n - 1, m, made[m], fp);
+        made[m] = u;
         if constexpr (!WIDE) __builtin_amdgcn_sched_barrier(0);
       }
       fp = fb;
@@ -229,24 +267,32 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
     if (more) {
       put_scales(cur ^ 1);
       stage_barrier();
-      if ((p.K & 127) && j + 1 == p.blocks - 1) {
+      if ((p.K & 127) && next_j == p.blocks - 1) {
         clear_tail(cur ^ 1);
         stage_barrier();
       }
     }
-  }
-  const bool whole = gridDim.y == 1;
-  void* c = whole ? p.c : p.part + int64_t(blockIdx.y) * p.M * p.N;
-  const bool bf16 = whole && p.out_bf16;
+    cur ^= 1;
+    j = next_j;
+    if (!last) continue;
+    const bool whole = p.splits == 1;
+    void* c = whole ? p.c : p.part + t.split * (p.M * p.N);
+    const bool bf16 = whole && p.out_bf16;
 #pragma unroll
-  for (int m = 0; m < TM; ++m) {
-    const int64_t gm = m0 + (wm * TM + m) * 16 + l;
-    if (gm >= p.M) continue;
+    for (int m = 0; m < TM; ++m) {
+      const int64_t gm = int64_t(t.down) * BM + (wm * TM + m) * 16 + l;
+      if (gm < p.M) {
 #pragma unroll
-    for (int n = 0; n < TN; ++n) {
-      const int64_t gn = n0 + (wn * TN + n) * 16 + h * 4;
-      if (gn < p.N) store4(c, gm * p.N + gn, acc[n][m][0], acc[n][m][1], acc[n][m][2], acc[n][m][3], p.N - gn, bf16);
+        for (int n = 0; n < TN; ++n) {
+          const int64_t gn = int64_t(t.across) * BN + (wn * TN + n) * 16 + h * 4;
+          if (gn < p.N) store4(c, gm * p.N + gn, acc[n][m][0], acc[n][m][1], acc[n][m][2], acc[n][m][3], p.N - gn, bf16);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < TN; ++n) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    if (!more) return;
+    t = then;
   }
 }
 
@@ -275,7 +321,7 @@ __global__ __launch_bounds__(256, 2) void k_few_rows(MatmulParams p) {
   const int j0 = blockIdx.y * p.per_split, j1 = min(p.blocks, j0 + p.per_split);
   const u32x4 ra = buffer_of(p.a, uint32_t(M) * uint32_t(p.ld_a));
   const u32x4 rb = buffer_of(p.b + n0 * p.ld_b, uint32_t(left_n) * uint32_t(p.ld_b));
-  const int row = tid >> 3, piece = ((tid & 7) ^ (row & 7)) << 4;
+  const int row = tid >> 3, piece = ((tid & 7) ^ ((row >> 1) & 7)) << 4;
   const uint32_t va = uint32_t(row) * uint32_t(p.ld_a) + piece, vb = uint32_t(row) * uint32_t(p.ld_b) + piece;
   const uint32_t lds0 = uint32_t(reinterpret_cast<uintptr_t>((lds_t*)&tile[0][0])) + wave * 1024;
   // workgroups start at blocks of their own: rows of one length would have them all at the same memory channels
@@ -298,9 +344,9 @@ __global__ __launch_bounds__(256, 2) void k_few_rows(MatmulParams p) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   load(0, 0);
   if (count > 1) load(1, 1);
-  const int lo = ((2 * h) ^ (l & 7)) << 4, hi = ((2 * h + 1) ^ (l & 7)) << 4;
+  const int front = (h ^ (l >> 1)) << 4, back = ((h + 4) ^ (l >> 1)) << 4;
   auto fragment = [&](const uint8_t* at) {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(at + lo), b = *reinterpret_cast<const u32x4*>(at + hi);
+    const u32x4 a = *reinterpret_cast<const u32x4*>(at + front), b = *reinterpret_cast<const u32x4*>(at + back);
     return i32x8{int(a.x), int(a.y), int(a.z), int(a.w), int(b.x), int(b.y), int(b.z), int(b.w)};
   };
   f32x4 acc[2][TM];
@@ -320,15 +366,15 @@ __global__ __launch_bounds__(256, 2) void k_few_rows(MatmulParams p) {
     if ((p.K & 127) && j == p.blocks - 1) {
       // K ends inside the block: zeros for what lies behind it
       for (int r = tid; r < BN + BM; r += 256)
-        for (int b = p.K & 127; b < 128; ++b) stage[r * 128 + (((b >> 4) ^ (r & 7)) << 4) + (b & 15)] = 0;
+        for (int b = p.K & 127; b < 128; ++b) stage[place_in_stage(r, b)] = 0;
       __syncthreads();
     }
     const uint8_t* tb = stage + (wave * 32 + l) * 128;
     const uint8_t* ta = stage + (BN + l) * 128;
-    const i32x8 xb[2] = {fragment(tb), fragment(tb + 16 * 128)};
+    const i32x8 xb[2] = {fragment(tb), fragment(tb + 2048)};
 #pragma unroll
     for (int m = 0; m < TM; ++m) {
-      const i32x8 xa = fragment(ta + m * 16 * 128);
+      const i32x8 xa = fragment(ta + m * 2048);
       const float fa = scale_m[j - j0][m * 16 + l];
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
@@ -361,11 +407,12 @@ __global__ __launch_bounds__(256, 2) void k_few_rows(MatmulParams p) {
 
 template <bool WIDE, int FA, int FB, bool SQUARE>
 hipError_t launch_square(const MatmulParams& p, const MatmulPlan& plan, hipStream_t stream) {
-  const dim3 grid(unsigned(int64_t(p.tiles_m) * p.tiles_n), unsigned(p.splits));
+  const unsigned total = unsigned(int64_t(p.tiles_m) * p.tiles_n * p.splits), most = plan.kind == 1 ? 2 * kCus : kCus;
+  const dim3 grid(total < most ? total : most), few(unsigned(p.tiles_n), unsigned(p.splits));
   if (plan.kind == 0 && p.M <= 16)
-    k_few_rows<WIDE, FA, FB, SQUARE, 1><<<grid, 256, 0, stream>>>(p);
+    k_few_rows<WIDE, FA, FB, SQUARE, 1><<<few, 256, 0, stream>>>(p);
   else if (plan.kind == 0)
-    k_few_rows<WIDE, FA, FB, SQUARE, 2><<<grid, 256, 0, stream>>>(p);
+    k_few_rows<WIDE, FA, FB, SQUARE, 2><<<few, 256, 0, stream>>>(p);
   else if (plan.kind == 1)
     k_tiles<WIDE, FA, FB, SQUARE, 4, 4, 2, 2><<<grid, 256, 0, stream>>>(p);
   else if constexpr (!WIDE)

@@ -12,8 +12,6 @@ extern template hipError_t launch_matmul_formats<1, 1>(const MatmulArgs&, const 
 
 namespace {
 
-constexpr int kCus = 256;
-
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, bool wide) {
