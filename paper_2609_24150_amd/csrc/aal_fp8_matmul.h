@@ -59,13 +59,13 @@ __device__ __forceinline__ float scale_of(uint32_t raw, int e8m0) {
 
 // 16 bytes per lane from base + voff (0 from `bytes` on) into LDS, lane l's at `to` + 16 l.  In assembly, since the
 // compiler takes every later LDS read for one of these bytes and waits; nothing here has a result
-// to wait for but LDS, which stage_barrier() does.
+// to wait for but LDS, which stage_barrier() does.  M0 is read one wait state after it is written at the soonest.
 __device__ __forceinline__ void load_lds(u32x4 rsrc, uint32_t voff, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "m0");
 }
 // The same for what is read once.
 __device__ __forceinline__ void load_lds_once(u32x4 rsrc, uint32_t voff, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(voff), "s"(rsrc) : "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(voff), "s"(rsrc) : "m0");
 }
 __device__ __forceinline__ u32x4 buffer_of(const uint8_t* base, uint32_t bytes) {
   const uint64_t b = reinterpret_cast<uint64_t>(base);
@@ -160,12 +160,13 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
   const int row = tid >> 3, piece = ((tid & 7) ^ ((row >> 1) & 7)) << 4;
   const uint32_t va = uint32_t(row) * uint32_t(p.ld_a) + piece, vb = uint32_t(row) * uint32_t(p.ld_b) + piece;
   const uint32_t lds0 = uint32_t(reinterpret_cast<uintptr_t>((lds_t*)&tile[0][0])) + wave * 1024;
-  auto load = [&](const Sources& t, int j, int to) {
-    const uint32_t k = uint32_t(j) * 128u, base = lds0 + uint32_t(to) * ((BN + BM) * 128);
-#pragma unroll
-    for (int i = 0; i < BN / RP; ++i) load_lds(t.rb, vb + (uint32_t(i * RP) * uint32_t(p.ld_b) + k), base + i * RP * 128);
-#pragma unroll
-    for (int i = 0; i < BM / RP; ++i) load_lds(t.ra, va + (uint32_t(i * RP) * uint32_t(p.ld_a) + k), base + (BN + i * RP) * 128);
+  constexpr int kLoads = (BN + BM) / RP;  // of a stage; the first BN / RP are b's
+  auto load = [&](const Sources& t, int j, int to, int i) {
+    const uint32_t k = uint32_t(j) * 128u, base = lds0 + uint32_t(to) * ((BN + BM) * 128) + i * RP * 128;
+    if (i < BN / RP)
+      load_lds(t.rb, vb + (uint32_t(i * RP) * uint32_t(p.ld_b) + k), base);
+    else
+      load_lds(t.ra, va + (uint32_t(i * RP - BN) * uint32_t(p.ld_a) + k), base);
   };
   uint32_t next = 0;
   auto load_scales = [&](const Sources& t, int j) { next = raw_scale(scale_base, t.scale + j * scale_step, p.e8m0); };
@@ -197,82 +198,110 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
     const u32x4 a = *reinterpret_cast<const u32x4*>(at + front), b = *reinterpret_cast<const u32x4*>(at + back);
     return i32x8{int(a.x), int(a.y), int(a.z), int(a.w), int(b.x), int(b.y), int(b.z), int(b.w)};
   };
-  // The blocks of all tiles that the workgroup takes follow each other without a break: a tile's first ones are
-  // loaded under the last ones of the tile before, and its results are stored under the next tile's.
-  int id = blockIdx.x, cur = 0;
-  Place t = place_of(id);
-  Sources from = sources_of(t);
-  load_scales(from, t.j0);
-  load(from, t.j0, 0);
-  put_scales(0);
-  stage_barrier();
-  if ((p.K & 127) && t.j0 == p.blocks - 1) {
-    clear_tail(0);
+  // The blocks of all tiles that the workgroup takes follow each other without a break, and nothing in it drains at the end
+  // of one: when the last row of products of a block begins, all of the block is in registers; there the workgroup
+  // meets, the next block has arrived, the one after it is sent for into the stage that has become free, and
+  // the next block's first fragments are read into the registers of those that have had their last use.
+  int load_id = blockIdx.x, load_j, stage = 0;
+  Place ahead = place_of(load_id), t = ahead;
+  Sources from = sources_of(ahead);
+  bool live = true;  // there is a block to load
+  load_j = ahead.j0;
+  auto advance = [&] {
+    if (++load_j < ahead.j1) return;
+    load_id += gridDim.x;
+    live = load_id < total;
+    if (!live) return;
+    ahead = place_of(load_id);
+    from = sources_of(ahead);
+    load_j = ahead.j0;
+  };
+  auto send = [&](int to) {
+    load_scales(from, load_j);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(from, load_j, to, i);
+  };
+  auto arrived = [&](int at, int j) {
+    put_scales(at);
     stage_barrier();
+    if ((p.K & 127) && j == p.blocks - 1) {
+      clear_tail(at);
+      stage_barrier();
+    }
+  };
+  send(0);
+  arrived(0, t.j0);
+  advance();
+  if (live) send(1);
+  const int at_b = (wn * TN * 16 + l) * 128, at_a = (BN + wm * TM * 16 + l) * 128;
+  i32x8 xa[TM], xb = fragment(tile[0] + at_b);
+  f32x4 made[TM], fb{}, fp{};
+  float fa[TM];
+  auto scales_b = [&](int at, int n) { return *reinterpret_cast<const f32x4*>(&scales[at][(wn * TN + n) * 16 + h * 4]); };
+  if constexpr (!SQUARE) fb = scales_b(0, 0);
+#pragma unroll
+  for (int m = 0; m < TM; ++m) {
+    xa[m] = fragment(tile[0] + at_a + m * 16 * 128);
+    made[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    fa[m] = 0.f;
   }
+  auto add = [&](int n, int m, const f32x4& t, float f, const f32x4& g) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[n][m][i] = __builtin_fmaf(t[i], SQUARE ? f : f * g[i], acc[n][m][i]);
+    // here, not where the compiler would rather have all of them: 128 registers of products
+    asm volatile("" : "+v"(acc[n][m]));
+  };
+  int id = blockIdx.x;
   for (int j = t.j0;;) {
     const bool last = j + 1 == t.j1;
-    int next_j = j + 1;
-    bool more = true;
+    const bool more = !last || id + int(gridDim.x) < total;
     Place then = t;
-    if (last) {
+    int next_j = j + 1;
+    if (last && more) {
       id += gridDim.x;
-      more = id < total;
-      if (more) {
-        then = place_of(id);
-        from = sources_of(then);
-        next_j = then.j0;
-      }
+      then = place_of(id);
+      next_j = then.j0;
     }
-    if (more) {
-      load_scales(from, next_j);
-      load(from, next_j, cur ^ 1);
-    }
-    const uint8_t* tb = tile[cur] + (wn * TN * 16 + l) * 128;
-    const uint8_t* ta = tile[cur] + (BN + wm * TM * 16 + l) * 128;
-    const float* sc = scales[cur];
-    i32x8 xa[TM];
-    float fa[TM];
-    auto add = [&](int n, int m, const f32x4& t, const f32x4& fb) {
+    const uint8_t* tb = tile[stage] + at_b;
+    const uint8_t* next_b = tile[stage ^ 1] + at_b;
+    const uint8_t* next_a = tile[stage ^ 1] + at_a;
+    float fn[TM];
+    // each row of products is added while the next one is in the matrix unit
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[n][m][i] = __builtin_fmaf(t[i], SQUARE ? fa[m] : fa[m] * fb[i], acc[n][m][i]);
-      // here, not where the compiler would rather have all of them: 128 registers of products
-      asm volatile("" : "+v"(acc[n][m]));
-    };
-#pragma unroll
-    for (int m = 0; m < TM; ++m) {
-      fa[m] = sc[BN + (wm * TM + m) * 16 + l];
-      if constexpr (SQUARE) fa[m] *= sc[wn * TN * 16];
-      xa[m] = fragment(ta + m * 2048);
-    }
-    // a row of products is added while the next one is in the matrix unit
-    i32x8 xb = fragment(tb);
-    f32x4 made[TM], fb{}, fp{};
-#pragma unroll
-    for (int n = 0; n <= TN; ++n) {
+    for (int n = 0; n < TN; ++n) {
       const i32x8 x = xb;
-      if (n + 1 < TN) xb = fragment(tb + (n + 1) * 2048);
-      if constexpr (!SQUARE)
-        if (n < TN) fb = *reinterpret_cast<const f32x4*>(&sc[(wn * TN + n) * 16 + h * 4]);
+      const f32x4 g = fb;
+      if (n == 0) {
+#pragma unroll
+        for (int m = 0; m < TM; ++m) {
+          fn[m] = scales[stage][BN + (wm * TM + m) * 16 + l];
+          if constexpr (SQUARE) fn[m] *= scales[stage][wn * TN * 16];
+        }
+      }
+      if (n + 1 < TN) {
+        xb = fragment(tb + (n + 1) * 16 * 128);
+        if constexpr (!SQUARE) fb = scales_b(stage, n + 1);
+      } else {
+        if (more) {
+          arrived(stage ^ 1, next_j);
+          advance();
+          if (live) send(stage);
+        }
+        xb = fragment(next_b);
+        if constexpr (!SQUARE) fb = scales_b(stage ^ 1, 0);
+      }
 #pragma unroll
       for (int m = 0; m < TM; ++m) {
-        f32x4 u{};
-        if (n < TN) u = dot128<WIDE, FB, FA>(x, xa[m]);
-        if (n > 0) add(n - 1, m, made[m], fp);
+        const f32x4 u = dot128<WIDE, FB, FA>(x, xa[m]);
+        if (n + 1 == TN) xa[m] = fragment(next_a + m * 16 * 128);
+        add(n > 0 ? n - 1 : TN - 1, m, made[m], fa[m], fp);
         made[m] = u;
+        if (n == 0) fa[m] = fn[m];
         if constexpr (!WIDE) __builtin_amdgcn_sched_barrier(0);
       }
-      fp = fb;
+      fp = g;
     }
-    if (more) {
-      put_scales(cur ^ 1);
-      stage_barrier();
-      if ((p.K & 127) && next_j == p.blocks - 1) {
-        clear_tail(cur ^ 1);
-        stage_barrier();
-      }
-    }
-    cur ^= 1;
+    stage ^= 1;
     j = next_j;
     if (!last) continue;
     const bool whole = p.splits == 1;
@@ -280,6 +309,9 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
     const bool bf16 = whole && p.out_bf16;
 #pragma unroll
     for (int m = 0; m < TM; ++m) {
+      add(TN - 1, m, made[m], fa[m], fp);
+      made[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+      fa[m] = 0.f;
       const int64_t gm = int64_t(t.down) * BM + (wm * TM + m) * 16 + l;
       if (gm < p.M) {
 #pragma unroll
@@ -291,6 +323,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
 #pragma unroll
       for (int n = 0; n < TN; ++n) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    fp = f32x4{0.f, 0.f, 0.f, 0.f};
     if (!more) return;
     t = then;
   }
