@@ -216,10 +216,14 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
     from = sources_of(ahead);
     load_j = ahead.j0;
   };
-  auto send = [&](int to) {
-    load_scales(from, load_j);
+  // A wave waits for each of its loads to be taken, and all eight waves send theirs at once: the first kFirst in the
+  // last row and kSend of them in each of the next block's first ones leave the matrix unit at work, and
+  // time to arrive (all eight in the last row: 1,000 of a block's 4,000 cycles; one a row: they come too late).
+  constexpr int kFirst = TN == 8 ? 4 : 3, kSend = TN == 8 ? 2 : 3;
+  auto send = [&](int to, int first, int count) {
+    if (first == 0) load_scales(from, load_j);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(from, load_j, to, i);
+    for (int i = first; i < first + count && i < kLoads; ++i) load(from, load_j, to, i);
   };
   auto arrived = [&](int at, int j) {
     put_scales(at);
@@ -229,12 +233,13 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
       stage_barrier();
     }
   };
-  send(0);
+  send(0, 0, kLoads);
   arrived(0, t.j0);
   advance();
-  if (live) send(1);
+  if (live) send(1, 0, kLoads);
+  bool sending = false;  // a block's loads are under way
   const int at_b = (wn * TN * 16 + l) * 128, at_a = (BN + wm * TM * 16 + l) * 128;
-  i32x8 xa[TM], xb = fragment(tile[0] + at_b);
+  i32x8 xa[TM], xb[2] = {fragment(tile[0] + at_b), fragment(tile[0] + at_b + 16 * 128)};
   f32x4 made[TM], fb{}, fp{};
   float fa[TM];
   auto scales_b = [&](int at, int n) { return *reinterpret_cast<const f32x4*>(&scales[at][(wn * TN + n) * 16 + h * 4]); };
@@ -269,7 +274,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
     // each row of products is added while the next one is in the matrix unit
 #pragma unroll
     for (int n = 0; n < TN; ++n) {
-      const i32x8 x = xb;
+      const i32x8 x = xb[n & 1];
       const f32x4 g = fb;
       if (n == 0) {
 #pragma unroll
@@ -278,21 +283,28 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
           if constexpr (SQUARE) fn[m] *= scales[stage][wn * TN * 16];
         }
       }
+      if (n + 2 < TN) xb[n & 1] = fragment(tb + (n + 2) * 16 * 128);
       if (n + 1 < TN) {
-        xb = fragment(tb + (n + 1) * 16 * 128);
         if constexpr (!SQUARE) fb = scales_b(stage, n + 1);
       } else {
         if (more) {
           arrived(stage ^ 1, next_j);
           advance();
-          if (live) send(stage);
+          sending = live;
+        } else {
+          sending = false;
         }
-        xb = fragment(next_b);
+        xb[0] = fragment(next_b);
+        xb[1] = fragment(next_b + 16 * 128);
         if constexpr (!SQUARE) fb = scales_b(stage ^ 1, 0);
       }
 #pragma unroll
       for (int m = 0; m < TM; ++m) {
         const f32x4 u = dot128<WIDE, FB, FA>(x, xa[m]);
+        if (m == 1 && sending) {
+          if (n + 1 == TN) send(stage, 0, kFirst);
+          if (kFirst + n * kSend < kLoads) send(stage ^ 1, kFirst + n * kSend, kSend);
+        }
         if (n + 1 == TN) xa[m] = fragment(next_a + m * 16 * 128);
         add(n > 0 ? n - 1 : TN - 1, m, made[m], fa[m], fp);
         made[m] = u;
