@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import functools
 
 import torch
 
@@ -729,10 +730,11 @@ def aal_fp8_quantize(x: torch.Tensor, *, block_rows: int = 1, rows: bool = True,
                                          _ptr(out["q"]), _pitch(Cn), _ptr(out["scale"]), _ptr(out["qt"]), _pitch(R),
                                          _ptr(out["scale_t"]), _raw_stream(dev, stream))
     _lib.check(st, "aal_fp8_quantize")
-    if rows:
-        out["q"], out["scale"] = out["q"][:, :Cn], out["scale"].t()
-    if columns:
-        out["qt"], out["scale_t"] = out["qt"][:, :R], out["scale_t"].t()
+    for want, q, s, m in ((rows, "q", "scale", Cn), (columns, "qt", "scale_t", R)):
+        if want:
+            out[s] = out[s].t()
+            if m % 16:
+                out[q] = out[q][:, :m]
     return out
 
 
@@ -890,14 +892,13 @@ def aal_beam_select(z: torch.Tensor, scores: torch.Tensor, n: int, *, temperatur
     if ws is not None and (ws.device != dev or not ws.is_contiguous()):
         raise ValueError(f"ws must be a contiguous tensor on {dev}")
     with _guard(dev, stream):
-        # the outputs are pieces of one allocation
-        words = torch.empty(5 * B * n, dtype=torch.int32, device=dev).split(B * n)
-        out = {"scores": words[0].view(torch.float32).view(B, n), "rank": words[1].view(torch.float32).view(B, n),
-               "parents": words[2].view(B, n), "tokens": words[3].view(B, n),
-               "finished": torch.empty(B, n, dtype=torch.bool, device=dev), "lengths": words[4].view(B, n)}
+        # the outputs of 32 bits are pieces of one allocation
+        scores_, rank, parents, tokens, lengths_ = torch.empty((5, B, n), dtype=torch.int32, device=dev).unbind(0)
+        out = {"scores": scores_.view(torch.float32), "rank": rank.view(torch.float32), "parents": parents,
+               "tokens": tokens, "finished": torch.empty((B, n), dtype=torch.bool, device=dev), "lengths": lengths_}
         if ws is None:
             ws = torch.empty(aal_beam_select_workspace_bytes(z.dtype, B, W, V, n), dtype=torch.uint8, device=dev)
-        o = _lib.BeamOut(*(_ptr(out[k]) for k in ("scores", "rank", "parents", "tokens", "finished", "lengths")))
+        o = _lib.BeamOut(*[t.data_ptr() for t in out.values()])
         st = _lib.lib().aal_beam_select(
             _ptr(z), code, B, W, V, int(n), float(temperature), _ptr(scores), _ptr(finished), _ptr(lengths),
             float(length_penalty), int(eos), int(pad), C.byref(o), _ptr(ws), ws.numel() * ws.element_size(),
@@ -906,10 +907,12 @@ def aal_beam_select(z: torch.Tensor, scores: torch.Tensor, n: int, *, temperatur
     return out
 
 
-def _segments(t: torch.Tensor):
-    """t's memory behind its first two dimensions: (segments, elements of one, elements from one to the next)."""
-    size, step = 1, 1  # of the contiguous end
-    dims = [(n, s) for n, s in zip(t.shape[2:], t.stride()[2:]) if n != 1]
+@functools.lru_cache(maxsize=4096)
+def _segments(shape: tuple, stride: tuple):
+    """The memory of a tensor of that shape and those strides behind its first two dimensions: (segments,
+    elements of one, elements from one to the next), None if it is not that regular."""
+    size = 1  # of the contiguous end
+    dims = [(n, s) for n, s in zip(shape[2:], stride[2:]) if n != 1]
     while dims and dims[-1][1] == size:
         size *= dims.pop()[0]
     count, step = 1, 0
@@ -923,10 +926,11 @@ def _segments(t: torch.Tensor):
     return count, size, step
 
 
-def _apart(t: torch.Tensor) -> bool:
-    """Whether no two of t's entries share memory (dimensions nested by their strides)."""
+@functools.lru_cache(maxsize=4096)
+def _apart(shape: tuple, stride: tuple) -> bool:
+    """Whether no two entries share memory (dimensions nested by their strides)."""
     end = 1
-    for step, n in sorted((s, n) for n, s in zip(t.shape, t.stride()) if n > 1):
+    for step, n in sorted((s, n) for n, s in zip(shape, stride) if n > 1):
         if step < end:
             return False
         end += step * (n - 1)
@@ -961,28 +965,27 @@ def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) ->
     if not 1 <= n <= AAL_BEAM_SELECT_MAX or (out is None and (n != W or n > AAL_BEAM_MAX)):
         raise ValueError(f"n must be in [1, {AAL_BEAM_SELECT_MAX}], in place W and at most {AAL_BEAM_MAX}; got {n}")
     table = (_lib.BeamState * len(states))()
-    for i, (s, o) in enumerate(zip(states, outs)):
-        if s.dim() < 2 or s.shape[:2] != (B, W) or s.device != dev:
-            raise ValueError(f"states must be [{B}, {W}, ...] on {dev}; got {tuple(s.shape)} on {s.device}")
-        cut = _segments(s)
+    for row, s, o in zip(table, states, outs):
+        shape, stride = tuple(s.shape), s.stride()
+        if len(shape) < 2 or shape[0] != B or shape[1] != W or s.device != dev:
+            raise ValueError(f"states must be [{B}, {W}, ...] on {dev}; got {shape} on {s.device}")
+        cut = _segments(shape, stride)
         if cut is None:
             raise ValueError("a state must be contiguous pieces at one distance behind its first two dimensions")
         e = s.element_size()
         count, size, step = cut
-        row = table[i]
-        row.src, row.dst = s.data_ptr(), None
-        row.src_request, row.src_beam, row.src_segment = s.stride(0) * e, s.stride(1) * e, step * e
+        row.src, row.src_request, row.src_beam, row.src_segment = s.data_ptr(), stride[0] * e, stride[1] * e, step * e
         row.segments, row.segment_bytes = count, size * e
-        if not _apart(o):
-            raise ValueError("the entries of what is written must not share memory")
         if out is not None:
-            if o.shape != (B, n, *s.shape[2:]) or o.dtype != s.dtype or o.device != dev:
+            if o.shape != (B, n, *shape[2:]) or o.dtype != s.dtype or o.device != dev:
                 raise ValueError(f"out must be [{B}, {n}, ...] of the states' shapes and dtypes on {dev}")
-            to = _segments(o)
+            shape, stride = tuple(o.shape), o.stride()
+            to = _segments(shape, stride)
             if to is None or to[:2] != (count, size):
                 raise ValueError("an output must be the same contiguous pieces as its state")
-            row.dst = o.data_ptr()
-            row.dst_request, row.dst_beam, row.dst_segment = o.stride(0) * e, o.stride(1) * e, to[2] * e
+            row.dst, row.dst_request, row.dst_beam, row.dst_segment = o.data_ptr(), stride[0] * e, stride[1] * e, to[2] * e
+        if not _apart(shape, stride):
+            raise ValueError("the entries of what is written must not share memory")
     with _guard(dev, stream):
         st = _lib.lib().aal_beam_reorder(table, len(states), B, W, n, _ptr(parents), _raw_stream(dev, stream))
     _lib.check(st, "aal_beam_reorder")
