@@ -1,6 +1,6 @@
 """Train a draft head on a target's stored top logits.
 
-    python examples/train_on_top_logits.py [--steps 30] [--vocab 32000] [--top 64]
+    python examples/train_on_top_logits.py [--steps 30] [--vocab 32000] [--top 64] [--fp8]
 
 What a training set of a large target keeps of every position is its top logits,
 taken after the penalties and grammars that the server applies:
@@ -10,7 +10,9 @@ taken after the penalties and grammars that the server applies:
             sliding over the sequences) -> aal_logits_process_bwd -> the head's gradient
 
 Target and draft are linear heads over random features (synthetic data); the draft's
-features are the target's with noise, so that it can learn most of the distribution.
+features are the target's with noise, so that it can learn most of the distribution.  With --fp8
+the draft's head works in 8 bits: its weights are quantised anew each step, and both its logits
+(aal_head_logits) and its gradient (aal_head_logits_bwd) are products of 8-bit operands.
 """
 from __future__ import annotations
 
@@ -51,6 +53,7 @@ def main(argv=None) -> list[float]:
     ap.add_argument("--top", type=int, default=64)
     ap.add_argument("--window", type=int, default=7)
     ap.add_argument("--lr", type=float, default=2.0)
+    ap.add_argument("--fp8", action="store_true")
     a = ap.parse_args(argv)
     dev, B, S, V, D, K = "cuda", a.batch, a.positions, a.vocab, a.width, a.window
     g = torch.Generator(dev).manual_seed(0)
@@ -70,12 +73,17 @@ def main(argv=None) -> list[float]:
     head = torch.zeros(V, D, device=dev)
     losses = []
     for step in range(a.steps):
-        raw = (seen @ head.t()).bfloat16()
+        if a.fp8:
+            held = aal.aal_fp8_quantize(head, block_rows=128, scale_dtype=torch.float8_e8m0fnu)
+            raw = aal.aal_head_logits(seen, held, out_dtype=torch.bfloat16)
+        else:
+            raw = (seen @ head.t()).bfloat16()
         z = aal.aal_logits_process(raw, **rules)
         out = aal.aal_topk_loss_fwd_bwd(z.view(B, S, V), top, ids, K, rest=rest, weights=(0.0, 0.1, 1.0, 0.0),
                                         layout=aal.AAL_LAYOUT_SEQUENCES)
         grad = aal.aal_logits_process_bwd(out["grad"].view(B * S, V), raw, **rules)
-        head -= a.lr * (grad.float().t() @ seen)
+        head -= a.lr * (aal.aal_head_logits_bwd(grad, seen, held, x_grad=False)["grad_w"] if a.fp8
+                        else grad.float().t() @ seen)
         losses.append(out["loss"].item())
         if step % 5 == 0 or step == a.steps - 1:
             kl, accept = out["terms"][2].item(), out["accept_tv"].mean().item()
