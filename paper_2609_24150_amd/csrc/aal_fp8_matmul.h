@@ -100,6 +100,19 @@ __device__ __forceinline__ void store4(void* c, int64_t at, float x, float y, fl
   }
 }
 
+// Eight consecutive bf16 results of a row, of which n exist.
+__device__ __forceinline__ void store8(void* c, int64_t at, u32x4 v, int64_t n) {
+  typedef u32x4 u32x4_e2 __attribute__((aligned(2)));
+  uint16_t* to = static_cast<uint16_t*>(c) + at;
+  if (n >= 8) {
+    *reinterpret_cast<u32x4_e2*>(to) = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) to[i] = uint16_t(v[i / 2] >> (16 * (i & 1)));
+  }
+}
+
 // Waits for this wave's loads into LDS and its LDS accesses, then for the workgroup.
 __device__ __forceinline__ void stage_barrier() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -324,12 +337,22 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
       add(TN - 1, m, made[m], fa[m], fp);
       made[m] = f32x4{0.f, 0.f, 0.f, 0.f};
       fa[m] = 0.f;
-      const int64_t gm = int64_t(t.down) * BM + (wm * TM + m) * 16 + l;
-      if (gm < p.M) {
+      const int64_t gm = int64_t(t.down) * BM + (wm * TM + m) * 16 + l, n0 = int64_t(t.across) * BN + wn * TN * 16;
+      if (bf16) {
+        // two tiles' columns change places between neighbouring rows of lanes: 8 side by side a lane, 64 bytes of a row of c
+#pragma unroll
+        for (int n = 0; n < TN; n += 2) {
+          const f32x4 &a = acc[n][m], &b = acc[n + 1][m];
+          const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[0], a[1]), pack_bf16x2(b[0], b[1]), false, false);
+          const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[2], a[3]), pack_bf16x2(b[2], b[3]), false, false);
+          const int64_t gn = n0 + (n + (h & 1)) * 16 + (h >> 1) * 8;
+          if (gm < p.M && gn < p.N) store8(c, gm * p.N + gn, u32x4{lo[0], hi[0], lo[1], hi[1]}, p.N - gn);
+        }
+      } else if (gm < p.M) {
 #pragma unroll
         for (int n = 0; n < TN; ++n) {
-          const int64_t gn = int64_t(t.across) * BN + (wn * TN + n) * 16 + h * 4;
-          if (gn < p.N) store4(c, gm * p.N + gn, acc[n][m][0], acc[n][m][1], acc[n][m][2], acc[n][m][3], p.N - gn, bf16);
+          const int64_t gn = n0 + n * 16 + h * 4;
+          if (gn < p.N) store4(c, gm * p.N + gn, acc[n][m][0], acc[n][m][1], acc[n][m][2], acc[n][m][3], p.N - gn, false);
         }
       }
 #pragma unroll
