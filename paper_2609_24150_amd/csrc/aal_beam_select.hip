@@ -85,6 +85,26 @@ __device__ __forceinline__ int block_count(int wave_value, int* sh) {
 
 typedef u32x4 u32x4_e2 __attribute__((aligned(2)));  // a vector at any element
 
+// The sum over the wave in 64 bits, without LDS: rows of 16 lanes, then across them.
+template <int Ctrl, int RowMask>
+__device__ __forceinline__ double dpp_d(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = uint32_t(__builtin_amdgcn_update_dpp(0, int(uint32_t(b)), Ctrl, RowMask, 0xF, false));
+  const uint32_t hi = uint32_t(__builtin_amdgcn_update_dpp(0, int(uint32_t(b >> 32)), Ctrl, RowMask, 0xF, false));
+  return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum_dpp(double v) {
+  v += dpp_d<0xB1, 0xF>(v);   // quad_perm [1,0,3,2]
+  v += dpp_d<0x4E, 0xF>(v);   // quad_perm [2,3,0,1]
+  v += dpp_d<0x141, 0xF>(v);  // row_half_mirror
+  v += dpp_d<0x140, 0xF>(v);  // row_mirror
+  v += dpp_d<0x142, 0xA>(v);  // row_bcast:15
+  v += dpp_d<0x143, 0xC>(v);  // row_bcast:31
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(b >> 32)), 63))) << 32 |
+                                        uint32_t(__builtin_amdgcn_readlane(int(uint32_t(b)), 63)));
+}
+
 // A value that all lanes have, as one of the wave.
 __device__ __forceinline__ float uniform(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
@@ -139,6 +159,7 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) pin(raw[u]);
+  const float own[1] = {m};
   m = wave_max(m);
   if (lane == 0) fsh[wv] = m;
   __syncthreads();
@@ -153,8 +174,9 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
     if (tid == 0) p.part[slot] = {0.0, kNegInf, 0};
     return;
   }
-  // at least n logits reach t, or all finite ones do
-  float t = uniform(threshold<TI, WV>(gm, p.n, m, fsh));
+  // At least n logits reach t, or all finite ones do.  Threads' maxima do for short lists, an eighth of the
+  // arithmetic; for more than a quarter of the threads they would let through half again as many.
+  float t = uniform(p.n <= BLK / 4 ? threshold<TI, WV>(own, p.n, m, fsh) : threshold<TI, WV>(gm, p.n, m, fsh));
   // the vectors that hold some, then their entries, each by a thread of its own
   auto collect = [&](float from) {
 #pragma unroll
@@ -260,39 +282,45 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
   // z sc_lo; what ref, m sc rounded, is off by is a factor of the whole sum and joins it in 64 bits.
   // References beyond 2^27 take the difference first.
   const float ref = m * p.sc_hi;
-  const bool steep = fabsf(ref) > 0x1p27f;
-  auto weight = [&](float z) {
-    if (steep) {
-      const float d = z - m;
-      return ex2(__builtin_fmaf(d, p.sc_hi, d * p.sc_lo));
-    }
-    return ex2(__builtin_fmaf(z, p.sc_lo, __builtin_fmaf(z, p.sc_hi, -ref)));
+  const bool steep = __builtin_amdgcn_readfirstlane(fabsf(ref) > 0x1p27f) != 0;
+  auto weight = [&](float z, bool by_difference) {
+    const float d = z - m;
+    return ex2(by_difference ? __builtin_fmaf(d, p.sc_hi, d * p.sc_lo)
+                             : __builtin_fmaf(z, p.sc_lo, __builtin_fmaf(z, p.sc_hi, -ref)));
+  };
+  // without a branch in it: what is listed counts as -inf
+  auto weights = [&](const u32x4& w, bool listed, bool by_difference) {
+    float x[E], us = 0.f;
+    TI::unpack(to_uint4(w), x);
+    if (listed)
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = x[e] < t ? x[e] : kNegInf;
+#pragma unroll
+    for (int e = 0; e < E; ++e) us += weight(x[e], by_difference);
+    return us;
   };
   float s = 0.f;
+  if (steep) {
+#pragma unroll 1
+    for (int u = 0; u < U; ++u) s += weights(vector(u), true, true);
+  } else {
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    float x[E], us = 0.f;
-    TI::unpack(to_uint4(raw[u]), x);
-    if (__builtin_amdgcn_ballot_w64(gm[u] >= t) != 0) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) us += x[e] < t ? weight(x[e]) : 0.f;
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) us += weight(x[e]);
+    for (int u = 0; u < U; ++u) {
+      s += weights(raw[u], __builtin_amdgcn_ballot_w64(gm[u] >= t) != 0, false);
+      __builtin_amdgcn_sched_barrier(0);  // not all vectors unpacked at once
     }
-    s += us;
   }
-  if (tid == 0 && left_ties) s += float(left_ties) * weight(t);
+  if (tid == 0 && left_ties) s += float(left_ties) * weight(t, steep);
   __syncthreads();
   double total = double(s);
   for (int i = tid; i < c; i += BLK)
-    if (i >= p.n) total += double(weight(entry_logit<TI>(sorted[i])));
+    if (i >= p.n) total += double(weight(entry_logit<TI>(sorted[i]), steep));
   if (!steep) total *= exp2(double(ref) - double(m) * (double(p.sc_hi) + double(p.sc_lo)));
   for (int i = tid; i < p.n; i += BLK) {
     list[i] = i < c ? sorted[i] : 0;
     if (i < c) total += exp((double(entry_logit<TI>(sorted[i])) - double(m)) * p.inv_t);
   }
-  total = wave_sum_d(total);
+  total = wave_sum_dpp(total);
   if (lane == 0) dsum[wv] = total;
   __syncthreads();
   if (tid == 0) {
