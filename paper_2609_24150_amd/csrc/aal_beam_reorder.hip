@@ -60,7 +60,7 @@ __global__ __launch_bounds__(256) void k_beam_reorder(ReorderParams p) {
     }
 #pragma unroll
     for (int j = 0; j < NB; ++j)
-      if (from[j] >= 0) *reinterpret_cast<T*>(dst + (j0 + j) * s.dst_beam) = r[j];
+      if (from[j] >= 0) __builtin_nontemporal_store(r[j], reinterpret_cast<T*>(dst + (j0 + j) * s.dst_beam));
   }
 }
 

@@ -14,6 +14,7 @@
 // to leave in whole lines.
 #include "aal_fp8_device.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace aal {
@@ -111,38 +112,46 @@ __global__ __launch_bounds__(256) void k_quant_rows(QuantParams p, int col_group
   }
 }
 
-// A workgroup takes a tile of 128 x 128: 16 threads for the columns, 16 groups of 8 rows.
-template <class TI, Fp8 F, Scale S, bool SQUARE>
-__global__ __launch_bounds__(256) void k_quant_tile(QuantParams p, int col_blocks) {
-  constexpr int kPitch = 136;
-  __shared__ uint32_t part[4][kFp8Block];
-  __shared__ int ce[kFp8Block];
-  alignas(16) __shared__ uint8_t turn[kFp8Block * kPitch];
+// A workgroup takes 128 rows of T blocks of columns: 16 T threads for the columns, 16 groups of 8 rows.  T: as many as
+// make 512 bytes of a row of x; 2,048 x 128,256 bf16 in both orders 247 us, 128 columns at a time 253, and
+// 16 tiles down before the next ones across 262.
+template <class TI, Fp8 F, Scale S, bool SQUARE, int T>
+__global__ __launch_bounds__(256 * T) void k_quant_tile(QuantParams p, int col_groups) {
+  constexpr int kPitch = 136, WV = 4 * T, kCols = kFp8Block * T;
+  __shared__ uint32_t part[WV][kCols];
+  __shared__ int ce[kCols];
+  alignas(16) __shared__ uint8_t turn[kCols * kPitch];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
-  const int64_t rb = p.first + blockIdx.x / col_blocks, cb = blockIdx.x % col_blocks;
-  const int rl = tid / 16 * 8, cl = tid % 16 * 8;  // in the tile
-  const int64_t r0 = rb * kFp8Block + rl, c0 = cb * kFp8Block + cl;
-  const int64_t row_blocks = (p.rows + kFp8Block - 1) / kFp8Block;
+  const int64_t rb = p.first + blockIdx.x / col_groups, cg = blockIdx.x % col_groups;
+  const int rl = tid / (16 * T) * 8, cl = tid % (16 * T) * 8;  // in the tile
+  const int64_t r0 = rb * kFp8Block + rl, c0 = cg * kCols + cl;
+  const int64_t row_blocks = (p.rows + kFp8Block - 1) / kFp8Block, col_blocks = (p.cols + kFp8Block - 1) / kFp8Block;
+  const int64_t cb = cg * T + cl / kFp8Block;  // the thread's block of columns
   float x[8][8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) load8<TI>(p, r0 + i, c0, x[i]);
   int er[8], ec[8];
+  // the largest over the row groups of the wave that share a column
+  auto rows_max = [&](uint32_t m) {
+    if constexpr (T == 1) m = max(m, uint32_t(__shfl_xor(int(m), 16, kWave)));
+    return max(m, uint32_t(__shfl_xor(int(m), 32, kWave)));
+  };
   if constexpr (SQUARE) {
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) m = max(m, finite_bits(x[i][e]));
-    m = row16_max(m);
-    m = max(m, uint32_t(__shfl_xor(int(m), 16, kWave)));
-    m = max(m, uint32_t(__shfl_xor(int(m), 32, kWave)));
-    if (lane == 0) part[wv][0] = m;
+    m = rows_max(row16_max(m));
+    if (lane % 16 == 0 && lane < 16 * T) part[wv][lane / 16] = m;
     __syncthreads();
-    m = max(max(part[0][0], part[1][0]), max(part[2][0], part[3][0]));
+    m = 0;
+#pragma unroll
+    for (int w = 0; w < WV; ++w) m = max(m, part[w][cl / kFp8Block]);
     const int e = scale_exponent<F>(m);
 #pragma unroll
     for (int i = 0; i < 8; ++i) er[i] = ec[i] = e;
-    if (tid == 0) {
+    if (rl == 0 && cl % kFp8Block == 0 && cb < col_blocks) {
       if (p.q) store_scale<S>(p.scale, cb * row_blocks + rb, e);
       if (p.qt) store_scale<S>(p.scale_t, rb * col_blocks + cb, e);
     }
@@ -154,7 +163,7 @@ __global__ __launch_bounds__(256) void k_quant_tile(QuantParams p, int col_block
 #pragma unroll
         for (int e = 0; e < 8; ++e) m = max(m, finite_bits(x[i][e]));
         er[i] = scale_exponent<F>(row16_max(m));
-        if (cl == 0 && r0 + i < p.rows) store_scale<S>(p.scale, cb * p.rows + r0 + i, er[i]);
+        if (cl % kFp8Block == 0 && cb < col_blocks && r0 + i < p.rows) store_scale<S>(p.scale, cb * p.rows + r0 + i, er[i]);
       }
     }
 #pragma unroll
@@ -162,15 +171,17 @@ __global__ __launch_bounds__(256) void k_quant_tile(QuantParams p, int col_block
       uint32_t m = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) m = max(m, finite_bits(x[i][e]));
-      m = max(m, uint32_t(__shfl_xor(int(m), 16, kWave)));
-      m = max(m, uint32_t(__shfl_xor(int(m), 32, kWave)));
-      if (lane < 16) part[wv][cl + e] = m;
+      m = rows_max(m);
+      if (lane < 16 * T) part[wv][cl + e] = m;
     }
     __syncthreads();
-    if (tid < kFp8Block) {
-      const int e = scale_exponent<F>(max(max(part[0][tid], part[1][tid]), max(part[2][tid], part[3][tid])));
-      ce[tid] = e;
-      const int64_t c = cb * kFp8Block + tid;
+    for (int i = tid; i < kCols; i += 256 * T) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int w = 0; w < WV; ++w) m = max(m, part[w][i]);
+      const int e = scale_exponent<F>(m);
+      ce[i] = e;
+      const int64_t c = cg * kCols + i;
       if (c < p.cols) store_scale<S>(p.scale_t, rb * p.cols + c, e);
     }
     __syncthreads();
@@ -199,8 +210,8 @@ __global__ __launch_bounds__(256) void k_quant_tile(QuantParams p, int col_block
   // 16 threads write a transposed row's 128 bytes
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int c = tid / 16 + i * 16, r = tid % 16 * 8;
-    const int64_t gc = cb * kFp8Block + c, gr = rb * kFp8Block + r;
+    const int c = tid / 16 + i * 16 * T, r = tid % 16 * 8;
+    const int64_t gc = cg * kCols + c, gr = rb * kFp8Block + r;
     if (gc >= p.cols || gr >= p.rows) continue;
     const u32x2 w = *reinterpret_cast<const u32x2*>(&turn[c * kPitch + r]);
     store8(p.qt + gc * p.ld_qt + gr, w.x, w.y, p.rows - gr);
@@ -212,17 +223,18 @@ hipError_t launch_typed(const QuantizeArgs& a) {
   QuantParams p{a.x, a.rows, a.cols, a.ld, a.q, a.ld_q, a.scale, a.qt, a.ld_qt, a.scale_t, 0};
   const bool tiles = a.block_rows != 1 || a.qt != nullptr;
   const int64_t down = tiles ? (a.rows + 127) / 128 : (a.rows + 15) / 16;
-  const int64_t across = tiles ? (a.cols + 127) / 128 : (a.cols + 511) / 512;
-  // a launch holds fewer than 2^32 threads: up to 2^23 workgroups (cols <= 2^30: a row of them fits)
-  const int64_t most = (int64_t(1) << 23) / across;
+  constexpr int T = TI::kVec == 8 ? 2 : 1;
+  const int64_t across = tiles ? (a.cols + 128 * T - 1) / (128 * T) : (a.cols + 511) / 512;
+  // a launch holds fewer than 2^32 threads: up to 2^22 workgroups, or a row of them (cols <= 2^30: 2^22, or 2^23 of 256)
+  const int64_t most = std::max<int64_t>(1, (int64_t(1) << 22) / across);
   for (; p.first < down; p.first += most) {
     const dim3 grid(unsigned((down - p.first < most ? down - p.first : most) * across));
     if (!tiles)
       k_quant_rows<TI, F, S><<<grid, 256, 0, a.stream>>>(p, int(across));
     else if (a.block_rows == 1)
-      k_quant_tile<TI, F, S, false><<<grid, 256, 0, a.stream>>>(p, int(across));
+      k_quant_tile<TI, F, S, false, T><<<grid, 256 * T, 0, a.stream>>>(p, int(across));
     else
-      k_quant_tile<TI, F, S, true><<<grid, 256, 0, a.stream>>>(p, int(across));
+      k_quant_tile<TI, F, S, true, T><<<grid, 256 * T, 0, a.stream>>>(p, int(across));
   }
   return hipGetLastError();
 }
