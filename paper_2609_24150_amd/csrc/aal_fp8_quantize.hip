@@ -32,26 +32,102 @@ struct QuantParams {
   int64_t first;  // row of workgroups that the launch starts with
 };
 
-// The 8 values of row r from column c on, 0 behind the row's end.
+// Eight values of a row as they are stored.
 template <class TI>
-__device__ __forceinline__ void load8(const QuantParams& p, int64_t r, int64_t c, float (&x)[8]) {
-  const typename TI::storage* at = static_cast<const typename TI::storage*>(p.x) + r * p.ld + c;
+struct Eight {
+  static constexpr int kWords = TI::kVec == 8 ? 4 : 8;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void values(float (&x)[8]) const {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = 0.f;
-  if (r >= p.rows) return;
+    for (int u = 0; u < kWords / 4; ++u) {
+      float y[TI::kVec];
+      TI::unpack(make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]), y);
+#pragma unroll
+      for (int e = 0; e < TI::kVec; ++e) x[u * TI::kVec + e] = y[e];
+    }
+  }
+};
+
+// Those of row r from column c on, 0 behind the row's end.
+template <class TI>
+__device__ __forceinline__ Eight<TI> load8(const QuantParams& p, int64_t r, int64_t c) {
+  using T = typename TI::storage;
+  const T* at = static_cast<const T*>(p.x) + r * p.ld + c;
+  Eight<TI> x{};
+  if (r >= p.rows) return x;
   if (c + 8 <= p.cols) {
-    constexpr int E = TI::kVec;
 #pragma unroll
-    for (int u = 0; u < 8 / E; ++u) {
-      float y[E];
-      TI::unpack(to_uint4(__builtin_nontemporal_load(reinterpret_cast<const u32x4_e2*>(at + u * E))), y);
+    for (int u = 0; u < Eight<TI>::kWords / 4; ++u) {
+      const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_e2*>(at + u * TI::kVec));
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[u * E + e] = y[e];
+      for (int i = 0; i < 4; ++i) x.w[4 * u + i] = v[i];
+    }
+  } else {
+    T v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + e < p.cols ? at[e] : T(0);
+    __builtin_memcpy(&x, v, sizeof x);
+  }
+  return x;
+}
+
+// Largest magnitudes, as bits of fp32, of the rows and of the columns of N x 8 values; what is not finite counts as 0.
+// bf16 by pairs, magnitudes being whole numbers that order as they do; values that are not finite show in the
+// result, and only then every value is looked at.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+template <class TI, int N>
+__device__ __forceinline__ void maxima(const Eight<TI> (&x)[N], uint32_t (&rows)[N], uint32_t (&cols)[8]) {
+  uint32_t all = 0;
+  if constexpr (TI::kVec == 8) {
+    uint32_t c[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      uint32_t a[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        a[k] = x[i].w[k] & 0x7fff7fffu;
+        c[k] = max_pair(c[k], a[k]);
+      }
+      const uint32_t m = max_pair(max_pair(a[0], a[1]), max_pair(a[2], a[3]));
+      rows[i] = max(m << 16, m & 0xffff0000u);
+      all = max(all, rows[i]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      cols[2 * k] = c[k] << 16;
+      cols[2 * k + 1] = c[k] & 0xffff0000u;
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (c + e < p.cols) x[e] = TI::load1(at, e);
+    for (int e = 0; e < 8; ++e) cols[e] = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      rows[i] = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t a = x[i].w[e % Eight<TI>::kWords] & 0x7fffffffu;
+        rows[i] = max(rows[i], a);
+        cols[e] = max(cols[e], a);
+      }
+      all = max(all, rows[i]);
+    }
+  }
+  if (all < 0x7f800000u) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) cols[e] = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float v[8];
+    x[i].values(v);
+    rows[i] = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      rows[i] = max(rows[i], finite_bits(v[e]));
+      cols[e] = max(cols[e], finite_bits(v[e]));
+    }
   }
 }
 
@@ -90,20 +166,21 @@ __global__ __launch_bounds__(256) void k_quant_rows(QuantParams p, int col_group
   const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
   const int64_t rg = p.first + blockIdx.x / col_groups, cg = blockIdx.x % col_groups;
   const int64_t r0 = rg * 16 + wv * R, c = cg * 512 + lane * 8;
-  float x[R][8];
+  Eight<TI> raw[R];
+  uint32_t rows[R], cols[8];
 #pragma unroll
-  for (int i = 0; i < R; ++i) load8<TI>(p, r0 + i, c, x[i]);
+  for (int i = 0; i < R; ++i) raw[i] = load8<TI>(p, r0 + i, c);
+  maxima<TI>(raw, rows, cols);
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m = max(m, finite_bits(x[i][e]));
-    const int e = scale_exponent<F>(row16_max(m));
+    float x[8];
+    raw[i].values(x);
+    const int e = scale_exponent<F>(row16_max(rows[i]));
     const float inv = power_of_two(-e);
     if ((lane & 15) == 0) se[lane / 16][wv * R + i] = e;
     if (r0 + i < p.rows && c < p.cols)
-      store8(p.q + (r0 + i) * p.ld_q + c, pack_fp8<F>(x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv),
-             pack_fp8<F>(x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv), p.cols - c);
+      store8(p.q + (r0 + i) * p.ld_q + c, pack_fp8<F>(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv),
+             pack_fp8<F>(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv), p.cols - c);
   }
   __syncthreads();
   if (threadIdx.x < 64) {
@@ -117,19 +194,23 @@ __global__ __launch_bounds__(256) void k_quant_rows(QuantParams p, int col_group
 // 16 tiles down before the next ones across 262.
 template <class TI, Fp8 F, Scale S, bool SQUARE, int T>
 __global__ __launch_bounds__(256 * T) void k_quant_tile(QuantParams p, int col_groups) {
-  constexpr int kPitch = 136, WV = 4 * T, kCols = kFp8Block * T;
+  constexpr int WV = 4 * T, kCols = kFp8Block * T;
   __shared__ uint32_t part[WV][kCols];
   __shared__ int ce[kCols];
-  alignas(16) __shared__ uint8_t turn[kCols * kPitch];
+  alignas(16) __shared__ uint8_t turn[kCols * kFp8Block];
+  // a column's 16 pieces of 8 rows stand in an order that its neighbours, which are written at a time, do not share
+  auto turned = [&](int c, int r) { return &turn[c * kFp8Block + ((r / 8) ^ (c / 8 % 16)) * 8]; };
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
   const int64_t rb = p.first + blockIdx.x / col_groups, cg = blockIdx.x % col_groups;
   const int rl = tid / (16 * T) * 8, cl = tid % (16 * T) * 8;  // in the tile
   const int64_t r0 = rb * kFp8Block + rl, c0 = cg * kCols + cl;
   const int64_t row_blocks = (p.rows + kFp8Block - 1) / kFp8Block, col_blocks = (p.cols + kFp8Block - 1) / kFp8Block;
   const int64_t cb = cg * T + cl / kFp8Block;  // the thread's block of columns
-  float x[8][8];
+  Eight<TI> raw[8];
+  uint32_t rows[8], cols[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) load8<TI>(p, r0 + i, c0, x[i]);
+  for (int i = 0; i < 8; ++i) raw[i] = load8<TI>(p, r0 + i, c0);
+  maxima<TI>(raw, rows, cols);
   int er[8], ec[8];
   // the largest over the row groups of the wave that share a column
   auto rows_max = [&](uint32_t m) {
@@ -139,9 +220,7 @@ __global__ __launch_bounds__(256 * T) void k_quant_tile(QuantParams p, int col_g
   if constexpr (SQUARE) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) m = max(m, finite_bits(x[i][e]));
+    for (int i = 0; i < 8; ++i) m = max(m, rows[i]);
     m = rows_max(row16_max(m));
     if (lane % 16 == 0 && lane < 16 * T) part[wv][lane / 16] = m;
     __syncthreads();
@@ -159,19 +238,13 @@ __global__ __launch_bounds__(256 * T) void k_quant_tile(QuantParams p, int col_g
     if (p.q) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) m = max(m, finite_bits(x[i][e]));
-        er[i] = scale_exponent<F>(row16_max(m));
+        er[i] = scale_exponent<F>(row16_max(rows[i]));
         if (cl % kFp8Block == 0 && cb < col_blocks && r0 + i < p.rows) store_scale<S>(p.scale, cb * p.rows + r0 + i, er[i]);
       }
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      uint32_t m = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, finite_bits(x[i][e]));
-      m = rows_max(m);
+      const uint32_t m = rows_max(cols[e]);
       if (lane < 16 * T) part[wv][cl + e] = m;
     }
     __syncthreads();
@@ -188,6 +261,9 @@ __global__ __launch_bounds__(256 * T) void k_quant_tile(QuantParams p, int col_g
 #pragma unroll
     for (int e = 0; e < 8; ++e) ec[e] = ce[cl + e];
   }
+  float x[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) raw[i].values(x[i]);
   if (p.q) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -204,7 +280,7 @@ __global__ __launch_bounds__(256 * T) void k_quant_tile(QuantParams p, int col_g
     const float inv = power_of_two(-ec[e]);
     const u32x2 w = {pack_fp8<F>(x[0][e] * inv, x[1][e] * inv, x[2][e] * inv, x[3][e] * inv),
                      pack_fp8<F>(x[4][e] * inv, x[5][e] * inv, x[6][e] * inv, x[7][e] * inv)};
-    *reinterpret_cast<u32x2*>(&turn[(cl + e) * kPitch + rl]) = w;
+    *reinterpret_cast<u32x2*>(turned(cl + e, rl)) = w;
   }
   __syncthreads();
   // 16 threads write a transposed row's 128 bytes
@@ -213,7 +289,7 @@ __global__ __launch_bounds__(256 * T) void k_quant_tile(QuantParams p, int col_g
     const int c = tid / 16 + i * 16 * T, r = tid % 16 * 8;
     const int64_t gc = cg * kCols + c, gr = rb * kFp8Block + r;
     if (gc >= p.cols || gr >= p.rows) continue;
-    const u32x2 w = *reinterpret_cast<const u32x2*>(&turn[c * kPitch + r]);
+    const u32x2 w = *reinterpret_cast<const u32x2*>(turned(c, r));
     store8(p.qt + gc * p.ld_qt + gr, w.x, w.y, p.rows - gr);
   }
 }
