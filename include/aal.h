@@ -757,7 +757,8 @@ size_t aal_beam_select_workspace_bytes(aal_dtype_t in_dtype, int64_t B, int32_t 
  * Candidates of total -inf (a masked token, a beam of score -inf) are never chosen; where
  * candidates run out, scores and rank are -inf, parents -1, tokens pad, finished 1, lengths 0.
  * z : [B, W, V] of in_dtype, 16-byte aligned, finite or -inf (a beam's whole row may be -inf).  Rows of
- *     beams that have ended, or whose score is -inf, are not read.
+ *     beams that have ended, or whose score is -inf, are not read.  NaN or +inf in a request's logits or scores
+ *     leave its choice unspecified, but parents stay in [-1, W) and tokens in [0, V), or pad.
  * scores : [B, W] finite or -inf.  finished : [B, W] bytes, nonzero for a beam that has ended, or NULL.
  * lengths : [B, W], at least 0 (1 for a beam that has ended), or NULL, which counts as 0 and asks for a
  *     length_penalty of 0.  temperature finite, > 0 and >= 1e-37; length_penalty finite.
@@ -786,7 +787,7 @@ typedef struct {
  * beams that keep their slot move no byte.  A parent outside [0, W) leaves its slot as it was.
  * states : host memory [n_states], read before the call returns; 0 <= n_states.  parents : device [B, n].
  * In place asks for n = W <= AAL_BEAM_MAX (src is written); otherwise 1 <= n <= AAL_BEAM_SELECT_MAX, and a
- * dst overlaps no src.  The slots of a state must not overlap each other.  Any alignment; states whose addresses,
+ * dst overlaps no src.  What is written must not overlap another state, nor a state's slots each other.  Any alignment; states whose addresses,
  * strides and sizes are multiples of 16 (or 4) bytes move in such pieces.
  */
 aal_status_t aal_beam_reorder(const aal_beam_state_t* states, int32_t n_states, int64_t B, int32_t W, int32_t n,

@@ -8,6 +8,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import functools
+import operator
 
 import torch
 
@@ -799,6 +800,18 @@ def aal_fp8_matmul_workspace_bytes(M: int, N: int, K: int) -> int:
     return int(_lib.lib().aal_fp8_matmul_workspace_bytes(int(M), int(N), int(K)))
 
 
+def _matrix(t: torch.Tensor, stream) -> torch.Tensor:
+    """t as rows of its last dimension, contiguous: a copy of it, where there has to be one, is the call's own work,
+    on its stream."""
+    if not t.is_cuda:
+        raise ValueError("tensors must be on a device")
+    with _guard(t.device, stream):
+        flat = t.reshape(-1, t.shape[-1])
+        if flat.shape[1] > 1 and flat.stride(1) != 1 or flat.shape[0] > 1 and flat.stride(0) < flat.shape[1]:
+            flat = flat.contiguous()
+    return flat
+
+
 def _check_head(head: dict, *names: str):
     for name in names:
         if head.get(name) is None:
@@ -816,8 +829,7 @@ def aal_head_logits(x: torch.Tensor, head: dict, *, out_dtype: torch.dtype | Non
     D = x.shape[-1] if x.dim() else 0
     if x.dim() < 1 or x.numel() == 0 or head["q"].shape[-1] != D:
         raise ValueError(f"x must be [..., {head['q'].shape[-1]}] with at least one row")
-    flat = x.reshape(-1, D)
-    r = aal_fp8_quantize(flat, scale_dtype=head["scale"].dtype, stream=stream)
+    r = aal_fp8_quantize(_matrix(x, stream), scale_dtype=head["scale"].dtype, stream=stream)
     z = aal_fp8_matmul(r["q"], r["scale"], head["q"], head["scale"], out_dtype=out_dtype or x.dtype, stream=stream)
     return z.view(*x.shape[:-1], z.shape[1])
 
@@ -833,21 +845,20 @@ def aal_head_logits_bwd(grad: torch.Tensor, x: torch.Tensor, head: dict, *, x_gr
     weight_dtype (None where not asked for)."""
     if not (x_grad or weight_grad):
         raise ValueError("x_grad or weight_grad must be asked for")
-    if x_grad:
-        _check_head(head, "qt", "scale_t")
+    _check_head(head, *(("qt", "scale_t") if x_grad else ("scale",)))
     if x.dim() < 1 or x.numel() == 0 or grad.dim() < 1 or grad.shape[:-1] != x.shape[:-1] or grad.numel() == 0:
         raise ValueError("grad must be [..., V] and x [..., D] of the same rows, one at least")
     D, V = x.shape[-1], grad.shape[-1]
     if x_grad and tuple(head["qt"].shape) != (D, V):
         raise ValueError(f"grad and x do not fit a head of {tuple(head['qt'].shape)[::-1]}")
     scale = (head["scale_t"] if x_grad else head["scale"]).dtype
-    g = aal_fp8_quantize(grad.reshape(-1, V), rows=x_grad, columns=weight_grad, scale_dtype=scale, stream=stream)
+    g = aal_fp8_quantize(_matrix(grad, stream), rows=x_grad, columns=weight_grad, scale_dtype=scale, stream=stream)
     out = {"grad_x": None, "grad_w": None}
     if x_grad:
         out["grad_x"] = aal_fp8_matmul(g["q"], g["scale"], head["qt"], head["scale_t"], out_dtype=x.dtype,
                                        stream=stream).view(x.shape)
     if weight_grad:
-        xt = aal_fp8_quantize(x.reshape(-1, D), rows=False, columns=True, scale_dtype=scale, stream=stream)
+        xt = aal_fp8_quantize(_matrix(x, stream), rows=False, columns=True, scale_dtype=scale, stream=stream)
         out["grad_w"] = aal_fp8_matmul(g["qt"], g["scale_t"], xt["qt"], xt["scale_t"], out_dtype=weight_dtype,
                                        stream=stream)
     return out
@@ -910,7 +921,7 @@ def aal_beam_select(z: torch.Tensor, scores: torch.Tensor, n: int, *, temperatur
 @functools.lru_cache(maxsize=4096)
 def _segments(shape: tuple, stride: tuple):
     """The memory of a tensor of that shape and those strides behind its first two dimensions: (segments,
-    elements of one, elements from one to the next), None if it is not that regular."""
+    elements of one, elements from one to the next) and the elements that all of it spans, None if it is not that regular."""
     size = 1  # of the contiguous end
     dims = [(n, s) for n, s in zip(shape[2:], stride[2:]) if n != 1]
     while dims and dims[-1][1] == size:
@@ -923,7 +934,7 @@ def _segments(shape: tuple, stride: tuple):
             count *= n
         else:
             return None
-    return count, size, step
+    return count, size, step, 1 + sum((n - 1) * s for n, s in zip(shape, stride))
 
 
 @functools.lru_cache(maxsize=4096)
@@ -937,6 +948,50 @@ def _apart(shape: tuple, stride: tuple) -> bool:
     return True
 
 
+def _meet(d: int, a: list, na: int, b: list, nb: int) -> bool:
+    """Whether two regular sets of bytes share one: pieces of na and nb bytes, at (stride, count)s that nest, the
+    largest first, the second set's first byte d behind the first's.  True as well where sets of different strides
+    would take long to tell."""
+    end_a, end_b = (n + sum(s * (c - 1) for s, c in dims) for dims, n in ((a, na), (b, nb)))
+    if d >= end_a or -d >= end_b:
+        return False
+    if not a and not b:
+        return True
+    if a and b and a[0][0] == b[0][0]:
+        (s, ca), cb = a[0], b[0][1]
+        rest_a, rest_b = end_a - s * (ca - 1), end_b - s * (cb - 1)
+        steps = range(max(1 - ca, -((d + rest_b - 1) // s)), min(cb - 1, (rest_a - 1 - d) // s) + 1)
+        return len(steps) > 64 or any(_meet(d + k * s, a[1:], na, b[1:], nb) for k in steps)
+    if not a or (b and b[0][0] > a[0][0]):
+        return _meet(-d, b, nb, a, na)
+    s, ca = a[0]
+    rest = end_a - s * (ca - 1)
+    steps = range(max(0, -((rest - 1 - d) // s)), min(ca - 1, (d + end_b - 1) // s) + 1)
+    return len(steps) > 64 or any(_meet(d - k * s, a[1:], na, b, nb) for k in steps)
+
+
+def _check_memory(spans: list):
+    """What is written shares no memory with anything else of a call.  spans: (first byte, bytes to the last one's
+    end, whether it is written, (segments, bytes of one, bytes between them), (stride, count) of requests and of beams)."""
+    spans.sort(key=_first)
+    if all(x[0] + x[1] <= y[0] for x, y in zip(spans, spans[1:])):
+        return
+    near, last = [], 0  # those that reach past the present one's start
+    for x in spans:
+        at, size, written, cut, lead = x
+        near = near if at < last else []
+        for y in near:
+            if written or y[2]:
+                a, b = (sorted(((s, c) for s, c in (*z[4], (z[3][2], z[3][0])) if c > 1 and s), reverse=True) for z in (y, x))
+                if _meet(at - y[0], a, y[3][1], b, cut[1]):
+                    raise ValueError("what is written must share no memory with another state or output")
+        near.append(x)
+        last = max(last, at + size)
+
+
+_first = operator.itemgetter(0)
+
+
 def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) -> list:
     """Each state's beams after a selection: state[b, j] becomes what
     state[b, parents[b, j]] was, for tensors [B, W, ...] of any dtype (caches,
@@ -944,7 +999,7 @@ def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) ->
 
     parents: [B, n] int32, as from aal_beam_select; a parent outside [0, W) leaves its slot as it
     was.  out: None, for in place (n = W; beams that keep their slot move nothing), or tensors
-    [B, n, ...] that overlap no state.  Behind its first two dimensions a state may be any view that is
+    [B, n, ...].  What is written shares no memory with another state or output.  Behind its first two dimensions a state may be any view that is
     contiguous pieces at one distance (state[:, :, :, t0:t1] of a [B, W, heads, length, dim] cache).
 
     Returns out, or the states."""
@@ -965,6 +1020,7 @@ def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) ->
     if not 1 <= n <= AAL_BEAM_SELECT_MAX or (out is None and (n != W or n > AAL_BEAM_MAX)):
         raise ValueError(f"n must be in [1, {AAL_BEAM_SELECT_MAX}], in place W and at most {AAL_BEAM_MAX}; got {n}")
     table = (_lib.BeamState * len(states))()
+    spans = []
     for row, s, o in zip(table, states, outs):
         shape, stride = tuple(s.shape), s.stride()
         if len(shape) < 2 or shape[0] != B or shape[1] != W or s.device != dev:
@@ -973,8 +1029,11 @@ def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) ->
         if cut is None:
             raise ValueError("a state must be contiguous pieces at one distance behind its first two dimensions")
         e = s.element_size()
-        count, size, step = cut
-        row.src, row.src_request, row.src_beam, row.src_segment = s.data_ptr(), stride[0] * e, stride[1] * e, step * e
+        count, size, step, span = cut
+        at = s.data_ptr()
+        if count and size:
+            spans.append((at, span * e, out is None, (count, size * e, step * e), ((stride[0] * e, B), (stride[1] * e, W))))
+        row.src, row.src_request, row.src_beam, row.src_segment = at, stride[0] * e, stride[1] * e, step * e
         row.segments, row.segment_bytes = count, size * e
         if out is not None:
             if o.shape != (B, n, *shape[2:]) or o.dtype != s.dtype or o.device != dev:
@@ -983,9 +1042,14 @@ def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) ->
             to = _segments(shape, stride)
             if to is None or to[:2] != (count, size):
                 raise ValueError("an output must be the same contiguous pieces as its state")
-            row.dst, row.dst_request, row.dst_beam, row.dst_segment = o.data_ptr(), stride[0] * e, stride[1] * e, to[2] * e
+            at = o.data_ptr()
+            if count and size:
+                spans.append((at, to[3] * e, True, (count, size * e, to[2] * e), ((stride[0] * e, B), (stride[1] * e, n))))
+            row.dst, row.dst_request, row.dst_beam, row.dst_segment = at, stride[0] * e, stride[1] * e, to[2] * e
         if not _apart(shape, stride):
             raise ValueError("the entries of what is written must not share memory")
+    if len(spans) > 1:
+        _check_memory(spans)
     with _guard(dev, stream):
         st = _lib.lib().aal_beam_reorder(table, len(states), B, W, n, _ptr(parents), _raw_stream(dev, stream))
     _lib.check(st, "aal_beam_reorder")

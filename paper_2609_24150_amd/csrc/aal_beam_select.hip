@@ -206,22 +206,24 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
   for (int u = 0; u < U; ++u) pin(raw[u]);
   if (c > kCand) {
     // ties or clusters: the n-th largest logit itself, what lies above it and the first of its ties; the
-    // part is read again, so that the common way keeps its registers
+    // part is read again, so that the common way keeps its registers.  Compared as whole numbers, which
+    // order NaN too: no entry is listed twice, whatever the logits are.
     uint32_t lo = order_key<TI>(kNegInf) >> kShift, hi = (order_key<TI>(m) >> kShift) + 1u;
     while (hi > lo + 1u) {
       const uint32_t mid = lo + (hi - lo) / 2;
-      const float f = key_logit<TI>(mid << kShift);
+      const uint32_t f = mid << kShift;
       int reach = 0;
 #pragma unroll 1
       for (int u = 0; u < U; ++u) {
         float x[E];
         TI::unpack(to_uint4(vector(u)), x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) reach += __popcll(__builtin_amdgcn_ballot_w64(x[e] >= f));
+        for (int e = 0; e < E; ++e) reach += __popcll(__builtin_amdgcn_ballot_w64(order_key<TI>(x[e]) >= f));
       }
       (block_count<WV>(reach, ish) >= p.n ? lo : hi) = mid;
     }
-    t = uniform(key_logit<TI>(lo << kShift));
+    const uint32_t bar = lo << kShift;
+    t = uniform(key_logit<TI>(bar));
     if (tid == 0) count = 0;
     __syncthreads();
     int ties = 0;  // before this vector's turn
@@ -232,8 +234,12 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
       int mine = 0;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        mine += x[e] == t;
-        if (x[e] > t) cand[atomicAdd(&count, 1)] = Key::of(order_key<TI>(x[e]), (u * BLK + tid) * E + e);  // under n of them
+        const uint32_t key = order_key<TI>(x[e]);
+        mine += key == bar;
+        if (key > bar) {  // fewer than n of them, NaN aside
+          const int at = atomicAdd(&count, 1);
+          if (at < p.n) cand[at] = Key::of(key, (u * BLK + tid) * E + e);
+        }
       }
       int before = mine;
       for (int off = 1; off < kWave; off <<= 1) {
@@ -252,13 +258,13 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
       // the first n ties, from the end of the list down
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (x[e] == t) {
-          if (at < p.n) cand[kCand - 1 - at] = Key::of(order_key<TI>(t), (u * BLK + tid) * E + e);
+        if (order_key<TI>(x[e]) == bar) {
+          if (at < p.n) cand[kCand - 1 - at] = Key::of(bar, (u * BLK + tid) * E + e);
           ++at;
         }
     }
     __syncthreads();
-    c = count;
+    c = min(count, p.n);
     const int taken = t != kNegInf ? min(p.n - c, ties) : 0;
     left_ties = t != kNegInf ? ties - taken : 0;
     typename Key::type tie{};
@@ -338,9 +344,18 @@ __device__ __forceinline__ int tie_beam(uint64_t t) { return kBeamMax - 1 - int(
 __device__ __forceinline__ uint64_t tie_entry(uint64_t t) {
   return (t >> 18) << 32 | 0xfffc0000u | (uint32_t(t) & 0x3ffffu);
 }
+// A rank as a whole number of the same order, -0 as +0; NaN has a place in it too, so that any inputs
+// end in a choice of existing beams and tokens.
+__device__ __forceinline__ uint64_t rank_key(double r) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, r + 0.0);
+  return b ^ (uint64_t(int64_t(b) >> 63) | uint64_t(1) << 63);
+}
+__device__ __forceinline__ double key_rank(uint64_t k) {
+  return __builtin_bit_cast(double, k ^ (k >> 63 ? uint64_t(1) << 63 : ~uint64_t(0)));
+}
 struct alignas(16) Candidate {
-  double rank;
-  uint64_t tie;
+  uint64_t rank;  // rank_key()
+  uint64_t tie;   // never 0
 };
 // without branches: both are read at once
 __device__ __forceinline__ bool before(const Candidate& a, const Candidate& b) {
@@ -405,7 +420,7 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
       lse[w] = st == 0 && m != kNegInf ? double(m) * p.inv_t + log(s) : 0.0;
       score[w] = double(sw);
       state[w] = st;
-      factor[w] = p.alpha != 0.0 ? pow(double(len + (st == 0)), p.alpha) : 1.0;
+      factor[w] = p.alpha != 0.0 ? pow(double(len) + double(st == 0), p.alpha) : 1.0;
       inverse[w] = 1.0 / factor[w];
     }
   }
@@ -477,7 +492,7 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
   auto consider = [&](int w, uint64_t e) {
     if (e == 0 || key_of(w, e) < least) return;
     const int at = atomicAdd(&count, 1);
-    if (at < kSurvivors) chosen[at] = {rank_of(w, e), tie_of(w, e)};
+    if (at < kSurvivors) chosen[at] = {rank_key(rank_of(w, e)), tie_of(w, e)};
   };
   // candidate i's beam and entry; false where there is none
   auto candidate = [&](int i, int& w, uint64_t& e) {
@@ -515,13 +530,13 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
     p.out.parents[o + j] = w;
     p.out.tokens[o + j] = token;
     if (p.out.scores) p.out.scores[o + j] = float(total_of(w, e));
-    if (p.out.rank) p.out.rank[o + j] = float(c.rank);
+    if (p.out.rank) p.out.rank[o + j] = float(key_rank(c.rank));
     if (p.out.finished) p.out.finished[o + j] = done || token == p.eos;
     if (p.out.lengths) p.out.lengths[o + j] = (p.lengths ? p.lengths[row0 + w] : 0) + !done;
   };
   if (c <= kSurvivors) {
     // counted by their 32-bit keys; those that share one, by what they are
-    for (int i = tid; i < c; i += NT) keys[i] = order_key<F32>(float(chosen[i].rank));
+    for (int i = tid; i < c; i += NT) keys[i] = order_key<F32>(float(key_rank(chosen[i].rank)));
     for (int i = c + tid; i < ((c + 7) & ~7); i += NT) keys[i] = 0u;
     for (int i = tid; i < c; i += NT) taken[i] = 0;
     __syncthreads();
@@ -557,18 +572,19 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
     }
   } else {
     // too many that the bound does not tell apart (rows of equal logits): one after the other
-    Candidate last{__builtin_huge_val(), ~uint64_t(0)};
+    Candidate last{~uint64_t(0), ~uint64_t(0)};
     for (int found = 0; found < p.n; ++found) {
-      Candidate best{-__builtin_huge_val(), 0};
+      Candidate best{0, 0};
       for (int i = tid; i < C + p.W; i += NT) {
         int w;
         uint64_t e;
         if (!candidate(i, w, e)) continue;
-        const Candidate c{rank_of(w, e), tie_of(w, e)};
+        const Candidate c{rank_key(rank_of(w, e)), tie_of(w, e)};
         if (before(last, c) && before(c, best)) best = c;
       }
       for (int off = 32; off > 0; off >>= 1) {
-        const Candidate c{__shfl_xor(best.rank, off, kWave), uint64_t(__shfl_xor((unsigned long long)best.tie, off, kWave))};
+        const Candidate c{uint64_t(__shfl_xor((unsigned long long)best.rank, off, kWave)),
+                          uint64_t(__shfl_xor((unsigned long long)best.tie, off, kWave))};
         if (before(c, best)) best = c;
       }
       __syncthreads();
