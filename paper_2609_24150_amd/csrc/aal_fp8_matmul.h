@@ -130,13 +130,24 @@ __device__ __forceinline__ int place_in_stage(int row, int byte) {
 // ------------------------------------------------------------------ tiles
 // A workgroup of WN x WM waves makes 16 TN WN x 16 TM WM results.  Both operands' rows of a block, 128 bytes
 // each, are loaded straight into LDS, the next block's while one is being multiplied.
-template <bool WIDE, int FA, int FB, bool SQUARE, int TN, int TM, int WN, int WM>
+//
+// A CU has 64 KB of tiles a stage and two stages of them, so that one tile of 256 x 256 (eight waves) or two of 128 x 128
+// (four each) are at work in it.  Bound by how fast stages arrive and by LDS: a block of 256 x 256 x 128 takes 3,700 to
+// 4,000 cycles, 2,048 of them in the matrix unit; 8,192 x 128,256 x 4,096 4.3 ms, 2.0 PFLOP/s.  WIDE has half the
+// matrix unit's rate, and 1.08 PFLOP/s at 8,192^3.  The library's products there: with one scale for all 2.6 to 3.2, bf16 1.3.
+//
+// POW (with WIDE, scales that are powers of two): the widening to bf16 applies them, which is exact, and sums stay in the
+// matrix unit from block to block: no arithmetic on sums, a third of the instructions.  128,256 x 4,096 x 2,048 into fp32 2.26
+// ms, with the scales applied to sums 2.53; 256 x 256 tiles, whose registers do not do, 3.11.
+template <bool WIDE, bool POW, int FA, int FB, bool SQUARE, int TN, int TM, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
+  static_assert(WIDE || !POW, "products of 8-bit instructions take scales on their sums");
   constexpr int NT = 64 * WN * WM, BN = 16 * TN * WN, BM = 16 * TM * WM, RP = NT / 8;  // RP: rows of a round of loads
   static_assert(BN + BM == NT, "one scale per thread");
   static_assert(!SQUARE || 128 % (16 * TN) == 0, "a wave's columns have one scale");
   __shared__ __attribute__((aligned(16))) uint8_t tile[2][(BN + BM) * 128];
   __shared__ __attribute__((aligned(16))) float scales[2][BN + BM];
+  __shared__ int far[2][POW ? WN * WM : 1];  // a wave's scales of a stage take bf16 out of its range
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l = lane & 15, h = lane >> 4;
   // A tile of c, and the blocks of a part of K.  Workgroups go round over the 8 XCDs: each XCD takes a stretch of
@@ -183,7 +194,14 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
   };
   uint32_t next = 0;
   auto load_scales = [&](const Sources& t, int j) { next = raw_scale(scale_base, t.scale + j * scale_step, p.e8m0); };
-  auto put_scales = [&](int to) { scales[to][tid] = scale_of(next, p.e8m0); };
+  auto put_scales = [&](int to) {
+    scales[to][tid] = scale_of(next, p.e8m0);
+    if constexpr (POW) {
+      // 2^-100 to 2^100 times what either format holds are normal numbers
+      const bool any = __builtin_amdgcn_ballot_w64(next - 27u > 200u) != 0;
+      if (lane == 0) far[to][wave] = any;
+    }
+  };
   // K ends inside the last block: zeros for what lies behind it
   auto clear_tail = [&](int to) {
     const int rem = p.K & 127;
@@ -252,20 +270,51 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
   if (live) send(1, 0, kLoads);
   bool sending = false;  // a block's loads are under way
   const int at_b = (wn * TN * 16 + l) * 128, at_a = (BN + wm * TM * 16 + l) * 128;
-  i32x8 xa[TM], xb[2] = {fragment(tile[0] + at_b), fragment(tile[0] + at_b + 16 * 128)};
+  // POW: half of a block at a time, a 16-byte piece of each row, and the scales of the lane's own rows
+  constexpr int SB = SQUARE ? 1 : TN;
+  u32x4 pa[TM], pb[TN];
+  float sa[TM], sb[SB];
+  bool plain = true;
+  auto is_plain = [&](int at) {
+    int any = 0;
+#pragma unroll
+    for (int w = 0; w < (POW ? WN * WM : 0); ++w) any |= far[at][w];
+    return __builtin_amdgcn_readfirstlane(any) == 0;
+  };
+  auto scale_a = [&](int at, int m) { return plain ? scales[at][BN + (wm * TM + m) * 16 + l] : 1.f; };
+  auto scale_b = [&](int at, int n) { return plain ? scales[at][wn * TN * 16 + (SQUARE ? 0 : n * 16 + l)] : 1.f; };
+  auto piece_at = [&](const uint8_t* at, int back_half) { return *reinterpret_cast<const u32x4*>(at + (back_half ? back : front)); };
+  i32x8 xa[TM], xb[2];
+  if constexpr (!POW) {
+    xb[0] = fragment(tile[0] + at_b);
+    xb[1] = fragment(tile[0] + at_b + 16 * 128);
+  }
   f32x4 made[TM], fb{}, fp{};
   float fa[TM];
   auto scales_b = [&](int at, int n) { return *reinterpret_cast<const f32x4*>(&scales[at][(wn * TN + n) * 16 + h * 4]); };
-  if constexpr (!SQUARE) fb = scales_b(0, 0);
+  if constexpr (!SQUARE && !POW) fb = scales_b(0, 0);
+  if constexpr (POW) {
+    plain = is_plain(0);
+#pragma unroll
+    for (int m = 0; m < TM; ++m) {
+      sa[m] = scale_a(0, m);
+      pa[m] = piece_at(tile[0] + at_a + m * 16 * 128, 0);
+    }
+#pragma unroll
+    for (int n = 0; n < TN; ++n) {
+      if (n < SB) sb[n] = scale_b(0, n);
+      pb[n] = piece_at(tile[0] + at_b + n * 16 * 128, 0);
+    }
+  }
 #pragma unroll
   for (int m = 0; m < TM; ++m) {
-    xa[m] = fragment(tile[0] + at_a + m * 16 * 128);
+    if constexpr (!POW) xa[m] = fragment(tile[0] + at_a + m * 16 * 128);
     made[m] = f32x4{0.f, 0.f, 0.f, 0.f};
     fa[m] = 0.f;
   }
   auto add = [&](int n, int m, const f32x4& t, float f, const f32x4& g) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[n][m][i] = __builtin_fmaf(t[i], SQUARE ? f : f * g[i], acc[n][m][i]);
+    for (int i = 0; i < 4; ++i) acc[n][m][i] = __builtin_fmaf(t[i], SQUARE && !POW ? f : f * g[i], acc[n][m][i]);
     // here, not where the compiler would rather have all of them: 128 registers of products
     asm volatile("" : "+v"(acc[n][m]));
   };
@@ -284,6 +333,68 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
     const uint8_t* next_b = tile[stage ^ 1] + at_b;
     const uint8_t* next_a = tile[stage ^ 1] + at_a;
     float fn[TM];
+    if constexpr (POW) {
+      // A quarter of the block at a time, widened; a piece's registers take the next one when it has had its last use.
+      const uint8_t* ta = tile[stage] + at_a;
+      const bool apply = plain;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int w0 = s % 2 * 2;
+        bf16x8 wa[TM];
+#pragma unroll
+        for (int m = 0; m < TM; ++m) wa[m] = widen<FA>(int(pa[m][w0]), int(pa[m][w0 + 1]), sa[m]);
+        if (!apply) {
+          // widened as they are: sums times the scales, which are read before another wave may replace them
+#pragma unroll
+          for (int n = 0; n < TN; ++n) {
+            const f32x4 g = SQUARE ? f32x4{1.f, 1.f, 1.f, 1.f} * scales[stage][wn * TN * 16] : scales_b(stage, n);
+            const bf16x8 w = widen<FB>(int(pb[n][w0]), int(pb[n][w0 + 1]));
+#pragma unroll
+            for (int m = 0; m < TM; ++m)
+              add(n, m, __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, wa[m], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0),
+                  scales[stage][BN + (wm * TM + m) * 16 + l], g);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          // and nothing is left to add to them below, which has no branch
+#pragma unroll
+          for (int n = 0; n < TN; ++n) pb[n][w0] = pb[n][w0 + 1] = 0u;
+#pragma unroll
+          for (int m = 0; m < TM; ++m) wa[m] = bf16x8{};
+        }
+        if (s == 3) {
+          if (more) {
+            arrived(stage ^ 1, next_j);
+            advance();
+            sending = live;
+          } else {
+            sending = false;
+          }
+          plain = is_plain(stage ^ 1);
+        }
+        if (s % 2) {
+#pragma unroll
+          for (int m = 0; m < TM; ++m) {
+            pa[m] = piece_at((s == 1 ? ta : next_a) + m * 16 * 128, s == 1);
+            if (s == 3) sa[m] = scale_a(stage ^ 1, m);
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < TN; ++n) {
+          const bf16x8 w = widen<FB>(int(pb[n][w0]), int(pb[n][w0 + 1]), sb[SQUARE ? 0 : n]);
+          if (s % 2) pb[n] = piece_at((s == 1 ? tb : next_b) + n * 16 * 128, s == 1);
+          if (s == 3 && !SQUARE) sb[n] = scale_b(stage ^ 1, n);
+          if (sending && n % (TN / 2) == 0) {
+            constexpr int kPart = kLoads / 4;
+            const int part = (s == 0 ? 2 : 0) + n / (TN / 2);
+            if (s == 3 || s == 0) send(s == 3 ? stage : stage ^ 1, part * kPart, kPart);
+          }
+#pragma unroll
+          for (int m = 0; m < TM; ++m) acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, wa[m], acc[n][m], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (s == 3 && SQUARE) sb[0] = scale_b(stage ^ 1, 0);
+      }
+    } else {
     // each row of products is added while the next one is in the matrix unit
 #pragma unroll
     for (int n = 0; n < TN; ++n) {
@@ -326,6 +437,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
       }
       fp = g;
     }
+    }
     stage ^= 1;
     j = next_j;
     if (!last) continue;
@@ -334,9 +446,11 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
     const bool bf16 = whole && p.out_bf16;
 #pragma unroll
     for (int m = 0; m < TM; ++m) {
-      add(TN - 1, m, made[m], fa[m], fp);
-      made[m] = f32x4{0.f, 0.f, 0.f, 0.f};
-      fa[m] = 0.f;
+      if constexpr (!POW) {
+        add(TN - 1, m, made[m], fa[m], fp);
+        made[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+        fa[m] = 0.f;
+      }
       const int64_t gm = int64_t(t.down) * BM + (wm * TM + m) * 16 + l, n0 = int64_t(t.across) * BN + wn * TN * 16;
       if (bf16) {
         // two tiles' columns change places between neighbouring rows of lanes: 8 side by side a lane, 64 bytes of a row of c
@@ -365,9 +479,10 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
 }
 
 // --------------------------------------------------------------- few rows
-// Up to 16 TM rows of a: b is read once and bounds the time.  A workgroup of four waves takes 128 rows of b and at
-// most kFewBlocks blocks, which run through a ring of kRing stages in LDS, two of them on their way while one is
-// being multiplied.  All its scales are in LDS before that, so that the loop waits for the stages alone.
+// Up to 16 TM rows of a: b is read once and bounds the time (7 x 128,256 x 4,096 85 us, 6.2 TB/s where a lone read has 7.1).
+// A workgroup of four waves takes 128 rows of b and at most kFewBlocks blocks, which run through a ring of kRing stages in
+// LDS, two of them on their way while one is being multiplied.  All its scales are in LDS before that, so that the
+// loop waits for the stages alone.
 constexpr int kFewBlocks = 32, kRing = 3;
 
 template <int N>
@@ -481,10 +596,12 @@ hipError_t launch_square(const MatmulParams& p, const MatmulPlan& plan, hipStrea
     k_few_rows<WIDE, FA, FB, SQUARE, 1><<<few, 256, 0, stream>>>(p);
   else if (plan.kind == 0)
     k_few_rows<WIDE, FA, FB, SQUARE, 2><<<few, 256, 0, stream>>>(p);
+  else if (WIDE && p.e8m0)
+    k_tiles<WIDE, WIDE, FA, FB, SQUARE, 4, 4, 2, 2><<<grid, 256, 0, stream>>>(p);
   else if (plan.kind == 1)
-    k_tiles<WIDE, FA, FB, SQUARE, 4, 4, 2, 2><<<grid, 256, 0, stream>>>(p);
+    k_tiles<WIDE, false, FA, FB, SQUARE, 4, 4, 2, 2><<<grid, 256, 0, stream>>>(p);
   else if constexpr (!WIDE)
-    k_tiles<WIDE, FA, FB, SQUARE, 8, 4, 2, 4><<<grid, 512, 0, stream>>>(p);
+    k_tiles<WIDE, false, FA, FB, SQUARE, 8, 4, 2, 4><<<grid, 512, 0, stream>>>(p);
   return hipGetLastError();
 }
 

@@ -21,11 +21,13 @@ MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, bool wide) {
     const int64_t s = std::min(want / std::max<int64_t>(groups, 1), blocks / least);
     return int(std::max<int64_t>(1, std::min<int64_t>(s, 64)));
   };
+  // few rows of a times 128,256 x 4,096 take 85 us in that kernel, 33 rows take 105 in tiles
   if (M <= 32) return {0, int(std::max<int64_t>(up(blocks, kFewBlocks), splits(up(N, 128), 4 * kCus, 8)))};
   const int64_t large = up(M, 256) * up(N, 256), small = up(M, 128) * up(N, 128);
   const int sl = splits(large, kCus, 8), ss = splits(small, 2 * kCus, 8);
   // turns of the chip times the work of a tile; small tiles take more LDS traffic per result
   const double tl = double(up(large * sl, kCus)) * 4.0 / sl, ts = double(up(small * ss, 2 * kCus)) * 2.0 * 1.25 / ss;
+  // fp32 results need widened operands, for which tiles of 256 x 256 have no registers left (3.1 ms instead of 2.3)
   return tl <= ts && !wide ? MatmulPlan{2, sl} : MatmulPlan{1, ss};
 }
 

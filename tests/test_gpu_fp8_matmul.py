@@ -2,7 +2,8 @@
 
 Tolerances, relative to M = sum_k |a b| with the scales.  fp32 results: the values are exact in bf16 and so are
 their products in fp32; a block's 128 additions round (or cut) by at most 2^-23 each, the product of the scales by
-2^-24, and so does the sum of each block: 128 2^-23 + (blocks + 2) 2^-24.  bf16 results: the matrix unit's sums of
+2^-24, and so does the sum of each block: 128 2^-23 + (blocks + 2) 2^-24 (asked as well where scales are powers of two,
+though sums run on from block to block there).  bf16 results: the matrix unit's sums of
 8-bit products keep, of each eight neighbours, what lies above 2^-13 of the largest product's power of two, so that each of
 eight is off by at most 2^-13 of the largest, the largest itself by nothing: 7 2^-13 of the eight's sum of
 |a b| and so of M; rounding to bf16 adds 2^-8 of the value."""

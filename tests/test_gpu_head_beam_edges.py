@@ -52,6 +52,27 @@ def test_products_at_each_number_of_rows(A, M, out):
         assert torch.equal(z, exact(a, b).to(out)), (N, K)
 
 
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("M,N", [(5, 300), (300, 260)])
+def test_products_of_scales_that_bf16_does_not_hold(A, M, N, block):
+    """Blocks whose scales are 2^-127 to 2^-101 and their inverses among others, which fp32 holds the products of."""
+    K = 128 * 11 + 60
+    (a, _), (b, _) = signs(M, K, 5), signs(N, K, 6)
+    g = torch.Generator().manual_seed(M)
+    nb = (K + 127) // 128
+    e = torch.where(torch.rand(nb, generator=g) < 0.5, torch.randint(101, 127, (nb,), generator=g), torch.zeros(nb, dtype=torch.int64))
+    e[:2], e[-1], e[4:7] = 0, 126, torch.tensor([127, 0, 127])
+    shift = torch.randint(-2, 3, (1 if block == 128 else N, 1), generator=g)
+    rows = (N + 127) // 128 if block == 128 else N
+    scale = lambda x: (x + 127).clamp(0, 254).to(torch.uint8).view(torch.float8_e8m0fnu).cuda()  # noqa: E731
+    sa = scale(-e[None].expand(M, nb) + 0)
+    sb = scale((e[None] - 2 * (e[None] > 0) + shift * (e[None] == 0)).expand(rows, nb))
+    k = torch.arange(K) // 128
+    factor = torch.exp2((-2.0 * (e[None] > 0) + shift * (e[None] == 0)))[:, k].cuda()  # of b's values, 1 or 128 rows alike
+    want = a.float() @ (b.float() * factor).t()
+    assert torch.equal(A.aal_fp8_matmul(a, sa, b, sb, out_dtype=F32), want)
+
+
 def test_products_past_32_bits(A):
     """Operands and results whose last entries lie 2^32 bytes behind the first."""
     (a, sa), (b, sb) = signs(40_000, 128, 1), signs(60_001, 128, 2)
