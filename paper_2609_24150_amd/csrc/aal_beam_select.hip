@@ -105,6 +105,17 @@ __device__ __forceinline__ double wave_sum_dpp(double v) {
                                         uint32_t(__builtin_amdgcn_readlane(int(uint32_t(b)), 63)));
 }
 
+// The largest over the wave, alike.
+template <int Ctrl, int RowMask>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+  return max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), Ctrl, RowMask, 0xF, false)));
+}
+__device__ __forceinline__ uint32_t wave_max_key(uint32_t v) {
+  v = dpp_max<0x140, 0xF>(dpp_max<0x141, 0xF>(dpp_max<0x4E, 0xF>(dpp_max<0xB1, 0xF>(v))));
+  v = dpp_max<0x143, 0xC>(dpp_max<0x142, 0xA>(v));
+  return uint32_t(__builtin_amdgcn_readlane(int(v), 63));
+}
+
 // A value that all lanes have, as one of the wave.
 __device__ __forceinline__ float uniform(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
@@ -455,9 +466,7 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
       heads[wv][k] = more;
       top = max(top, more);
     }
-    top = max(top, ended);
-    for (int off = 32; off > 0; off >>= 1) top = max(top, uint32_t(__shfl_xor(int(top), off, kWave)));
-    top = uint32_t(__builtin_amdgcn_readfirstlane(int(top)));
+    top = wave_max_key(max(top, ended));
     const int r = (p.n + number - 1) / number, enough = r + r / 8;
     uint32_t lo = 0u, hi = top + 1u;  // lo is reached by r or is 0
     while (hi > lo + 1u) {
@@ -535,23 +544,29 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
     if (p.out.lengths) p.out.lengths[o + j] = (p.lengths ? p.lengths[row0 + w] : 0) + !done;
   };
   if (c <= kSurvivors) {
-    // counted by their 32-bit keys; those that share one, by what they are
+    // counted by their 32-bit keys; those that share one, by what they are: found through a chain of them, or, of many,
+    // among all (the next one of a chain is known when this one has been read)
+    int *first = reinterpret_cast<int*>(heads[0]), *following = reinterpret_cast<int*>(heads[1]);
     for (int i = tid; i < c; i += NT) keys[i] = order_key<F32>(float(key_rank(chosen[i].rank)));
-    for (int i = c + tid; i < ((c + 7) & ~7); i += NT) keys[i] = 0u;
-    for (int i = tid; i < c; i += NT) taken[i] = 0;
+    for (int i = c + tid; i < ((c + 15) & ~15); i += NT) keys[i] = 0u;
+    for (int i = tid; i < c; i += NT) {
+      taken[i] = 0;
+      first[i] = -1;
+    }
     __syncthreads();
     // as many threads to one as there are
     const int g = c <= NT / 8 ? 8 : c <= NT / 4 ? 4 : c <= NT / 2 ? 2 : 1;
     for (int i = tid / g; i < c; i += NT / g) {
       const uint32_t mine = keys[i];
       int at = 0;
-      for (int j = tid % g * 8; j < c; j += g * 8)
+      for (int j = tid % g * 16; j < c; j += g * 16)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) at += keys[j + k] > mine;
+        for (int k = 0; k < 16; ++k) at += keys[j + k] > mine;
       for (int off = 1; off < g; off <<= 1) at += __shfl_xor(at, off, kWave);
       if (tid % g == 0) {
         place[i] = uint16_t(at);
         atomicAdd(&taken[at], 1);
+        following[i] = atomicExch(&first[at], i);
       }
     }
     __syncthreads();
@@ -559,7 +574,10 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
       const Candidate mine = chosen[i];
       int at = place[i];
       if (at >= p.n) continue;
-      if (taken[at] > 1) {
+      const int alike = taken[at];
+      if (alike > 1 && alike <= 16) {
+        for (int j = first[at], k = 0; k < alike; ++k, j = following[j]) at += before(chosen[j], mine);
+      } else if (alike > 1) {
         const uint32_t key = keys[i];
         for (int j = 0; j < c; j += 8) {
           uint32_t same = 0;
