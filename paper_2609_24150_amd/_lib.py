@@ -162,7 +162,7 @@ _SIGNATURES = {
         _vp, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, _vp, _vp, _vp, C.c_float, C.c_int32,
         C.c_int32, C.POINTER(BeamOut), _vp, C.c_size_t, _vp]),
     "aal_beam_reorder": (C.c_int, [
-        C.POINTER(BeamState), C.c_int32, C.c_int64, C.c_int32, C.c_int32, _vp, _vp]),
+        _vp, C.c_int32, C.c_int64, C.c_int32, C.c_int32, _vp, _vp]),
     "aal_stream_probe": (C.c_int, [_vp, _vp, _vp, _vp, C.c_size_t, _vp, _vp]),
     "aal_vp_grad": (C.c_int, [
         _vp, _vp, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_int, C.c_float, C.c_float, _vp, _vp, C.c_int,

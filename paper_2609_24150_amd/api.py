@@ -9,6 +9,7 @@ import contextlib
 import ctypes as C
 import functools
 import operator
+import struct
 
 import torch
 
@@ -796,6 +797,7 @@ def aal_fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_sc
     return out
 
 
+@functools.lru_cache(maxsize=4096)
 def aal_fp8_matmul_workspace_bytes(M: int, N: int, K: int) -> int:
     return int(_lib.lib().aal_fp8_matmul_workspace_bytes(int(M), int(N), int(K)))
 
@@ -867,6 +869,7 @@ def aal_head_logits_bwd(grad: torch.Tensor, x: torch.Tensor, head: dict, *, x_gr
 # ----------------------------------------------------------------------------
 # Beam search.
 
+@functools.lru_cache(maxsize=4096)
 def aal_beam_select_workspace_bytes(dtype: torch.dtype, B: int, W: int, V: int, n: int) -> int:
     return int(_lib.lib().aal_beam_select_workspace_bytes(_dtype_code(dtype), int(B), int(W), int(V), int(n)))
 
@@ -1019,9 +1022,8 @@ def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) ->
     W = states[0].shape[1] if states[0].dim() >= 2 else 0
     if not 1 <= n <= AAL_BEAM_SELECT_MAX or (out is None and (n != W or n > AAL_BEAM_MAX)):
         raise ValueError(f"n must be in [1, {AAL_BEAM_SELECT_MAX}], in place W and at most {AAL_BEAM_MAX}; got {n}")
-    table = (_lib.BeamState * len(states))()
-    spans = []
-    for row, s, o in zip(table, states, outs):
+    table, spans = [], []  # what aal_beam_state_t holds, one state after the other
+    for s, o in zip(states, outs):
         shape, stride = tuple(s.shape), s.stride()
         if len(shape) < 2 or shape[0] != B or shape[1] != W or s.device != dev:
             raise ValueError(f"states must be [{B}, {W}, ...] on {dev}; got {shape} on {s.device}")
@@ -1030,28 +1032,31 @@ def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) ->
             raise ValueError("a state must be contiguous pieces at one distance behind its first two dimensions")
         e = s.element_size()
         count, size, step, span = cut
-        at = s.data_ptr()
-        if count and size:
-            spans.append((at, span * e, out is None, (count, size * e, step * e), ((stride[0] * e, B), (stride[1] * e, W))))
-        row.src, row.src_request, row.src_beam, row.src_segment = at, stride[0] * e, stride[1] * e, step * e
-        row.segments, row.segment_bytes = count, size * e
-        if out is not None:
+        moves = count and size
+        at, request, beam, step, piece = s.data_ptr(), stride[0] * e, stride[1] * e, step * e, size * e
+        if moves:
+            spans.append((at, span * e, out is None, (count, piece, step), ((request, B), (beam, W))))
+        if out is None:
+            row = (at, 0, request, beam, step, 0, 0, 0, count, piece)
+        else:
             if o.shape != (B, n, *shape[2:]) or o.dtype != s.dtype or o.device != dev:
                 raise ValueError(f"out must be [{B}, {n}, ...] of the states' shapes and dtypes on {dev}")
             shape, stride = tuple(o.shape), o.stride()
             to = _segments(shape, stride)
             if to is None or to[:2] != (count, size):
                 raise ValueError("an output must be the same contiguous pieces as its state")
-            at = o.data_ptr()
-            if count and size:
-                spans.append((at, to[3] * e, True, (count, size * e, to[2] * e), ((stride[0] * e, B), (stride[1] * e, n))))
-            row.dst, row.dst_request, row.dst_beam, row.dst_segment = at, stride[0] * e, stride[1] * e, to[2] * e
+            row = (at, o.data_ptr(), request, beam, step, stride[0] * e, stride[1] * e, to[2] * e, count, piece)
+            if moves:
+                spans.append((row[1], to[3] * e, True, (count, piece, row[7]), ((row[5], B), (row[6], n))))
         if not _apart(shape, stride):
             raise ValueError("the entries of what is written must not share memory")
+        if moves:
+            table += row
     if len(spans) > 1:
         _check_memory(spans)
     with _guard(dev, stream):
-        st = _lib.lib().aal_beam_reorder(table, len(states), B, W, n, _ptr(parents), _raw_stream(dev, stream))
+        st = _lib.lib().aal_beam_reorder(struct.pack(f"{len(table)}q", *table), len(table) // 10, B, W, n, _ptr(parents),
+                                         _raw_stream(dev, stream))
     _lib.check(st, "aal_beam_reorder")
     return outs
 

@@ -13,12 +13,15 @@
 namespace aal {
 namespace {
 
-constexpr int kStates = 40;  // of a launch: their descriptions are kernel arguments, under 4 KiB
+// States of a launch: their descriptions are kernel arguments, under 4 KiB, and under 1 KiB where there are few, which is
+// less to hand over.
+constexpr int kStates = 40, kFew = 8;
 
+template <int STATES>
 struct ReorderParams {
-  BeamState s[kStates];
-  int64_t end[kStates];      // workgroups up to and with each state's
-  uint32_t chunks[kStates];  // workgroups per request
+  BeamState s[STATES];
+  int64_t end[STATES];      // workgroups up to and with each state's
+  uint32_t chunks[STATES];  // workgroups per request
   int64_t first;             // workgroup that the launch starts with
   int n_states, W, n;
   const int32_t* parents;
@@ -31,8 +34,8 @@ template <> struct PieceOf<4> { using type = uint32_t; };
 template <> struct PieceOf<1> { using type = uint8_t; };
 
 // VB: bytes of a piece, NB: slots held at a time (in place: all of them)
-template <int VB, int NB, bool IN_PLACE>
-__global__ __launch_bounds__(256) void k_beam_reorder(ReorderParams p) {
+template <int VB, int NB, bool IN_PLACE, int STATES>
+__global__ __launch_bounds__(256) void k_beam_reorder(ReorderParams<STATES> p) {
   using T = typename PieceOf<VB>::type;
   const int64_t block = p.first + blockIdx.x;
   int k = 0;
@@ -64,8 +67,8 @@ __global__ __launch_bounds__(256) void k_beam_reorder(ReorderParams p) {
   }
 }
 
-template <int VB, int NB>
-void enqueue(const ReorderParams& p, unsigned grid, bool in_place, hipStream_t stream) {
+template <int VB, int NB, int STATES>
+void enqueue(const ReorderParams<STATES>& p, unsigned grid, bool in_place, hipStream_t stream) {
   if (in_place)
     k_beam_reorder<VB, NB, true><<<grid, 256, 0, stream>>>(p);
   else if constexpr (NB <= 32)
@@ -82,8 +85,8 @@ int piece_of(const BeamState& s, int W, int n, int64_t B) {
   return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1;
 }
 
-template <int VB>
-void enqueue_piece(const ReorderParams& p, unsigned grid, bool in_place, hipStream_t stream) {
+template <int VB, int STATES>
+void enqueue_piece(const ReorderParams<STATES>& p, unsigned grid, bool in_place, hipStream_t stream) {
   if (p.n <= 4)
     enqueue<VB, 4>(p, grid, in_place, stream);
   else if (p.n <= 8)
@@ -96,46 +99,51 @@ void enqueue_piece(const ReorderParams& p, unsigned grid, bool in_place, hipStre
     enqueue<VB, 64>(p, grid, in_place, stream);
 }
 
-hipError_t launch_piece(const ReorderArgs& a, int piece) {
+// The next states of that piece, from number `next` on, as many as a launch takes.
+template <int STATES>
+void launch_some(const ReorderArgs& a, int piece, int& next) {
   // slots beyond 32 in place are held in pieces of 8 bytes: 128 registers
   const int bytes = piece == 16 && a.in_place && a.n > 32 ? 8 : piece;
-  for (int next = 0; next < a.n_states;) {
-    ReorderParams p{};
-    p.W = a.W;
-    p.n = a.n;
-    p.parents = a.parents;
-    int64_t total = 0;
-    for (; next < a.n_states && p.n_states < kStates; ++next) {
-      const BeamState& s = a.states[next];
-      if (s.segments == 0 || s.segment_bytes == 0 || piece_of(s, a.W, a.n, a.B) != piece) continue;
-      const int64_t chunks = (s.segments * (s.segment_bytes / bytes) + 255) / 256;
-      total += a.B * chunks;
-      p.s[p.n_states] = s;
-      p.chunks[p.n_states] = uint32_t(chunks);
-      p.end[p.n_states++] = total;
-    }
-    // a launch holds fewer than 2^32 threads
-    for (; p.first < total; p.first += int64_t(1) << 23) {
-      const unsigned grid = unsigned(total - p.first < (int64_t(1) << 23) ? total - p.first : int64_t(1) << 23);
-      if (bytes == 16)
-        enqueue_piece<16>(p, grid, a.in_place, a.stream);
-      else if (bytes == 8)
-        enqueue<8, 64>(p, grid, true, a.stream);
-      else if (bytes == 4)
-        enqueue_piece<4>(p, grid, a.in_place, a.stream);
-      else
-        enqueue_piece<1>(p, grid, a.in_place, a.stream);
-    }
+  ReorderParams<STATES> p;
+  p.n_states = 0;
+  p.first = 0;
+  p.W = a.W;
+  p.n = a.n;
+  p.parents = a.parents;
+  int64_t total = 0;
+  for (; next < a.n_states && p.n_states < STATES; ++next) {
+    const BeamState& s = a.states[next];
+    if (s.segments == 0 || s.segment_bytes == 0 || piece_of(s, a.W, a.n, a.B) != piece) continue;
+    const int64_t chunks = (s.segments * (s.segment_bytes / bytes) + 255) / 256;
+    total += a.B * chunks;
+    p.s[p.n_states] = s;
+    p.chunks[p.n_states] = uint32_t(chunks);
+    p.end[p.n_states++] = total;
   }
-  return hipGetLastError();
+  // a launch holds fewer than 2^32 threads
+  for (; p.first < total; p.first += int64_t(1) << 23) {
+    const unsigned grid = unsigned(total - p.first < (int64_t(1) << 23) ? total - p.first : int64_t(1) << 23);
+    if (bytes == 16)
+      enqueue_piece<16>(p, grid, a.in_place, a.stream);
+    else if (bytes == 8)
+      enqueue<8, 64>(p, grid, true, a.stream);
+    else if (bytes == 4)
+      enqueue_piece<4>(p, grid, a.in_place, a.stream);
+    else
+      enqueue_piece<1>(p, grid, a.in_place, a.stream);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_beam_reorder(const ReorderArgs& a) {
   for (int piece : {16, 4, 1})
-    if (hipError_t e = launch_piece(a, piece); e != hipSuccess) return e;
-  return hipSuccess;
+    for (int next = 0; next < a.n_states;)
+      if (a.n_states - next <= kFew)
+        launch_some<kFew>(a, piece, next);
+      else
+        launch_some<kStates>(a, piece, next);
+  return hipGetLastError();
 }
 
 }  // namespace aal

@@ -253,3 +253,26 @@ def test_states_that_share_memory(A):
     assert np.array_equal(u.double().cpu().numpy(), want) and torch.equal(u, v)
     A.aal_beam_reorder([t[:, :, 0], t[:, :, 1, :20], t[:, :, 1, 20:]], p)
     assert torch.equal(t, u)
+
+
+def test_states_without_bytes(A):
+    """A cache of no positions yet, among others, into other buffers and in place."""
+    p = torch.tensor([[1, 0, 1]], dtype=torch.int32, device="cuda")
+    full = torch.arange(6, device="cuda").view(1, 2, 3)
+    empty, out = torch.zeros(1, 2, 0, 8, device="cuda"), torch.zeros(1, 3, 3, dtype=torch.int64, device="cuda")
+    A.aal_beam_reorder([empty, full], p, out=[torch.zeros(1, 3, 0, 8, device="cuda"), out])
+    assert out.tolist() == [[[3, 4, 5], [0, 1, 2], [3, 4, 5]]]
+    A.aal_beam_reorder([empty, full], p[:, :2].contiguous())
+    assert full.tolist() == [[[3, 4, 5], [0, 1, 2]]]
+    assert A.aal_beam_reorder([empty], p[:, :2].contiguous())[0] is empty
+
+
+@pytest.mark.parametrize("count", [1, 7, 8, 9, 40, 41, 49, 130])
+def test_any_number_of_states(A, count):
+    p = torch.tensor([[1, 0, 1], [2, 1, 0]], dtype=torch.int32, device="cuda")
+    g = torch.Generator("cuda").manual_seed(count)
+    states = [torch.randint(0, 99, (2, 3, 3 + i % 5), generator=g, device="cuda", dtype=(torch.uint8, torch.int32, torch.int64)[i % 3])
+              for i in range(count)]
+    want = [s[torch.arange(2, device="cuda")[:, None], p.long()] for s in states]
+    A.aal_beam_reorder(states, p)
+    assert all(torch.equal(s, w) for s, w in zip(states, want))
