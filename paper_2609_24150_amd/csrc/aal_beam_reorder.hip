@@ -6,7 +6,8 @@
 // addresses and strides divide) at one place of a request's slots: it loads that place of every slot's
 // parent, then stores them, so that in place no slot is overwritten before it has been
 // read, and nothing waits for another thread.  In place, slots that are their own parent are
-// neither loaded nor stored.  Bound by memory: two bytes of traffic for each byte that moves.
+// neither loaded nor stored.  Bound by memory: two bytes of traffic for each byte that moves.  0.8 GB of caches in place 300
+// us, 5.4 TB/s, into other buffers 424 us for 1.2 GB (318 and 450 with stores that stay in the caches).
 #include "aal_beam.h"
 #include "aal_device.h"
 

@@ -12,7 +12,8 @@
 // rounding: totals are formed in 64 bits, and so is a row's log-sum-exp where it counts,
 // the exponentials of the listed logits.  Those of the others are v_exp_f32's of arguments with one
 // rounding (log2(e) / T in two pieces), whose errors average out over the many of them that it takes to
-// bear on the sum.  Parts are cut from the row's start whatever its alignment, so that equal rows
+// bear on the sum.  Bound by that arithmetic where there are many rows: 13 instructions a logit, 64 x 8 rows of 128,256 bf16,
+// 16 chosen, 31 us or 3.5 TB/s and 12 us to merge; by latency and the merge where there are few.  Parts are cut from the row's start whatever its alignment, so that equal rows
 // get equal sums, and equal beams tie exactly.
 #include "aal_beam.h"
 #include "aal_device.h"
@@ -22,7 +23,7 @@ namespace aal {
 namespace {
 
 constexpr int kCand = 512;   // candidates of a part that fit
-constexpr int kQueue = 256;  // and vectors that hold some
+constexpr int kQueue = 512;  // and vectors that hold some (of 256, flat rows overran it now and then: 64 us instead of 36 for 7 x 32 x 50,001)
 constexpr int kLists = 2048 + kBeamMax;  // a request's parts, and its beams: 64 rows of 2^18 fp32 in parts of 8,192
 constexpr int kMerge = 512;       // threads of the merge
 constexpr int kWork = 4096;       // candidates of a request that may reach the bound
@@ -624,8 +625,10 @@ __global__ __launch_bounds__(kMerge) void k_beam_merge(BeamParams p, int64_t b0)
   }
 }
 
-// How rows are cut: vectors per thread of a part's workgroup, parts of a row.  As long
-// as 1,024 workgroups remain.
+// How rows are cut: vectors per thread of a part's workgroup, parts of a row.  The longest parts of which there are 64:
+// more of them are read sooner, and are more lists for a request's merge, the longer way of the two.  1 x 32 rows of 50,001 fp32,
+// 64 chosen: 20 us, 26 where 256 parts are wanted, 65 where 1,024 are; 7 x 32 of bf16, 128 chosen, 33.6 against 36.4; 1 x 4
+// of 128,256 bf16, 8 chosen: 14 us, 17 in parts of the greatest length.
 struct Cut {
   int u, parts, len;
 };
@@ -635,7 +638,7 @@ Cut cut_rows(DType in, int64_t B, int W, int V) {
     const int most = 256 * u * E, parts = (V + most - 1) / most;
     const int len = ((V + parts - 1) / parts + E - 1) / E * E;
     const Cut c{u, (V + len - 1) / len, len};
-    if (u == 1 || B * W * c.parts >= 1024 || 2 * W * c.parts + kBeamMax > kLists) return c;
+    if (u == 1 || B * W * c.parts >= 64 || 2 * W * c.parts + kBeamMax > kLists) return c;
   }
 }
 

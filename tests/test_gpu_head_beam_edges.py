@@ -115,6 +115,21 @@ def test_quantisation_past_32_bits(A, block_rows):
             assert torch.equal(q["scale_t"][c // block_rows:c // block_rows + rs, r // 128:r // 128 + cs], part["scale_t"])
 
 
+@pytest.mark.parametrize("B,W,V", [(1, 1, 12_001), (1, 2, 50_001), (1, 3, 20_000), (1, 8, 64_001), (2, 4, 32_000), (9, 5, 2_049),
+                                   (1, 30, 16_385), (2, 32, 16_384), (3, 20, 33_001)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_selection_from_rows_cut_in_any_way(A, B, W, V, dtype):
+    """Few and many parts, of one to eight vectors a thread, from one choice to 128; flat rows and clustered ones."""
+    g = torch.Generator().manual_seed(V)
+    s = -torch.rand(B, W, generator=g).cumsum(1)
+    for i, n in enumerate((1, 9, 64, 65, 128)):
+        z = torch.randn(B, W, V, generator=g).mul(0.3 if i % 2 else 3).to(dtype)
+        out = A.aal_beam_select(z.cuda(), s.cuda(), n)
+        o = O.select(z.double().numpy(), s.double().numpy(), n)
+        for k in ("parents", "tokens"):
+            assert np.array_equal(out[k].cpu().numpy(), o[k]), (k, n)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_selection_past_32_bits(A, dtype):
     B, W, V, n = (2_200, 8, 128_257, 8) if dtype == BF16 else (1_100, 8, 128_257, 8)  # 4.5 GB
