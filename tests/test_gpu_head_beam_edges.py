@@ -291,3 +291,23 @@ def test_any_number_of_states(A, count):
     want = [s[torch.arange(2, device="cuda")[:, None], p.long()] for s in states]
     A.aal_beam_reorder(states, p)
     assert all(torch.equal(s, w) for s, w in zip(states, want))
+
+
+@pytest.mark.parametrize("W", [2, 5, 12, 20, 40])
+def test_pieces_at_any_address(A, W):
+    """Segments of 1 to 70 bytes that start anywhere, several of them a slot, in place and from one alignment to another."""
+    g = torch.Generator("cuda").manual_seed(W)
+    p = torch.randint(0, W, (2, W), generator=g, device="cuda", dtype=torch.int32)
+    make = lambda: torch.randint(0, 256, (2, W, 3, 90), generator=g, device="cuda", dtype=torch.uint8)  # noqa: E731
+    sizes = [(i % 17, n) for i, n in enumerate((*range(1, 40), 47, 48, 49, 63, 64, 65, 70))]
+    full, other = [make() for _ in sizes], [make() for _ in sizes]
+    rows = torch.arange(2, device="cuda")[:, None]
+    want, moved = [f.clone() for f in full], [o.clone() for o in other]
+    for (at, n), f, w, m in zip(sizes, full, want, moved):
+        m[..., 3:3 + n] = f[..., at:at + n][rows, p.long()]
+        w[..., at:at + n] = m[..., 3:3 + n]
+    views = [f[..., at:at + n] for (at, n), f in zip(sizes, full)]
+    A.aal_beam_reorder(views, p, out=[o[..., 3:3 + n] for (_, n), o in zip(sizes, other)])
+    assert all(torch.equal(o, m) for o, m in zip(other, moved))
+    A.aal_beam_reorder(views, p)
+    assert all(torch.equal(f, w) for f, w in zip(full, want))
