@@ -22,7 +22,7 @@
 namespace aal {
 namespace {
 
-constexpr int kCand = 512;   // candidates of a part that fit
+constexpr int kCand = 1024;  // candidates of a part that fit: all entries of fewer than n vectors do
 constexpr int kQueue = 512;  // and vectors that hold some (of 256, flat rows overran it now and then: 64 us instead of 36 for 7 x 32 x 50,001)
 constexpr int kLists = 2048 + kBeamMax;  // a request's parts, and its beams: 64 rows of 2^18 fp32 in parts of 8,192
 constexpr int kMerge = 512;       // threads of the merge
@@ -133,11 +133,12 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
   constexpr int kShift = 32 - key_bits<TI>();
   using Key = LocalKey<TI>;
   __shared__ __attribute__((aligned(16))) typename Key::type cand[kCand];
-  __shared__ uint64_t sorted[kCand];
   __shared__ double dsum[WV];
   __shared__ float fsh[WV];
   __shared__ int ish[WV];
   __shared__ __attribute__((aligned(16))) u32x4 queue[kQueue];
+  static_assert(sizeof(queue) >= kCand * sizeof(uint64_t), "the sorted candidates take the queue's place");
+  uint64_t* sorted = reinterpret_cast<uint64_t*>(queue);
   __shared__ int place[kQueue];
   __shared__ int count, vectors;
   const int64_t row = p.row0 + blockIdx.x / p.parts;
@@ -171,12 +172,24 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) pin(raw[u]);
+  // how many threads and how many vectors have something finite, by waves
   const float own[1] = {m};
+  const int threads = __popcll(__builtin_amdgcn_ballot_w64(m != kNegInf));
+  int groups = 0, all = 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) groups += __popcll(__builtin_amdgcn_ballot_w64(gm[u] != kNegInf));
   m = wave_max(m);
-  if (lane == 0) fsh[wv] = m;
+  if (lane == 0) {
+    fsh[wv] = m;
+    ish[wv] = groups << 16 | threads;
+  }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < WV; ++i) m = fmaxf(m, fsh[i]);
+  for (int i = 0; i < WV; ++i) {
+    m = fmaxf(m, fsh[i]);
+    all += ish[i];
+  }
+  all = __builtin_amdgcn_readfirstlane(all);
   m = uniform(m);
   __syncthreads();
   const int64_t slot = row * int64_t(p.parts) + part;
@@ -187,8 +200,15 @@ __global__ __launch_bounds__(BLK, 7) void k_beam_parts(BeamParams p) {
     return;
   }
   // At least n logits reach t, or all finite ones do.  Threads' maxima do for short lists, an eighth of the
-  // arithmetic; for more than a quarter of the threads they would let through half again as many.
-  float t = uniform(p.n <= BLK / 4 ? threshold<TI, WV>(own, p.n, m, fsh) : threshold<TI, WV>(gm, p.n, m, fsh));
+  // arithmetic; for more than a quarter of the threads they would let through half again as many.  A wave's share of n is
+  // that of the finite maxima that it has: with equal shares a wave without any would let all of a short row through
+  // (51 x 4 rows of 688: 102 us instead of 21, calls and all).
+  float t = kNegInf;
+  if (p.n <= BLK / 4 && (all & 0xffff) >= p.n)
+    t = threshold_of_shares<TI, WV>(own, (p.n * threads + (all & 0xffff) - 1) / (all & 0xffff), m, fsh);
+  else if ((all >> 16) >= p.n)
+    t = threshold_of_shares<TI, WV>(gm, (p.n * groups + (all >> 16) - 1) / (all >> 16), m, fsh);
+  t = uniform(t);
   // the vectors that hold some, then their entries, each by a thread of its own
   auto collect = [&](float from) {
 #pragma unroll

@@ -23,13 +23,13 @@ __device__ __forceinline__ float key_logit(uint32_t key) {
 // A threshold that at least k of the block's values (N per thread) reach, and
 // few more: every wave bisects for one that its share of k reaches, without a
 // barrier, and the lowest of them serves for all.  -inf where some wave has
-// fewer finite values than its share.
+// fewer finite values than its share.  Shares may differ, if they make k together.
 template <class TI, int WAVES, int N>
-__device__ __forceinline__ float threshold(const float (&x)[N], int k, float top, float* sh) {
+__device__ __forceinline__ float threshold_of_shares(const float (&x)[N], int share, float top, float* sh) {
   constexpr int kShift = 32 - key_bits<TI>();
   const uint32_t least = order_key<TI>(kNegInf) >> kShift;
   uint32_t lo = least, hi = (order_key<TI>(top) >> kShift) + 1u;  // lo is reached by the share or all, hi by none
-  const int share = (k + WAVES - 1) / WAVES, most = share + share / 8 + 1;
+  const int most = share + share / 8 + 1;
   // the first probe two octaves below the top, where the share mostly is above: less to bisect
   const uint32_t octaves = 2u << (23 - kShift);
   uint32_t probe = hi > least + octaves ? hi - octaves : lo + (hi - lo) / 2;
@@ -46,7 +46,7 @@ __device__ __forceinline__ float threshold(const float (&x)[N], int k, float top
     }
     probe = lo + (hi - lo) / 2;
   }
-  float t = key_logit<TI>(lo << kShift);
+  float t = share == 0 ? top : key_logit<TI>(lo << kShift);
   if constexpr (WAVES > 1) {
     if ((threadIdx.x & (kWave - 1)) == 0) sh[threadIdx.x / kWave] = t;
     __syncthreads();
@@ -55,6 +55,10 @@ __device__ __forceinline__ float threshold(const float (&x)[N], int k, float top
     __syncthreads();
   }
   return t;
+}
+template <class TI, int WAVES, int N>
+__device__ __forceinline__ float threshold(const float (&x)[N], int k, float top, float* sh) {
+  return threshold_of_shares<TI, WAVES>(x, (k + WAVES - 1) / WAVES, top, sh);
 }
 
 }  // namespace
