@@ -311,3 +311,22 @@ def test_pieces_at_any_address(A, W):
     assert all(torch.equal(o, m) for o, m in zip(other, moved))
     A.aal_beam_reorder(views, p)
     assert all(torch.equal(f, w) for f, w in zip(full, want))
+
+
+@pytest.mark.parametrize("W", [1, 2, 4, 7, 9])
+def test_large_states_in_place(A, W):
+    """More pieces than are looked at one by one, requests that stay whole among others, ends of segments too."""
+    B, L = 5, 1 << 20
+    g = torch.Generator("cuda").manual_seed(W)
+    state = torch.randint(0, 1 << 30, (B, W, 4, L + 7), generator=g, device="cuda", dtype=torch.int32).view(torch.uint8)
+    p = torch.randint(-1, W + 1, (B, W), generator=g, device="cuda", dtype=torch.int32)
+    p[1] = torch.arange(W)
+    p[3] = -1
+    view = state[..., 3:-2]
+    before = state.clone()
+    A.aal_beam_reorder([view], p)
+    take = torch.where((p >= 0) & (p < W), p, torch.arange(W, dtype=torch.int32, device="cuda")).long()
+    for b in range(B):
+        for j in range(W):
+            assert torch.equal(state[b, j, :, 3:-2], before[b, take[b, j], :, 3:-2])
+    assert torch.equal(state[..., :3], before[..., :3]) and torch.equal(state[..., -2:], before[..., -2:])
