@@ -19,6 +19,9 @@
 #include "aal_device.h"
 #include "aal_select.h"
 
+#include <algorithm>
+#include <limits>
+
 namespace aal {
 namespace {
 
@@ -674,11 +677,12 @@ hipError_t launch_typed(const BeamArgs& a) {
   p.parts = c.parts;
   p.part_len = c.len;
   p.inv_t = 1.0 / double(a.temperature);
-  // the lower piece is above 0, so that a logit of -inf is no NaN
+  // the lower piece is above 0, so that a logit of -inf is no NaN; from T = 2^120 on it may be less than half of the
+  // least fp32 number, which stands for it then: 2^-150 of a logit, 2^-22 at most, more in an exponent
   const double sc = 1.4426950408889634073599246810019 / double(a.temperature);
   p.sc_hi = float(sc);
   if (double(p.sc_hi) >= sc) p.sc_hi = __builtin_nextafterf(p.sc_hi, 0.f);
-  p.sc_lo = float(sc - double(p.sc_hi));
+  p.sc_lo = std::max(float(sc - double(p.sc_hi)), std::numeric_limits<float>::denorm_min());
   p.scores = a.scores;
   p.finished = a.finished;
   p.lengths = a.lengths;
