@@ -719,7 +719,8 @@ size_t aal_fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K);
  * c[m, n] = sum_j sa[m, j] sb[n, j] sum_{k in block j} a[m, k] b[n, k],   blocks of 128 of K
  *
  * in fp32, rounded once to c_dtype.  a : M rows, b : N rows, in host memory (read before the call
- * returns); both scales of one type, formats as they are.  c : [M, N] contiguous, 16-byte aligned, no overlap
+ * returns); both scales of one type and any size (their product may leave fp32's range
+ * where a block's share of the result does not), formats as they are; values that are not finite make their row or column so.  c : [M, N] contiguous, 16-byte aligned, no overlap
  * with an operand.  1 <= M, N, K < 2^31.
  * workspace : at least aal_fp8_matmul_workspace_bytes(M, N, K) bytes, 256-byte aligned (NULL where that is 0).
  */

@@ -57,6 +57,41 @@ __device__ __forceinline__ float scale_of(uint32_t raw, int e8m0) {
   return __builtin_bit_cast(float, e8m0 ? e : raw);
 }
 
+// Two scales may leave fp32's range together where the result does not.  Blocks with such scales are looked for and scaled
+// in 64 bits, in two to four times a block's time: first whether any scale lies outside of [2^LESS, 2^HIGH], which
+// rarely is so, and then what it meets: in range are two of 2^LESS, one of 2^LEAST and one of 2^SMALL, 0, and what lies above
+// them up to 2^HIGH.  Looking costs 1 to 3% of a product (8,192 x 128,256 x 4,096 3.99 -> 4.05 ms; 128,256 x 4,096 x 2,048 into fp32 with any
+// scales 2.52 -> 2.63; the same for the workgroup at once, with a flag in LDS, 5%).
+template <int HIGH, int SMALL, int LESS, int LEAST>
+struct ScaleRange {
+  static __device__ __forceinline__ uint32_t power(int e) { return uint32_t(e + 127) << 23; }
+  static __device__ __forceinline__ bool unusual(float scale) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, scale) & 0x7fffffffu;
+    return b - power(LESS) > power(HIGH) - power(LESS);
+  }
+  // bit 0: beyond it whatever the others are, 1: below 2^SMALL, 2: below 2^LESS
+  static __device__ __forceinline__ uint32_t bits(float scale) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, scale) & 0x7fffffffu;
+    auto below = [&](int e) { return b - 1u < power(e) - 1u ? 1u : 0u; };
+    return (b > power(HIGH) ? 1u : below(LEAST)) | below(SMALL) << 1 | below(LESS) << 2;
+  }
+  // of a's scales and of b's, whatever lanes hold them
+  static __device__ __forceinline__ bool left(uint32_t a, uint32_t b) {
+    auto any = [](uint32_t v) { return __builtin_amdgcn_ballot_w64(v != 0u) != 0; };
+    return any((a | b) & 1u) || (any(a & 4u) && any(b & 2u)) || (any(a & 2u) && any(b & 4u));
+  }
+};
+typedef ScaleRange<63, -16, -62, -110> SumRange;   // of scales that sums are multiplied by
+typedef ScaleRange<40, -16, -46, -78> ValueRange;  // and values of 2^-16 to 2^16 in bf16, whose products are normal numbers
+// Of a product of two scales: 0 is none, since it may be what is left of two others.
+__device__ __forceinline__ bool is_normal(float x) {
+  return (__builtin_bit_cast(uint32_t, x) & 0x7fffffffu) - 0x800000u < 0x7f000000u;
+}
+// sum + t x y for scales of any size.
+__device__ __forceinline__ float add_far(float sum, float t, float x, float y) {
+  return float(__builtin_fma(double(t) * double(x), double(y), double(sum)));
+}
+
 // 16 bytes per lane from base + voff (0 from `bytes` on) into LDS, lane l's at `to` + 16 l.  In assembly, since the
 // compiler takes every later LDS read for one of these bytes and waits; nothing here has a result
 // to wait for but LDS, which stage_barrier() does.  M0 is read one wait state after it is written at the soonest.
@@ -147,7 +182,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
   static_assert(!SQUARE || 128 % (16 * TN) == 0, "a wave's columns have one scale");
   __shared__ __attribute__((aligned(16))) uint8_t tile[2][(BN + BM) * 128];
   __shared__ __attribute__((aligned(16))) float scales[2][BN + BM];
-  __shared__ int far[2][POW ? WN * WM : 1];  // a wave's scales of a stage take bf16 out of its range
+  __shared__ __attribute__((aligned(4))) uint8_t unusual[2][POW ? WN * WM : 1];  // a wave's scales of a stage are
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l = lane & 15, h = lane >> 4;
   // A tile of c, and the blocks of a part of K.  Workgroups go round over the 8 XCDs: each XCD takes a stretch of
@@ -195,11 +230,11 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
   uint32_t next = 0;
   auto load_scales = [&](const Sources& t, int j) { next = raw_scale(scale_base, t.scale + j * scale_step, p.e8m0); };
   auto put_scales = [&](int to) {
-    scales[to][tid] = scale_of(next, p.e8m0);
+    const float s = scale_of(next, p.e8m0);
+    scales[to][tid] = s;
     if constexpr (POW) {
-      // 2^-100 to 2^100 times what either format holds are normal numbers
-      const bool any = __builtin_amdgcn_ballot_w64(next - 27u > 200u) != 0;
-      if (lane == 0) far[to][wave] = any;
+      const bool any = __builtin_amdgcn_ballot_w64(ValueRange::unusual(s)) != 0;
+      if (lane == 0) unusual[to][wave] = any;
     }
   };
   // K ends inside the last block: zeros for what lies behind it
@@ -275,11 +310,14 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
   u32x4 pa[TM], pb[TN];
   float sa[TM], sb[SB];
   bool plain = true;
+  // POW: whether the stage's scales may be applied to values (four waves' flags are read at a time)
   auto is_plain = [&](int at) {
-    int any = 0;
-#pragma unroll
-    for (int w = 0; w < (POW ? WN * WM : 0); ++w) any |= far[at][w];
-    return __builtin_amdgcn_readfirstlane(any) == 0;
+    static_assert(!POW || WN * WM == 4, "flags of four waves");
+    if (__builtin_amdgcn_readfirstlane(*reinterpret_cast<const int*>(unusual[at])) == 0) return true;
+    uint32_t of_a = 0, of_b = 0;
+    for (int i = lane; i < BN; i += 64) of_b |= ValueRange::bits(scales[at][i]);
+    for (int i = lane; i < BM; i += 64) of_a |= ValueRange::bits(scales[at][BN + i]);
+    return !ValueRange::left(of_a, of_b);
   };
   auto scale_a = [&](int at, int m) { return plain ? scales[at][BN + (wm * TM + m) * 16 + l] : 1.f; };
   auto scale_b = [&](int at, int n) { return plain ? scales[at][wn * TN * 16 + (SQUARE ? 0 : n * 16 + l)] : 1.f; };
@@ -314,9 +352,34 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
   }
   auto add = [&](int n, int m, const f32x4& t, float f, const f32x4& g) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[n][m][i] = __builtin_fmaf(t[i], SQUARE && !POW ? f : f * g[i], acc[n][m][i]);
+    for (int i = 0; i < 4; ++i) acc[n][m][i] = __builtin_fmaf(t[i], SQUARE ? f : f * g[i], acc[n][m][i]);
     // here, not where the compiler would rather have all of them: 128 registers of products
     asm volatile("" : "+v"(acc[n][m]));
+  };
+  // Whether the wave's scales of the block, of which fa has a's, leave fp32's range (SQUARE: fa has their products).
+  auto scales_left = [&] {
+    bool any = false;
+    if constexpr (SQUARE) {
+#pragma unroll
+      for (int m = 0; m < TM; ++m) any |= !is_normal(fa[m]);
+      return __builtin_amdgcn_ballot_w64(any) != 0;
+    } else {
+      float own[TN / 4];
+#pragma unroll
+      for (int i = 0; i < TN / 4; ++i) {
+        own[i] = scales[stage][wn * TN * 16 + i * 64 + lane];
+        any |= SumRange::unusual(own[i]);
+      }
+#pragma unroll
+      for (int m = 0; m < TM; ++m) any |= SumRange::unusual(fa[m]);
+      if (__builtin_amdgcn_ballot_w64(any) == 0) return false;
+      uint32_t of_a = 0, of_b = 0;
+#pragma unroll
+      for (int i = 0; i < TN / 4; ++i) of_b |= SumRange::bits(own[i]);
+#pragma unroll
+      for (int m = 0; m < TM; ++m) of_a |= SumRange::bits(fa[m]);
+      return SumRange::left(of_a, of_b);
+    }
   };
   int id = blockIdx.x;
   for (int j = t.j0;;) {
@@ -350,9 +413,13 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
             const f32x4 g = SQUARE ? f32x4{1.f, 1.f, 1.f, 1.f} * scales[stage][wn * TN * 16] : scales_b(stage, n);
             const bf16x8 w = widen<FB>(int(pb[n][w0]), int(pb[n][w0 + 1]));
 #pragma unroll
-            for (int m = 0; m < TM; ++m)
-              add(n, m, __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, wa[m], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0),
-                  scales[stage][BN + (wm * TM + m) * 16 + l], g);
+            for (int m = 0; m < TM; ++m) {
+              const f32x4 u = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, wa[m], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+              const float f = scales[stage][BN + (wm * TM + m) * 16 + l];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[n][m][i] = add_far(acc[n][m][i], u[i], f, g[i]);
+              asm volatile("" : "+v"(acc[n][m]));
+            }
             __builtin_amdgcn_sched_barrier(0);
           }
           // and nothing is left to add to them below, which has no branch
@@ -436,6 +503,25 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
         if constexpr (!WIDE) __builtin_amdgcn_sched_barrier(0);
       }
       fp = g;
+      if (n == 0 && scales_left()) {
+        // the block's sums are formed and added here, and what follows adds nothing (NaN where values are not finite)
+#pragma unroll
+        for (int k = 0; k < TN; ++k) {
+          const i32x8 y = fragment(tb + k * 16 * 128);
+          const f32x4 of_b = SQUARE ? f32x4{1.f, 1.f, 1.f, 1.f} * scales[stage][wn * TN * 16] : scales_b(stage, k);
+#pragma unroll
+          for (int m = 0; m < TM; ++m) {
+            const f32x4 u = dot128<WIDE, FB, FA>(y, xa[m]);
+            const float of_a = scales[stage][BN + (wm * TM + m) * 16 + l];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[k][m][i] = add_far(acc[k][m][i], u[i], of_a, of_b[i]);
+            asm volatile("" : "+v"(acc[k][m]));
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < TM; ++m) fa[m] = 0.f;
+      }
     }
     }
     stage ^= 1;
@@ -516,14 +602,23 @@ __global__ __launch_bounds__(256, 2) void k_few_rows(MatmulParams p) {
     for (int r = 0; r < BN / RP; ++r) load_lds_once(rb, vb + (uint32_t(r * RP) * uint32_t(p.ld_b) + k), base + r * RP * 128);
     load_lds(ra, va + k, base + BN * 128);
   };
+  bool unusual = false;
   for (int i = tid; i < (j1 - j0) * BM; i += 256) {
     const int j = i / BM, m = min(i % BM, M - 1);
-    scale_m[j][i % BM] = scale_of(raw_scale(p.sa, int64_t(m >> p.ra) * p.sa_row + (j0 + j) * p.sa_block, p.e8m0), p.e8m0);
+    const float s = scale_of(raw_scale(p.sa, int64_t(m >> p.ra) * p.sa_row + (j0 + j) * p.sa_block, p.e8m0), p.e8m0);
+    scale_m[j][i % BM] = s;
+    unusual |= SumRange::unusual(s);
   }
   for (int i = tid; i < (j1 - j0) * SN; i += 256) {
     const int j = i / SN, n = min(i % SN, left_n - 1);
-    scale_n[j][i % SN] = scale_of(raw_scale(p.sb, ((n0 + n) >> p.rb) * p.sb_row + (j0 + j) * p.sb_block, p.e8m0), p.e8m0);
+    const float s = scale_of(raw_scale(p.sb, ((n0 + n) >> p.rb) * p.sb_row + (j0 + j) * p.sb_block, p.e8m0), p.e8m0);
+    scale_n[j][i % SN] = s;
+    unusual |= SumRange::unusual(s);
   }
+  // for each wave to read in the part of the last stage that it loads itself, later: the two workgroups of a CU take 160 KB to
+  // the byte
+  unusual = __builtin_amdgcn_ballot_w64(unusual) != 0;
+  if (lane < 4) tile[kRing - 1][lane * 1024 + wave] = unusual;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   load(0, 0);
   if (count > 1) load(1, 1);
@@ -538,12 +633,23 @@ __global__ __launch_bounds__(256, 2) void k_few_rows(MatmulParams p) {
 #pragma unroll
     for (int m = 0; m < TM; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
   int at = 0;  // i's stage
+  bool plain = true;
   for (int i = 0; i < count; ++i) {
     const int j = block(i);
     if (i + 1 < count)
       ring_barrier<kLoads>();
     else
       ring_barrier<0>();
+    if (i == 0) {
+      int any = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const int*>(&tile[kRing - 1][wave * 1024]));
+      asm volatile("" : "+s"(any)::"memory");  // read before the load below takes its place
+      if (any) {
+        uint32_t of_a = 0, of_b = 0;
+        for (int k = lane; k < count * BM; k += 64) of_a |= SumRange::bits((&scale_m[0][0])[k]);
+        for (int k = lane; k < count * SN; k += 64) of_b |= SumRange::bits((&scale_n[0][0])[k]);
+        plain = !SumRange::left(of_a, of_b);
+      }
+    }
     if (i + 2 < count) load(i + 2, at == 0 ? 2 : at - 1);
     uint8_t* stage = tile[at];
     if ((p.K & 127) && j == p.blocks - 1) {
@@ -567,8 +673,13 @@ __global__ __launch_bounds__(256, 2) void k_few_rows(MatmulParams p) {
           fb = f32x4{1.f, 1.f, 1.f, 1.f} * scale_n[j - j0][0];
         else
           fb = *reinterpret_cast<const f32x4*>(&scale_n[j - j0][wave * 32 + n * 16 + h * 4]);
+        if (plain) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[n][m][i] = __builtin_fmaf(t[i], fa * fb[i], acc[n][m][i]);
+          for (int i = 0; i < 4; ++i) acc[n][m][i] = __builtin_fmaf(t[i], fa * fb[i], acc[n][m][i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[n][m][i] = add_far(acc[n][m][i], t[i], fa, fb[i]);
+        }
       }
     }
     at = at == 2 ? 0 : at + 1;
