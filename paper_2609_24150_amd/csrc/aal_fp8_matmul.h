@@ -8,19 +8,11 @@
 #pragma once
 
 #include "aal_fp8_device.h"
+#include "aal_fp8_plan.h"
 
 #include <type_traits>
 
 namespace aal {
-
-constexpr unsigned kCus = 256;  // of an MI355X: workgroups of tiles of 256 x 256 that run at once, of 128 x 128 twice as many
-
-// How a product is cut (plan_of): few rows of a, or tiles of 128 or 256 in both directions; the inner
-// dimension in `splits` parts, whose sums are joined by a second kernel.
-struct MatmulPlan {
-  int kind;  // 0: few rows, 1: tiles of 128 x 128, 2: of 256 x 256
-  int splits;
-};
 
 struct MatmulParams {
   const uint8_t* a;
@@ -569,7 +561,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
 // A workgroup of four waves takes 128 rows of b and at most kFewBlocks blocks, which run through a ring of kRing stages in
 // LDS, two of them on their way while one is being multiplied.  All its scales are in LDS before that, so that the
 // loop waits for the stages alone.
-constexpr int kFewBlocks = 32, kRing = 3;
+constexpr int kRing = 3;
 
 template <int N>
 __device__ __forceinline__ void ring_barrier() {

@@ -12,48 +12,6 @@ extern template hipError_t launch_matmul_formats<1, 1>(const MatmulArgs&, const 
 
 namespace {
 
-int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// The cut whose time is estimated to be the least.  Microseconds, measured over 1 to 2,048 rows of 250 to 128,256 columns and
-// 512 to 128,256 values: a block of 128 takes a workgroup `step`, less where half the chip's places or fewer are
-// taken, a tile `tile` besides; parts are written, read again and joined by another launch.  Against this, a rule by turns
-// of the chip alone took 67 us instead of 49 for 256 x 32,000 x 4,096, 65 instead of 42 for 2,048 x 4,096 x 4,096.
-struct TileTimes {
-  int side, places;
-  double step, step_few, tile;
-};
-constexpr TileTimes kSmall{128, 2 * kCus, 1.3, 1.1, 4.0}, kLarge{256, kCus, 1.75, 1.6, 8.0};
-constexpr TileTimes kSmallWide{128, 2 * kCus, 2.0, 1.55, 6.0};
-
-MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, bool wide) {
-  const int64_t blocks = up(K, kFp8Block);
-  if (M <= 32) {
-    // Few rows of a: b is read once, for which 250 workgroups do (32 x 32,000 x 4,096 24.8 us, in four parts 36.8); of
-    // eight blocks at least.  33 rows of 128,256 x 4,096 take 112 us in tiles, up to 32 take 84 to 93 here.
-    const int64_t s = std::min<int64_t>(kCus / up(N, 128), blocks / 8);
-    return {0, int(std::max<int64_t>(up(blocks, kFewBlocks), std::min<int64_t>(s, 64)))};
-  }
-  MatmulPlan best{1, 1};
-  double least = 1e300;
-  auto consider = [&](int kind, const TileTimes& t) {
-    const int64_t tiles = up(M, t.side) * up(N, t.side);
-    for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-      if (s > 1 && (blocks < 4 * s || tiles * s > t.places)) break;
-      const double turns = double(up(tiles * s, t.places)), steps = double(up(blocks, s));
-      const double join = s > 1 ? 4.0 + double(s) * (0.4 + double(M) * double(N) * (8.0 / 7e6)) : 0.0;
-      const double us = turns * (steps * (tiles * s <= t.places / 2 ? t.step_few : t.step) + t.tile) + join;
-      if (us < least) {
-        least = us;
-        best = {kind, s};
-      }
-    }
-  };
-  consider(1, wide ? kSmallWide : kSmall);
-  // fp32 results need widened operands, for which tiles of 256 x 256 have no registers left (3.1 ms instead of 2.3)
-  if (!wide) consider(2, kLarge);
-  return best;
-}
-
 __global__ __launch_bounds__(256) void k_join(const float* part, int64_t n, int splits, void* c, int out_bf16) {
   const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
   if (i >= n) return;
