@@ -718,7 +718,10 @@ size_t aal_fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K);
 /*
  * c[m, n] = sum_j sa[m, j] sb[n, j] sum_{k in block j} a[m, k] b[n, k],   blocks of 128 of K
  *
- * in fp32, rounded once to c_dtype.  a : M rows, b : N rows, in host memory (read before the call
+ * c_dtype fp32: sums in fp32, off by at most 2^-16 + (blocks + 2) 2^-24 of sum |sa sb a b|.  c_dtype bf16: 8-bit matrix
+ * instructions, which cut each eight neighbours' products below 2^-13 of the largest: off by 7 2^-13 of that sum at most
+ * besides, where large products cancel (1.5e-5 of it, root mean square, for random values), and rounded once to bf16.  Where that is
+ * too much, ask for fp32.  a : M rows, b : N rows, in host memory (read before the call
  * returns); both scales of one type and any size (their product may leave fp32's range
  * where a block's share of the result does not), formats as they are; values that are not finite make their row or column so.  c : [M, N] contiguous, 16-byte aligned, no overlap
  * with an operand.  1 <= M, N, K < 2^31.

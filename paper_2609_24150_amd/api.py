@@ -766,8 +766,11 @@ def aal_fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_sc
     each block of 128 along K and of 1 or 128 rows (which of them, the scale's
     shape tells): a_scale [M or ceil(M / 128), ceil(K / 128)], b_scale alike, both
     float32 or both float8_e8m0fnu, any strides.  Values: float8_e4m3fn or float8_e5m2, rows at multiples
-    of 16 bytes (as aal_fp8_quantize makes them).  Sums are fp32, rounded once to out_dtype (bf16
-    or fp32).
+    of 16 bytes (as aal_fp8_quantize makes them).
+
+    out_dtype fp32: sums in fp32.  bf16: sums of 8-bit matrix instructions, which cut each eight
+    neighbours' products below 2^-13 of the largest: off by up to 7 2^-13 of sum |a b| with the scales where large
+    products cancel (1.5e-5 of it, root mean square, for random values), then rounded to bf16.
 
     Returns out, [M, N]."""
     dev = a.device
@@ -826,7 +829,7 @@ def aal_head_logits(x: torch.Tensor, head: dict, *, out_dtype: torch.dtype | Non
     aal_fp8_quantize(W, block_rows=128, columns=True).  x is quantised here, in
     blocks of 1 x 128, to e4m3 with scales of the head's type.
 
-    Returns [..., V] of out_dtype (x's dtype if None)."""
+    Returns [..., V] of out_dtype (x's dtype if None), as exact as aal_fp8_matmul's results of it are."""
     _check_head(head, "q", "scale")
     D = x.shape[-1] if x.dim() else 0
     if x.dim() < 1 or x.numel() == 0 or head["q"].shape[-1] != D:
@@ -844,7 +847,7 @@ def aal_head_logits_bwd(grad: torch.Tensor, x: torch.Tensor, head: dict, *, x_gr
     (x's gradient: V, against head["qt"] and head["scale_t"]; the weights': the rows).
 
     Returns a dict: grad_x [..., D] of x's dtype and grad_w [V, D] of
-    weight_dtype (None where not asked for)."""
+    weight_dtype (None where not asked for), as exact as aal_fp8_matmul's results of those are."""
     if not (x_grad or weight_grad):
         raise ValueError("x_grad or weight_grad must be asked for")
     _check_head(head, *(("qt", "scale_t") if x_grad else ("scale",)))

@@ -80,8 +80,9 @@ __device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale = 1.f) {
 //
 // The matrix unit aligns the products of eight neighbouring 8-bit values to the largest of them and
 // cuts what lies 2^-13 below its power of two (measured; sums of the eights are fp32): 1.5e-5 of a sum of
-// random values, root mean square.  A result that is rounded to bf16 (1.7e-3) does not feel that, one in fp32
-// would: WIDE goes through bf16, whose products and sums are exact to fp32 (7e-9), at half the rate.
+// random values, root mean square, 7 2^-13 of the sum of magnitudes at most, where large products cancel.  Results that are
+// rounded to bf16 (1.7e-3) take that, as their contract says: one in some hundred becomes the neighbouring bf16 value.  For those in fp32
+// WIDE goes through bf16, whose products and sums are exact to fp32 (7e-9), at half the rate.
 template <bool WIDE, int FX, int FY>
 __device__ __forceinline__ f32x4 dot128(const i32x8& x, const i32x8& y) {
   f32x4 t = {0.f, 0.f, 0.f, 0.f};
