@@ -697,7 +697,7 @@ aal_status_t aal_fp8_quantize(const void* x, aal_dtype_t in_dtype, int64_t rows,
                               void* scale, void* qt, int64_t ld_qt, void* scale_t, hipStream_t stream);
 
 /* One operand of a product: [rows, K] 8-bit values, K along the row.
- *   values       16-byte aligned; ld bytes from row to row, a multiple of 16, at least K (what lies
+ *   values       16-byte aligned; ld bytes from row to row, a multiple of 16, at least K and below 2^24 (what lies
  *                behind a row's K values bears on nothing, and is memory in the last row too)
  *   scale        of scale_type; row block r's scale of column block j is scale[r * scale_row + j * scale_block]
  *   block_rows   1 or 128 */
@@ -712,7 +712,7 @@ typedef struct {
   int32_t block_rows;
 } aal_fp8_operand_t;
 
-/* Workspace bytes of aal_fp8_matmul for these sizes (0 for invalid ones, or where it needs none). */
+/* Workspace bytes of aal_fp8_matmul for these sizes: 0 where it needs none, and for sizes that it refuses. */
 size_t aal_fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K);
 
 /*
@@ -724,7 +724,7 @@ size_t aal_fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K);
  * too much, ask for fp32.  a : M rows, b : N rows, in host memory (read before the call
  * returns); both scales of one type and any size (their product may leave fp32's range
  * where a block's share of the result does not), formats as they are; values that are not finite make their row or column so.  c : [M, N] contiguous, 16-byte aligned, no overlap
- * with an operand.  1 <= M, N, K < 2^31.
+ * with an operand.  1 <= M, N <= 2^28, M * N < 2^37, 1 <= K < 2^24.
  * workspace : at least aal_fp8_matmul_workspace_bytes(M, N, K) bytes, 256-byte aligned (NULL where that is 0).
  */
 aal_status_t aal_fp8_matmul(const aal_fp8_operand_t* a, const aal_fp8_operand_t* b, int64_t M, int64_t N, int64_t K,

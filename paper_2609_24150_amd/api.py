@@ -766,7 +766,8 @@ def aal_fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_sc
     each block of 128 along K and of 1 or 128 rows (which of them, the scale's
     shape tells): a_scale [M or ceil(M / 128), ceil(K / 128)], b_scale alike, both
     float32 or both float8_e8m0fnu, any strides.  Values: float8_e4m3fn or float8_e5m2, rows at multiples
-    of 16 bytes (as aal_fp8_quantize makes them).
+    of 16 bytes (as aal_fp8_quantize makes them).  M and N up to 2^28, M N below 2^37, K and the rows'
+    distances below 2^24.
 
     out_dtype fp32: sums in fp32.  bf16: sums of 8-bit matrix instructions, which cut each eight
     neighbours' products below 2^-13 of the largest: off by up to 7 2^-13 of sum |a b| with the scales where large
