@@ -818,6 +818,10 @@ def _matrix(t: torch.Tensor, stream) -> torch.Tensor:
     return flat
 
 
+def _blocks(n: int) -> int:
+    return (n + AAL_FP8_BLOCK - 1) // AAL_FP8_BLOCK
+
+
 def _check_head(head: dict, *names: str):
     for name in names:
         if head.get(name) is None:
@@ -855,8 +859,12 @@ def aal_head_logits_bwd(grad: torch.Tensor, x: torch.Tensor, head: dict, *, x_gr
     if x.dim() < 1 or x.numel() == 0 or grad.dim() < 1 or grad.shape[:-1] != x.shape[:-1] or grad.numel() == 0:
         raise ValueError("grad must be [..., V] and x [..., D] of the same rows, one at least")
     D, V = x.shape[-1], grad.shape[-1]
-    if x_grad and tuple(head["qt"].shape) != (D, V):
-        raise ValueError(f"grad and x do not fit a head of {tuple(head['qt'].shape)[::-1]}")
+    for values, scale, rows, cols in (("q", "scale", V, D), ("qt", "scale_t", D, V)):
+        v, s = head.get(values), head.get(scale)
+        if v is not None and tuple(v.shape) != (rows, cols):
+            raise ValueError(f"grad and x of {V} and {D} columns do not fit a head whose {values} is {tuple(v.shape)}")
+        if s is not None and (s.shape[0] not in (rows, _blocks(rows)) or s.shape[1] != _blocks(cols)):
+            raise ValueError(f"grad and x of {V} and {D} columns do not fit a head whose {scale} is {tuple(s.shape)}")
     scale = (head["scale_t"] if x_grad else head["scale"]).dtype
     g = aal_fp8_quantize(_matrix(grad, stream), rows=x_grad, columns=weight_grad, scale_dtype=scale, stream=stream)
     out = {"grad_x": None, "grad_w": None}
