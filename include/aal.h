@@ -791,7 +791,7 @@ typedef struct {
  * beams that keep their slot move no byte.  A parent outside [0, W) leaves its slot as it was.
  * states : host memory [n_states], read before the call returns; 0 <= n_states.  parents : device [B, n].
  * In place asks for n = W <= AAL_BEAM_MAX (src is written); otherwise 1 <= n <= AAL_BEAM_SELECT_MAX, and a
- * dst overlaps no src.  What is written must not overlap another state, nor a state's slots each other.  Any alignment; states move in pieces
+ * dst overlaps no src.  What is written must not overlap another state or parents, nor a state's slots each other.  Any alignment; states move in pieces
  * of 16 bytes, and segments that are no number of them have ends of fewer.
  */
 aal_status_t aal_beam_reorder(const aal_beam_state_t* states, int32_t n_states, int64_t B, int32_t W, int32_t n,

@@ -999,7 +999,7 @@ def _check_memory(spans: list):
             if written or y[2]:
                 a, b = (sorted(((s, c) for s, c in (*z[4], (z[3][2], z[3][0])) if c > 1 and s), reverse=True) for z in (y, x))
                 if _meet(at - y[0], a, y[3][1], b, cut[1]):
-                    raise ValueError("what is written must share no memory with another state or output")
+                    raise ValueError("what is written must share no memory with another state or output, nor with parents")
         near.append(x)
         last = max(last, at + size)
 
@@ -1014,7 +1014,7 @@ def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) ->
 
     parents: [B, n] int32, as from aal_beam_select; a parent outside [0, W) leaves its slot as it
     was.  out: None, for in place (n = W; beams that keep their slot move nothing), or tensors
-    [B, n, ...].  What is written shares no memory with another state or output.  Behind its first two dimensions a state may be any view that is
+    [B, n, ...].  What is written shares no memory with another state or output, nor with parents.  Behind its first two dimensions a state may be any view that is
     contiguous pieces at one distance (state[:, :, :, t0:t1] of a [B, W, heads, length, dim] cache).
 
     Returns out, or the states."""
@@ -1064,7 +1064,8 @@ def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) ->
             raise ValueError("the entries of what is written must not share memory")
         if moves:
             table += row
-    if len(spans) > 1:
+    if spans:
+        spans.append((parents.data_ptr(), 4 * B * n, False, (1, 4 * B * n, 0), ()))
         _check_memory(spans)
     with _guard(dev, stream):
         st = _lib.lib().aal_beam_reorder(struct.pack(f"{len(table)}q", *table), len(table) // 10, B, W, n, _ptr(parents),
