@@ -8,6 +8,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import functools
+import itertools
 import operator
 import struct
 
@@ -963,10 +964,14 @@ def _apart(shape: tuple, stride: tuple) -> bool:
     return True
 
 
-def _meet(d: int, a: list, na: int, b: list, nb: int) -> bool:
+def _meet(d: int, a: list, na: int, b: list, nb: int, budget: list | None = None) -> bool:
     """Whether two regular sets of bytes share one: pieces of na and nb bytes, at (stride, count)s that nest, the
-    largest first, the second set's first byte d behind the first's.  True as well where sets of different strides
-    would take long to tell."""
+    largest first, the second set's first byte d behind the first's.  Sets of different strides are looked through step
+    by step; True as well where that takes more steps than budget, a list of one number, has left."""
+    budget = [_STEPS] if budget is None else budget
+    budget[0] -= 1
+    if budget[0] < 0:
+        return True
     end_a, end_b = (n + sum(s * (c - 1) for s, c in dims) for dims, n in ((a, na), (b, nb)))
     if d >= end_a or -d >= end_b:
         return False
@@ -976,13 +981,53 @@ def _meet(d: int, a: list, na: int, b: list, nb: int) -> bool:
         (s, ca), cb = a[0], b[0][1]
         rest_a, rest_b = end_a - s * (ca - 1), end_b - s * (cb - 1)
         steps = range(max(1 - ca, -((d + rest_b - 1) // s)), min(cb - 1, (rest_a - 1 - d) // s) + 1)
-        return len(steps) > 64 or any(_meet(d + k * s, a[1:], na, b[1:], nb) for k in steps)
+        return any(_meet(d + k * s, a[1:], na, b[1:], nb, budget) for k in steps)
     if not a or (b and b[0][0] > a[0][0]):
-        return _meet(-d, b, nb, a, na)
+        return _meet(-d, b, nb, a, na, budget)
     s, ca = a[0]
     rest = end_a - s * (ca - 1)
     steps = range(max(0, -((rest - 1 - d) // s)), min(ca - 1, (d + end_b - 1) // s) + 1)
-    return len(steps) > 64 or any(_meet(d - k * s, a[1:], na, b, nb) for k in steps)
+    return any(_meet(d - k * s, a[1:], na, b, nb, budget) for k in steps)
+
+
+_STEPS = 1 << 14  # for two sets; some 20 ms
+
+
+@functools.lru_cache(maxsize=4096)
+def _nested(cut: tuple, lead: tuple) -> tuple:
+    """The (stride, count)s of a state's pieces, the largest first."""
+    return tuple(sorted(((s, c) for s, c in (*lead, (cut[2], cut[0])) if c > 1 and s), reverse=True))
+
+
+def _runs(sets: list) -> list:
+    """Sets (first byte, bytes to the last one's end, ...) in order of their first bytes, as runs of those whose ranges meet."""
+    sets.sort(key=_first)
+    runs, last = [], None
+    for x in sets:
+        if last is None or x[0] >= last:
+            runs.append([])
+            last = x[0]
+        runs[-1].append(x)
+        last = max(last, x[0] + x[1])
+    return runs
+
+
+def _apart_by_steps(sets: list) -> bool:
+    """Whether regular sets of bytes, (first byte, bytes to the last one's end, (stride, count)s, ...), are seen to be apart by what
+    is left of them in one step of the stride that they all have: views of one tensor are, in one sort a stride.  False
+    where they are not, or may not be."""
+    if len(sets) < 2:
+        return True
+    if not all(x[2] for x in sets) or len({x[2][0][0] for x in sets}) > 1:
+        return False
+    step, base, inner = sets[0][2][0][0], min(x[0] for x in sets), []
+    for at, size, dims, *_ in sets:
+        inner.append(((at - base) % step, size - step * (dims[0][1] - 1), dims[1:]))
+    runs = _runs(inner)
+    end = max(x[0] + x[1] for x in runs[-1])
+    if end - runs[0][0][0] > step:  # the last of a step reach into the next one's first
+        return False
+    return all(_apart_by_steps(run) for run in runs)
 
 
 def _check_memory(spans: list):
@@ -991,17 +1036,16 @@ def _check_memory(spans: list):
     spans.sort(key=_first)
     if all(x[0] + x[1] <= y[0] for x, y in zip(spans, spans[1:])):
         return
-    near, last = [], 0  # those that reach past the present one's start
-    for x in spans:
-        at, size, written, cut, lead = x
-        near = near if at < last else []
-        for y in near:
-            if written or y[2]:
-                a, b = (sorted(((s, c) for s, c in (*z[4], (z[3][2], z[3][0])) if c > 1 and s), reverse=True) for z in (y, x))
-                if _meet(at - y[0], a, y[3][1], b, cut[1]):
-                    raise ValueError("what is written must share no memory with another state or output, nor with parents")
-        near.append(x)
-        last = max(last, at + size)
+    for run in _runs([(x[0], x[1], _nested(x[3], x[4]), x[3][1], x[2]) for x in spans]):
+        alike = {}  # by their largest stride
+        for x in run:
+            alike.setdefault(x[2][0][0] if x[2] else 0, []).append(x)
+        groups = list(alike.values())
+        pairs = [itertools.combinations(sets, 2) for sets in groups if not _apart_by_steps(sets)]
+        pairs += [itertools.product(x, y) for x, y in itertools.combinations(groups, 2)]
+        for x, y in itertools.chain.from_iterable(pairs):
+            if (x[4] or y[4]) and _meet(y[0] - x[0], x[2], x[3], y[2], y[3]):
+                raise ValueError("what is written must share no memory with another state or output, nor with parents")
 
 
 _first = operator.itemgetter(0)
@@ -1014,7 +1058,8 @@ def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) ->
 
     parents: [B, n] int32, as from aal_beam_select; a parent outside [0, W) leaves its slot as it
     was.  out: None, for in place (n = W; beams that keep their slot move nothing), or tensors
-    [B, n, ...].  What is written shares no memory with another state or output, nor with parents.  Behind its first two dimensions a state may be any view that is
+    [B, n, ...].  What is written shares no memory with another state or output, nor with parents (views of one
+    memory at different strides are refused as well where it would take long to tell that they are apart).  Behind its first two dimensions a state may be any view that is
     contiguous pieces at one distance (state[:, :, :, t0:t1] of a [B, W, heads, length, dim] cache).
 
     Returns out, or the states."""

@@ -1,6 +1,7 @@
 """What aal_beam_reorder checks before it launches anything, on the CPU: its tensors
 claim to be on a device, and the library's entry point is a stand-in that keeps its arguments."""
 import contextlib
+import random
 import struct
 
 import pytest
@@ -62,3 +63,95 @@ def test_parents_of_the_call_before_in_one_buffer(calls):
     with pytest.raises(ValueError, match="parents"):
         api.aal_beam_reorder([state], pool[B * W * L - 1:-2].view(B, W))
     assert len(calls) == 1
+
+
+def layers(n, B=2, W=3, heads=2, length=5, dim=4):
+    """Caches of n layers as views of one tensor, narrowed to some positions."""
+    return list(on(torch.zeros(B, W, n, heads, length, dim))[:, :, :, :, 1:3].unbind(2))
+
+
+def test_layers_of_one_tensor_take_one_look_each(calls, monkeypatch):
+    """Views whose ranges interleave are told apart by sorting them, not pair by pair; one that is there twice, or reaches
+    into its neighbour, is found."""
+    pairs = []
+    meet = api._meet
+    monkeypatch.setattr(api, "_meet", lambda *a: pairs.append(a) or meet(*a))
+    parents = on(torch.zeros(2, 3, dtype=torch.int32))
+    for n in (2, 50, 400):
+        views = layers(n)
+        api.aal_beam_reorder(views, parents)
+        assert not pairs and len(calls.pop()) == n
+        api.aal_beam_reorder(views, parents, out=layers(n))
+        assert not pairs
+        with pytest.raises(ValueError):
+            api.aal_beam_reorder(views + [views[n // 2]], parents)
+        pairs.clear()
+    whole = on(torch.zeros(2, 3, 60, 2, 5, 4))
+    views = list(whole[:, :, :50].unbind(2))
+    # what lies between the layers' memory, and other states of other strides there
+    api.aal_beam_reorder(views + [whole[:, :, 50:54, 1], whole[:, :, 55:, 0, 0], whole[:, :, 54, :, :, 1:3]], parents)
+    assert len(pairs) < 400
+    with pytest.raises(ValueError):
+        api.aal_beam_reorder(views + [whole[:, :, 49:54, 1]], parents)
+
+
+@pytest.mark.parametrize("kind", ["requests", "beams", "heads", "rows"])
+def test_views_in_any_order_of_dimensions(calls, kind):
+    """Layers outside of requests, between requests and beams, inside of heads, inside of positions."""
+    n, B, W, heads, length, dim = 20, 2, 3, 2, 5, 4
+    parents = on(torch.zeros(B, W, dtype=torch.int32))
+    order = {"requests": (n, B, W, heads, length, dim), "beams": (B, n, W, heads, length, dim),
+             "heads": (B, W, heads, n, length, dim), "rows": (B, W, heads, length, n, dim)}[kind]
+    at = order.index(n)
+    t = on(torch.zeros(order))
+    views = list(t.unbind(at))
+    api.aal_beam_reorder(views, parents)
+    assert len(calls) == 1
+    with pytest.raises(ValueError):
+        api.aal_beam_reorder(views + [t.select(at, 7)], parents)
+
+
+def test_views_of_different_strides(calls):
+    """Every piece of one and every third of another, in one array: disjoint for as many steps as there are."""
+    t = on(torch.zeros(1, 2, 400, 12))
+    parents = on(torch.zeros(1, 2, dtype=torch.int32))
+    api.aal_beam_reorder([t[:, :, :, :4], t[:, :, ::3, 8:]], parents)
+    assert len(calls) == 1
+    with pytest.raises(ValueError):
+        api.aal_beam_reorder([t[:, :, :, :4], t[:, :, ::3, 3:]], parents)
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_lists_of_sets_against_bytes_written_out(seed):
+    """Sets of the same strides and of others: an error where bytes are shared, none where they are not."""
+    g = random.Random(seed)
+
+    def places(first, dims, n):
+        at = {first}
+        for s, c in dims:
+            at = {x + s * k for x in at for k in range(c)}
+        return {x + i for x in at for i in range(n)}
+
+    found = [0, 0]
+    for _ in range(1500):
+        s2 = g.randint(2, 6)
+        s1 = s2 * g.randint(2, 4) + g.choice([0, 0, 1])
+        s0 = s1 * g.randint(2, 4) + g.choice([0, 0, 3])
+        spans, bytes_ = [], []
+        for _ in range(g.randint(2, 5)):
+            c0, c1, c2, n = g.randint(1, 3), g.randint(1, 2), g.randint(1, 2), g.randint(1, s2)
+            first = 1000 + g.randint(0, 2 * s0)
+            step = s2 if g.random() < 0.8 else s2 + 1
+            dims = [(s0, c0), (s1, c1), (step, c2)]
+            spans.append((first, n + sum(s * (c - 1) for s, c in dims), g.random() < 0.6, (c2, n, step), ((s0, c0), (s1, c1))))
+            bytes_.append(places(first, dims, n))
+        shared = any((x[2] or y[2]) and (bytes_[i] & bytes_[i + 1 + k])
+                     for i, x in enumerate(spans) for k, y in enumerate(spans[i + 1:]))
+        try:
+            api._check_memory(list(spans))
+            raised = False
+        except ValueError:
+            raised = True
+        assert raised == shared, spans
+        found[shared] += 1
+    assert min(found) > 100
