@@ -1058,9 +1058,11 @@ def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) ->
 
     parents: [B, n] int32, as from aal_beam_select; a parent outside [0, W) leaves its slot as it
     was.  out: None, for in place (n = W; beams that keep their slot move nothing), or tensors
-    [B, n, ...].  What is written shares no memory with another state or output, nor with parents (views of one
-    memory at different strides are refused as well where it would take long to tell that they are apart).  Behind its first two dimensions a state may be any view that is
-    contiguous pieces at one distance (state[:, :, :, t0:t1] of a [B, W, heads, length, dim] cache).
+    [B, n, ...].  What is written shares no memory with another state or output, nor with parents (views of
+    one memory at different strides are refused as well where it would take long to tell that they are
+    apart).  Behind its first two dimensions a state may be any view that is contiguous pieces at one
+    distance (state[:, :, :, t0:t1] of a [B, W, heads, length, dim] cache), and so may its output: the
+    same pieces, or as a whole contiguous in one of the two.
 
     Returns out, or the states."""
     states = list(states)
@@ -1100,11 +1102,17 @@ def aal_beam_reorder(states, parents: torch.Tensor, *, out=None, stream=None) ->
                 raise ValueError(f"out must be [{B}, {n}, ...] of the states' shapes and dtypes on {dev}")
             shape, stride = tuple(o.shape), o.stride()
             to = _segments(shape, stride)
-            if to is None or to[:2] != (count, size):
-                raise ValueError("an output must be the same contiguous pieces as its state")
-            row = (at, o.data_ptr(), request, beam, step, stride[0] * e, stride[1] * e, to[2] * e, count, piece)
+            if to is None or (to[0] != count and 1 not in (to[0], count)):
+                raise ValueError("an output must be contiguous as a whole or the same contiguous pieces as its state, unless that is")
+            to_at, to_request, to_beam, to_step, to_piece = o.data_ptr(), stride[0] * e, stride[1] * e, to[2] * e, to[1] * e
             if moves:
-                spans.append((row[1], to[3] * e, True, (count, piece, row[7]), ((row[5], B), (row[6], n))))
+                spans.append((to_at, to[3] * e, True, (to[0], to_piece, to_step), ((to_request, B), (to_beam, n))))
+            # what is contiguous as a whole goes by the pieces of the other
+            if to[0] < count:
+                to_step = piece
+            elif to[0] > count:
+                count, piece, step = to[0], to_piece, to_piece
+            row = (at, to_at, request, beam, step, to_request, to_beam, to_step, count, piece)
         if not _apart(shape, stride):
             raise ValueError("the entries of what is written must not share memory")
         if moves:

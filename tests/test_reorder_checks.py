@@ -1,6 +1,7 @@
 """What aal_beam_reorder checks before it launches anything, on the CPU: its tensors
 claim to be on a device, and the library's entry point is a stand-in that keeps its arguments."""
 import contextlib
+import ctypes
 import random
 import struct
 
@@ -155,3 +156,42 @@ def test_lists_of_sets_against_bytes_written_out(seed):
         assert raised == shared, spans
         found[shared] += 1
     assert min(found) > 100
+
+
+def moved(calls, B, n, parents):
+    """What the last call's table asks for, done by the byte."""
+    for src, dst, sr, sb, ss, dr, db, ds, segments, size in calls[-1]:
+        for b in range(B):
+            for j in range(n):
+                for k in range(segments):
+                    ctypes.memmove(dst + b * dr + j * db + k * ds, src + b * sr + parents[b, j].item() * sb + k * ss, size)
+
+
+def test_a_narrowed_cache_and_a_contiguous_one(calls):
+    """From a range of positions into a tensor of that length and back, and other pairs of layouts."""
+    B, W, n, heads, length, dim = 2, 3, 4, 2, 7, 5
+    parents = on(torch.tensor([[2, 0, 1, 1], [0, 0, 2, 1]], dtype=torch.int32))
+    full = lambda k, *s: on(torch.randn(B, k, *s))  # noqa: E731
+    pairs = [(full(W, heads, length, dim)[:, :, :, 2:6], full(n, heads, 4, dim)),
+             (full(W, heads, 4, dim), full(n, heads, length, dim)[:, :, :, 1:5]),
+             (full(W, heads, length, dim)[:, :, :, 2:6], full(n, heads, 2 * length, dim)[:, :, :, 9:13]),
+             (full(W, 6, 4)[..., :1], full(n, 6, 1)), (full(W, 6, 1), full(n, 6, 3)[..., 1:2]),
+             (full(W, 1, 4)[..., :3], full(n, 1, 3)), (full(W, 6, 4), full(n, 6, 4))]
+    for s, o in pairs:
+        api.aal_beam_reorder([s], parents, out=[o])
+        moved(calls, B, n, parents)
+        assert torch.equal(o, s[torch.arange(B)[:, None], parents.long()])
+    api.aal_beam_reorder([s for s, _ in pairs], parents, out=[torch.zeros_like(o).as_subclass(OnDevice) for _, o in pairs])
+    assert len(calls[-1]) == len(pairs)
+    # two layouts of pieces that do not fit each other, and more than one distance
+    for s, o in ((full(W, heads, length, dim)[:, :, :, :4], full(n, heads, 4, 2 * dim)[..., :dim]),
+                 (full(W, heads, 4, dim), full(n, heads, length, 2 * dim)[:, :, :, :4, :dim])):
+        with pytest.raises(ValueError):
+            api.aal_beam_reorder([s], parents, out=[o])
+    # and they are still told apart from what else is written
+    cache = full(W, heads, length, dim)
+    out = full(n, heads, 4, dim)
+    for outs in ([out, out], [out, out[:, :, :1]], [out, out[:, :, 1]]):
+        states = [cache[:, :, :, 2:6], cache[:, :, :, 2:6] if outs[1] is out else cache[:, :, :1, 2:6] if outs[1].dim() == 5 else cache[:, :, 1, 2:6]]
+        with pytest.raises(ValueError):
+            api.aal_beam_reorder(states, parents, out=outs)
