@@ -760,6 +760,12 @@ def _fp8_operand(v: torch.Tensor, s: torch.Tensor, name: str, dev) -> _lib.Fp8Op
                            _code(_SCALE, s.dtype, "scale dtype"), 1 if s.shape[0] == R else AAL_FP8_BLOCK)
 
 
+def _operand_memory(o: _lib.Fp8Operand, v: torch.Tensor, s: torch.Tensor) -> tuple:
+    """First byte and end of an operand's values and of its scale."""
+    end = s.element_size() * (1 + (s.shape[0] - 1) * o.scale_row + (s.shape[1] - 1) * o.scale_block)
+    return (o.values, o.values + v.shape[0] * o.ld), (o.scale, o.scale + end)
+
+
 def aal_fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, *,
                    out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
                    ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
@@ -768,7 +774,7 @@ def aal_fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_sc
     shape tells): a_scale [M or ceil(M / 128), ceil(K / 128)], b_scale alike, both
     float32 or both float8_e8m0fnu, any strides.  Values: float8_e4m3fn or float8_e5m2, rows at multiples
     of 16 bytes (as aal_fp8_quantize makes them).  M and N up to 2^28, M N below 2^37, K and the rows'
-    distances below 2^24.
+    distances below 2^24.  out, if given, and ws share no memory with the operands.
 
     out_dtype fp32: sums in fp32.  bf16: sums of 8-bit matrix instructions, which cut each eight
     neighbours' products below 2^-13 of the largest: off by up to 7 2^-13 of sum |a b| with the scales where large
@@ -791,6 +797,11 @@ def aal_fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_sc
     need = aal_fp8_matmul_workspace_bytes(M, N, K)
     if ws is not None and (ws.device != dev or not ws.is_contiguous()):
         raise ValueError(f"ws must be a contiguous tensor on {dev}")
+    written = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in (out, ws) if t is not None]
+    if written:
+        read = _operand_memory(oa, a, a_scale) + _operand_memory(ob, b, b_scale)
+        if any(x[0] < y[1] and y[0] < x[1] for i, x in enumerate(written) for y in (*read, *written[i + 1:])):
+            raise ValueError("out and ws must share no memory with each other, an operand or its scale")
     with _guard(dev, stream):
         if out is None:
             out = torch.empty(M, N, dtype=out_dtype, device=dev)
