@@ -741,7 +741,7 @@ def aal_fp8_quantize(x: torch.Tensor, *, block_rows: int = 1, rows: bool = True,
     return out
 
 
-def _fp8_operand(v: torch.Tensor, s: torch.Tensor, name: str, dev) -> _lib.Fp8Operand:
+def _fp8_operand(v: torch.Tensor, s: torch.Tensor, name: str, dev) -> tuple:
     if v.dim() != 2 or v.numel() == 0 or s.dim() != 2:
         raise ValueError(f"{name} must be [rows, K] with a 2-d scale")
     R, K = v.shape
@@ -756,14 +756,17 @@ def _fp8_operand(v: torch.Tensor, s: torch.Tensor, name: str, dev) -> _lib.Fp8Op
     square = (R + AAL_FP8_BLOCK - 1) // AAL_FP8_BLOCK
     if s.shape[1] != blocks or s.shape[0] not in (R, square):
         raise ValueError(f"{name}: its scale must be [{R} or {square}, {blocks}]; got {tuple(s.shape)}")
-    return _lib.Fp8Operand(v.data_ptr(), s.data_ptr(), ld, s.stride(0), s.stride(1), _code(_FP8, v.dtype, "dtype"),
-                           _code(_SCALE, s.dtype, "scale dtype"), 1 if s.shape[0] == R else AAL_FP8_BLOCK)
+    at, scale, (row, block) = v.data_ptr(), s.data_ptr(), s.stride()
+    o = _lib.Fp8Operand(at, scale, ld, row, block, _code(_FP8, v.dtype, "dtype"), _code(_SCALE, s.dtype, "scale dtype"),
+                        1 if s.shape[0] == R else AAL_FP8_BLOCK)
+    # and the memory that it is, values and scale
+    return o, ((at, at + R * ld), (scale, scale + s.element_size() * (1 + (s.shape[0] - 1) * row + (blocks - 1) * block)))
 
 
-def _operand_memory(o: _lib.Fp8Operand, v: torch.Tensor, s: torch.Tensor) -> tuple:
-    """First byte and end of an operand's values and of its scale."""
-    end = s.element_size() * (1 + (s.shape[0] - 1) * o.scale_row + (s.shape[1] - 1) * o.scale_block)
-    return (o.values, o.values + v.shape[0] * o.ld), (o.scale, o.scale + end)
+def _check_apart(at: int, end: int, read: tuple):
+    for other, other_end in read:
+        if at < other_end and other < end:
+            raise ValueError("out and ws must share no memory with each other, an operand or its scale")
 
 
 def aal_fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, *,
@@ -782,7 +785,7 @@ def aal_fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_sc
 
     Returns out, [M, N]."""
     dev = a.device
-    oa, ob = _fp8_operand(a, a_scale, "a", dev), _fp8_operand(b, b_scale, "b", dev)
+    (oa, read_a), (ob, read_b) = _fp8_operand(a, a_scale, "a", dev), _fp8_operand(b, b_scale, "b", dev)
     (M, K), N = a.shape, b.shape[0]
     if b.shape[1] != K:
         raise ValueError(f"a and b must agree in K; got {K} and {b.shape[1]}")
@@ -797,11 +800,14 @@ def aal_fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_sc
     need = aal_fp8_matmul_workspace_bytes(M, N, K)
     if ws is not None and (ws.device != dev or not ws.is_contiguous()):
         raise ValueError(f"ws must be a contiguous tensor on {dev}")
-    written = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in (out, ws) if t is not None]
-    if written:
-        read = _operand_memory(oa, a, a_scale) + _operand_memory(ob, b, b_scale)
-        if any(x[0] < y[1] and y[0] < x[1] for i, x in enumerate(written) for y in (*read, *written[i + 1:])):
-            raise ValueError("out and ws must share no memory with each other, an operand or its scale")
+    if out is not None or ws is not None:
+        read = (*read_a, *read_b)
+        if ws is not None:
+            at, end = ws.data_ptr(), ws.data_ptr() + ws.nbytes
+            _check_apart(at, end, read)
+            read += ((at, end),)
+        if out is not None:
+            _check_apart(out.data_ptr(), out.data_ptr() + out.nbytes, read)
     with _guard(dev, stream):
         if out is None:
             out = torch.empty(M, N, dtype=out_dtype, device=dev)
