@@ -790,6 +790,7 @@ typedef struct {
  * states after a selection.  In place, src[b, j] becomes what src[b, parents[b, j]] was before the call, and
  * beams that keep their slot move no byte.  A parent outside [0, W) leaves its slot as it was.
  * states : host memory [n_states], read before the call returns; 0 <= n_states.  parents : device [B, n].
+ * segments * segment_bytes is in [0, 2^39], and B * n times that in [0, 2^50].
  * In place asks for n = W <= AAL_BEAM_MAX (src is written); otherwise 1 <= n <= AAL_BEAM_SELECT_MAX, and a
  * dst overlaps no src.  What is written must not overlap another state or parents, nor a state's slots each other.  Any alignment; states move in pieces
  * of 16 bytes, and segments that are no number of them have ends of fewer.

@@ -91,6 +91,9 @@ aal_status_t aal_beam_reorder(const aal_beam_state_t* states, int32_t n_states, 
         (s.segment_bytes > 0 && s.segments > (int64_t(1) << 39) / s.segment_bytes))
       return fail(AAL_ERR_ARG, "state %d: segments * segment_bytes must be in [0, 2^39]", i);
     if (!s.src && s.segments * s.segment_bytes > 0) return fail(AAL_ERR_ARG, "state %d: src must be non-NULL", i);
+    // more than any memory holds: sums of such sizes would overflow, and their launches never end
+    if (s.segments * s.segment_bytes > (int64_t(1) << 50) / (B * n))
+      return fail(AAL_ERR_ARG, "state %d: B * n * segments * segment_bytes must be in [0, 2^50]", i);
     for (int64_t st : {s.src_request, s.src_beam, s.src_segment, s.dst_request, s.dst_beam, s.dst_segment})
       if (!stride_in_range(st)) return fail(AAL_ERR_ARG, "state %d: a stride is out of range", i);
     in_place += s.dst == nullptr;
