@@ -52,15 +52,17 @@ __device__ __forceinline__ float scale_of(uint32_t raw, int e8m0) {
 // Two scales may leave fp32's range together where the result does not.  Blocks with such scales are looked for and scaled
 // in 64 bits, in two to four times a block's time: first whether any scale lies outside of [2^LESS, 2^HIGH], which
 // rarely is so, and then what it meets: in range are two of 2^LESS, one of 2^LEAST and one of 2^SMALL, 0, and what lies above
-// them up to 2^HIGH.  Looking costs 1 to 3% of a product (8,192 x 128,256 x 4,096 3.99 -> 4.05 ms; 128,256 x 4,096 x 2,048 into fp32 with any
-// scales 2.52 -> 2.63; the same for the workgroup at once, with a flag in LDS, 5%).
+// them up to 2^HIGH.  Looking costs 1% of a product (8,192^3 482 -> 483 us, 64 x 128,256 x 4,096 125 -> 127; 128,256 x 4,096 x 2,048
+// into fp32 with any scales 2.55 -> 2.62 ms); once for a whole workgroup, through a flag in LDS, it cost 5%.
 template <int HIGH, int SMALL, int LESS, int LEAST>
 struct ScaleRange {
   static __device__ __forceinline__ uint32_t power(int e) { return uint32_t(e + 127) << 23; }
-  static __device__ __forceinline__ bool unusual(float scale) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, scale) & 0x7fffffffu;
-    return b - power(LESS) > power(HIGH) - power(LESS);
+  // least and most: of scales' magnitudes (a NaN bears on neither, and ends as one either way)
+  static __device__ __forceinline__ bool unusual(float least, float most) {
+    return least < __builtin_bit_cast(float, power(LESS)) || most > __builtin_bit_cast(float, power(HIGH));
   }
+  // a scale that is a power of two, as it is stored
+  static __device__ __forceinline__ bool unusual(uint32_t e8m0) { return e8m0 - uint32_t(LESS + 127) > uint32_t(HIGH - LESS); }
   // bit 0: beyond it whatever the others are, 1: below 2^SMALL, 2: below 2^LESS
   static __device__ __forceinline__ uint32_t bits(float scale) {
     const uint32_t b = __builtin_bit_cast(uint32_t, scale) & 0x7fffffffu;
@@ -77,7 +79,7 @@ typedef ScaleRange<63, -16, -62, -110> SumRange;   // of scales that sums are mu
 typedef ScaleRange<40, -16, -46, -78> ValueRange;  // and values of 2^-16 to 2^16 in bf16, whose products are normal numbers
 // Of a product of two scales: 0 is none, since it may be what is left of two others.
 __device__ __forceinline__ bool is_normal(float x) {
-  return (__builtin_bit_cast(uint32_t, x) & 0x7fffffffu) - 0x800000u < 0x7f000000u;
+  return __builtin_amdgcn_classf(x, 0x108);
 }
 // sum + t x y for scales of any size.
 __device__ __forceinline__ float add_far(float sum, float t, float x, float y) {
@@ -225,7 +227,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
     const float s = scale_of(next, p.e8m0);
     scales[to][tid] = s;
     if constexpr (POW) {
-      const bool any = __builtin_amdgcn_ballot_w64(ValueRange::unusual(s)) != 0;
+      const bool any = __builtin_amdgcn_ballot_w64(ValueRange::unusual(next)) != 0;
       if (lane == 0) unusual[to][wave] = any;
     }
   };
@@ -350,21 +352,22 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
   };
   // Whether the wave's scales of the block, of which fa has a's, leave fp32's range (SQUARE: fa has their products).
   auto scales_left = [&] {
-    bool any = false;
     if constexpr (SQUARE) {
+      bool any = false;
 #pragma unroll
       for (int m = 0; m < TM; ++m) any |= !is_normal(fa[m]);
       return __builtin_amdgcn_ballot_w64(any) != 0;
     } else {
-      float own[TN / 4];
+      float own[TN / 4], least = fabsf(fa[0]), most = least;
+      auto meet = [&](float f) {
+        least = fminf(least, fabsf(f));
+        most = fmaxf(most, fabsf(f));
+      };
 #pragma unroll
-      for (int i = 0; i < TN / 4; ++i) {
-        own[i] = scales[stage][wn * TN * 16 + i * 64 + lane];
-        any |= SumRange::unusual(own[i]);
-      }
+      for (int i = 0; i < TN / 4; ++i) meet(own[i] = scales[stage][wn * TN * 16 + i * 64 + lane]);
 #pragma unroll
-      for (int m = 0; m < TM; ++m) any |= SumRange::unusual(fa[m]);
-      if (__builtin_amdgcn_ballot_w64(any) == 0) return false;
+      for (int m = 1; m < TM; ++m) meet(fa[m]);
+      if (__builtin_amdgcn_ballot_w64(SumRange::unusual(least, most)) == 0) return false;
       uint32_t of_a = 0, of_b = 0;
 #pragma unroll
       for (int i = 0; i < TN / 4; ++i) of_b |= SumRange::bits(own[i]);
@@ -594,22 +597,24 @@ __global__ __launch_bounds__(256, 2) void k_few_rows(MatmulParams p) {
     for (int r = 0; r < BN / RP; ++r) load_lds_once(rb, vb + (uint32_t(r * RP) * uint32_t(p.ld_b) + k), base + r * RP * 128);
     load_lds(ra, va + k, base + BN * 128);
   };
-  bool unusual = false;
+  float least = 1.f, most = 1.f;
   for (int i = tid; i < (j1 - j0) * BM; i += 256) {
     const int j = i / BM, m = min(i % BM, M - 1);
     const float s = scale_of(raw_scale(p.sa, int64_t(m >> p.ra) * p.sa_row + (j0 + j) * p.sa_block, p.e8m0), p.e8m0);
     scale_m[j][i % BM] = s;
-    unusual |= SumRange::unusual(s);
+    least = fminf(least, fabsf(s));
+    most = fmaxf(most, fabsf(s));
   }
   for (int i = tid; i < (j1 - j0) * SN; i += 256) {
     const int j = i / SN, n = min(i % SN, left_n - 1);
     const float s = scale_of(raw_scale(p.sb, ((n0 + n) >> p.rb) * p.sb_row + (j0 + j) * p.sb_block, p.e8m0), p.e8m0);
     scale_n[j][i % SN] = s;
-    unusual |= SumRange::unusual(s);
+    least = fminf(least, fabsf(s));
+    most = fmaxf(most, fabsf(s));
   }
   // for each wave to read in the part of the last stage that it loads itself, later: the two workgroups of a CU take 160 KB to
   // the byte
-  unusual = __builtin_amdgcn_ballot_w64(unusual) != 0;
+  const bool unusual = __builtin_amdgcn_ballot_w64(SumRange::unusual(least, most)) != 0;
   if (lane < 4) tile[kRing - 1][lane * 1024 + wave] = unusual;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   load(0, 0);
