@@ -757,7 +757,8 @@ size_t aal_beam_select_workspace_bytes(aal_dtype_t in_dtype, int64_t B, int32_t 
  *   a beam that has ended stands for itself alone: token pad, total scores[w], rank total / lengths[w]^length_penalty
  *   order       : larger rank first; among equal ones the lower beam, the larger logit, the lower token
  *
- * Totals and ranks are formed in 64 bits, the exponentials of all but each part's n largest logits in 32.
+ * Totals and ranks are formed in 64 bits, the exponentials of all but each part's n largest logits in 32: lse is off by
+ * 2^-20 at most, within which candidates of two beams may change places.
  * Candidates of total -inf (a masked token, a beam of score -inf) are never chosen; where
  * candidates run out, scores and rank are -inf, parents -1, tokens pad, finished 1, lengths 0.
  * z : [B, W, V] of in_dtype, 16-byte aligned, finite or -inf (a beam's whole row may be -inf).  Rows of

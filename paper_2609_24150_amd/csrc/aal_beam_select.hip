@@ -8,11 +8,11 @@
 // leaves the part's n largest logits in order, its largest one and the sum of exp((z - that) / T).
 // k_beam_merge, one workgroup per request, joins the parts' sums, forms every candidate's rank and chooses.
 //
-// Two beams' candidates may differ by less than 32 bits tell apart, and a choice cannot be off by a
-// rounding: totals are formed in 64 bits, and so is a row's log-sum-exp where it counts,
-// the exponentials of the listed logits.  Those of the others are v_exp_f32's of arguments with one
-// rounding (log2(e) / T in two pieces), whose errors average out over the many of them that it takes to
-// bear on the sum.  Bound by that arithmetic where there are many rows: 13 instructions a logit, 64 x 8 rows of 128,256 bf16,
+// Two beams' candidates may differ by less than 32 bits tell apart: totals are formed in 64 bits, and so is a
+// row's log-sum-exp where it counts, the exponentials of the listed logits.  Those of the others are v_exp_f32's of
+// arguments with one rounding (log2(e) / T in two pieces), whose errors average out over the many of them that it
+// takes to bear on the sum; it is off by 2^-20 at most, and by no more can candidates of two beams be misjudged, those of
+// one not at all.  Bound by that arithmetic where there are many rows: 13 instructions a logit, 64 x 8 rows of 128,256 bf16,
 // 16 chosen, 31 us or 3.5 TB/s and 12 us to merge; by latency and the merge where there are few.  Parts are cut from the row's start whatever its alignment, so that equal rows
 // get equal sums, and equal beams tie exactly.
 #include "aal_beam.h"

@@ -9,7 +9,6 @@ namespace {
 
 typedef u32x4 u32x4_e2 __attribute__((aligned(2)));  // a vector at any element
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // 2^e, e in [-126, 127].
 __device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, uint32_t(e + 127) << 23); }
@@ -41,17 +40,6 @@ __device__ __forceinline__ uint32_t pack_fp8(float a, float b, float c, float d)
     w = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, w, true);
   }
   return uint32_t(w);
-}
-
-// A scale of either type as a float.
-template <Scale S>
-__device__ __forceinline__ float load_scale(const void* s, int64_t i) {
-  if constexpr (S == Scale::kF32) {
-    return static_cast<const float*>(s)[i];
-  } else {
-    const uint32_t b = static_cast<const uint8_t*>(s)[i];
-    return __builtin_bit_cast(float, b == 0u ? 0x400000u : b == 255u ? 0x7fc00000u : b << 23);
-  }
 }
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));

@@ -162,12 +162,13 @@ __device__ __forceinline__ int place_in_stage(int row, int byte) {
 //
 // A CU has 64 KB of tiles a stage and two stages of them, so that one tile of 256 x 256 (eight waves) or two of 128 x 128
 // (four each) are at work in it.  Bound by how fast stages arrive and by LDS: a block of 256 x 256 x 128 takes 3,700 to
-// 4,000 cycles, 2,048 of them in the matrix unit; 8,192 x 128,256 x 4,096 4.3 ms, 2.0 PFLOP/s.  WIDE has half the
-// matrix unit's rate, and 1.08 PFLOP/s at 8,192^3.  The library's products there: with one scale for all 2.6 to 3.2, bf16 1.3.
+// 4,000 cycles, 2,048 of them in the matrix unit; 8,192 x 128,256 x 4,096 4.2 ms, 2.0 PFLOP/s; 4.9 where
+// both operands have a scale for each row, whose tiles of 256 x 256 spill 12 registers.  WIDE has half the
+// matrix unit's rate, and 1.04 PFLOP/s at 8,192^3.  The library's products there: with one scale for all 2.6 to 3.2, bf16 1.3.
 //
 // POW (with WIDE, scales that are powers of two): the widening to bf16 applies them, which is exact, and sums stay in the
-// matrix unit from block to block: no arithmetic on sums, a third of the instructions.  128,256 x 4,096 x 2,048 into fp32 2.26
-// ms, with the scales applied to sums 2.53; 256 x 256 tiles, whose registers do not do, 3.11.
+// matrix unit from block to block: no arithmetic on sums, a third of the instructions.  128,256 x 4,096 x 2,048 into fp32 2.37
+// ms, with the scales applied to sums 2.66; 256 x 256 tiles, whose registers do not do, 3.11.
 template <bool WIDE, bool POW, int FA, int FB, bool SQUARE, int TN, int TM, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM, 2) void k_tiles(MatmulParams p) {
   static_assert(WIDE || !POW, "products of 8-bit instructions take scales on their sums");

@@ -1,5 +1,5 @@
-// The product of 8-bit operands (aal_fp8_matmul): how it is cut, and the sum of
-// the parts where the inner dimension is.  The kernels are in aal_fp8_matmul.h.
+// The product of 8-bit operands (aal_fp8_matmul): its launch, and the sum of the parts where the
+// inner dimension is cut.  The kernels are in aal_fp8_matmul.h, the cut is aal_fp8_plan.h's.
 #include "aal_fp8_matmul.h"
 
 #include <algorithm>

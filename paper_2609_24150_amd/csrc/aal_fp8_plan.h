@@ -33,7 +33,7 @@ inline MatmulPlan plan_of(int64_t M, int64_t N, int64_t K, bool wide) {
   const int64_t blocks = up(K, 128);
   if (M <= 32) {
     // Few rows of a: b is read once, for which 250 workgroups do (32 x 32,000 x 4,096 24.8 us, in four parts 36.8); of
-    // eight blocks at least.  33 rows of 128,256 x 4,096 take 112 us in tiles, up to 32 take 84 to 93 here.
+    // eight blocks at least.  33 rows of 128,256 x 4,096 take 120 us in tiles, up to 32 take 84 to 92 here.
     const int64_t s = std::min<int64_t>(kCus / up(N, 128), blocks / 8);
     return {0, int(std::max<int64_t>(up(blocks, kFewBlocks), std::min<int64_t>(s, 64)))};
   }
