@@ -911,7 +911,7 @@ def aal_beam_select(z: torch.Tensor, scores: torch.Tensor, n: int, *, temperatur
     """The n best continuations of each request's beams, over all its beams and
     the vocabulary.
 
-    z [B, W, V]: logits (bf16 or fp32).  scores [B, W] float32: the beams' cumulative
+    z [B, W, V]: logits (bf16 or fp32), W up to 64, V up to 2^18.  scores [B, W] float32: the beams' cumulative
     log-probabilities, -inf for one that is not to go on.  finished [B, W] bool: beams that have
     ended, each of which stands for itself with token pad and its own score.  lengths [B, W] int32: tokens so
     far.  Candidates are ordered by (score + log softmax(z / temperature)) / (lengths + 1) **
