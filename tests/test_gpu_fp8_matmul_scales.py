@@ -3,8 +3,11 @@ not hold while the results are ordinary numbers, against the fp64 oracle.
 
 Tolerances are those of test_gpu_fp8_matmul.py: a block's sum takes the two scales with one rounding more at
 most, which is counted there as that of the scales' product."""
+import numpy as np
 import pytest
 import torch
+
+from oracle import head_oracle as H
 
 from test_gpu_fp8_matmul import A, BF16, E8M0, F32, check, operand  # noqa: F401
 
@@ -92,3 +95,67 @@ def test_far_blocks_beside_any_others(A, M, N, K):  # noqa: F811
             sa[:, 0] = torch.tensor(2.0 ** -75).to(scale)
             sb[:, 0] = torch.tensor(2.0 ** -76).to(scale)
             check(A.aal_fp8_matmul(a[0], sa, b[0], sb, out_dtype=out), (a[0], sa), (b[0], sb), out)
+
+
+@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("out", [BF16, F32])
+@pytest.mark.parametrize("block", [1, 128])
+def test_negative_scales_and_zeros(A, M, N, K, out, block):  # noqa: F811
+    """Scales of either sign, zeros among them, beside others and in blocks that are out of range.  Results below
+    2^-126 are rounded to steps of 2^-149, once a block, or of bf16's 2^-133 in the end."""
+    a, b = operand(M, K, "e4m3", F32, 1, 11), operand(N, K, "e4m3", F32, block, 12)
+    g = torch.Generator("cuda").manual_seed(13)
+    for s in (a[1], b[1]):
+        s.mul_(torch.randint(-1, 2, s.shape, generator=g, device="cuda"))
+
+    def compare():
+        got = A.aal_fp8_matmul(*a, *b, out_dtype=out).double().cpu().numpy()
+        host = [t.float().double().cpu().numpy() for t in (*a, *b)]
+        want, mag, blocks = H.product(*host), H.magnitude(*host), a[1].shape[1]
+        tol = (128 * 2.0 ** -23 + (blocks + 2) * 2.0 ** -24) * mag + blocks * 2.0 ** -149
+        if out == BF16:
+            tol = tol + 7 * 2.0 ** -13 * mag
+            tol = tol + 2.0 ** -8 * (np.abs(want) + tol) + 2.0 ** -134
+        assert np.all(np.abs(got - want) <= tol), np.max(np.abs(got - want) / tol)
+
+    compare()
+    a[1][:, ::2] *= 2.0 ** -70
+    b[1][:, ::2] *= 2.0 ** -66
+    compare()
+    a[1][:, 1::2] = 0
+    compare()
+
+
+@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("out", [BF16, F32])
+@pytest.mark.parametrize("scale", [F32, E8M0])
+def test_scales_that_are_not_numbers(A, M, N, K, out, scale):  # noqa: F811
+    """A row's and a column's scale that is NaN (or infinite): theirs are not finite, the others are what they were."""
+    a, b = operand(M, K, "e4m3", scale, 1, 14), operand(N, K, "e4m3", scale, 1, 15)
+    want = A.aal_fp8_matmul(*a, *b, out_dtype=out)
+    for bad in (float("nan"), float("inf")) if scale == F32 else (float("nan"),):
+        sa, sb = a[1].float(), b[1].float()
+        sa[2, 1], sb[N - 3, 2] = bad, bad
+        got = A.aal_fp8_matmul(a[0], sa.to(scale), b[0], sb.to(scale), out_dtype=out)
+        there = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+        there[2], there[:, N - 3] = True, True
+        assert torch.equal(got.isfinite(), ~there)
+        tol = 2.0 ** -7 if out == BF16 else 2.0 ** -18  # one bf16 step, or other rounding of the blocks beside it
+        assert ((got - want)[~there].abs() <= tol * want[~there].abs() + 2.0 ** -13 * want.abs().max()).all()
+
+
+@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("out", [BF16, F32])
+@pytest.mark.parametrize("scale", [F32, E8M0])
+@pytest.mark.parametrize("block", [1, 128])
+def test_infinite_values(A, M, N, K, out, scale, block):  # noqa: F811
+    """e5m2's infinities, in blocks of ordinary scales and of scales out of range: their rows and columns are not finite, the
+    others are."""
+    a, b = operand(M, K, "e5m2", scale, 1, 16), operand(N, K, "e5m2", scale, block, 17)
+    a[0].view(torch.uint8)[3, 200] = 0x7c
+    b[0].view(torch.uint8)[N - 5, 3] = 0xfc
+    there = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+    there[3], there[:, N - 5] = True, True
+    for e in (0, -70):
+        sa, sb = ((s.float() * 2.0 ** e).to(scale) for s in (a[1], b[1]))
+        assert torch.equal(A.aal_fp8_matmul(a[0], sa, b[0], sb, out_dtype=out).isfinite(), ~there)
